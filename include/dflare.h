@@ -107,6 +107,11 @@ typedef enum { DFLARE_BF16 = 0, DFLARE_F32 = 1 } dflare_dtype;
 #define DFLARE_DEVERR_CAPACITY  0x2u    /* ctx_len + n_new > max_ctx, or n_new outside [0, n_max]:
                                            that sequence appended nothing */
 #define DFLARE_DEVERR_TIMEOUT   0x4u    /* a pipeline wait inside a GEMM gave up (results invalid) */
+/* the same word of a paged cache (dflare_cache_error) and of the tree calls: TIMEOUT as above, CAPACITY
+   when pages or room ran out, and */
+#define DFLARE_DEVERR_PAGE      0x8u    /* a sequence or page number out of range, a fork into a sequence
+                                           that holds pages, or a page table that contradicts itself */
+#define DFLARE_DEVERR_TREE      0x10u   /* a node count, parent, accepted length or path that no tree has */
 
 typedef struct {
     int d;                /* hidden size; multiple of 64 */
@@ -368,6 +373,196 @@ dflare_status dflare_synthetic_target(const int32_t* draft_tokens_dev, const uin
  */
 dflare_status dflare_argmax_noalloc(const float* logits_dev, int rows, int vocab,
                                     int32_t* tokens_dev, void* stream);
+
+/*
+ * Verification of a tree of drafted tokens over a paged key/value cache: the target model's side of a
+ * block step whose drafts branch. Per step, in this order:
+ *   dflare_tree_plan       ancestor bits and depths of the drafted trees
+ *   dflare_cache_reserve   pages for the trees' keys and values
+ *   per target layer: dflare_cache_append (rotary positions, keys and values into the pages), then
+ *   dflare_cache_attend    every node against its sequence's cache and its own ancestors
+ *   dflare_tree_accept     the walk from the root along the target's own choices
+ *   dflare_cache_commit    the accepted path's rows moved together, the other pages given back
+ * dflare_cache_fork shares a sequence's pages with a new one, dflare_cache_truncate takes tokens back
+ * (to zero: the sequence ends), dflare_cache_copy_pages copies whole pages.
+ *
+ * A tree has nodes 0 .. n-1; node 0 is x_t (the last committed token's successor, as block row 0 of
+ * dflare_verify_accept) and parent[i] < i is the node that node i follows. Node i of sequence b is the
+ * token at position lens[b] + depth(i), and its key and value lie in slot lens[b] + i of the cache. A
+ * chain (parent[i] = i - 1) makes the same calls serve single tokens (n = 1) and prompts.
+ *
+ * These calls take no dflare_ctx. Messages of failing calls are in dflare_last_error(NULL) of the
+ * calling thread. They are stream-ordered, asynchronous unless they say otherwise, allocate nothing
+ * except dflare_cache_create, and may be captured into CUDA graphs.
+ */
+
+/* Rotary frequencies. Pair j of rot_dim / 2 turns by inv_j = theta^(-2 j / rot_dim) radians per position;
+ * scaled for contexts of `factor` (>= 1) times the trained length:
+ *   DFLARE_ROPE_LINEAR  inv_j / factor (position interpolation)
+ *   DFLARE_ROPE_NTK     theta multiplied by factor^(rot_dim / (rot_dim - 2)); needs rot_dim > 2
+ *   DFLARE_ROPE_YARN    pairs that turn more than beta_fast times within `trained` positions keep inv_j,
+ *                       those under beta_slow turns take inv_j / factor, those between a mix linear in
+ *                       j; values are multiplied by 0.1 ln(factor) + 1 */
+typedef enum { DFLARE_ROPE_PLAIN = 0, DFLARE_ROPE_LINEAR = 1, DFLARE_ROPE_NTK = 2, DFLARE_ROPE_YARN = 3 } dflare_rope_scaling;
+typedef struct {
+    int rot_dim;          /* rotated elements of each head, even, 2..1024 */
+    int scaling;          /* dflare_rope_scaling */
+    double theta;         /* > 1 */
+    double factor;        /* >= 1; not read by DFLARE_ROPE_PLAIN */
+    double trained;       /* DFLARE_ROPE_YARN: positions the model was trained on, >= 1 */
+    double beta_fast;     /* DFLARE_ROPE_YARN: turns, > beta_slow */
+    double beta_slow;     /* DFLARE_ROPE_YARN: turns, > 0 */
+} dflare_rope_config;
+
+/* Host only: phase_host[rot_dim / 2] = inv_j / (2 pi) in units of 2^-64 turns, and the factor on the
+ * rotated values. The phases are what the rotary calls read from device memory: position * phase modulo
+ * 2^64 is the angle modulo one turn, to position * 2^-65 turns, for every int32 position. */
+dflare_status dflare_rope_phases(const dflare_rope_config* cfg, uint64_t* phase_host, float* magnitude_host);
+
+typedef enum { DFLARE_ROPE_HALF = 0, DFLARE_ROPE_INTERLEAVED = 1 } dflare_rope_layout;
+
+/*
+ * Rotary embedding of [rows][heads][head_dim] T at positions_dev [rows] int32. Pair j of a head is
+ * elements (j, rot_dim/2 + j) (DFLARE_ROPE_HALF) or (2j, 2j+1) (DFLARE_ROPE_INTERLEAVED); elements from
+ * rot_dim on are copied. (y1, y2) = magnitude (x1 cos a - x2 sin a, x2 cos a + x1 sin a) in fp32, rounded
+ * once. backward != 0 applies the transposed map (a negated): the gradient with respect to x of a
+ * gradient with respect to y.
+ *   x_row, x_head, out_row, out_head   strides in elements between rows and between heads (elements of
+ *                                      a head are adjacent); out may be x itself with the same strides.
+ * Fast where the pointers are 16-byte aligned, strides and rot_dim and head_dim multiples of 16.
+ */
+dflare_status dflare_rope(const void* x_dev, long long x_row, long long x_head, void* out_dev,
+                          long long out_row, long long out_head, const int32_t* positions_dev,
+                          const uint64_t* phase_dev, int rows, int heads, int head_dim, int rot_dim,
+                          int layout, float magnitude, int backward, int dtype, void* stream);
+
+/* A paged cache of one model's keys and values. */
+typedef struct {
+    int n_layers;         /* layers of the model, 1..256 */
+    int n_pages;          /* pages of the pool, 1..2^24 */
+    int page_size;        /* tokens per page: 16, 32, 64 or 128 */
+    int n_q_heads;        /* query heads of dflare_cache_attend; a multiple of n_kv_heads, up to 64 times it */
+    int n_kv_heads;       /* 1..128 */
+    int head_dim;         /* 64 or 128 */
+    int max_batch;        /* sequences, 1..256 */
+    int max_pages;        /* pages per sequence (columns of the table), 1..2^20 */
+    int max_nodes;        /* largest tree or chunk of one dflare_cache_attend, 1..1024 */
+    int dtype;            /* dflare_dtype */
+} dflare_cache_config;
+
+/* Caller-owned device memory of a cache, borrowed until dflare_cache_destroy. A new cache has lens,
+ * held and refs zero, free_pages a permutation of 0 .. n_pages-1 and *n_free = n_pages. */
+typedef struct {
+    void* k;              /* [n_layers][n_pages][n_kv_heads][page_size][head_dim] T, 16-byte aligned */
+    void* v;              /* the same */
+    int32_t* table;       /* [max_batch][max_pages]: page numbers, in the order of the tokens */
+    int32_t* lens;        /* [max_batch]: committed tokens */
+    int32_t* held;        /* [max_batch]: pages the sequence holds */
+    int32_t* refs;        /* [n_pages]: sequences that hold the page */
+    int32_t* free_pages;  /* [n_pages]: stack of free pages, the last one taken first */
+    int32_t* n_free;      /* [1] */
+} dflare_cache_buffers;
+
+typedef struct dflare_cache dflare_cache;
+
+/* Validate (host only: DFLARE_EINVAL without touching the GPU), then make the cache's handle on the
+ * current device; it owns an error word and the attention's workspace, of at most 100 MB. The pages'
+ * contents need no initialisation: nothing is read that was not written. */
+dflare_status dflare_cache_create(const dflare_cache_config* cfg, const dflare_cache_buffers* buffers,
+                                  dflare_cache** out);
+/* Free what dflare_cache_create allocated (synchronises the device first). NULL is a no-op. */
+dflare_status dflare_cache_destroy(dflare_cache* cache);
+/* Synchronous: as dflare_device_error, for the cache's error word. */
+dflare_status dflare_cache_error(dflare_cache* cache, uint32_t* bits_host, void* stream);
+
+/* Give sequences 0 .. batch-1 room for n_new_dev[b] tokens behind their lens[b]: pages are taken from
+ * the free stack, by sequence and then by position. A sequence with n_new > 0 whose last, partly filled
+ * page is shared first gets a copy of that page's tokens (over all layers) as its own; the last sharer
+ * keeps the page. All sequences get their room or, when pages or table columns do not suffice or an
+ * n_new is negative, none does and DFLARE_DEVERR_CAPACITY is set. */
+dflare_status dflare_cache_reserve(dflare_cache* cache, const int32_t* n_new_dev, int batch, void* stream);
+
+/*
+ * The new tokens of one layer: rows i < n_new[b] of sequence b (b < batch).
+ *   q_dev, k_dev, v_dev  [batch][n_max][heads][head_dim] T with `*_row` elements between rows (heads
+ *                        adjacent): three parts of one projection's rows will do.
+ *   q_out_dev            [batch][n_max][n_q_heads][head_dim] T, rotated queries; q_dev itself (with
+ *                        out_row = q_row) rotates in place. NULL (with q_dev NULL) leaves queries out.
+ *   depth_dev            [batch][n_max] int32: the row's position is lens[b] + depth; NULL: lens[b] + i.
+ *   phase_dev ... magnitude  as in dflare_rope; rot_dim = 0 stores keys as they are.
+ * Rotated keys and the values go to slot lens[b] + i; a row whose slot lies beyond the sequence's pages
+ * is left out and sets DFLARE_DEVERR_CAPACITY (its query is still written). Rows from n_new[b] on are
+ * neither read nor written.
+ */
+dflare_status dflare_cache_append(dflare_cache* cache, int layer, const void* q_dev, long long q_row,
+                                  const void* k_dev, long long k_row, const void* v_dev, long long v_row,
+                                  void* q_out_dev, long long out_row, const int32_t* depth_dev,
+                                  const int32_t* n_new_dev, int batch, int n_max,
+                                  const uint64_t* phase_dev, int rot_dim, int layout, float magnitude,
+                                  void* stream);
+
+/*
+ * Attention of one layer: node i < n_nodes[b] of sequence b sees the sequence's lens[b] tokens and those
+ * nodes j whose bit j of its mask row is set (bit j % 32 of word j / 32); mask_dev NULL: nodes j <= i.
+ *   q_dev     [batch][n_max][n_q_heads][head_dim] T, `q_row` elements between rows; 16-byte aligned,
+ *             q_row a multiple of 8. Query head h reads kv head h / (n_q_heads / n_kv_heads).
+ *   mask_dev  [batch][n_max][(n_max + 31) / 32] int32, of dflare_tree_plan.
+ *   scale     on the scores; finite.
+ *   out_dev   [batch][n_max][n_q_heads][head_dim] T, 16-byte aligned.
+ *   lse_dev   optional [batch][n_max][n_q_heads] fp32: natural logarithm of the row's sum of exp(score).
+ * Rows that see nothing, and rows from n_nodes[b] on, are zero with lse = -inf. What lies in a row's
+ * unseen slots (any bits, infinities and NaN included) does not reach its result.
+ */
+dflare_status dflare_cache_attend(dflare_cache* cache, int layer, const void* q_dev, long long q_row,
+                                  const int32_t* mask_dev, const int32_t* n_nodes_dev, int batch, int n_max,
+                                  float scale, void* out_dev, float* lse_dev, void* stream);
+
+/* Accept nodes path[b][0 .. accept_len[b]) of each sequence's tree ([batch][path_row] int32, increasing):
+ * their rows of all layers move to slots lens[b] .. lens[b] + accept_len[b] - 1, lens grows by accept_len,
+ * and pages past the new length are given back (by sequence, then by position). A length or path that no
+ * tree has sets DFLARE_DEVERR_TREE and commits nothing of that sequence. */
+dflare_status dflare_cache_commit(dflare_cache* cache, const int32_t* accept_len_dev, const int32_t* path_dev,
+                                  int path_row, int batch, void* stream);
+
+/* lens[b] = min(lens[b], max(new_len[b], 0)) for b < batch; pages past that, reserved ones among them, are
+ * given back: a page is free once the last sequence that holds it lets go. */
+dflare_status dflare_cache_truncate(dflare_cache* cache, const int32_t* new_len_dev, int batch, void* stream);
+
+/* Sequence dst_dev[i] (which must hold no pages) becomes a copy of sequence src_dev[i], i < n <= max_batch,
+ * by sharing its pages. A pair whose numbers are out of range, whose dst is taken or listed twice, or whose
+ * src is also a dst of this call sets DFLARE_DEVERR_PAGE and is left out. */
+dflare_status dflare_cache_fork(dflare_cache* cache, const int32_t* src_dev, const int32_t* dst_dev, int n,
+                                void* stream);
+
+/* Copy page src_dev[i] to page dst_dev[i] in every layer, i < n. Pages of dst are distinct and none is
+ * also a src; numbers out of range set DFLARE_DEVERR_PAGE and are left out. */
+dflare_status dflare_cache_copy_pages(dflare_cache* cache, const int32_t* src_dev, const int32_t* dst_dev, int n,
+                                      void* stream);
+
+/*
+ * Ancestor bits and depths of trees with n_nodes_dev[b] <= n_max nodes.
+ *   parents_dev  [batch][n_max] int32: parent[0] = -1; -1 (straight behind the context) or less than i.
+ *   mask_dev     [batch][n_max][(n_max + 31) / 32] int32 out: bit j of row i set where j is i or above it.
+ *   depth_dev    [batch][n_max] int32 out: edges from i to the top of its branch.
+ * Rows from n_nodes[b] on are zero. err_dev: optional error word; an impossible parent or count sets
+ * DFLARE_DEVERR_TREE there (the node counts as attached to the context, the count as clamped).
+ */
+dflare_status dflare_tree_plan(const int32_t* parents_dev, const int32_t* n_nodes_dev, int batch, int n_max,
+                               int32_t* mask_dev, int32_t* depth_dev, uint32_t* err_dev, void* stream);
+
+/*
+ * Greedy acceptance in a tree: from node 0 on, the walk goes to the lowest-numbered child whose token is
+ * the target's choice after the current node, until there is none.
+ *   tokens_dev [batch][n_max] int32 drafted tokens (token 0 is x_t and not compared), parents_dev as above,
+ *   choice_dev [batch][n_max] int32 the target's argmax after each node.
+ *   accept_len_dev [batch] int32 out: nodes on the walk, node 0 among them (0 for an empty tree).
+ *   path_dev       [batch][n_max] int32 out: their numbers, then -1.
+ *   next_token_dev [batch] int32 out: the target's choice after the last of them (-1 for an empty tree).
+ * For a chain this is dflare_verify_accept.
+ */
+dflare_status dflare_tree_accept(const int32_t* tokens_dev, const int32_t* parents_dev, const int32_t* choice_dev,
+                                 const int32_t* n_nodes_dev, int batch, int n_max, int32_t* accept_len_dev,
+                                 int32_t* path_dev, int32_t* next_token_dev, uint32_t* err_dev, void* stream);
 
 #ifdef __cplusplus
 }

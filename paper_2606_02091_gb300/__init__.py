@@ -14,7 +14,8 @@ from ._lib import (  # noqa: F401
     DFlareError, DFLARE_BF16, DFLARE_F32, FLAG_NO_BLOCK_ROPE, FLAG_RAW_FUSION, FLAG_SIMT_GEMM,
     FLAG_SERIAL_LAUNCH, FLAG_SHARED_KV, FLAG_FUSION_FC, FLAG_DFLASH_FC, FLAG_DETERMINISTIC,
     FLAG_MMA_SYNC_ATTENTION,
-    DEVERR_TOKEN, DEVERR_CAPACITY, DEVERR_TIMEOUT, EXPORTS, WEIGHT_FIELDS, NOALLOC_MAX_ROWS, load,
+    DEVERR_TOKEN, DEVERR_CAPACITY, DEVERR_TIMEOUT, DEVERR_PAGE, DEVERR_TREE, EXPORTS, WEIGHT_FIELDS,
+    NOALLOC_MAX_ROWS, load,
 )
 
 
@@ -253,3 +254,6 @@ def synthetic_target(draft_tokens, u, r, last, step, threshold, batch, block, ta
     _lib.check(L.dflare_synthetic_target(_ptr(draft_tokens), _ptr(u), _ptr(r), _ptr(last), n_steps,
                                          _ptr(step), ctypes.c_uint32(threshold), batch, block,
                                          _ptr(target_out), _stream(stream)))
+
+
+from .paged import PagedCache, rope, rope_phases, tree_accept, tree_plan  # noqa: E402,F401

@@ -1,0 +1,282 @@
+"""Verification of a tree of drafted tokens over a paged key/value cache: torch-tensor arguments for the
+``dflare_cache_*``, ``dflare_rope*`` and ``dflare_tree_*`` calls of include/dflare.h, which says what each
+computes. Tensors are CUDA tensors; calls are enqueued on the current torch stream unless one is given, and
+a tensor that was made on another stream must be ready there. Nothing is computed here.
+
+A block step of a target model:
+
+    tree_plan(parents, n_nodes, mask, depth)
+    cache.reserve(n_nodes)
+    for layer in range(n_layers):
+        cache.append(layer, q, k, v, n_nodes, phase, q, depth=depth)      # q rotated in place
+        cache.attend(layer, q, n_nodes, out, mask=mask)
+    tree_accept(tokens, parents, choice, n_nodes, accept_len, path, next_token)
+    cache.commit(accept_len, path)
+"""
+from __future__ import annotations
+
+import ctypes
+
+from . import _lib
+
+
+def _stream(stream):
+    import torch
+    return (stream if stream is not None else torch.cuda.current_stream()).cuda_stream
+
+
+def _check(status):
+    if status:
+        _lib.check(status, None)
+
+
+def _ints(name, t, numel):
+    """An int32 CUDA tensor of at least numel elements, without gaps; its address."""
+    import torch
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.dtype is not torch.int32:
+        raise ValueError(f"{name} must be torch.int32, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if t.numel() < numel:
+        raise ValueError(f"{name} holds {t.numel()} elements, needs at least {numel}")
+    return t.data_ptr()
+
+
+def _typed(name, t, dtype):
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+
+
+def _rows(name, t, dtype, shape):
+    """A [batch][rows][heads][head_dim] tensor whose heads are adjacent and whose rows are evenly spaced
+    (a part of a fused projection's rows, for one); its address and row stride in elements."""
+    _typed(name, t, dtype)
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    b, n, heads, hd = shape
+    sb, sn, sh, sd = t.stride()
+    if n == 1:
+        sn = sb if b > 1 else heads * hd       # one row per sequence: their distance is the stride
+    if (sd != 1 and hd > 1) or (sh != hd and heads > 1) or (b > 1 and sb != n * sn):
+        raise ValueError(f"{name}: heads must be adjacent and rows evenly spaced, got strides {list(t.stride())}")
+    return t.data_ptr(), sn
+
+
+def rope_phases(rot_dim, theta=1e6, scaling="none", factor=1.0, trained=4096, beta_fast=32.0, beta_slow=1.0,
+                device="cuda"):
+    """The phases of ``rot_dim`` rotated elements (int64 [rot_dim / 2], what the rotary calls take) and the
+    factor on the rotated values. scaling: "none", "linear", "ntk" or "yarn"."""
+    import torch
+    if scaling not in _lib.ROPE_SCALINGS:
+        raise ValueError(f"scaling must be one of {sorted(_lib.ROPE_SCALINGS)}, got {scaling!r}")
+    g = _lib.RopeConfig(rot_dim, _lib.ROPE_SCALINGS[scaling], theta, factor, trained, beta_fast, beta_slow)
+    out = torch.zeros(max(int(rot_dim) // 2, 1), dtype=torch.int64)
+    magnitude = ctypes.c_float(0.0)
+    _check(_lib.load().dflare_rope_phases(ctypes.byref(g), out.data_ptr(), ctypes.byref(magnitude)))
+    return out.to(device), magnitude.value
+
+
+def _phase(phase):
+    import torch
+    _typed("phase", phase, torch.int64)
+    if not phase.is_contiguous():
+        raise ValueError("phase must be contiguous")
+    return phase.data_ptr()
+
+
+def _layout(layout):
+    if layout not in _lib.ROPE_LAYOUTS:
+        raise ValueError(f"layout must be one of {sorted(_lib.ROPE_LAYOUTS)}, got {layout!r}")
+    return _lib.ROPE_LAYOUTS[layout]
+
+
+def rope(x, positions, phase, out, *, layout="half", magnitude=1.0, backward=False, stream=None):
+    """Rotary embedding of x [rows][heads][head_dim] at int32 positions [rows] into out (x itself: in place).
+    The first 2 * len(phase) elements of each head are rotated, the others copied. ``backward=True`` applies
+    the transposed map, the gradient's."""
+    import torch
+    if x.dim() != 3 or out.shape != x.shape:
+        raise ValueError(f"x and out must be [rows][heads][head_dim], got {list(x.shape)} and {list(out.shape)}")
+    if x.dtype is not torch.bfloat16 and x.dtype is not torch.float32:
+        raise ValueError(f"x must be torch.bfloat16 or torch.float32, got {x.dtype}")
+    _typed("x", x, x.dtype)
+    _typed("out", out, x.dtype)
+    rows, heads, hd = x.shape
+    xs, os_ = x.stride(), out.stride()
+    if (xs[2] != 1 or os_[2] != 1) and hd > 1:
+        raise ValueError("the elements of a head must be adjacent")
+    pos = _ints("positions", positions, rows)
+    _check(_lib.load().dflare_rope(x.data_ptr(), xs[0], xs[1], out.data_ptr(), os_[0], os_[1], pos, _phase(phase), rows, heads,
+                                   hd, 2 * phase.numel(), _layout(layout), magnitude, 1 if backward else 0,
+                                   _lib.DFLARE_BF16 if x.dtype is torch.bfloat16 else _lib.DFLARE_F32, _stream(stream)))
+
+
+def tree_plan(parents, n_nodes, mask, depth, stream=None):
+    """Ancestor bits (int32 [batch][n][ceil(n / 32)]) and depths (int32 [batch][n]) of the trees with parent
+    numbers ``parents`` int32 [batch][n]."""
+    if parents.dim() != 2:
+        raise ValueError(f"parents must be [batch][n], got {list(parents.shape)}")
+    batch, n = parents.shape
+    _check(_lib.load().dflare_tree_plan(_ints("parents", parents, 0), _ints("n_nodes", n_nodes, batch), batch, n,
+                                        _ints("mask", mask, batch * n * ((n + 31) // 32)),
+                                        _ints("depth", depth, batch * n), None, _stream(stream)))
+
+
+def tree_accept(tokens, parents, choice, n_nodes, accept_len, path, next_token, stream=None):
+    """Greedy acceptance in drafted trees: tokens, parents and choice (the target's argmax after each node)
+    int32 [batch][n]; writes accept_len [batch], path [batch][n], next_token [batch]."""
+    if parents.dim() != 2:
+        raise ValueError(f"parents must be [batch][n], got {list(parents.shape)}")
+    batch, n = parents.shape
+    _check(_lib.load().dflare_tree_accept(
+        _ints("tokens", tokens, batch * n), _ints("parents", parents, 0), _ints("choice", choice, batch * n),
+        _ints("n_nodes", n_nodes, batch), batch, n, _ints("accept_len", accept_len, batch), _ints("path", path, batch * n),
+        _ints("next_token", next_token, batch), None, _stream(stream)))
+
+
+class PagedCache:
+    """Keys and values of a model in pages that sequences share (see dflare_cache_create).
+
+    ``PagedCache.allocate`` makes an empty one; the constructor takes a caller's tensors:
+    k, v [n_layers][n_pages][n_kv_heads][page_size][head_dim] (bf16 or fp32) and the int32 tables. The
+    tensors stay the caller's to read between calls.
+    """
+
+    def __init__(self, *, k, v, table, lens, held, refs, free, n_free, n_q_heads, max_nodes):
+        import torch
+        self._cache = ctypes.c_void_p()
+        if k.dim() != 5 or v.shape != k.shape:
+            raise ValueError("k and v must be [n_layers][n_pages][n_kv_heads][page_size][head_dim]")
+        if k.dtype is not torch.bfloat16 and k.dtype is not torch.float32:
+            raise ValueError(f"k must be torch.bfloat16 or torch.float32, got {k.dtype}")
+        for name, t in (("k", k), ("v", v)):
+            _typed(name, t, k.dtype)
+            if not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous")
+        if table.dim() != 2:
+            raise ValueError("table must be [max_batch][max_pages]")
+        self._L = _lib.load()
+        self.n_layers, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
+        self.max_batch, self.max_pages = table.shape
+        self.n_q_heads, self.max_nodes, self.dtype = n_q_heads, max_nodes, k.dtype
+        b = _lib.CacheBuffers(k.data_ptr(), v.data_ptr(), _ints("table", table, 0), _ints("lens", lens, self.max_batch),
+                              _ints("held", held, self.max_batch), _ints("refs", refs, self.n_pages),
+                              _ints("free", free, self.n_pages), _ints("n_free", n_free, 1))
+        self.cfg = _lib.CacheConfig(self.n_layers, self.n_pages, self.page_size, n_q_heads, self.n_kv_heads, self.head_dim,
+                                    self.max_batch, self.max_pages, max_nodes,
+                                    _lib.DFLARE_BF16 if k.dtype is torch.bfloat16 else _lib.DFLARE_F32)
+        self.k, self.v, self.table, self.lens, self.held = k, v, table, lens, held
+        self.refs, self.free, self.n_free = refs, free, n_free
+        with torch.cuda.device(k.device):
+            _check(self._L.dflare_cache_create(ctypes.byref(self.cfg), ctypes.byref(b), ctypes.byref(self._cache)))
+
+    @classmethod
+    def allocate(cls, *, n_layers, n_pages, page_size, n_q_heads, n_kv_heads, head_dim, max_batch, max_pages, max_nodes,
+                 dtype="bf16", device="cuda"):
+        """An empty cache with memory of its own."""
+        import torch
+        t = torch.bfloat16 if dtype == "bf16" else torch.float32
+        shape = (n_layers, n_pages, n_kv_heads, page_size, head_dim)
+
+        def ints(*s):
+            return torch.zeros(s, dtype=torch.int32, device=device)
+
+        return cls(k=torch.empty(shape, dtype=t, device=device), v=torch.empty(shape, dtype=t, device=device),
+                   table=ints(max_batch, max_pages) - 1, lens=ints(max_batch), held=ints(max_batch), refs=ints(n_pages),
+                   free=torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device), n_free=ints(1) + n_pages,
+                   n_q_heads=n_q_heads, max_nodes=max_nodes)
+
+    def close(self):
+        if self._cache:
+            self._L.dflare_cache_destroy(self._cache)
+            self._cache = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def error(self, stream=None) -> int:
+        """DEVERR_* bits that kernels have set since the last call (synchronises the stream)."""
+        bits = ctypes.c_uint32(0)
+        st = self._L.dflare_cache_error(self._cache, ctypes.byref(bits), _stream(stream))
+        if st not in (_lib.DFLARE_OK, _lib.DFLARE_EDEVICE):
+            _check(st)
+        return bits.value
+
+    def reserve(self, n_new, stream=None):
+        """Room for n_new [batch] tokens behind every sequence's length (all sequences or none)."""
+        _check(self._L.dflare_cache_reserve(self._cache, _ints("n_new", n_new, 1), n_new.numel(), _stream(stream)))
+
+    def append(self, layer, q, k, v, n_new, phase, q_out, *, depth=None, layout="half", magnitude=1.0, stream=None):
+        """A layer's new tokens: q [batch][n][n_q_heads][head_dim] rotated into q_out (q itself: in place), k
+        and v [batch][n][n_kv_heads][head_dim] into the pages. q and q_out None: keys and values only. phase
+        None: no rotation. depth int32 [batch][n]: positions relative to lens (None: 0, 1, 2, ...)."""
+        batch, n = k.shape[:2]
+        kv = (batch, n, self.n_kv_heads, self.head_dim)
+        kp, ks = _rows("k", k, self.dtype, kv)
+        vp, vs = _rows("v", v, self.dtype, kv)
+        qp = op = None
+        qs = os_ = 0
+        if q is not None or q_out is not None:
+            if q is None or q_out is None:
+                raise ValueError("q and q_out go together")
+            shape = (batch, n, self.n_q_heads, self.head_dim)
+            qp, qs = _rows("q", q, self.dtype, shape)
+            op, os_ = (qp, qs) if q_out is q else _rows("q_out", q_out, self.dtype, shape)
+        _check(self._L.dflare_cache_append(
+            self._cache, layer, qp, qs, kp, ks, vp, vs, op, os_,
+            None if depth is None else _ints("depth", depth, batch * n), _ints("n_new", n_new, batch), batch, n,
+            None if phase is None else _phase(phase), 0 if phase is None else 2 * phase.numel(), _layout(layout), magnitude,
+            _stream(stream)))
+
+    def attend(self, layer, q, n_nodes, out, *, mask=None, scale=None, lse=None, stream=None):
+        """Attention of q [batch][n][n_q_heads][head_dim] over the pages into out (contiguous). mask: the
+        ancestor bits of tree_plan (None: node i sees nodes 0 .. i). scale: head_dim^-0.5 if None. lse: optional
+        fp32 [batch][n][n_q_heads]."""
+        import torch
+        if q.dim() != 4:
+            raise ValueError(f"q must be [batch][n][n_q_heads][head_dim], got {list(q.shape)}")
+        batch, n = q.shape[:2]
+        qp, qs = _rows("q", q, self.dtype, (batch, n, self.n_q_heads, self.head_dim))
+        _typed("out", out, self.dtype)
+        if out.shape != q.shape or not out.is_contiguous():
+            raise ValueError(f"out must be contiguous {list(q.shape)}, got {list(out.shape)}")
+        lp = None
+        if lse is not None:
+            _typed("lse", lse, torch.float32)
+            if lse.numel() < batch * n * self.n_q_heads or not lse.is_contiguous():
+                raise ValueError(f"lse must be contiguous and hold {batch * n * self.n_q_heads} elements")
+            lp = lse.data_ptr()
+        _check(self._L.dflare_cache_attend(
+            self._cache, layer, qp, qs, None if mask is None else _ints("mask", mask, batch * n * ((n + 31) // 32)),
+            _ints("n_nodes", n_nodes, batch), batch, n, self.head_dim ** -0.5 if scale is None else scale, out.data_ptr(), lp,
+            _stream(stream)))
+
+    def commit(self, accept_len, path, stream=None):
+        """Keep the nodes path[b][: accept_len[b]] (int32 [batch], [batch][n]) behind every length, moved
+        together, and give the other pages back."""
+        if path.dim() != 2:
+            raise ValueError(f"path must be [batch][n], got {list(path.shape)}")
+        batch, row = path.shape
+        _check(self._L.dflare_cache_commit(self._cache, _ints("accept_len", accept_len, batch), _ints("path", path, 0), row, batch,
+                                           _stream(stream)))
+
+    def truncate(self, new_len, stream=None):
+        """Cut sequences to new_len [batch] tokens at most; 0 ends one. Pages past that are given back."""
+        _check(self._L.dflare_cache_truncate(self._cache, _ints("new_len", new_len, 1), new_len.numel(), _stream(stream)))
+
+    def fork(self, src, dst, stream=None):
+        """Sequences dst [n] (which hold nothing) become copies of sequences src [n] that share their pages."""
+        _check(self._L.dflare_cache_fork(self._cache, _ints("src", src, 1), _ints("dst", dst, src.numel()), src.numel(),
+                                         _stream(stream)))
+
+    def copy_pages(self, src, dst, stream=None):
+        """Copy pages src [n] to pages dst [n] in every layer."""
+        _check(self._L.dflare_cache_copy_pages(self._cache, _ints("src", src, 1), _ints("dst", dst, src.numel()), src.numel(),
+                                               _stream(stream)))
