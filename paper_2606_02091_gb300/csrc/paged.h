@@ -35,7 +35,6 @@ struct dflare_cache {
     int32_t* copies = nullptr;     // [1 + 3 * kMaxSeqs]: count, then (source page, page, tokens) of a reserve
     float* part_o = nullptr;       // attention: partial outputs of rows whose keys several CTAs read
     float2* part_ml = nullptr;     // their (maximum in log2 units, sum)
-    int32_t* plan = nullptr;       // attention: the launch's division of the work (see tree_sched.cuh)
     size_t part_rows = 0;          // rows of part_o
     CUtensorMap maps[2];           // K and V pools (bf16)
 };
@@ -53,17 +52,19 @@ struct TreeArgs {
     float* lse;                // [batch][n_max][hq], optional
     float* part_o;
     float2* part_ml;
-    int32_t* plan;
     int layer, batch, n_max, words, hq, G;   // G: query heads per kv head
+    uint32_t G_inv;            // 2^32 / G, rounded up (G > 1)
     int QG, C;                 // groups of query rows, and CTAs along the keys for each
     float scale_log2;
 };
 
+// the tcgen05 kernel's keys per tile, and how its work is divided (see tree_sched.cuh)
+constexpr int kTcKeys = 128, kTcExtra = 2, kTcLeast = 3;
+
 cudaError_t launch_tree_attention(dflare_cache* c, TreeArgs a, cudaStream_t s);
-// tcgen05 kernel for many query rows per kv head (bf16)
-cudaError_t launch_tree_attention_tc(dflare_cache* c, TreeArgs a, cudaStream_t s);
+// tcgen05 kernel for many query rows per kv head (bf16); sets a.QG, a.C and the rows of a query group
+cudaError_t launch_tree_attention_tc(dflare_cache* c, TreeArgs& a, int* QT, cudaStream_t s);
 // rows of the partial buffers that any launch of a cache may use
 size_t tree_partial_rows(const dflare_cache_config& g, int num_sms);
-size_t tree_plan_size(const dflare_cache_config& g);      // ints of the plan
 
 }  // namespace dfl

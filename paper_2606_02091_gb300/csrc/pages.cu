@@ -437,8 +437,7 @@ dflare_status dflare_cache_create(const dflare_cache_config* cfg, const dflare_c
         cudaMalloc(&c->last, (size_t)cfg->n_pages * sizeof(int32_t)) != cudaSuccess ||
         cudaMalloc(&c->copies, (1 + 3 * kMaxSeqs) * sizeof(int32_t)) != cudaSuccess ||
         cudaMalloc(&c->part_o, c->part_rows * cfg->head_dim * sizeof(float)) != cudaSuccess ||
-        cudaMalloc(&c->part_ml, c->part_rows * sizeof(float2)) != cudaSuccess ||
-        cudaMalloc(&c->plan, tree_plan_size(*cfg) * sizeof(int32_t)) != cudaSuccess) {
+        cudaMalloc(&c->part_ml, c->part_rows * sizeof(float2)) != cudaSuccess) {
         cudaGetLastError();
         return give_up(DFLARE_ENOMEM, "dflare_cache_create: device memory");
     }
@@ -472,7 +471,6 @@ dflare_status dflare_cache_destroy(dflare_cache* c) {
     cudaFree(c->copies);
     cudaFree(c->part_o);
     cudaFree(c->part_ml);
-    cudaFree(c->plan);
     delete c;
     return DFLARE_OK;
 }

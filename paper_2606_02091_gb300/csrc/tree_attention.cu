@@ -55,34 +55,37 @@ __device__ __forceinline__ uint32_t tile_at(int r, int c) {
 __device__ __forceinline__ void compute_barrier() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
 constexpr int kKeys = 64;           // keys per tile
-constexpr int kStages = 3;
+constexpr int kRows = 16;
+constexpr int kStages = 2;
 constexpr int kMmaThreads = 160;
-constexpr int kMinTiles = 2;
+constexpr int kExtra = 3, kLeast = 4;      // see tree_sched.cuh
 
 template <int HD>
 struct MmaLayout {
     static constexpr uint32_t TB = HD * 128;                    // a tile of K or V
-    static constexpr uint32_t SCRATCH = kStages * 2 * TB;       // partial outputs between warps: half of a row's elements
-    static constexpr uint32_t BARS = SCRATCH + 64 * HD;
+    static constexpr uint32_t Q = kStages * 2 * TB;             // two pairs' rows, [HD / 64][16][128 B] each
+    static constexpr uint32_t SWAP = Q + 2 * kRows * HD * 2;    // [4 owners][3][HD / 32][32 lanes] float4
+    static constexpr uint32_t BARS = SWAP + 4 * 3 * HD * 16;
     static constexpr uint32_t BYTES = BARS + 2 * kStages * 8;
 };
 
-// bf16, up to 16 WR query rows. Four warps: WR row blocks of 16 x (4 / WR) parts of each 64-key tile; a
-// fifth warp's thread streams the tiles' pages by TMA into a ring of stages. Every warp keeps its own running
-// maximum and sum; the parts are joined in shared memory when a pair's keys are done.
-template <int HD, int WR>
+// bf16, up to 16 query rows per kv head (single tokens, small trees). Four warps take 16 keys of each 64-key tile
+// each; a fifth warp streams the tiles' pages by TMA into a ring of stages. Every warp keeps its own running
+// maximum and sum; when a pair's keys are done each warp sums up a quarter of the head dims of all four.
+// HBM-bound for long contexts; for short ones by its chain of latencies (lengths, page table, keys).
+template <int HD>
 __global__ void __launch_bounds__(kMmaThreads, 2) tree_mma_kernel(const __grid_constant__ CUtensorMap mk,
                                                                   const __grid_constant__ CUtensorMap mv, const TreeArgs a) {
     using LY = MmaLayout<HD>;
-    constexpr int QT = 16 * WR, WK = 4 / WR, KW = kKeys / WK;   // rows, key parts, keys per part
     constexpr uint32_t TB = LY::TB;
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ int32_t cum[kMaxSeqs + 1];
     __shared__ uint32_t odd[kMaxNodes / 32];    // nodes with an infinite or NaN value
     __shared__ int odd_any;
     __shared__ int abort_flag;
+    __shared__ float2 ml[4][kRows];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int qg = blockIdx.x % a.QG, c = blockIdx.x / a.QG;
+    const int c = blockIdx.x;
     const uint32_t sb = smem_u32(smem), full = sb + LY::BARS, empty = full + 8 * kStages;
     if (tid == 0) {
         for (int i = 0; i < kStages; ++i) {
@@ -95,185 +98,199 @@ __global__ void __launch_bounds__(kMmaThreads, 2) tree_mma_kernel(const __grid_c
     }
     if (tid < kMaxNodes / 32) odd[tid] = 0;
     pdl_wait();
-    int t0, t1;
-    tree_runs<QT, kKeys, kMinTiles>(a, qg, c, cum, t0, t1);
-    pdl_trigger();
+    pdl_trigger();      // the joining launch reads the lengths at once: after this kernel's own wait
+    int v, v1;
+    tree_runs<kRows, kKeys, kExtra, kLeast>(a, 0, c, cum, v, v1);
+    const int v0 = v;
+    TreePair p, after;
+    if (!tree_pair<kExtra>(a, cum, v, v1, p)) return;
 
     if (warp == 4) {
-        // ---------------- stream the tiles: box = up to 64 tokens of a page x 64 head dims; slots without
-        // a page take a box outside the pool, which reads as zero
-        if (elect_one()) {
-            const int rows = min(a.pg.ps, kKeys), boxes = kKeys / rows;
-            const int nowhere = (int)min(0x7fffffffLL, (long long)a.pg.layers * a.pg.pages * a.pg.hkv);
-            bool ok = true;
-            int i = 0;
-            for (int t = t0; t < t1 && ok;) {
-                const TreeItem it = tree_item(cum, a.batch, a.pg.hkv, t);
-                const int end = min(t1, it.start + it.tiles);
-                const int32_t* table = a.pg.table + (size_t)it.b * a.pg.max_pages;
-                const int pages = min(max(a.pg.held[it.b], 0), a.pg.max_pages);
-                for (; t < end && ok; ++t, ++i) {
-                    const int st = i % kStages;
-                    if (i >= kStages && !(ok = bar_wait(empty + 8 * st, (uint32_t)(i / kStages - 1) & 1u, &abort_flag, a.pg.err))) break;
-                    const uint32_t bar = full + 8 * st, kd = sb + st * 2 * TB;
-                    mbar_expect_tx(bar, 2 * TB);
-                    for (int x = 0; x < boxes; ++x) {
-                        const long long slot = (long long)(t - it.start) * kKeys + x * rows;
-                        const int pi = (int)(slot / a.pg.ps);
-                        const int page = pi < pages ? table[pi] : -1;
-                        const int z = page >= 0 && page < a.pg.pages ? (a.layer * a.pg.pages + page) * a.pg.hkv + it.h : nowhere;
-                        const int y = (int)(slot % a.pg.ps);
-                        for (int h = 0; h < HD / 64; ++h) {
-                            tma_load_3d(kd + h * 8192 + x * rows * 128, &mk, h * 64, y, z, bar);
-                            tma_load_3d(kd + TB + h * 8192 + x * rows * 128, &mv, h * 64, y, z, bar);
-                        }
+        // ---------------- stream the tiles: a box is up to 64 tokens of a page x 64 head dims
+        const bool leader = elect_one();
+        const int rows = min(a.pg.ps, kKeys), boxes = kKeys / rows;
+        bool ok = true, more = true;
+        int i = 0;
+        TileBoxes next = tile_boxes(a, p, p.lo, kKeys, rows, lane);
+        // the first pair's queries go first: behind the ring's tiles they would arrive after all of them
+        asm volatile("bar.sync 2, 160;" ::: "memory");
+        for (int t = p.lo; more; ++i) {
+            const TileBoxes now = next;
+            if (++t == p.hi) {
+                more = tree_pair<kExtra>(a, cum, v, v1, p);
+                t = p.lo;
+            }
+            if (more) next = tile_boxes(a, p, t, kKeys, rows, lane);
+            const int st = i % kStages;
+            if (i >= kStages) ok = __all_sync(0xffffffffu, bar_wait(empty + 8 * st, (uint32_t)(i / kStages - 1) & 1u, &abort_flag, a.pg.err));
+            if (!ok) break;
+            const uint32_t bar = full + 8 * st, kd = sb + st * 2 * TB;
+            if (leader) mbar_expect_tx(bar, 2 * TB);
+            for (int x = 0; x < boxes; ++x) {
+                const int z = __shfl_sync(0xffffffffu, now.plane, x);
+                const int y = (now.first_slot + x * rows) & (a.pg.ps - 1);
+                if (leader) {
+#pragma unroll
+                    for (int h = 0; h < HD / 64; ++h) {
+                        tma_load_3d(kd + h * 8192 + x * rows * 128, &mk, h * 64, y, z, bar);
+                        tma_load_3d(kd + TB + h * 8192 + x * rows * 128, &mv, h * 64, y, z, bar);
                     }
                 }
             }
-            if (!ok) {   // the copies in flight land before the CTA's shared memory is given up
-                volatile int never = 0;
-                for (int j = max(0, i - kStages); j < i; ++j)
-                    bar_wait(full + 8 * (j % kStages), (uint32_t)(j / kStages) & 1u, &never, a.pg.err);
-            }
+        }
+        if (!ok && leader) {   // the copies in flight land before the CTA's shared memory is given up
+            volatile int never = 0;
+            for (int j = max(0, i - kStages); j < i; ++j)
+                bar_wait(full + 8 * (j % kStages), (uint32_t)(j / kStages) & 1u, &never, a.pg.err);
         }
         return;
     }
 
-    const int wr = warp % WR, wk = warp / WR;    // row block, key part
-    const int r0 = wr * 16 + (lane >> 2);        // this thread's rows r0 and r0 + 8 of the group
+    const int r0 = lane >> 2;                    // this thread's rows r0 and r0 + 8
     const int cp = (lane & 3) * 2;
+    // Q of a pair into half `buf` of its memory, asynchronously: rows past R are never looked at
+    auto load_q = [&](const TreePair& p, int R, int buf) {
+        constexpr int PC = HD / 8;
+#pragma unroll
+        for (int x = tid; x < kRows * PC; x += 128) {
+            const int r = x / PC, pc = x % PC, nd = group_of(a, r);
+            if (r < R)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(sb + LY::Q + buf * (kRows * HD * 2) + (pc >> 3) * (kRows * 128) + r * 128 + (((pc & 7) ^ (r & 7)) << 4)),
+                             "l"(static_cast<const bf16*>(a.q) + ((size_t)p.b * a.n_max + nd) * a.q_row + (size_t)(p.h * a.G + r - nd * a.G) * HD + pc * 8)
+                             : "memory");
+        }
+    };
+    TreeRaw raw = tree_raw(a, p.b);
+    int n, ctx, keys;
+    tree_lengths(a, raw, n, ctx, keys);
+    load_q(p, n * a.G, 0);
+    asm volatile("bar.arrive 2, 160;" ::: "memory");
     // After a wait that gave up the warps go on without waiting: the results are invalid and the error is
     // set, and every barrier among the four still meets.
-    bool ok = true;
+    bool ok = true, more = true;
     int i = 0;
-    for (int t = t0; t < t1;) {
-        const TreeItem it = tree_item(cum, a.batch, a.pg.hkv, t);
-        const int first = t, end = min(t1, it.start + it.tiles);
-        int n, ctx, keys;
-        tree_lengths(a, it.b, n, ctx, keys);
-        const int R = n * a.G, base = qg * QT;
-        // Q fragments straight from global memory: rows past R are zero
-        uint32_t qa[HD / 16][4];
+    for (int pair = 0; more; ++pair) {
+        const int R = n * a.G;
         int node[2];
+        SeenRow row[2];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            const int r = base + r0 + 8 * half;
-            node[half] = min(r, R - 1) / a.G;
-            const bf16* q = static_cast<const bf16*>(a.q) + ((size_t)it.b * a.n_max + node[half]) * a.q_row +
-                            (size_t)(it.h * a.G + min(r, R - 1) % a.G) * HD + cp;
+            node[half] = group_of(a, min(r0 + 8 * half, R - 1));
+            row[half] = seen_row(a, p.b, node[half]);
+        }
+        more = tree_pair<kExtra>(a, cum, v, v1, after);
+        if (more) raw = tree_raw(a, after.b);
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        compute_barrier();
+        uint32_t qa[HD / 16][4];
 #pragma unroll
-            for (int kk = 0; kk < HD / 16; ++kk) {
-                qa[kk][half] = r < R ? *reinterpret_cast<const uint32_t*>(q + kk * 16) : 0u;
-                qa[kk][2 + half] = r < R ? *reinterpret_cast<const uint32_t*>(q + kk * 16 + 8) : 0u;
-            }
+        for (int kk = 0; kk < HD / 16; ++kk) {
+            const int r = lane & 15, pc = kk * 2 + (lane >> 4);
+            ldsm4(sb + LY::Q + (pair & 1) * (kRows * HD * 2) + (pc >> 3) * (kRows * 128) + r * 128 + (((pc & 7) ^ (r & 7)) << 4), qa[kk][0], qa[kk][1],
+                  qa[kk][2], qa[kk][3]);
         }
         float o[HD / 8][4];
 #pragma unroll
         for (int x = 0; x < HD / 8; ++x) o[x][0] = o[x][1] = o[x][2] = o[x][3] = 0.f;
         float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+        int n2 = 0, ctx2 = 0, keys2 = 0;
 
-        for (; t < end; ++t, ++i) {
+        for (int t = p.lo; t < p.hi; ++t, ++i) {
             const int st = i % kStages;
             if (ok) ok = __all_sync(0xffffffffu, bar_wait(full + 8 * st, (uint32_t)(i / kStages) & 1u, &abort_flag, a.pg.err));
+            if (more && t == p.lo) {    // the next pair's queries, a pair ahead
+                tree_lengths(a, raw, n2, ctx2, keys2);
+                load_q(after, n2 * a.G, (pair + 1) & 1);
+            }
             const uint32_t sK = sb + st * 2 * TB, sV = sK + TB;
-            const int k0 = (t - it.start) * kKeys;
+            const int k0 = t * kKeys, kw = k0 + warp * 16;      // this warp's keys: kw .. kw + 15
             const bool edge = k0 + kKeys > ctx;          // nodes of the tree, or slots past the last key
-            if (edge) {
-                // values: slots past the last key and infinite or NaN values of nodes become 0
-                for (int x = tid; x < kKeys * (HD / 8); x += 128) {
-                    const int r = x / (HD / 8), key = k0 + r;
-                    if (key < ctx) continue;
-                    uint4* p = reinterpret_cast<uint4*>(smem + st * 2 * TB + TB + tile_at(r, x % (HD / 8)));
-                    uint4 v = key < keys ? *p : make_uint4(0u, 0u, 0u, 0u);
-                    uint32_t* w = reinterpret_cast<uint32_t*>(&v);
-                    bool bad = false;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if ((w[e] & 0x7f80u) == 0x7f80u) { w[e] &= 0xffff0000u; bad = true; }
-                        if ((w[e] & 0x7f800000u) == 0x7f800000u) { w[e] &= 0xffffu; bad = true; }
+            if (kw < keys) {
+                if (kw + 16 > ctx) {
+                    // this warp's values: slots past the last key and infinite or NaN values of nodes become 0
+#pragma unroll 1
+                    for (int x = lane; x < 16 * (HD / 8); x += 32) {
+                        const int r = warp * 16 + x / (HD / 8), key = k0 + r;
+                        if (key < ctx) continue;
+                        uint4* at = reinterpret_cast<uint4*>(smem + st * 2 * TB + TB + tile_at(r, x % (HD / 8)));
+                        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                        bool bad = key >= keys;
+                        if (!bad) {
+                            v = *at;
+                            bad = drop_odd(v);
+                            if (bad) {
+                                atomicOr(&odd[(key - ctx) >> 5], 1u << ((key - ctx) & 31));
+                                odd_any = 1;
+                            }
+                        }
+                        if (bad) *at = v;
                     }
-                    if (bad) {
-                        atomicOr(&odd[(key - ctx) >> 5], 1u << ((key - ctx) & 31));
-                        odd_any = 1;
+                    // (these stores before the stage's next copy)
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                }
+                float s[2][4];
+#pragma unroll
+                for (int x = 0; x < 2; ++x) s[x][0] = s[x][1] = s[x][2] = s[x][3] = 0.f;
+#pragma unroll
+                for (int kk = 0; kk < HD / 16; kk += 2) {
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        uint32_t b0, b1, b2, b3;
+                        ldsm4(sK + tile_at(warp * 16 + x * 8 + (lane & 7), kk * 2 + (lane >> 3)), b0, b1, b2, b3);
+                        mma_bf16(s[x], qa[kk], b0, b1);
+                        mma_bf16(s[x], qa[kk + 1], b2, b3);
                     }
-                    if (bad || key >= keys) *p = v;
                 }
-                // (these stores before the stage's next copy)
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                compute_barrier();
-            }
-            float s[KW / 8][4];
+                if (edge) {
 #pragma unroll
-            for (int x = 0; x < KW / 8; ++x) s[x][0] = s[x][1] = s[x][2] = s[x][3] = 0.f;
+                    for (int half = 0; half < 2; ++half) {
+                        const uint32_t seen = seen32(a, row[half], p.b, node[half], ctx, keys, kw);
 #pragma unroll
-            for (int kk = 0; kk < HD / 16; kk += 2) {
+                        for (int x = 0; x < 2; ++x)
 #pragma unroll
-                for (int x = 0; x < KW / 8; ++x) {
-                    uint32_t b0, b1, b2, b3;
-                    ldsm4(sK + tile_at(wk * KW + x * 8 + (lane & 7), kk * 2 + (lane >> 3)), b0, b1, b2, b3);
-                    mma_bf16(s[x], qa[kk], b0, b1);
-                    mma_bf16(s[x], qa[kk + 1], b2, b3);
+                            for (int e = 0; e < 2; ++e)
+                                if (!((seen >> (x * 8 + cp + e)) & 1u)) s[x][2 * half + e] = -INFINITY;
+                    }
                 }
-            }
-            if (edge) {
+                float alpha[2];
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
-                    const uint64_t seen = tree_seen(a, it.b, node[half], ctx, keys, k0) >> (wk * KW);
+                    float mx = fmaxf(fmaxf(s[0][2 * half], s[0][2 * half + 1]), fmaxf(s[1][2 * half], s[1][2 * half + 1])) * a.scale_log2;
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+                    const float top = fmaxf(m[half], mx), ref = top == -INFINITY ? 0.f : top;
+                    alpha[half] = pow2(m[half] - ref);
+                    m[half] = top;
+                    float sum = 0.f;
 #pragma unroll
-                    for (int x = 0; x < KW / 8; ++x)
+                    for (int x = 0; x < 2; ++x) {
 #pragma unroll
-                        for (int e = 0; e < 2; ++e)
-                            if (!((seen >> (x * 8 + cp + e)) & 1)) s[x][2 * half + e] = -INFINITY;
+                        for (int e = 0; e < 2; ++e) {
+                            const float w = pow2(fmaf(s[x][2 * half + e], a.scale_log2, -ref));
+                            s[x][2 * half + e] = w;
+                            sum += w;
+                        }
+                    }
+                    l[half] = l[half] * alpha[half] + sum;
                 }
-            }
-            uint32_t pa[KW / 16][4];
-            float alpha[2];
+                // weights rounded to bf16 for the product (relative error 2^-8 at most); the sum is of unrounded ones
+                const uint32_t pa[4] = {two_bf16(s[0][0], s[0][1]), two_bf16(s[0][2], s[0][3]), two_bf16(s[1][0], s[1][1]), two_bf16(s[1][2], s[1][3])};
+                if (__any_sync(0xffffffffu, alpha[0] != 1.f || alpha[1] != 1.f)) {
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                float mx = -INFINITY;
-#pragma unroll
-                for (int x = 0; x < KW / 8; ++x) mx = fmaxf(mx, fmaxf(s[x][2 * half] * a.scale_log2, s[x][2 * half + 1] * a.scale_log2));
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-                const float top = fmaxf(m[half], mx), ref = top == -INFINITY ? 0.f : top;
-                alpha[half] = pow2(m[half] - ref);
-                m[half] = top;
-                float sum = 0.f;
-#pragma unroll
-                for (int x = 0; x < KW / 8; ++x) {
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const float p = pow2(fmaf(s[x][2 * half + e], a.scale_log2, -ref));
-                        s[x][2 * half + e] = p;
-                        sum += p;
+                    for (int x = 0; x < HD / 8; ++x) {
+                        o[x][0] *= alpha[0];
+                        o[x][1] *= alpha[0];
+                        o[x][2] *= alpha[1];
+                        o[x][3] *= alpha[1];
                     }
                 }
-                l[half] = l[half] * alpha[half] + sum;
-            }
-#pragma unroll
-            for (int x = 0; x < KW / 16; ++x) {
-                pa[x][0] = two_bf16(s[2 * x][0], s[2 * x][1]);
-                pa[x][1] = two_bf16(s[2 * x][2], s[2 * x][3]);
-                pa[x][2] = two_bf16(s[2 * x + 1][0], s[2 * x + 1][1]);
-                pa[x][3] = two_bf16(s[2 * x + 1][2], s[2 * x + 1][3]);
-            }
-            if (__any_sync(0xffffffffu, alpha[0] != 1.f || alpha[1] != 1.f)) {
-#pragma unroll
-                for (int x = 0; x < HD / 8; ++x) {
-                    o[x][0] *= alpha[0];
-                    o[x][1] *= alpha[0];
-                    o[x][2] *= alpha[1];
-                    o[x][3] *= alpha[1];
-                }
-            }
-#pragma unroll
-            for (int kk = 0; kk < KW / 16; ++kk) {
 #pragma unroll
                 for (int x = 0; x < HD / 16; ++x) {
                     uint32_t b0, b1, b2, b3;
-                    ldsm4t(sV + tile_at(wk * KW + kk * 16 + (lane & 15), x * 2 + (lane >> 4)), b0, b1, b2, b3);
-                    mma_bf16(o[2 * x], pa[kk], b0, b1);
-                    mma_bf16(o[2 * x + 1], pa[kk], b2, b3);
+                    ldsm4t(sV + tile_at(warp * 16 + (lane & 15), x * 2 + (lane >> 4)), b0, b1, b2, b3);
+                    mma_bf16(o[2 * x], pa, b0, b1);
+                    mma_bf16(o[2 * x + 1], pa, b2, b3);
                 }
             }
             __syncwarp();
@@ -284,109 +301,94 @@ __global__ void __launch_bounds__(kMmaThreads, 2) tree_mma_kernel(const __grid_c
         for (int half = 0; half < 2; ++half) {
             l[half] += __shfl_xor_sync(0xffffffffu, l[half], 1);
             l[half] += __shfl_xor_sync(0xffffffffu, l[half], 2);
+            if ((lane & 3) == 0) ml[warp][r0 + 8 * half] = make_float2(m[half], l[half]);
         }
-        // join the key parts: parts 1 and 3 into 0 and 2, then 2 into 0
-        float* scratch = reinterpret_cast<float*>(smem + LY::SCRATCH);
-        if constexpr (WK > 1) {
-            __shared__ float2 ml[4][16];
-#pragma unroll
-            for (int step = 1; step < WK; step *= 2) {
-                const bool gives = (wk & (2 * step - 1)) == step, takes = (wk & (2 * step - 1)) == 0;
-                float* at = scratch + ((wk / (2 * step)) * WR + wr) * (8 * HD);
-                float mine[2] = {1.f, 1.f}, other[2] = {0.f, 0.f};
-                if (gives && (lane & 3) == 0) {
-                    ml[warp][lane >> 2] = make_float2(m[0], l[0]);
-                    ml[warp][(lane >> 2) + 8] = make_float2(m[1], l[1]);
-                }
-#pragma unroll
-                for (int part = 0; part < 2; ++part) {
-                    if (gives) {
-#pragma unroll
-                        for (int x = 0; x < HD / 16; ++x) {
-                            const float* v = o[part * (HD / 16) + x];
-                            *reinterpret_cast<float4*>(at + (x * 32 + lane) * 4) = make_float4(v[0], v[1], v[2], v[3]);
-                        }
-                    }
-                    compute_barrier();
-                    if (takes) {
-                        if (part == 0) {
-#pragma unroll
-                            for (int half = 0; half < 2; ++half) {
-                                const float2 v = ml[warp + step * WR][(lane >> 2) + 8 * half];
-                                const float top = fmaxf(m[half], v.x), ref = top == -INFINITY ? 0.f : top;
-                                mine[half] = pow2(m[half] - ref);
-                                other[half] = pow2(v.x - ref);
-                                m[half] = top;
-                                l[half] = l[half] * mine[half] + v.y * other[half];
-                            }
-                        }
-#pragma unroll
-                        for (int x = 0; x < HD / 16; ++x) {
-                            const float4 v = *reinterpret_cast<const float4*>(at + (x * 32 + lane) * 4);
-                            float* w = o[part * (HD / 16) + x];
-                            w[0] = w[0] * mine[0] + v.x * other[0];
-                            w[1] = w[1] * mine[0] + v.y * other[0];
-                            w[2] = w[2] * mine[1] + v.z * other[1];
-                            w[3] = w[3] * mine[1] + v.w * other[1];
-                        }
-                    }
-                    compute_barrier();
-                }
-            }
-        }
-        if (wk == 0) {
-            const bool partial = first != it.start || end != it.start + it.tiles;
-            const int slot = it.start < t0 ? 0 : 1;
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const int r = base + r0 + 8 * half;
-                if (r >= R) continue;
-                if (odd_any) {
-                    // infinite and NaN values of the nodes that this row sees, in this run's part of the keys
-                    for (int w = 0; w < a.words; ++w) {
-                        uint32_t bits = odd[w];
-                        while (bits) {
-                            const int j = w * 32 + __ffs(bits) - 1;
-                            bits &= bits - 1;
-                            if (!(tree_seen(a, it.b, node[half], ctx, keys, ctx + j) & 1)) continue;
-                            const int key = ctx + j, page = a.pg.table[(size_t)it.b * a.pg.max_pages + key / a.pg.ps];
-                            const bf16* v = static_cast<const bf16*>(a.pg.v) +
-                                            ((((size_t)a.layer * a.pg.pages + page) * a.pg.hkv + it.h) * a.pg.ps + key % a.pg.ps) * HD;
-                            for (int x = 0; x < HD / 8; ++x)
-#pragma unroll
-                                for (int e = 0; e < 2; ++e) {
-                                    const float f = to_f(v[x * 8 + cp + e]);
-                                    if (!isfinite(f)) o[x][2 * half + e] += f;
-                                }
-                        }
-                    }
-                }
-                if (partial) {
-                    const size_t row = (((size_t)c * a.QG + qg) * 2 + slot) * QT + r0 + 8 * half;
-#pragma unroll
-                    for (int x = 0; x < HD / 8; ++x)
-                        *reinterpret_cast<float2*>(a.part_o + row * HD + x * 8 + cp) = make_float2(o[x][2 * half], o[x][2 * half + 1]);
-                    if ((lane & 3) == 0) a.part_ml[row] = make_float2(m[half], l[half]);
-                } else {
-                    const size_t row = ((size_t)it.b * a.n_max + node[half]) * a.hq + it.h * a.G + r % a.G;
-                    const float inv = l[half] > 0.f ? 1.f / l[half] : l[half] == 0.f ? 0.f : l[half];
-#pragma unroll
-                    for (int x = 0; x < HD / 8; ++x)
-                        *reinterpret_cast<uint32_t*>(static_cast<bf16*>(a.out) + row * HD + x * 8 + cp) =
-                            two_bf16(o[x][2 * half] * inv, o[x][2 * half + 1] * inv);
-                    if (a.lse && (lane & 3) == 0)
-                        a.lse[row] = l[half] == 0.f ? -INFINITY : (m[half] + log2f(l[half])) * 0.69314718055994531f;
-                }
-            }
-        }
-        // the next pair starts with no odd nodes, once every warp has looked
         compute_barrier();
-        if (odd_any) {
+        // every warp's output against the common maximum; quarter q of the head dims goes to warp q
+        float M[2], L[2];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            float2 x[4];
+#pragma unroll
+            for (int w = 0; w < 4; ++w) x[w] = ml[w][r0 + 8 * half];
+            M[half] = fmaxf(fmaxf(x[0].x, x[1].x), fmaxf(x[2].x, x[3].x));
+            const float ref = M[half] == -INFINITY ? 0.f : M[half];
+            L[half] = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) L[half] += x[w].y * pow2(x[w].x - ref);
+            const float f = pow2(m[half] - ref);
+#pragma unroll
+            for (int y = 0; y < HD / 8; ++y) {
+                o[y][2 * half] *= f;
+                o[y][2 * half + 1] *= f;
+            }
+        }
+        const bool odds = odd_any != 0;
+        constexpr int QB = HD / 32;      // blocks of eight head dims in a quarter
+        float4* swap = reinterpret_cast<float4*>(smem + LY::SWAP);
+        float mine[QB][4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+#pragma unroll
+            for (int y = 0; y < QB; ++y) {
+                if (q == warp) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) mine[y][e] = o[q * QB + y][e];
+                } else {
+                    swap[((q * 3 + ((warp - q) & 3) - 1) * QB + y) * 32 + lane] = make_float4(o[q * QB + y][0], o[q * QB + y][1], o[q * QB + y][2], o[q * QB + y][3]);
+                }
+            }
+        }
+        compute_barrier();
+#pragma unroll
+        for (int w = 0; w < 3; ++w)
+#pragma unroll
+            for (int y = 0; y < QB; ++y) {
+                const float4 x = swap[((warp * 3 + w) * QB + y) * 32 + lane];
+                mine[y][0] += x.x;
+                mine[y][1] += x.y;
+                mine[y][2] += x.z;
+                mine[y][3] += x.w;
+            }
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int r = r0 + 8 * half, col = warp * (HD / 4) + cp;
+            if (r >= R) continue;
+            if (odds)
+                each_odd(a, odd, p, node[half], ctx, keys, [&](size_t at) {
+                    for (int y = 0; y < QB; ++y)
+                        for (int e = 0; e < 2; ++e) {
+                            const float f = to_f(static_cast<const bf16*>(a.pg.v)[at + col + y * 8 + e]);
+                            if (!isfinite(f)) mine[y][2 * half + e] += f;
+                        }
+                });
+            if (p.partial()) {
+                const size_t row = ((size_t)c * 2 + (p.start < v0 ? 0 : 1)) * kRows + r;
+#pragma unroll
+                for (int y = 0; y < QB; ++y)
+                    *reinterpret_cast<float2*>(a.part_o + row * HD + col + y * 8) = make_float2(mine[y][2 * half], mine[y][2 * half + 1]);
+                if (warp == 0 && (lane & 3) == 0) a.part_ml[row] = make_float2(M[half], L[half]);
+            } else {
+                const size_t row = ((size_t)p.b * a.n_max + node[half]) * a.hq + p.h * a.G + r - node[half] * a.G;
+                const float inv = L[half] == 0.f ? 0.f : 1.f / L[half];
+#pragma unroll
+                for (int y = 0; y < QB; ++y)
+                    *reinterpret_cast<uint32_t*>(static_cast<bf16*>(a.out) + row * HD + col + y * 8) =
+                        two_bf16(mine[y][2 * half] * inv, mine[y][2 * half + 1] * inv);
+                if (a.lse && warp == 0 && (lane & 3) == 0)
+                    a.lse[row] = L[half] == 0.f ? -INFINITY : (M[half] + log2f(L[half])) * 0.69314718055994531f;
+            }
+        }
+        if (odds) {     // the next pair starts with none, once every warp has looked
             compute_barrier();
             if (tid < kMaxNodes / 32) odd[tid] = 0;
             if (tid == 0) odd_any = 0;
             compute_barrier();
         }
+        p = after;
+        n = n2;
+        ctx = ctx2;
+        keys = keys2;
     }
 }
 
@@ -395,7 +397,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) tree_mma_kernel(const __grid_c
 constexpr int kFKeys = 32;
 constexpr int kFRows = 16;
 constexpr int kFThreads = 128;
-constexpr int kFMinTiles = 2;
+constexpr int kFExtra = 2, kFLeast = 3;
 
 template <int HD>
 struct F32Layout {
@@ -413,20 +415,20 @@ __global__ void __launch_bounds__(kFThreads) tree_f32_kernel(const TreeArgs a) {
     float *Qs = fs + LY::Q, *Ks = fs + LY::K, *Vs = fs + LY::V, *Ps = fs + LY::P, *As = fs + LY::A;
     const int tid = threadIdx.x, qg = blockIdx.x % a.QG, c = blockIdx.x / a.QG;
     pdl_wait();
-    int t0, t1;
-    tree_runs<kFRows, kFKeys, kFMinTiles>(a, qg, c, cum, t0, t1);
     pdl_trigger();
+    int v, v1;
+    tree_runs<kFRows, kFKeys, kFExtra, kFLeast>(a, qg, c, cum, v, v1);
+    const int v0 = v;
     const int ry = tid / 16, kx = tid % 16;         // scores: rows 2 ry, 2 ry + 1, keys kx, kx + 16
     const int rg = tid / DG, dg = tid % DG;         // output: rows rg RR .., head dims 4 dg ..
-    for (int t = t0; t < t1;) {
-        const TreeItem it = tree_item(cum, a.batch, a.pg.hkv, t);
-        const int first = t, end = min(t1, it.start + it.tiles);
+    TreePair it;
+    while (tree_pair<kFExtra>(a, cum, v, v1, it)) {
         int n, ctx, keys;
-        tree_lengths(a, it.b, n, ctx, keys);
+        tree_lengths(a, tree_raw(a, it.b), n, ctx, keys);
         const int R = n * a.G, base = qg * kFRows;
         const int32_t* table = a.pg.table + (size_t)it.b * a.pg.max_pages;
         auto load = [&](int tile, int st) {
-            const int k0 = (tile - it.start) * kFKeys;
+            const int k0 = tile * kFKeys;
             for (int x = tid; x < kFKeys * DG; x += kFThreads) {
                 const int r = x / DG, d = x % DG * 4, key = k0 + r;
                 const int page = key < keys ? table[key / a.pg.ps] : -1;
@@ -440,7 +442,7 @@ __global__ void __launch_bounds__(kFThreads) tree_f32_kernel(const TreeArgs a) {
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
-        load(t, 0);
+        load(it.lo, 0);
         for (int x = tid; x < kFRows * DG; x += kFThreads) {
             const int r = x / DG, d = x % DG * 4, rr = base + r;
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -454,9 +456,9 @@ __global__ void __launch_bounds__(kFThreads) tree_f32_kernel(const TreeArgs a) {
         float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, o[RR][4];
 #pragma unroll
         for (int r = 0; r < RR; ++r) o[r][0] = o[r][1] = o[r][2] = o[r][3] = 0.f;
-        for (; t < end; ++t) {
-            const int st = (t - first) & 1, k0 = (t - it.start) * kFKeys;
-            if (t + 1 < end) {
+        for (int t = it.lo; t < it.hi; ++t) {
+            const int st = (t - it.lo) & 1, k0 = t * kFKeys;
+            if (t + 1 < it.hi) {
                 load(t + 1, st ^ 1);
                 asm volatile("cp.async.wait_group 1;" ::: "memory");
             } else {
@@ -547,14 +549,14 @@ __global__ void __launch_bounds__(kFThreads) tree_f32_kernel(const TreeArgs a) {
                 As[kFRows + 2 * ry + i] = l[i];
             }
         __syncthreads();
-        const bool partial = first != it.start || end != it.start + it.tiles;
+        const bool partial = it.partial();
 #pragma unroll
         for (int r = 0; r < RR; ++r) {
             const int lr = rg * RR + r, rr = base + lr;
             if (rr >= R) continue;
             const float mr = As[lr], sr = As[kFRows + lr];
             if (partial) {
-                const size_t row = (((size_t)c * a.QG + qg) * 2 + (it.start < t0 ? 0 : 1)) * kFRows + lr;
+                const size_t row = (((size_t)c * a.QG + qg) * 2 + (it.start < v0 ? 0 : 1)) * kFRows + lr;
                 *reinterpret_cast<float4*>(a.part_o + row * HD + 4 * dg) = make_float4(o[r][0], o[r][1], o[r][2], o[r][3]);
                 if (dg == 0) a.part_ml[row] = make_float2(mr, sr);
             } else {
@@ -574,26 +576,44 @@ __global__ void __launch_bounds__(kFThreads) tree_f32_kernel(const TreeArgs a) {
 constexpr int kJoinThreads = 256;
 
 template <class T, int HD>
-__global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(const TreeArgs a, int QT, int KT) {
+__global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(const TreeArgs a, int QT, int KT, int extra, int least, bool blocks) {
     constexpr int E = HD / 32;      // elements per lane
-    pdl_wait();
+    // The kernel before this one let it start after its own dependency wait, so the lengths are final here and
+    // the division of the work is found while that kernel still runs.
     const long long row = (long long)blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5);
     const int lane = threadIdx.x & 31;
     if (row >= (long long)a.batch * a.n_max * a.hq) return;
     const int head = (int)(row % a.hq), node = (int)(row / a.hq % a.n_max), b = (int)(row / a.hq / a.n_max);
     int n, ctx, keys;
-    tree_lengths(a, b, n, ctx, keys);
+    tree_lengths(a, tree_raw(a, b), n, ctx, keys);
     float acc[E], m = -INFINITY, l = 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e) acc[e] = 0.f;
-    if (node < n && keys > 0) {
-        const int r = node * a.G + head % a.G, qg = r / QT;
-        const TreePlan p = tree_plan_of(a);
-        const int32_t* cum = p.cum + (size_t)qg * (a.batch + 1);
-        const int per = p.per[qg], tiles = cum[b + 1] - cum[b];
-        const int start = cum[b] * a.pg.hkv + head / a.G * tiles;
-        const int c0 = start / per, c1 = (start + tiles - 1) / per;
-        if (c0 == c1) return;       // written by the CTA that read all of them
+    const bool some = node < n && keys > 0;
+    const int r = node * a.G + head % a.G, qg = r / QT;
+    int per = 1, start = 0, c0 = 0, c1 = 0;
+    if (some) {
+        int before = 0, total = 0;
+        for (int x = lane; x < a.batch; x += 32) {
+            const int t = tree_cost(tree_tiles(a, x, qg, QT, KT), extra);
+            total += t;
+            if (x < b) before += t;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            total += __shfl_xor_sync(0xffffffffu, total, o);
+            before += __shfl_xor_sync(0xffffffffu, before, o);
+        }
+        per = tree_run(a, total * a.pg.hkv, least);
+        const int tiles = tree_tiles(a, b, qg, QT, KT);
+        start = before * a.pg.hkv + head / a.G * tree_cost(tiles, extra);
+        c0 = start / per;
+        c1 = (start + tiles - 1) / per;
+    }
+    // every row's warp waits, so this launch does not end before the one it depends on
+    pdl_wait();
+    if (some && c0 == c1) return;       // written by the CTA that read all of them
+    if (some) {
         auto at = [&](int c) { return (((size_t)c * a.QG + qg) * 2 + (start < c * per ? 0 : 1)) * QT + r % QT; };
         for (int c = c0 + lane; c <= c1; c += 32) m = fmaxf(m, a.part_ml[at(c)].x);
         m = warp_max(m);
@@ -610,7 +630,11 @@ __global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(const TreeArgs 
 #pragma unroll 4
             for (int j = 0; j < upto; ++j) {
                 const float wj = __shfl_sync(0xffffffffu, w, j);
-                const float* src = a.part_o + at(cb + j) * HD + lane * E;
+                const size_t row = at(cb + j);
+                // the tcgen05 kernel's rows lie in blocks of 32 rows x 32 elements, 16-byte pieces swizzled
+                const float* src = a.part_o + (!blocks ? row * HD + lane * E
+                                                       : (row & ~(size_t)31) * HD + (lane * E >> 5) * 1024 + (row & 31) * 32 +
+                                                             ((((lane * E & 31) >> 2) ^ (int)(row & 7)) << 2) + (lane * E & 3));
                 float x[E];
                 if constexpr (E == 4) {
                     const float4 v = *reinterpret_cast<const float4*>(src);
@@ -634,23 +658,23 @@ __global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(const TreeArgs 
 }
 
 template <class T, int HD>
-cudaError_t launch_join(const TreeArgs& a, int QT, int KT, cudaStream_t s) {
+cudaError_t launch_join(const TreeArgs& a, int QT, int KT, int extra, int least, bool blocks, cudaStream_t s) {
     const long long rows = (long long)a.batch * a.n_max * a.hq;
     return launch_kernel(true, tree_join_kernel<T, HD>, dim3((unsigned)((rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32))),
-                         dim3(kJoinThreads), 0, s, a, QT, KT);
+                         dim3(kJoinThreads), 0, s, a, QT, KT, extra, least, blocks);
 }
 
-template <int HD, int WR>
+template <int HD>
 cudaError_t launch_mma(dflare_cache* c, TreeArgs a, cudaStream_t s) {
     static PerDeviceOnce once;
     cudaError_t e = once([] {
-        return cudaFuncSetAttribute(tree_mma_kernel<HD, WR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MmaLayout<HD>::BYTES);
+        return cudaFuncSetAttribute(tree_mma_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MmaLayout<HD>::BYTES);
     });
     if (e != cudaSuccess) return e;
-    a.QG = (a.n_max * a.G + 16 * WR - 1) / (16 * WR);
-    a.C = std::max(1, 2 * c->num_sms / a.QG);
-    e = launch_kernel(true, tree_mma_kernel<HD, WR>, dim3(a.QG * a.C), dim3(kMmaThreads), MmaLayout<HD>::BYTES, s, c->maps[0], c->maps[1], a);
-    return e == cudaSuccess ? launch_join<bf16, HD>(a, 16 * WR, kKeys, s) : e;
+    a.QG = 1;
+    a.C = 2 * c->num_sms;
+    e = launch_kernel(true, tree_mma_kernel<HD>, dim3(a.C), dim3(kMmaThreads), MmaLayout<HD>::BYTES, s, c->maps[0], c->maps[1], a);
+    return e == cudaSuccess ? launch_join<bf16, HD>(a, kRows, kKeys, kExtra, kLeast, false, s) : e;
 }
 
 template <int HD>
@@ -662,27 +686,25 @@ cudaError_t launch_f32(dflare_cache* c, TreeArgs a, cudaStream_t s) {
     a.QG = (a.n_max * a.G + kFRows - 1) / kFRows;
     a.C = std::max(1, 2 * c->num_sms / a.QG);
     e = launch_kernel(true, tree_f32_kernel<HD>, dim3(a.QG * a.C), dim3(kFThreads), bytes, s, a);
-    return e == cudaSuccess ? launch_join<float, HD>(a, kFRows, kFKeys, s) : e;
+    return e == cudaSuccess ? launch_join<float, HD>(a, kFRows, kFKeys, kFExtra, kFLeast, false, s) : e;
 }
 
 template <int HD>
-cudaError_t launch_hd(dflare_cache* c, const TreeArgs& a, cudaStream_t s) {
+cudaError_t launch_hd(dflare_cache* c, TreeArgs a, cudaStream_t s) {
     if (c->cfg.dtype == DFLARE_F32) return launch_f32<HD>(c, a, s);
     const int R = a.n_max * a.G;
-    if (R <= 16) return launch_mma<HD, 1>(c, a, s);
-    if (R <= 32) return launch_mma<HD, 2>(c, a, s);
-    return launch_mma<HD, 4>(c, a, s);
+    if (R <= kRows) return launch_mma<HD>(c, a, s);
+    int QT;
+    const cudaError_t e = launch_tree_attention_tc(c, a, &QT, s);
+    return e == cudaSuccess ? launch_join<bf16, HD>(a, QT, kTcKeys, kTcExtra, kTcLeast, true, s) : e;
 }
 
 }  // namespace
 
 size_t tree_partial_rows(const dflare_cache_config& g, int num_sms) {
-    // two partial results per CTA: 2 CTAs per SM of 16 (fp32) or up to 64 rows
-    return (size_t)num_sms * 2 * 2 * (g.dtype == DFLARE_F32 ? kFRows : 64);
-}
-size_t tree_plan_size(const dflare_cache_config& g) {
+    // two partial results per CTA: two CTAs per SM of 16 rows, or one of up to 256 rows
     const int R = g.max_nodes * (g.n_q_heads / g.n_kv_heads);
-    return tree_plan_ints((R + 15) / 16, g.max_batch);
+    return (size_t)num_sms * 2 * (g.dtype == DFLARE_F32 || R <= 16 ? 2 * kFRows : R <= 128 ? 128 : 256);
 }
 
 cudaError_t launch_tree_attention(dflare_cache* c, TreeArgs a, cudaStream_t s) {
@@ -718,13 +740,13 @@ extern "C" dflare_status dflare_cache_attend(dflare_cache* c, int layer, const v
     a.lse = lse_dev;
     a.part_o = c->part_o;
     a.part_ml = c->part_ml;
-    a.plan = c->plan;
     a.layer = layer;
     a.batch = batch;
     a.n_max = n_max;
     a.words = (n_max + 31) / 32;
     a.hq = g.n_q_heads;
     a.G = g.n_q_heads / g.n_kv_heads;
+    a.G_inv = a.G > 1 ? 0xffffffffu / (uint32_t)a.G + 1u : 0u;
     a.scale_log2 = scale * 1.4426950408889634f;
     DeviceGuard guard(c->device);
     const cudaError_t e = launch_tree_attention(c, a, static_cast<cudaStream_t>(stream));

@@ -3,8 +3,9 @@
 // The query rows of one kv head are n * G (row r: node r / G, query head r % G of the group), cut into
 // groups of QT rows. For one group index qg the work is the list of all (sequence, kv head) pairs that have
 // such rows, each with ceil(keys / KT) key tiles; C CTAs take equal runs of that list, wherever they begin
-// and end, so contexts of any lengths load the CTAs evenly. The CTAs of different qg with the same place in
-// the list are neighbours in the grid: they read the same keys at about the same time, once from HBM.
+// and end, so contexts of any lengths load the CTAs evenly. A pair counts EXTRA tiles beyond its own for what
+// beginning and ending it costs. The CTAs of different qg with the same place in the list are neighbours in
+// the grid: they read the same keys at about the same time, once from HBM.
 // Rows whose keys lie in one run are written by that CTA; rows whose keys several CTAs read leave partial
 // results (at most two per CTA: of the pair it begins in and of the pair it ends in) that a second launch
 // joins in a fixed order.
@@ -14,40 +15,40 @@
 
 namespace dfl {
 
-// tiles up to sequence b (exclusive), per query group; behind them the run length and the lengths
-struct TreePlan {
-    int32_t* cum;       // [QG][batch + 1]
-    int32_t* per;       // [QG]
+// What memory says of sequence b, and what follows: nodes, tokens, and keys that exist (tokens and nodes as
+// far as the sequence's pages reach). In two steps, so that the loads can be under way long before their use.
+struct TreeRaw {
+    int n, held, len;
 };
-__host__ __device__ inline size_t tree_plan_ints(int QG, int batch) { return (size_t)QG * (batch + 2); }
-__device__ __forceinline__ TreePlan tree_plan_of(const TreeArgs& a) { return {a.plan, a.plan + (size_t)a.QG * (a.batch + 1)}; }
-
-// keys of sequence b that exist: its tokens and its nodes, as far as its pages reach
-__device__ __forceinline__ void tree_lengths(const TreeArgs& a, int b, int& n, int& ctx, int& keys) {
-    n = min(max(a.n_nodes[b], 0), a.n_max);
-    const long long room = (long long)min(max(a.pg.held[b], 0), a.pg.max_pages) * a.pg.ps;
-    ctx = max(a.pg.lens[b], 0);
+__device__ __forceinline__ TreeRaw tree_raw(const TreeArgs& a, int b) { return {a.n_nodes[b], a.pg.held[b], a.pg.lens[b]}; }
+__device__ __forceinline__ void tree_lengths(const TreeArgs& a, const TreeRaw& x, int& n, int& ctx, int& keys) {
+    n = min(max(x.n, 0), a.n_max);
+    const long long room = (long long)min(max(x.held, 0), a.pg.max_pages) * a.pg.ps;
+    ctx = max(x.len, 0);
     keys = (int)min((long long)ctx + n, room);
     ctx = min(ctx, keys);
 }
 
-// The run [t0, t1) of this CTA, and cum[0 .. batch] (tiles of one kv head before sequence b) in shared
-// memory. All threads of the CTA call it; it ends with a barrier. The first CTA of each group writes the
-// division down for the joining launch.
-template <int QT, int KT, int MIN>
-__device__ __forceinline__ void tree_runs(const TreeArgs& a, int qg, int c, int32_t* cum, int& t0, int& t1) {
+// key tiles of sequence b for query group qg, and what they count in the list
+__device__ __forceinline__ int tree_tiles(const TreeArgs& a, int b, int qg, int QT, int KT) {
+    int n, ctx, keys;
+    tree_lengths(a, tree_raw(a, b), n, ctx, keys);
+    return n * a.G > qg * QT ? (int)(((long long)keys + KT - 1) / KT) : 0;
+}
+__device__ __forceinline__ int tree_cost(int tiles, int extra) { return tiles ? tiles + extra : 0; }
+// length of a run; below `least` it would cost more in joining than it saves
+__device__ __forceinline__ int tree_run(const TreeArgs& a, int total, int least) { return max((total + a.C - 1) / a.C, least); }
+
+// The run [v0, v1) of this CTA, and cum[0 .. batch] (cost of one kv head before sequence b) in shared memory.
+// All threads of the CTA call it; it ends with a barrier.
+template <int QT, int KT, int EXTRA, int LEAST>
+__device__ __forceinline__ void tree_runs(const TreeArgs& a, int qg, int c, int32_t* cum, int& v0, int& v1) {
     const int tid = threadIdx.x;
     if (tid < 32) {
         int base = 0;
         for (int b0 = 0; b0 < a.batch; b0 += 32) {
             const int b = b0 + tid;
-            int tiles = 0;
-            if (b < a.batch) {
-                int n, ctx, keys;
-                tree_lengths(a, b, n, ctx, keys);
-                if (n * a.G > qg * QT) tiles = (int)(((long long)keys + KT - 1) / KT);
-            }
-            int v = tiles;
+            int v = b < a.batch ? tree_cost(tree_tiles(a, b, qg, QT, KT), EXTRA) : 0;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const int x = __shfl_up_sync(0xffffffffu, v, o);
@@ -59,38 +60,72 @@ __device__ __forceinline__ void tree_runs(const TreeArgs& a, int qg, int c, int3
         if (tid == 0) cum[0] = 0;
     }
     __syncthreads();
-    const int total = cum[a.batch] * a.pg.hkv;
-    // a run below MIN tiles costs more in joining than it saves
-    const int per = max((total + a.C - 1) / a.C, MIN);
-    t0 = (int)min((long long)c * per, (long long)total);
-    t1 = (int)min((long long)t0 + per, (long long)total);
-    if (c == 0) {
-        const TreePlan p = tree_plan_of(a);
-        for (int b = tid; b <= a.batch; b += blockDim.x) p.cum[(size_t)qg * (a.batch + 1) + b] = cum[b];
-        if (tid == 0) p.per[qg] = per;
-    }
+    const int total = cum[a.batch] * a.pg.hkv, per = tree_run(a, total, LEAST);
+    v0 = (int)min((long long)c * per, (long long)total);
+    v1 = (int)min((long long)v0 + per, (long long)total);
 }
 
-// The (sequence, kv head) pair that tile t of the list belongs to.
-struct TreeItem {
-    int b, h;        // sequence, kv head
-    int start;       // its first tile in the list
-    int tiles;
+// A run's part of one pair: tiles [lo, hi) of the `tiles` of kv head h of sequence b; the pair's place in the
+// list is `start`.
+struct TreePair {
+    int b, h, start, tiles, lo, hi;
+    __device__ __forceinline__ bool partial() const { return lo != 0 || hi != tiles; }
 };
-__device__ __forceinline__ TreeItem tree_item(const int32_t* cum, int batch, int hkv, int t) {
-    int lo = 0, hi = batch;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (cum[mid] * hkv <= t) lo = mid; else hi = mid;
+// The next part from place v on (v moves behind its pair); false at the end of the run.
+template <int EXTRA>
+__device__ __forceinline__ bool tree_pair(const TreeArgs& a, const int32_t* cum, int& v, int v1, TreePair& p) {
+    const int hkv = a.pg.hkv;
+    while (v < v1) {
+        int lo = 0, hi = a.batch;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (cum[mid] * hkv <= v) lo = mid; else hi = mid;
+        }
+        const int cost = cum[lo + 1] - cum[lo];
+        p.b = lo;
+        p.tiles = cost - EXTRA;
+        p.h = (v - cum[lo] * hkv) / cost;
+        p.start = cum[lo] * hkv + p.h * cost;
+        p.lo = v - p.start;
+        p.hi = min(v1 - p.start, p.tiles);
+        v = p.start + cost;
+        if (p.lo < p.tiles) return true;
     }
-    TreeItem it;
-    it.b = lo;
-    it.tiles = cum[lo + 1] - cum[lo];
-    const int in = t - cum[lo] * hkv;
-    it.h = in / it.tiles;
-    it.start = cum[lo] * hkv + it.h * it.tiles;
-    return it;
+    return false;
 }
+
+// The pages of one key tile, for the warp that streams tiles by TMA: lane x holds the tensor-map plane of the
+// tile's box x (`rows` tokens, a divisor of the tile), read by all lanes at once so that a tile costs one trip
+// to the table. Slots without a page take a plane outside the pool, which reads as zero.
+struct TileBoxes {
+    int plane, first_slot;
+};
+__device__ __forceinline__ TileBoxes tile_boxes(const TreeArgs& a, const TreePair& p, int tile, int KT, int rows, int lane) {
+    TileBoxes x;
+    x.first_slot = tile * KT;
+    x.plane = (int)min(0x7fffffffLL, (long long)a.pg.layers * a.pg.pages * a.pg.hkv);
+    const int pages = min(max(a.pg.held[p.b], 0), a.pg.max_pages);
+    const int pi = (int)(((unsigned)x.first_slot + (unsigned)(lane * rows)) / (unsigned)a.pg.ps);
+    if (lane * rows < KT && pi < pages) {
+        const int page = a.pg.table[(size_t)p.b * a.pg.max_pages + pi];
+        if (page >= 0 && page < a.pg.pages) x.plane = (a.layer * a.pg.pages + page) * a.pg.hkv + p.h;
+    }
+    return x;
+}
+
+// Infinite and NaN bf16 values of a 16-byte piece become 0; whether there were any.
+__device__ __forceinline__ bool drop_odd(uint4& v) {
+    uint32_t* e = reinterpret_cast<uint32_t*>(&v);
+    bool bad = false;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        if ((e[q] & 0x7f80u) == 0x7f80u) { e[q] &= 0xffff0000u; bad = true; }
+        if ((e[q] & 0x7f800000u) == 0x7f800000u) { e[q] &= 0xffffu; bad = true; }
+    }
+    return bad;
+}
+// row / G for the rows of a kv head (below 2^16): a multiplication by the rounded-up reciprocal
+__device__ __forceinline__ int group_of(const TreeArgs& a, int row) { return a.G == 1 ? row : (int)__umulhi((unsigned)row, a.G_inv); }
 
 // 64 bits of a node's mask row from bit x >= 0 on
 __device__ __forceinline__ uint64_t mask_bits(const int32_t* row, int words, int x) {
@@ -113,6 +148,48 @@ __device__ __forceinline__ uint64_t tree_seen(const TreeArgs& a, int b, int node
         v |= low_bits(node + 1 - rel);
     }
     return v & low_bits(keys - k0);
+}
+
+// The same for 32 keys with the first four words of the node's mask row held in registers, so that a tile at
+// the end of the context does not wait for memory that is busy with keys (more words: read when needed).
+struct SeenRow {
+    uint32_t w[4];
+};
+__device__ __forceinline__ SeenRow seen_row(const TreeArgs& a, int b, int node) {
+    SeenRow r;
+    const int32_t* row = a.mask + ((size_t)b * a.n_max + node) * a.words;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.w[i] = a.mask && i < a.words ? (uint32_t)row[i] : 0u;
+    return r;
+}
+__device__ __forceinline__ uint32_t seen_word(const TreeArgs& a, const SeenRow& r, int b, int node, int i) {
+    uint32_t v = 0;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) v = i == x ? r.w[x] : v;
+    if (i >= 4 && i < a.words) v = (uint32_t)a.mask[((size_t)b * a.n_max + node) * a.words + i];
+    return v;
+}
+__device__ __forceinline__ uint32_t seen32(const TreeArgs& a, const SeenRow& r, int b, int node, int ctx, int keys, int k0) {
+    const int rel = k0 - ctx;
+    uint32_t v;
+    if (a.mask) v = __funnelshift_r(seen_word(a, r, b, node, rel >> 5), seen_word(a, r, b, node, (rel >> 5) + 1), rel & 31);
+    else v = (uint32_t)low_bits(node + 1 - rel);
+    return (v | (uint32_t)low_bits(-rel)) & (uint32_t)low_bits(keys - k0);
+}
+
+// f(value address) for every node in odd[] (one bit per node) that `node` sees, in the layer's values of kv head h
+template <class F>
+__device__ __forceinline__ void each_odd(const TreeArgs& a, const uint32_t* odd, const TreePair& p, int node, int ctx, int keys, F f) {
+    for (int word = 0; word < a.words; ++word) {
+        uint32_t bits = odd[word];
+        while (bits) {
+            const int key = ctx + word * 32 + __ffs(bits) - 1;
+            bits &= bits - 1;
+            if (!(tree_seen(a, p.b, node, ctx, keys, key) & 1)) continue;
+            const int page = a.pg.table[(size_t)p.b * a.pg.max_pages + key / a.pg.ps];
+            f(((((size_t)a.layer * a.pg.pages + page) * a.pg.hkv + p.h) * a.pg.ps + key % a.pg.ps) * a.pg.hd);
+        }
+    }
 }
 
 }  // namespace dfl

@@ -129,20 +129,20 @@ def attend_reference(p, q, seen, scale, layer=0):
             see = seen[b][i]
             if not see.any():
                 continue
-            for h in range(p.hq):
-                kk, vv = k[see, h // g], v[see, h // g]
-                z = kk @ q[b, i, h] * scale
-                delta = (p.hd + 4) * EPS32 * scale * (np.abs(kk) @ np.abs(q[b, i, h])).max()
-                w = np.exp(z - z.max())
-                w /= w.sum()
-                out[b, i, h] = w @ vv
-                lse[b, i, h] = z.max() + math.log(np.exp(z - z.max()).sum())
-                rel = 2 * delta + (len(z) + 64) * EPS32
-                mean = w @ np.abs(vv)
-                bound[b, i, h] = rel * mean
-                lse_bound[b, i, h] = rel + 4 * EPS32 * (abs(lse[b, i, h]) + np.abs(z).max())
-                if p.t == torch.bfloat16:
-                    bound[b, i, h] += EPS16 * 1.01 * (mean + np.abs(out[b, i, h]))
+            kk, vv, qq = k[see], v[see], q[b, i].reshape(p.hkv, g, p.hd)
+            z = np.einsum("hgd,khd->hgk", qq, kk) * scale
+            delta = (p.hd + 4) * EPS32 * scale * np.einsum("hgd,khd->hgk", np.abs(qq), np.abs(kk)).max(-1)
+            w = np.exp(z - z.max(-1, keepdims=True))
+            total = w.sum(-1, keepdims=True)
+            w /= total
+            o, mean = np.einsum("hgk,khd->hgd", w, vv), np.einsum("hgk,khd->hgd", w, np.abs(vv))
+            rel = 2 * delta + (z.shape[-1] + 64) * EPS32
+            out[b, i] = o.reshape(p.hq, p.hd)
+            lse[b, i] = (z.max(-1) + np.log(total[..., 0])).reshape(p.hq)
+            bound[b, i] = (rel[..., None] * mean).reshape(p.hq, p.hd)
+            lse_bound[b, i] = rel.reshape(p.hq) + 4 * EPS32 * (np.abs(lse[b, i]) + np.abs(z).max(-1).reshape(p.hq))
+            if p.t == torch.bfloat16:
+                bound[b, i] += EPS16 * 1.01 * (mean.reshape(p.hq, p.hd) + np.abs(out[b, i]))
     return out, lse, bound, lse_bound
 
 
@@ -224,6 +224,30 @@ def test_attend_for_many_shapes_of_rows(nodes, hq, hkv):
     q = queries(rng, p, 2, nodes)
     mask, seen = tree_masks(rng, lens, counts, nodes)
     check_attend(p, q, seen, mask)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nodes,hq,hkv,hd,batch,top", [(1, 16, 8, 64, 40, 900), (2, 16, 4, 128, 60, 1300), (5, 32, 8, 64, 24, 1100),
+                                                        (18, 32, 4, 128, 30, 1500), (34, 32, 4, 64, 20, 2500), (70, 32, 8, 128, 12, 1500)])
+def test_runs_that_cross_from_pair_to_pair(nodes, hq, hkv, hd, batch, top, dtype):
+    """So many sequences and heads that a CTA's share of the keys spans several of them, some of them whole; lengths
+    from nothing on, some sequences without nodes. Three launches follow one another without a wait."""
+    rng = np.random.default_rng(nodes)
+    lens = [int(x) for x in rng.integers(0, top, batch)]
+    lens[1] = 0
+    counts = [int(x) for x in rng.integers(1, nodes + 1, batch)]
+    counts[2] = 0
+    p = Paged(rng, lens, counts, hq=hq, hkv=hkv, hd=hd, page=32, dtype=dtype, nodes=nodes)
+    q = queries(rng, p, batch, nodes)
+    mask, seen = tree_masks(rng, lens, counts, nodes)
+    n = i32(counts)
+    outs = [torch.empty_like(q) for _ in range(3)]
+    for o in outs:
+        p.cache.attend(0, q, n, o, mask=mask)
+    check_attend(p, q, seen, mask)
+    out, _ = run_attend(p, q, mask)
+    assert all(torch.equal(o, out) for o in outs)
 
 
 @pytest.mark.gpu
