@@ -573,7 +573,7 @@ __global__ void __launch_bounds__(kFThreads) tree_f32_kernel(const TreeArgs a) {
 
 // Rows whose keys several CTAs read: their partial results in the order of the keys. Also the rows that no
 // CTA had anything for: no keys, or past the tree's nodes. A warp per row.
-constexpr int kJoinThreads = 256;
+constexpr int kJoinThreads = 128;      // few enough registers to be resident beside the tcgen05 kernel's CTA
 
 template <class T, int HD>
 __global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(const TreeArgs a, int QT, int KT, int extra, int least, bool blocks) {
@@ -615,36 +615,44 @@ __global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(const TreeArgs 
     if (some && c0 == c1) return;       // written by the CTA that read all of them
     if (some) {
         auto at = [&](int c) { return (((size_t)c * a.QG + qg) * 2 + (start < c * per ? 0 : 1)) * QT + r % QT; };
-        for (int c = c0 + lane; c <= c1; c += 32) m = fmaxf(m, a.part_ml[at(c)].x);
-        m = warp_max(m);
-        const float ref = m == -INFINITY ? 0.f : m;
-        for (int cb = c0; cb <= c1; cb += 32) {
-            float w = 0.f, sum = 0.f;
-            if (cb + lane <= c1) {
-                const float2 v = a.part_ml[at(cb + lane)];
-                w = exp2f(v.x - ref);
-                sum = v.y * w;
-            }
-            l += warp_sum(sum);
-            const int upto = min(32, c1 - cb + 1);
-#pragma unroll 4
-            for (int j = 0; j < upto; ++j) {
-                const float wj = __shfl_sync(0xffffffffu, w, j);
-                const size_t row = at(cb + j);
+        // eight partial rows in flight at a time, the first ones together with the (m, l) that weigh them
+        float x[8][E];
+        auto load = [&](int cb) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const size_t row = at(min(cb + j, c1));
                 // the tcgen05 kernel's rows lie in blocks of 32 rows x 32 elements, 16-byte pieces swizzled
                 const float* src = a.part_o + (!blocks ? row * HD + lane * E
                                                        : (row & ~(size_t)31) * HD + (lane * E >> 5) * 1024 + (row & 31) * 32 +
                                                              ((((lane * E & 31) >> 2) ^ (int)(row & 7)) << 2) + (lane * E & 3));
-                float x[E];
                 if constexpr (E == 4) {
                     const float4 v = *reinterpret_cast<const float4*>(src);
-                    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+                    x[j][0] = v.x; x[j][1] = v.y; x[j][2] = v.z; x[j][3] = v.w;
                 } else {
                     const float2 v = *reinterpret_cast<const float2*>(src);
-                    x[0] = v.x; x[1] = v.y;
+                    x[j][0] = v.x; x[j][1] = v.y;
                 }
+            }
+        };
+        load(c0);
+        float2 v = c0 + lane <= c1 ? a.part_ml[at(c0 + lane)] : make_float2(-INFINITY, 0.f);
+        m = v.x;
+        for (int c = c0 + 32 + lane; c <= c1; c += 32) m = fmaxf(m, a.part_ml[at(c)].x);
+        m = warp_max(m);
+        const float ref = m == -INFINITY ? 0.f : m;
+        for (int cb = c0; cb <= c1; cb += 32) {
+            if (cb > c0) v = cb + lane <= c1 ? a.part_ml[at(cb + lane)] : make_float2(-INFINITY, 0.f);
+            const float w = exp2f(v.x - ref);       // 0 past the last one
+            l += warp_sum(v.y * w);
+            for (int j0 = 0; j0 < min(32, c1 - cb + 1); j0 += 8) {
+                if (cb + j0 > c0) load(cb + j0);
 #pragma unroll
-                for (int e = 0; e < E; ++e) acc[e] = fmaf(wj, x[e], acc[e]);
+                for (int j = 0; j < 8; ++j) {
+                    const float wj = __shfl_sync(0xffffffffu, w, j0 + j);
+                    if (cb + j0 + j > c1) continue;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) acc[e] = fmaf(wj, x[j][e], acc[e]);
+                }
             }
         }
         const float inv = l == 0.f ? 0.f : 1.f / l;

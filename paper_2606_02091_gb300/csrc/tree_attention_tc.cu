@@ -173,9 +173,6 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         int i = 0;
         if (more) {
             TileBoxes next = tile_boxes(a, p, p.lo, kKeys, rows, lane);
-            // the first pair's queries go first: behind the ring's tiles they would arrive after all of them
-            // (measured: 3.5 us later, the time in which 152 x 128 KB come from memory)
-            asm volatile("bar.sync 2, 288;" ::: "memory");
             for (int t = p.lo; more && ok; ++i) {
                 const TileBoxes now = next;
                 if (++t == p.hi) {
@@ -185,6 +182,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                 if (more) next = tile_boxes(a, p, t, kKeys, rows, lane);
 #pragma unroll
                 for (int kv = 0; kv < 2 && ok; ++kv) {
+                    // After the first K tile the first pair's queries: behind the whole ring they would arrive
+                    // last (measured: 3.5 us later, the time in which 152 x 128 KB come from memory).
+                    if (i == 0 && kv == 1) asm volatile("bar.sync 2, 288;" ::: "memory");
                     const int N = kv ? NV : NK, st = i % N;
                     if (i >= N)
                         ok = __all_sync(0xffffffffu, bar_wait(kv ? vempty(st) : kempty(st), (uint32_t)(i / N - 1) & 1u, &abort_flag, a.pg.err));
@@ -351,7 +351,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                         // of nodes become 0
                         const int x = base + tile, st = x % NV, rows = min(kKeys, (keys - k0 + 15) & ~15);
                         wait(vfull(st), (uint32_t)(x / NV) & 1u);
-#pragma unroll 2
+#pragma unroll 4
                         for (int y = max(ctx - k0, 0) * (HD / 8) + r; y < rows * (HD / 8); y += 128) {
                             const int kr = y / (HD / 8), pc = y % (HD / 8), key = k0 + kr;
                             uint4* at = reinterpret_cast<uint4*>(smem + LY::V + st * TB + (pc >> 3) * 16384 + kr * 128 + (((pc & 7) ^ (kr & 7)) << 4));
@@ -374,7 +374,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                     // scores of unseen keys become -inf where they are (in the loop below a branch for it costs
                     // every tile 0.1 us)
 #pragma unroll 1
-                    for (int x = 0; x < 4; ++x) {
+                    for (int x = max(ctx - k0, 0) >> 5; x < 4; ++x) {
                         const uint32_t see = seen32(a, row, p.b, node, ctx, keys, k0 + 32 * x);
                         uint32_t s[32];
                         tmem_ld32_async(tS(w) + lanes + 32 * x, s);
@@ -389,22 +389,30 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                 }
                 if (warp_live) {
                     // One read of the row's scores, 32 at a time: weights against the maximum so far, and the
-                    // tile's own maximum. Only where that is above the other by 2^8 (or there was none yet) the
-                    // scores are read a second time.
+                    // tile's own maximum. Only where that is above the other by 2^8 the scores are read a second
+                    // time. A pair's first tile goes by the maximum of its first 32 keys (by that of the first key
+                    // alone, rows go on raising theirs: 248 us instead of 203 for 64 nodes over 8 x 32768 keys).
                     uint32_t pw[64];
                     uint64_t sum[2];
                     const uint64_t scale = pack2(a.scale_log2, a.scale_log2);
 #pragma unroll 1
                     for (bool again = false;; again = true) {
-                        const float neg1 = m == -INFINITY ? 0.f : -m;
-                        const uint64_t neg = pack2(neg1, neg1);
                         float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                         sum[0] = sum[1] = 0ull;
                         uint32_t s[2][32];
                         tmem_ld32_async(tS(w) + lanes, s[0]);
+                        tmem_wait_ld();
+                        if (__any_sync(0xffffffffu, m == -INFINITY)) {
+                            float mx = -INFINITY;
+#pragma unroll
+                            for (int e = 0; e < 32; e += 2) mx = max3(mx, __uint_as_float(s[0][e]), __uint_as_float(s[0][e + 1]));
+                            if (m == -INFINITY) m = mx * a.scale_log2;
+                        }
+                        const float neg1 = m == -INFINITY ? 0.f : -m;
+                        const uint64_t neg = pack2(neg1, neg1);
 #pragma unroll
                         for (int x = 0; x < 4; ++x) {
-                            tmem_wait_ld();
+                            if (x) tmem_wait_ld();
                             if (x < 3) tmem_ld32_async(tS(w) + lanes + 32 * (x + 1), s[(x + 1) & 1]);
                             const uint32_t* v = s[x & 1];
 #pragma unroll
@@ -421,7 +429,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                         }
                         if (again) break;
                         const float mx = fmaxf(max3(mx4[0], mx4[1], mx4[2]), mx4[3]) * a.scale_log2;
-                        const bool raise = mx > m + kRaise;      // also the first finite maximum
+                        const bool raise = mx > m + kRaise;      // (also from -inf)
                         if (!__any_sync(0xffffffffu, raise)) break;
                         const float alpha = raise ? pow2(m - mx) : 1.0f;
                         if (j > 0) {    // (the stream's PV before S(i) has completed: its O is at rest)
@@ -546,8 +554,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                         if (upper || CH == 1) {
                             constexpr int pieces = CH > 1 ? 8 : 4;
                             __syncwarp();
-                            for (int y = lane; y < 32 * pieces; y += 32) {
-                                const int lr = y / pieces, pc = y % pieces;
+#pragma unroll
+                            for (int y = 0; y < pieces; ++y) {
+                                const int lr = (32 / pieces) * y + lane / pieces, pc = lane % pieces;
                                 const uint4 v = *reinterpret_cast<const uint4*>(turn + lr * 128 + ((pc ^ (lr & 7)) << 4));
                                 const size_t to = __shfl_sync(0xffffffffu, orow, lr);
                                 if (lr < rows)
