@@ -107,7 +107,6 @@ __global__ void __launch_bounds__(kMmaThreads, 2) tree_mma_kernel(const __grid_c
 
     if (warp == 4) {
         // ---------------- stream the tiles: a box is up to 64 tokens of a page x 64 head dims
-        const bool leader = elect_one();
         const int rows = min(a.pg.ps, kKeys), boxes = kKeys / rows;
         bool ok = true, more = true;
         int i = 0;
@@ -125,11 +124,11 @@ __global__ void __launch_bounds__(kMmaThreads, 2) tree_mma_kernel(const __grid_c
             if (i >= kStages) ok = __all_sync(0xffffffffu, bar_wait(empty + 8 * st, (uint32_t)(i / kStages - 1) & 1u, &abort_flag, a.pg.err));
             if (!ok) break;
             const uint32_t bar = full + 8 * st, kd = sb + st * 2 * TB;
-            if (leader) mbar_expect_tx(bar, 2 * TB);
+            if (elect_one()) mbar_expect_tx(bar, 2 * TB);
             for (int x = 0; x < boxes; ++x) {
                 const int z = __shfl_sync(0xffffffffu, now.plane, x);
                 const int y = (now.first_slot + x * rows) & (a.pg.ps - 1);
-                if (leader) {
+                if (elect_one()) {
 #pragma unroll
                     for (int h = 0; h < HD / 64; ++h) {
                         tma_load_3d(kd + h * 8192 + x * rows * 128, &mk, h * 64, y, z, bar);
@@ -138,7 +137,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) tree_mma_kernel(const __grid_c
                 }
             }
         }
-        if (!ok && leader) {   // the copies in flight land before the CTA's shared memory is given up
+        if (!ok && elect_one()) {   // the copies in flight land before the CTA's shared memory is given up
             volatile int never = 0;
             for (int j = max(0, i - kStages); j < i; ++j)
                 bar_wait(full + 8 * (j % kStages), (uint32_t)(j / kStages) & 1u, &never, a.pg.err);
@@ -572,104 +571,127 @@ __global__ void __launch_bounds__(kFThreads) tree_f32_kernel(const TreeArgs a) {
 }
 
 // Rows whose keys several CTAs read: their partial results in the order of the keys. Also the rows that no
-// CTA had anything for: no keys, or past the tree's nodes. A warp per row.
+// CTA had anything for: no keys, or past the tree's nodes. RW rows per warp: one where rows are few (a row's parts
+// in flight are what counts), four where they are many (measured: 64 nodes over 8 x 32768 keys, 16384 rows, 12 us
+// less than with one).
 constexpr int kJoinThreads = 128;      // few enough registers to be resident beside the tcgen05 kernel's CTA
+constexpr int kJoinMany = 8192;        // rows from which on a warp takes four
 
-template <class T, int HD>
+template <class T, int HD, int RW>
 __global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(const TreeArgs a, int QT, int KT, int extra, int least, bool blocks) {
-    constexpr int E = HD / 32;      // elements per lane
+    constexpr int LPR = 32 / RW, E = HD / LPR, V = E < 4 ? E : 4, J = RW == 1 ? 8 : 4;
+    // lane l of a row: elements g LPR V + l V .. of its groups g
     // The kernel before this one let it start after its own dependency wait, so the lengths are final here and
     // the division of the work is found while that kernel still runs.
-    const long long row = (long long)blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31;
-    if (row >= (long long)a.batch * a.n_max * a.hq) return;
-    const int head = (int)(row % a.hq), node = (int)(row / a.hq % a.n_max), b = (int)(row / a.hq / a.n_max);
+    const int lane = threadIdx.x & 31, l = lane % LPR;
+    const long long row = ((long long)blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5)) * RW + lane / LPR;
+    const bool there = row < (long long)a.batch * a.n_max * a.hq;
+    const int head = (int)(row % a.hq), node = (int)(row / a.hq % a.n_max), b = there ? (int)(row / a.hq / a.n_max) : 0;
     int n, ctx, keys;
     tree_lengths(a, tree_raw(a, b), n, ctx, keys);
-    float acc[E], m = -INFINITY, l = 0.f;
+    const bool some = there && node < n && keys > 0;
+    const int r = node * a.G + head % a.G, qg = r / QT;
+    int before = 0, total = 0;
+    for (int x = l; x < a.batch; x += LPR) {
+        const int t = tree_cost(tree_tiles(a, x, qg, QT, KT), extra);
+        total += t;
+        if (x < b) before += t;
+    }
+#pragma unroll
+    for (int o = LPR / 2; o > 0; o >>= 1) {
+        total += __shfl_xor_sync(0xffffffffu, total, o);
+        before += __shfl_xor_sync(0xffffffffu, before, o);
+    }
+    const int per = tree_run(a, total * a.pg.hkv, least), tiles = tree_tiles(a, b, qg, QT, KT);
+    const int start = before * a.pg.hkv + head / a.G * tree_cost(tiles, extra);
+    const int c0 = start / per;
+    int parts = some ? (start + tiles - 1) / per - c0 + 1 : 0;
+    const bool written = parts == 1;        // by the CTA that read all of the row's keys
+    if (written) parts = 0;
+    // every warp waits, so this launch does not end before the one it depends on
+    pdl_wait();
+    const int most = __reduce_max_sync(0xffffffffu, parts);
+    auto at = [&](int i) { return (((size_t)(c0 + i) * a.QG + qg) * 2 + (start < (c0 + i) * per ? 0 : 1)) * QT + r % QT; };
+    float acc[E], x[J][E], m = -INFINITY, sum = 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e) acc[e] = 0.f;
-    const bool some = node < n && keys > 0;
-    const int r = node * a.G + head % a.G, qg = r / QT;
-    int per = 1, start = 0, c0 = 0, c1 = 0;
-    if (some) {
-        int before = 0, total = 0;
-        for (int x = lane; x < a.batch; x += 32) {
-            const int t = tree_cost(tree_tiles(a, x, qg, QT, KT), extra);
-            total += t;
-            if (x < b) before += t;
-        }
+    auto load = [&](int i) {        // parts i .. i + J - 1
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            total += __shfl_xor_sync(0xffffffffu, total, o);
-            before += __shfl_xor_sync(0xffffffffu, before, o);
-        }
-        per = tree_run(a, total * a.pg.hkv, least);
-        const int tiles = tree_tiles(a, b, qg, QT, KT);
-        start = before * a.pg.hkv + head / a.G * tree_cost(tiles, extra);
-        c0 = start / per;
-        c1 = (start + tiles - 1) / per;
-    }
-    // every row's warp waits, so this launch does not end before the one it depends on
-    pdl_wait();
-    if (some && c0 == c1) return;       // written by the CTA that read all of them
-    if (some) {
-        auto at = [&](int c) { return (((size_t)c * a.QG + qg) * 2 + (start < c * per ? 0 : 1)) * QT + r % QT; };
-        // eight partial rows in flight at a time, the first ones together with the (m, l) that weigh them
-        float x[8][E];
-        auto load = [&](int cb) {
+        for (int j = 0; j < J; ++j) {
+            const size_t row = at(min(i + j, max(parts - 1, 0)));
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const size_t row = at(min(cb + j, c1));
+            for (int g = 0; g < E / V; ++g) {
+                const int e = (g * LPR + l) * V;
                 // the tcgen05 kernel's rows lie in blocks of 32 rows x 32 elements, 16-byte pieces swizzled
-                const float* src = a.part_o + (!blocks ? row * HD + lane * E
-                                                       : (row & ~(size_t)31) * HD + (lane * E >> 5) * 1024 + (row & 31) * 32 +
-                                                             ((((lane * E & 31) >> 2) ^ (int)(row & 7)) << 2) + (lane * E & 3));
-                if constexpr (E == 4) {
-                    const float4 v = *reinterpret_cast<const float4*>(src);
-                    x[j][0] = v.x; x[j][1] = v.y; x[j][2] = v.z; x[j][3] = v.w;
+                const float* src = a.part_o + (!blocks ? row * HD + e
+                                                       : (row & ~(size_t)31) * HD + (e >> 5) * 1024 + (row & 31) * 32 +
+                                                             ((((e & 31) >> 2) ^ (int)(row & 7)) << 2) + (e & 3));
+                if constexpr (V == 4) {
+                    const float4 v = i < parts ? *reinterpret_cast<const float4*>(src) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    x[j][4 * g] = v.x; x[j][4 * g + 1] = v.y; x[j][4 * g + 2] = v.z; x[j][4 * g + 3] = v.w;
                 } else {
-                    const float2 v = *reinterpret_cast<const float2*>(src);
+                    const float2 v = i < parts ? *reinterpret_cast<const float2*>(src) : make_float2(0.f, 0.f);
                     x[j][0] = v.x; x[j][1] = v.y;
                 }
             }
-        };
-        load(c0);
-        float2 v = c0 + lane <= c1 ? a.part_ml[at(c0 + lane)] : make_float2(-INFINITY, 0.f);
-        m = v.x;
-        for (int c = c0 + 32 + lane; c <= c1; c += 32) m = fmaxf(m, a.part_ml[at(c)].x);
-        m = warp_max(m);
-        const float ref = m == -INFINITY ? 0.f : m;
-        for (int cb = c0; cb <= c1; cb += 32) {
-            if (cb > c0) v = cb + lane <= c1 ? a.part_ml[at(cb + lane)] : make_float2(-INFINITY, 0.f);
-            const float w = exp2f(v.x - ref);       // 0 past the last one
-            l += warp_sum(v.y * w);
-            for (int j0 = 0; j0 < min(32, c1 - cb + 1); j0 += 8) {
-                if (cb + j0 > c0) load(cb + j0);
+        }
+    };
+    // the first J parts come in together with the (m, l) that weigh them
+    load(0);
+    float2 v = l < parts ? a.part_ml[at(l)] : make_float2(-INFINITY, 0.f);
+    m = v.x;
+    for (int i = LPR + l; i < parts; i += LPR) m = fmaxf(m, a.part_ml[at(i)].x);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float wj = __shfl_sync(0xffffffffu, w, j0 + j);
-                    if (cb + j0 + j > c1) continue;
-#pragma unroll
-                    for (int e = 0; e < E; ++e) acc[e] = fmaf(wj, x[j][e], acc[e]);
-                }
+    for (int o = LPR / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    const float ref = m == -INFINITY ? 0.f : m;
+    float w = exp2f(v.x - ref);             // 0 past the last part
+    sum = v.y * w;
+    for (int i = 0; i < most; i += J) {
+        if (i) {
+            load(i);
+            if (i % LPR == 0) {
+                v = i + l < parts ? a.part_ml[at(i + l)] : make_float2(-INFINITY, 0.f);
+                w = exp2f(v.x - ref);
+                sum = fmaf(v.y, w, sum);
             }
         }
-        const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] *= inv;
+        for (int j = 0; j < J; ++j) {
+            const float wj = __shfl_sync(0xffffffffu, w, i % LPR + j, LPR);
+            if (i + j >= parts) continue;
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[e] = fmaf(wj, x[j][e], acc[e]);
+        }
     }
-    T* out = static_cast<T*>(a.out) + row * HD + lane * E;
 #pragma unroll
-    for (int e = 0; e < E; ++e) out[e] = from_f<T>(acc[e]);
-    if (a.lse && lane == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+    for (int o = LPR / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (!there || written) return;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    T* out = static_cast<T*>(a.out) + row * HD;
+#pragma unroll
+    for (int g = 0; g < E / V; ++g) {
+        const int e = (g * LPR + l) * V;
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int y = 0; y < V; y += 2)
+                *reinterpret_cast<uint32_t*>(out + e + y) = two_bf16(acc[g * V + y] * inv, acc[g * V + y + 1] * inv);
+        } else {
+#pragma unroll
+            for (int y = 0; y < V; ++y) out[e + y] = acc[g * V + y] * inv;
+        }
+    }
+    if (a.lse && l == 0) a.lse[row] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * 0.69314718055994531f;
 }
 
 template <class T, int HD>
 cudaError_t launch_join(const TreeArgs& a, int QT, int KT, int extra, int least, bool blocks, cudaStream_t s) {
     const long long rows = (long long)a.batch * a.n_max * a.hq;
-    return launch_kernel(true, tree_join_kernel<T, HD>, dim3((unsigned)((rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32))),
-                         dim3(kJoinThreads), 0, s, a, QT, KT, extra, least, blocks);
+    const int warps = kJoinThreads / 32;
+    if (rows < kJoinMany)
+        return launch_kernel(true, tree_join_kernel<T, HD, 1>, dim3((unsigned)((rows + warps - 1) / warps)), dim3(kJoinThreads), 0, s, a,
+                             QT, KT, extra, least, blocks);
+    return launch_kernel(true, tree_join_kernel<T, HD, 4>, dim3((unsigned)((rows + 4 * warps - 1) / (4 * warps))), dim3(kJoinThreads), 0, s,
+                         a, QT, KT, extra, least, blocks);
 }
 
 template <int HD>

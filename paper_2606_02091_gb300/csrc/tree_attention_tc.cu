@@ -216,54 +216,61 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
             constexpr uint32_t kId = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 4) << 24);
             constexpr uint32_t kIdS = kId | ((128u >> 3) << 17), kIdO = kId | (1u << 16) | (((uint32_t)HD >> 3) << 17);
             bool ok = true;
-            int base = 0;               // tiles of the pairs before this one
-            int ps[2] = {0, 0};         // P handed over by each stream
-            int pair = 0;
+            uint32_t base = 0;              // tiles of the pairs before this one
+            uint32_t ps0 = 0, ps1 = 0;      // P handed over by each stream
+            uint32_t pair = 0;
+            auto wait = [&](uint32_t bar, uint32_t parity) {
+                if (ok) ok = bar_wait(bar, parity & 1u, &abort_flag, a.pg.err);
+            };
+            // S of tile x of the run by stream w (a constant where it is called)
+            auto issue_s = [&](uint32_t x, int w) {
+                const uint32_t st = x % NK;
+                if (NQ == 1 || w == 0) wait(kfull(st), x / NK);
+                if (!ok) return;
+                tc_fence_after();
+                const uint64_t dq = smem_desc(sb + LY::Q + (NQ == 2 ? w * TB : 0));
+                const uint64_t dk = smem_desc(sb + LY::K + st * TB);
+#pragma unroll
+                for (int kk = 0; kk < HD / 16; ++kk) {
+                    const uint64_t at = (uint64_t)((kk >> 2) * (16384 / 16) + (kk & 3) * 2);
+                    umma_bf16(tS(w), dq + at, dk + at, kIdS, kk > 0 ? 1u : 0u);
+                }
+                umma_commit(sfull(w));
+                if (NQ == 1 || w == 1) umma_commit(kempty(st));
+            };
             TreeRaw raw = more ? tree_raw(a, p.b) : TreeRaw{};
             for (; more; ++pair) {
-                const int n = p.hi - p.lo, steps = n * NQ;
+                const int n = p.hi - p.lo;
                 int nodes, ctx, keys;
                 tree_lengths(a, raw, nodes, ctx, keys);
                 const bool next = tree_pair<kTcExtra>(a, cum, v, v1, after);
                 if (next) raw = tree_raw(a, after.b);
-                auto wait = [&](uint32_t bar, uint32_t parity) {
-                    if (ok) ok = bar_wait(bar, parity, &abort_flag, a.pg.err);
-                };
-                auto issue_s = [&](int i) {
-                    const int x = base + i / NQ, w = i & 1, st = x % NK;
-                    if (NQ == 1 || w == 0) wait(kfull(st), (uint32_t)(x / NK) & 1u);
+                // PV of tile j of the pair by stream w, then the stream's next S
+                auto step = [&](int j, int w) {
+                    constexpr int stride = NQ == 1 ? 2 : 1;
+                    const uint32_t x = base + j, st = x % NV;
+                    if (NQ == 1 || w == 0) wait(vfull(st), x / NV);
+                    wait(pfull(w), w ? ps1++ : ps0++);
                     if (!ok) return;
-                    tc_fence_after();
-                    const uint64_t dq = smem_desc(sb + LY::Q + (NQ == 2 ? w * TB : 0));
-                    const uint64_t dk = smem_desc(sb + LY::K + st * TB);
-#pragma unroll
-                    for (int kk = 0; kk < HD / 16; ++kk) {
-                        const uint64_t at = (uint64_t)((kk >> 2) * (16384 / 16) + (kk & 3) * 2);
-                        umma_bf16(tS(w), dq + at, dk + at, kIdS, kk > 0 ? 1u : 0u);
-                    }
-                    umma_commit(sfull(w));
-                    if (NQ == 1 || w == 1) umma_commit(kempty(st));
-                };
-                wait(qfull, (uint32_t)pair & 1u);
-                if (ok) tc_fence_after();
-                issue_s(0);
-                if (steps > 1) issue_s(1);
-                for (int i = 0; i < steps && ok; ++i) {
-                    const int x = base + i / NQ, w = i & 1, st = x % NV;
-                    if (NQ == 1 || w == 0) wait(vfull(st), (uint32_t)(x / NV) & 1u);
-                    wait(pfull(w), (uint32_t)ps[w] & 1u);
-                    ++ps[w];
-                    if (!ok) break;
                     tc_fence_after();
                     const uint64_t dv = smem_desc_mn(sb + LY::V + st * TB, 16384);
                     // (weights and values past the last key are not multiplied, up to the 16 of a step)
-                    const int ks = min(kKeys / 16, (keys - (p.lo + i / NQ) * kKeys + 15) / 16);
+                    const int ks = min(kKeys / 16, (keys - (p.lo + j) * kKeys + 15) / 16);
 #pragma unroll
                     for (int kk = 0; kk < kKeys / 16; ++kk)
-                        if (kk < ks) umma_bf16_ts(tO(w), tS(w) + kk * 8, dv + (uint64_t)(kk * 128), kIdO, (i >= 2 || kk > 0) ? 1u : 0u);
+                        if (kk < ks) umma_bf16_ts(tO(w), tS(w) + kk * 8, dv + (uint64_t)(kk * 128), kIdO, (j >= stride || kk > 0) ? 1u : 0u);
                     if (NQ == 1 || w == 1) umma_commit(vempty(st));
-                    if (i + 2 >= steps) umma_commit(ofull(w));
-                    if (i + 2 < steps) issue_s(i + 2);
+                    if (j + stride < n) issue_s(x + stride, w);
+                    else umma_commit(ofull(w));
+                };
+                wait(qfull, pair);
+                if (ok) tc_fence_after();
+                issue_s(base, 0);
+                if (NQ == 2) issue_s(base, 1);
+                else if (n > 1) issue_s(base + 1, 1);
+                for (int j = 0; j < n && ok; j += NQ == 1 ? 2 : 1) {
+                    step(j, 0);
+                    if (NQ == 2 || j + 1 < n) step(NQ == 2 ? j : j + 1, 1);
                 }
                 if (!ok) break;
                 base += n;
