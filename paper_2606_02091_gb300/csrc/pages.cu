@@ -1,6 +1,8 @@
 // Pages of a paged cache: taking them from the free stack (with copy on write), sharing, giving back,
 // copying, and moving an accepted path's rows together.
 //
+// Every kernel here lets the next one start as soon as its own dependency wait is over: the next one's launch and
+// prologue then overlap, and its own wait still lasts until this one has ended.
 // Who holds what is kept in four small integer arrays (page table, pages held, reference counts, free
 // stack). One CTA works on them per call, so that the order in which pages are taken and given back, and
 // with it every page number, is the same on every run; the bytes are moved by kernels over the whole GPU.
@@ -67,10 +69,11 @@ __device__ __forceinline__ bool path_fits(const PagesView& pg, const int32_t* pa
 }
 
 // lens and the pages past them. Entry e of the call is one page that a sequence lets go, numbered by
-// sequence and then by position. Three passes over the entries: the reference counts go down; entries
-// whose page has none left leave their number behind, the largest wins (a page that several sequences
-// let go at once is pushed once, where the last of them stands); the winners are pushed in order.
-// add != NULL: lens grows by the accepted lengths; else it is cut to new_len.
+// sequence and then by position. All entries take one off their page's count and leave their number with the
+// page, where the largest stays; then those whose page has no count left and still holds their number (a page
+// that several sequences let go at once is pushed once, where the last of them stands) are pushed in order.
+// add != NULL: lens grows by the accepted lengths; else it is cut to new_len. Latency-bound: a chain of four
+// trips to memory.
 __global__ void __launch_bounds__(kMetaThreads) trim_kernel(const PagesView pg, const int32_t* __restrict__ new_len,
                                                             const int32_t* __restrict__ add,
                                                             const int32_t* __restrict__ path, int path_row,
@@ -78,6 +81,8 @@ __global__ void __launch_bounds__(kMetaThreads) trim_kernel(const PagesView pg, 
     __shared__ int first[kMaxSeqs + 1], from[kMaxSeqs], tmp[32];
     const int tid = threadIdx.x;
     pdl_wait();
+    pdl_trigger();
+    int top = *pg.n_free;
     if (add) {
         // a path that does not fit commits nothing (the moving kernel decided the same); from[] holds
         // the new length until the pages are counted
@@ -93,9 +98,10 @@ __global__ void __launch_bounds__(kMetaThreads) trim_kernel(const PagesView pg, 
     }
     int gone = 0;
     if (tid < n) {
-        const int len = add ? from[tid] : min(pg.lens[tid], max(new_len[tid], 0));
+        const int old = pg.lens[tid];
+        const int len = add ? from[tid] : min(old, max(new_len[tid], 0));
         const int held = min(max(pg.held[tid], 0), pg.max_pages), keep = pages_of(max(len, 0), pg.ps);
-        pg.lens[tid] = len;
+        if (len != old) pg.lens[tid] = len;
         gone = max(held - keep, 0);
         from[tid] = keep;
         if (gone) pg.held[tid] = keep;
@@ -115,19 +121,23 @@ __global__ void __launch_bounds__(kMetaThreads) trim_kernel(const PagesView pg, 
     int slot;
     for (int e = tid; e < total; e += kMetaThreads) {
         const int p = entry(e, &slot);
-        if (p < 0 || atomicSub(&pg.refs[p], 1) < 1) atomicOr(pg.err, DFLARE_DEVERR_PAGE);
+        if (p >= 0) {
+            atomicSub(&pg.refs[p], 1);
+            atomicMax(&last[p], e);
+        } else {
+            atomicOr(pg.err, DFLARE_DEVERR_PAGE);
+        }
     }
     __syncthreads();
-    for (int e = tid; e < total; e += kMetaThreads) {
-        const int p = entry(e, &slot);
-        if (p >= 0 && __ldcg(&pg.refs[p]) == 0) atomicMax(&last[p], e);
-    }
-    __syncthreads();
-    int top = *pg.n_free;
     for (int e0 = 0; e0 < total; e0 += kMetaThreads) {
         const int e = e0 + tid;
         const int p = e < total ? entry(e, &slot) : -1;
-        const bool push = p >= 0 && __ldcg(&last[p]) == e;
+        bool push = false;
+        if (p >= 0) {
+            const int refs = __ldcg(&pg.refs[p]), winner = __ldcg(&last[p]);
+            push = refs == 0 && winner == e;
+            if (refs < 0) atomicOr(pg.err, DFLARE_DEVERR_PAGE);
+        }
         int pushed;
         const int at = top + block_scan(push ? 1 : 0, tmp, &pushed) - 1;
         if (push && at < pg.pages) pg.free_pages[at] = p;
@@ -154,6 +164,8 @@ __global__ void __launch_bounds__(kMetaThreads) reserve_kernel(const PagesView p
     const int tid = threadIdx.x;
     if (tid == 0) bad = 0;
     pdl_wait();
+    pdl_trigger();
+    const int top = *pg.n_free;
     int grow = 0, len = 0, held = 0, fresh = 0, page = -1;
     if (tid < n) {
         grow = n_new[tid];
@@ -189,7 +201,6 @@ __global__ void __launch_bounds__(kMetaThreads) reserve_kernel(const PagesView p
     }
     if (tid == 0) first[0] = 0;
     __syncthreads();
-    const int top = *pg.n_free;
     if (bad || total > top || total < 0) {     // (a total past 2^31 would need more columns than tables have)
         if (tid == 0) {
             copies[0] = 0;
@@ -233,6 +244,7 @@ __global__ void __launch_bounds__(128) fork_kernel(const PagesView pg, const int
     const int i = blockIdx.x, tid = threadIdx.x;
     if (tid == 0) clash = 0;
     pdl_wait();
+    pdl_trigger();
     __syncthreads();
     const int a = src[i], b = dst[i];
     const bool range = a >= 0 && a < pg.max_batch && b >= 0 && b < pg.max_batch;
@@ -266,6 +278,7 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const PagesView pg, 
                                                             const int32_t* __restrict__ src,
                                                             const int32_t* __restrict__ dst, int n, int row_units) {
     pdl_wait();
+    pdl_trigger();
     const int pairs = list ? list[0] : n;
     const long long items = (long long)pairs * pg.layers * 2;
     const size_t page_units = (size_t)pg.hkv * pg.ps * row_units;     // of 16 bytes
@@ -306,16 +319,18 @@ __global__ void __launch_bounds__(kCopyThreads) move_kernel(const PagesView pg, 
     __shared__ int move_from[kMaxNodes], move_to[kMaxNodes];     // page * page size + offset
     __shared__ int n_moves;
     pdl_wait();
+    pdl_trigger();
     const int b = blockIdx.y, tid = threadIdx.x;
-    const int len = pg.lens[b], a = accept[b];
     path += (size_t)b * path_row;
+    const int first = tid < path_row && tid < 32 ? path[tid] : 0;     // under way together with the lengths
+    const int len = pg.lens[b], a = accept[b], held = pg.held[b];
     if (tid < 32) {
         int count = 0;
-        if (path_fits(pg, path, a, path_row, len, pg.held[b])) {
+        if (path_fits(pg, path, a, path_row, len, held)) {
             const int32_t* row = pg.table + (size_t)b * pg.max_pages;
             for (int j0 = 0; j0 < a; j0 += 32) {
                 const int j = j0 + tid;
-                const int x = j < a ? path[j] : j;
+                const int x = j >= a ? j : j0 ? path[j] : first;
                 bool moves = x != j;
                 int pa = 0, pb = 0;
                 if (moves) {

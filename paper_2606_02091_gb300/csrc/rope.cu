@@ -49,12 +49,6 @@ __device__ __forceinline__ void pair_turn(long long pos, uint64_t phase, float s
     s *= magnitude * sign;
 }
 
-// Where a head of a row is read and written. In an append heads are numbered q, then k, then v.
-struct Place {
-    const char* from;
-    char* to;
-};
-
 // row -> position, and whether there is anything to do; slot: where its key and value go (-1: nowhere)
 template <bool APPEND>
 __device__ __forceinline__ bool row_of(const RopeArgs& a, int row, long long& pos, long long& slot) {
@@ -78,6 +72,8 @@ __device__ __forceinline__ bool row_of(const RopeArgs& a, int row, long long& po
     return true;
 }
 
+// Where head h of a row is read and written (in an append heads are numbered q, then k, then v), and whether it
+// turns; false: nowhere.
 template <class T, bool APPEND>
 __device__ __forceinline__ bool place_of(const RopeArgs& a, int row, int h, long long slot, const T*& from, T*& to, bool& turn) {
     turn = true;
@@ -94,10 +90,37 @@ __device__ __forceinline__ bool place_of(const RopeArgs& a, int row, int h, long
     return slot >= 0;
 }
 
-// Vector form: rot and hd multiples of 16, everything 16-byte aligned.
+// 16 elements of storage in two runs of eight, as loaded; and their values
+template <class T> struct Unit { uint4 v[sizeof(T)]; };      // bf16: one 16-byte piece per run, fp32: two
+template <class T>
+__device__ __forceinline__ void load_unit(Unit<T>& x, const T* p0, const T* p1) {
+    constexpr int H = sizeof(T) / 2;
+#pragma unroll
+    for (int i = 0; i < H; ++i) {
+        x.v[i] = reinterpret_cast<const uint4*>(p0)[i];
+        x.v[H + i] = reinterpret_cast<const uint4*>(p1)[i];
+    }
+}
+template <class T>
+__device__ __forceinline__ void store_unit(const Unit<T>& x, T* p0, T* p1) {
+    constexpr int H = sizeof(T) / 2;
+#pragma unroll
+    for (int i = 0; i < H; ++i) {
+        reinterpret_cast<uint4*>(p0)[i] = x.v[i];
+        reinterpret_cast<uint4*>(p1)[i] = x.v[H + i];
+    }
+}
+__device__ __forceinline__ float2 get2(const Unit<bf16>& x, int i) { return __bfloat1622float2(reinterpret_cast<const __nv_bfloat162*>(x.v)[i]); }
+__device__ __forceinline__ float2 get2(const Unit<float>& x, int i) { return reinterpret_cast<const float2*>(x.v)[i]; }
+__device__ __forceinline__ void set2(Unit<bf16>& x, int i, float a, float b) { reinterpret_cast<__nv_bfloat162*>(x.v)[i] = __floats2bfloat162_rn(a, b); }
+__device__ __forceinline__ void set2(Unit<float>& x, int i, float a, float b) { reinterpret_cast<float2*>(x.v)[i] = make_float2(a, b); }
+
+// Vector form: rot and hd multiples of 16, everything 16-byte aligned. A thread's first heads are on their way
+// before it works out its cosines, and stay as they were stored until they are turned.
 template <class T, bool INTER, bool APPEND>
-__global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeArgs a) {
+__global__ void __launch_bounds__(kRopeThreads, sizeof(T) == 2 ? 3 : 2) rope_kernel(const RopeArgs a) {
     pdl_wait();
+    pdl_trigger();
     const int units = a.hd / 16, rot_units = a.rot / 16, half = a.rot / 2;
     const int total_heads = a.heads + (APPEND ? 2 * a.pg.hkv : 0);
     const long long t = (long long)blockIdx.x * kRopeThreads + threadIdx.x;
@@ -112,51 +135,44 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeArgs a) {
     // the unit's two runs of eight elements
     const int e0 = rotates && !INTER ? u * 8 : u * 16, e1 = rotates && !INTER ? half + u * 8 : u * 16 + 8;
     float c[8], s[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        c[j] = 1.f;
-        s[j] = 0.f;
-        if (rotates) pair_turn(pos, a.phase[u * 8 + j], a.sign, a.magnitude, c[j], s[j]);
-    }
     for (int h = h0; h < total_heads; h += a.slots * kBatchHeads) {
-        float x0[kBatchHeads][8], x1[kBatchHeads][8];
-        T* to[kBatchHeads];
-        bool turn[kBatchHeads];
+        Unit<T> x[kBatchHeads];
 #pragma unroll
         for (int k = 0; k < kBatchHeads; ++k) {
             const int hk = h + k * a.slots;
             const T* from;
-            to[k] = nullptr;
-            if (hk < total_heads && place_of<T, APPEND>(a, (int)row, hk, slot, from, to[k], turn[k])) {
-                load8(from + e0, x0[k]);
-                load8(from + e1, x1[k]);
-            } else {
-                to[k] = nullptr;
-            }
+            T* to;
+            bool turn;
+            if (hk < total_heads && place_of<T, APPEND>(a, (int)row, hk, slot, from, to, turn)) load_unit(x[k], from + e0, from + e1);
+        }
+        if (h == h0 && rotates) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) pair_turn(pos, a.phase[u * 8 + j], a.sign, a.magnitude, c[j], s[j]);
         }
 #pragma unroll
         for (int k = 0; k < kBatchHeads; ++k) {
-            if (!to[k]) continue;
-            if (rotates && turn[k]) {
-                float y0[8], y1[8];
+            const int hk = h + k * a.slots;
+            const T* from;
+            T* to;
+            bool turn;
+            if (hk >= total_heads || !place_of<T, APPEND>(a, (int)row, hk, slot, from, to, turn)) continue;
+            if (rotates && turn) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    if (INTER) {
-                        float* p = j < 4 ? x0[k] + 2 * j : x1[k] + 2 * j - 8;
-                        float* q = j < 4 ? y0 + 2 * j : y1 + 2 * j - 8;
-                        q[0] = p[0] * c[j] - p[1] * s[j];
-                        q[1] = p[1] * c[j] + p[0] * s[j];
-                    } else {
-                        y0[j] = x0[k][j] * c[j] - x1[k][j] * s[j];
-                        y1[j] = x1[k][j] * c[j] + x0[k][j] * s[j];
+                for (int j = 0; j < 8; j += 2) {
+                    if (INTER) {        // pairs are neighbours: two of them in a float2 each
+#pragma unroll
+                        for (int i = j; i < j + 2; ++i) {
+                            const float2 v = get2(x[k], i);
+                            set2(x[k], i, v.x * c[i] - v.y * s[i], v.y * c[i] + v.x * s[i]);
+                        }
+                    } else {            // pairs are eight (here four float2) apart
+                        const float2 v = get2(x[k], j / 2), w = get2(x[k], 4 + j / 2);
+                        set2(x[k], j / 2, v.x * c[j] - w.x * s[j], v.y * c[j + 1] - w.y * s[j + 1]);
+                        set2(x[k], 4 + j / 2, w.x * c[j] + v.x * s[j], w.y * c[j + 1] + v.y * s[j + 1]);
                     }
                 }
-                store8(to[k] + e0, y0);
-                store8(to[k] + e1, y1);
-            } else {
-                store8(to[k] + e0, x0[k]);
-                store8(to[k] + e1, x1[k]);
             }
+            store_unit(x[k], to + e0, to + e1);
         }
     }
 }
@@ -165,6 +181,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeArgs a) {
 template <class T, bool INTER, bool APPEND>
 __global__ void __launch_bounds__(kRopeThreads) rope_any_kernel(const RopeArgs a) {
     pdl_wait();
+    pdl_trigger();
     const int half = a.rot / 2, units = half + (a.hd - a.rot + 1) / 2;
     const int total_heads = a.heads + (APPEND ? 2 * a.pg.hkv : 0);
     const long long t = (long long)blockIdx.x * kRopeThreads + threadIdx.x;

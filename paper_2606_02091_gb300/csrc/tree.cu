@@ -1,5 +1,6 @@
 // Drafted trees: ancestor bits and depths from parent numbers, and greedy acceptance. Both calls are a few
-// hundred bytes to a few hundred kilobytes of integers: bound by the latency of a walk up (or down) a branch.
+// hundred bytes to a few hundred kilobytes of integers: bound by latency.
+#include <algorithm>
 #include <string>
 
 #include "common.cuh"
@@ -22,38 +23,64 @@ __device__ __forceinline__ void load_parents(const int32_t* __restrict__ parents
     }
 }
 
-// One CTA per tree, a thread per node (and per further node 256 on). A node's ancestors come up in
-// decreasing order, so its mask row is finished word by word from the last word down and needs no storage.
-__global__ void __launch_bounds__(kTreeThreads) tree_plan_kernel(const int32_t* __restrict__ parents,
+// One CTA per tree, rows of ancestor bits in shared memory, a thread per node (two above 512). Every node starts with
+// itself and looks one node up; each round it takes over the bits of the node it looks at (whose words end at that
+// node's own) and then looks where that one looks, so a branch of depth d is done in log2(d) rounds. Rows are taken
+// over while others write theirs: what is read early or late are ancestors of an ancestor either way. Rows go out as
+// whole lines. Measured for 64 trees of 255 nodes: walking up edge by edge 11 us (37 for chains).
+constexpr int kPlanThreads = 512, kPlanNodes = kMaxNodes / kPlanThreads;
+
+__global__ void __launch_bounds__(kPlanThreads) tree_plan_kernel(const int32_t* __restrict__ parents,
                                                                  const int32_t* __restrict__ n_nodes, int n_max,
                                                                  int words, uint32_t* __restrict__ mask,
                                                                  int32_t* __restrict__ depth, uint32_t* err) {
-    __shared__ int32_t up[kMaxNodes];
+    extern __shared__ uint32_t rows[];          // [n_max][words | 1]: an odd stride spreads the rows over the banks
+    __shared__ int32_t up[kMaxNodes];           // the node looked at, -1: above the top
+    __shared__ int16_t edges[kMaxNodes];        // edges up to there; at the end up to the top, plus one
     pdl_wait();
-    const int b = blockIdx.x;
+    pdl_trigger();
+    const int b = blockIdx.x, tid = threadIdx.x, stride = words | 1;
     const int told = n_nodes[b], n = min(max(told, 0), n_max);
     bool bad = told != n;
     load_parents(parents + (size_t)b * n_max, n, up, &bad);
     if (bad && err) atomicOr(err, DFLARE_DEVERR_TREE);
-    __syncthreads();
-    for (int i = threadIdx.x; i < n_max; i += kTreeThreads) {
-        uint32_t* row = mask + ((size_t)b * n_max + i) * words;
-        int w = words - 1, edges = -1;
-        uint32_t bits = 0;
-        for (int j = i < n ? i : -1; j >= 0; j = up[j]) {
-            while (w > (j >> 5)) {
-                row[w--] = bits;
-                bits = 0;
-            }
-            bits |= 1u << (j & 31);
-            ++edges;
-        }
-        while (w >= 0) {
-            row[w--] = bits;
-            bits = 0;
-        }
-        depth[(size_t)b * n_max + i] = max(edges, 0);
+    for (int i = tid; i < n_max; i += blockDim.x) {
+        for (int w = 0; w < words; ++w) rows[i * stride + w] = i < n && (i >> 5) == w ? 1u << (i & 31) : 0u;
+        edges[i] = 1;
     }
+    bool more = n > 0;
+    while (__syncthreads_or(more)) {
+        int to[kPlanNodes], len[kPlanNodes];
+        more = false;
+#pragma unroll
+        for (int k = 0; k < kPlanNodes; ++k) {
+            const int i = tid + k * kPlanThreads, u = i < n ? up[i] : -1;
+            to[k] = -1;
+            len[k] = 0;
+            if (u < 0) continue;
+            uint32_t* mine = rows + i * stride;
+            const uint32_t* theirs = rows + u * stride;
+#pragma unroll 4
+            for (int w = 0; w <= u >> 5; ++w) mine[w] |= theirs[w];
+            to[k] = up[u];
+            len[k] = edges[i] + edges[u];
+            more |= to[k] >= 0;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kPlanNodes; ++k) {
+            const int i = tid + k * kPlanThreads;
+            if (len[k]) {
+                edges[i] = (int16_t)len[k];
+                up[i] = to[k];
+            }
+        }
+    }
+    for (int x = tid; x < n_max * words; x += blockDim.x) {
+        const int i = x / words;
+        mask[(size_t)b * n_max * words + x] = rows[i * stride + x - i * words];
+    }
+    for (int i = tid; i < n_max; i += blockDim.x) depth[(size_t)b * n_max + i] = i < n ? edges[i] - 1 : 0;
 }
 
 // One CTA per tree. All nodes at once: whether the node's token is what the target chose after its parent,
@@ -65,6 +92,7 @@ __global__ void __launch_bounds__(kTreeThreads) tree_accept_kernel(
     __shared__ int32_t up[kMaxNodes], child[kMaxNodes], walk[kMaxNodes];
     __shared__ int steps;
     pdl_wait();
+    pdl_trigger();
     const int b = blockIdx.x, tid = threadIdx.x;
     const int told = n_nodes[b], n = min(max(told, 0), n_max);
     const int32_t* tok = tokens + (size_t)b * n_max;
@@ -108,9 +136,14 @@ dflare_status dflare_tree_plan(const int32_t* parents_dev, const int32_t* n_node
         return refuse(DFLARE_EINVAL, "dflare_tree_plan: NULL argument");
     if (batch < 1 || batch > 65535 || n_max < 1 || n_max > kMaxNodes)
         return refuse(DFLARE_EINVAL, "dflare_tree_plan: batch must be in [1, 65535], n_max in [1, 1024]");
-    const cudaError_t e = launch_kernel(true, tree_plan_kernel, dim3(batch), dim3(kTreeThreads), 0, static_cast<cudaStream_t>(stream),
-                                        parents_dev, n_nodes_dev, n_max, (n_max + 31) / 32,
-                                        reinterpret_cast<uint32_t*>(mask_dev), depth_dev, err_dev);
+    static PerDeviceOnce once;
+    const int words = (n_max + 31) / 32;
+    cudaError_t e = once([] {
+        return cudaFuncSetAttribute(tree_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxNodes * (kMaxNodes / 32 + 1) * 4);
+    });
+    if (e == cudaSuccess)
+        e = launch_kernel(true, tree_plan_kernel, dim3(batch), dim3(std::min(kPlanThreads, (n_max + 31) / 32 * 32)), (size_t)n_max * (words | 1) * 4, static_cast<cudaStream_t>(stream),
+                          parents_dev, n_nodes_dev, n_max, words, reinterpret_cast<uint32_t*>(mask_dev), depth_dev, err_dev);
     return e == cudaSuccess ? DFLARE_OK : refuse(DFLARE_ECUDA, std::string("dflare_tree_plan: ") + cudaGetErrorString(e));
 }
 
