@@ -256,4 +256,15 @@ def synthetic_target(draft_tokens, u, r, last, step, threshold, batch, block, ta
                                          _ptr(target_out), _stream(stream)))
 
 
-from .paged import PagedCache, rope, rope_phases, tree_accept, tree_plan  # noqa: E402,F401
+
+# The paged cache's binding works with torch at module level, so it is imported when one of its names is first asked for
+# (importing the package alone, as a build does, does not load torch).
+_PAGED = ("PagedCache", "rope", "rope_phases", "tree_accept", "tree_plan")
+
+
+def __getattr__(name):
+    if name in _PAGED:
+        from . import paged
+        globals().update((n, getattr(paged, n)) for n in _PAGED)
+        return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

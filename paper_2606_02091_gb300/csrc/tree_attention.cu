@@ -571,20 +571,24 @@ __global__ void __launch_bounds__(kFThreads) tree_f32_kernel(const TreeArgs a) {
 }
 
 // Rows whose keys several CTAs read: their partial results in the order of the keys. Also the rows that no
-// CTA had anything for: no keys, or past the tree's nodes. RW rows per warp: one where rows are few (a row's parts
-// in flight are what counts), four where they are many (measured: 64 nodes over 8 x 32768 keys, 16384 rows, 12 us
-// less than with one).
+// CTA had anything for: no keys, or past the tree's nodes. Where rows are few, four warps share a row's parts (PW), of
+// which one long context on one kv head leaves 304; where they are many, a warp takes four rows (RW). Measured, the
+// whole attention: one token over 100000 keys on one kv head 37 us with a warp per row and 21 with four; 16 nodes over
+// four contexts (2048 rows) 20 with one and 23 with four; 33 nodes at head_dim 64 (4224 rows) 35 with a warp per row
+// and 39 with one for four rows; 64 nodes over 8 x 32768 keys (16384 rows) 217 and 205.
 constexpr int kJoinThreads = 128;      // few enough registers to be resident beside the tcgen05 kernel's CTA
-constexpr int kJoinMany = 8192;        // rows from which on a warp takes four
+constexpr int kJoinFew = 1024, kJoinMany = 8192;    // rows below which a row takes four warps, from which on a warp takes four rows
 
-template <class T, int HD, int RW>
+template <class T, int HD, int RW, int PW>
 __global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(const TreeArgs a, int QT, int KT, int extra, int least, bool blocks) {
-    constexpr int LPR = 32 / RW, E = HD / LPR, V = E < 4 ? E : 4, J = RW == 1 ? 8 : 4;
-    // lane l of a row: elements g LPR V + l V .. of its groups g
+    static_assert(RW == 1 || PW == 1, "several rows per warp or several warps per row");
+    constexpr int LPR = 32 / RW, E = HD / LPR, V = E < 4 ? E : 4, J = RW == 1 && PW == 1 ? 8 : 4;
+    __shared__ float others[PW][HD + 2];    // of a row's warps: output, maximum, sum
     // The kernel before this one let it start after its own dependency wait, so the lengths are final here and
     // the division of the work is found while that kernel still runs.
-    const int lane = threadIdx.x & 31, l = lane % LPR;
-    const long long row = ((long long)blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5)) * RW + lane / LPR;
+    // Lane l of a row has the elements (g LPR + l) V .. of its groups g; warp pw of a row the parts pw, pw + PW, ...
+    const int lane = threadIdx.x & 31, l = lane % LPR, warp = threadIdx.x >> 5, pw = warp % PW;
+    const long long row = ((long long)blockIdx.x * (kJoinThreads / 32 / PW) + warp / PW) * RW + lane / LPR;
     const bool there = row < (long long)a.batch * a.n_max * a.hq;
     const int head = (int)(row % a.hq), node = (int)(row / a.hq % a.n_max), b = there ? (int)(row / a.hq / a.n_max) : 0;
     int n, ctx, keys;
@@ -607,11 +611,14 @@ __global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(const TreeArgs 
     const int c0 = start / per;
     int parts = some ? (start + tiles - 1) / per - c0 + 1 : 0;
     const bool written = parts == 1;        // by the CTA that read all of the row's keys
-    if (written) parts = 0;
+    parts = written ? 0 : (parts - pw + PW - 1) / PW;       // this warp's
     // every warp waits, so this launch does not end before the one it depends on
     pdl_wait();
     const int most = __reduce_max_sync(0xffffffffu, parts);
-    auto at = [&](int i) { return (((size_t)(c0 + i) * a.QG + qg) * 2 + (start < (c0 + i) * per ? 0 : 1)) * QT + r % QT; };
+    auto at = [&](int i) {
+        const int c = c0 + pw + i * PW;
+        return (((size_t)c * a.QG + qg) * 2 + (start < c * per ? 0 : 1)) * QT + r % QT;
+    };
     float acc[E], x[J][E], m = -INFINITY, sum = 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e) acc[e] = 0.f;
@@ -627,10 +634,10 @@ __global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(const TreeArgs 
                                                        : (row & ~(size_t)31) * HD + (e >> 5) * 1024 + (row & 31) * 32 +
                                                              ((((e & 31) >> 2) ^ (int)(row & 7)) << 2) + (e & 3));
                 if constexpr (V == 4) {
-                    const float4 v = i < parts ? *reinterpret_cast<const float4*>(src) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    const float4 v = i + j < parts ? *reinterpret_cast<const float4*>(src) : make_float4(0.f, 0.f, 0.f, 0.f);
                     x[j][4 * g] = v.x; x[j][4 * g + 1] = v.y; x[j][4 * g + 2] = v.z; x[j][4 * g + 3] = v.w;
                 } else {
-                    const float2 v = i < parts ? *reinterpret_cast<const float2*>(src) : make_float2(0.f, 0.f);
+                    const float2 v = i + j < parts ? *reinterpret_cast<const float2*>(src) : make_float2(0.f, 0.f);
                     x[j][0] = v.x; x[j][1] = v.y;
                 }
             }
@@ -665,6 +672,32 @@ __global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(const TreeArgs 
     }
 #pragma unroll
     for (int o = LPR / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if constexpr (PW > 1) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) others[pw][l * E + e] = acc[e];
+        if (l == 0) {
+            others[pw][HD] = m;
+            others[pw][HD + 1] = sum;
+        }
+        __syncthreads();
+        if (pw) return;
+        float top = m;
+#pragma unroll
+        for (int q = 1; q < PW; ++q) top = fmaxf(top, others[q][HD]);
+        const float ref = top == -INFINITY ? 0.f : top;
+        float f = exp2f(m - ref);
+        sum *= f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] *= f;
+#pragma unroll
+        for (int q = 1; q < PW; ++q) {
+            f = exp2f(others[q][HD] - ref);
+            sum = fmaf(others[q][HD + 1], f, sum);
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[e] = fmaf(others[q][l * E + e], f, acc[e]);
+        }
+        m = top;
+    }
     if (!there || written) return;
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     T* out = static_cast<T*>(a.out) + row * HD;
@@ -685,12 +718,14 @@ __global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(const TreeArgs 
 
 template <class T, int HD>
 cudaError_t launch_join(const TreeArgs& a, int QT, int KT, int extra, int least, bool blocks, cudaStream_t s) {
-    const long long rows = (long long)a.batch * a.n_max * a.hq;
-    const int warps = kJoinThreads / 32;
+    const long long rows = (long long)a.batch * a.n_max * a.hq, warps = kJoinThreads / 32;
+    if (rows < kJoinFew)
+        return launch_kernel(true, tree_join_kernel<T, HD, 1, 4>, dim3((unsigned)((rows * 4 + warps - 1) / warps)), dim3(kJoinThreads), 0, s,
+                             a, QT, KT, extra, least, blocks);
     if (rows < kJoinMany)
-        return launch_kernel(true, tree_join_kernel<T, HD, 1>, dim3((unsigned)((rows + warps - 1) / warps)), dim3(kJoinThreads), 0, s, a,
+        return launch_kernel(true, tree_join_kernel<T, HD, 1, 1>, dim3((unsigned)((rows + warps - 1) / warps)), dim3(kJoinThreads), 0, s, a,
                              QT, KT, extra, least, blocks);
-    return launch_kernel(true, tree_join_kernel<T, HD, 4>, dim3((unsigned)((rows + 4 * warps - 1) / (4 * warps))), dim3(kJoinThreads), 0, s,
+    return launch_kernel(true, tree_join_kernel<T, HD, 4, 1>, dim3((unsigned)((rows + 4 * warps - 1) / (4 * warps))), dim3(kJoinThreads), 0, s,
                          a, QT, KT, extra, least, blocks);
 }
 

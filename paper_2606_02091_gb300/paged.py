@@ -17,24 +17,25 @@ from __future__ import annotations
 
 import ctypes
 
+import torch
+
 from . import _lib
+
+_I32, _I64, _F32, _BF16 = torch.int32, torch.int64, torch.float32, torch.bfloat16
 
 
 # These calls take a few microseconds on the device, so the host's part counts: torch.cuda.current_stream()
-# makes a Stream object in 2.9 us (measured on the host's Arm cores), the plain handle is there in 0.1.
-_raw_stream = None
+# makes a Stream object in 2.9 us (measured on the host's Arm cores), the plain handle is there in 0.2.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_device = getattr(torch._C, "_cuda_getDevice", None)
 
 
 def _stream(stream):
-    global _raw_stream
     if stream is not None:
         return stream.cuda_stream
-    if _raw_stream is None:
-        import torch
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        device = torch.cuda.current_device
-        _raw_stream = (lambda: raw(device())) if raw else (lambda: torch.cuda.current_stream().cuda_stream)
-    return _raw_stream()
+    if _raw_stream is None or _device is None:
+        return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(_device())
 
 
 def _check(status):
@@ -44,12 +45,11 @@ def _check(status):
 
 def _ints(name, t, numel):
     """An int32 CUDA tensor of at least numel elements, without gaps; its address."""
-    import torch
-    if t.dtype is torch.int32 and t.is_cuda and t.is_contiguous() and t.numel() >= numel:
+    if t.dtype is _I32 and t.is_cuda and t.is_contiguous() and t.numel() >= numel:
         return t.data_ptr()
     if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
-    if t.dtype is not torch.int32:
+    if t.dtype is not _I32:
         raise ValueError(f"{name} must be torch.int32, got {t.dtype}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
@@ -83,19 +83,17 @@ def rope_phases(rot_dim, theta=1e6, scaling="none", factor=1.0, trained=4096, be
                 device="cuda"):
     """The phases of ``rot_dim`` rotated elements (int64 [rot_dim / 2], what the rotary calls take) and the
     factor on the rotated values. scaling: "none", "linear", "ntk" or "yarn"."""
-    import torch
     if scaling not in _lib.ROPE_SCALINGS:
         raise ValueError(f"scaling must be one of {sorted(_lib.ROPE_SCALINGS)}, got {scaling!r}")
     g = _lib.RopeConfig(rot_dim, _lib.ROPE_SCALINGS[scaling], theta, factor, trained, beta_fast, beta_slow)
-    out = torch.zeros(max(int(rot_dim) // 2, 1), dtype=torch.int64)
+    out = torch.zeros(max(int(rot_dim) // 2, 1), dtype=_I64)
     magnitude = ctypes.c_float(0.0)
     _check(_lib.load().dflare_rope_phases(ctypes.byref(g), out.data_ptr(), ctypes.byref(magnitude)))
     return out.to(device), magnitude.value
 
 
 def _phase(phase):
-    import torch
-    _typed("phase", phase, torch.int64)
+    _typed("phase", phase, _I64)
     if not phase.is_contiguous():
         raise ValueError("phase must be contiguous")
     return phase.data_ptr()
@@ -111,21 +109,21 @@ def rope(x, positions, phase, out, *, layout="half", magnitude=1.0, backward=Fal
     """Rotary embedding of x [rows][heads][head_dim] at int32 positions [rows] into out (x itself: in place).
     The first 2 * len(phase) elements of each head are rotated, the others copied. ``backward=True`` applies
     the transposed map, the gradient's."""
-    import torch
     if x.dim() != 3 or out.shape != x.shape:
         raise ValueError(f"x and out must be [rows][heads][head_dim], got {list(x.shape)} and {list(out.shape)}")
-    if x.dtype is not torch.bfloat16 and x.dtype is not torch.float32:
-        raise ValueError(f"x must be torch.bfloat16 or torch.float32, got {x.dtype}")
-    _typed("x", x, x.dtype)
-    _typed("out", out, x.dtype)
+    dtype = x.dtype
+    if dtype is not _BF16 and dtype is not _F32:
+        raise ValueError(f"x must be torch.bfloat16 or torch.float32, got {dtype}")
+    _typed("x", x, dtype)
+    _typed("out", out, dtype)
     rows, heads, hd = x.shape
-    xs, os_ = x.stride(), out.stride()
-    if (xs[2] != 1 or os_[2] != 1) and hd > 1:
+    x0, x1, x2 = x.stride()
+    o0, o1, o2 = out.stride()
+    if (x2 != 1 or o2 != 1) and hd > 1:
         raise ValueError("the elements of a head must be adjacent")
-    pos = _ints("positions", positions, rows)
-    _check(_lib.load().dflare_rope(x.data_ptr(), xs[0], xs[1], out.data_ptr(), os_[0], os_[1], pos, _phase(phase), rows, heads,
-                                   hd, 2 * phase.numel(), _layout(layout), magnitude, 1 if backward else 0,
-                                   _lib.DFLARE_BF16 if x.dtype is torch.bfloat16 else _lib.DFLARE_F32, _stream(stream)))
+    _check(_lib.load().dflare_rope(x.data_ptr(), x0, x1, out.data_ptr(), o0, o1, _ints("positions", positions, rows), _phase(phase),
+                                   rows, heads, hd, 2 * phase.numel(), _layout(layout), magnitude, backward,
+                                   _lib.DFLARE_BF16 if dtype is _BF16 else _lib.DFLARE_F32, _stream(stream)))
 
 
 def tree_plan(parents, n_nodes, mask, depth, stream=None):
@@ -160,11 +158,10 @@ class PagedCache:
     """
 
     def __init__(self, *, k, v, table, lens, held, refs, free, n_free, n_q_heads, max_nodes):
-        import torch
         self._cache = ctypes.c_void_p()
         if k.dim() != 5 or v.shape != k.shape:
             raise ValueError("k and v must be [n_layers][n_pages][n_kv_heads][page_size][head_dim]")
-        if k.dtype is not torch.bfloat16 and k.dtype is not torch.float32:
+        if k.dtype is not _BF16 and k.dtype is not _F32:
             raise ValueError(f"k must be torch.bfloat16 or torch.float32, got {k.dtype}")
         for name, t in (("k", k), ("v", v)):
             _typed(name, t, k.dtype)
@@ -181,7 +178,7 @@ class PagedCache:
                               _ints("free", free, self.n_pages), _ints("n_free", n_free, 1))
         self.cfg = _lib.CacheConfig(self.n_layers, self.n_pages, self.page_size, n_q_heads, self.n_kv_heads, self.head_dim,
                                     self.max_batch, self.max_pages, max_nodes,
-                                    _lib.DFLARE_BF16 if k.dtype is torch.bfloat16 else _lib.DFLARE_F32)
+                                    _lib.DFLARE_BF16 if k.dtype is _BF16 else _lib.DFLARE_F32)
         self.k, self.v, self.table, self.lens, self.held = k, v, table, lens, held
         self.refs, self.free, self.n_free = refs, free, n_free
         with torch.cuda.device(k.device):
@@ -191,16 +188,15 @@ class PagedCache:
     def allocate(cls, *, n_layers, n_pages, page_size, n_q_heads, n_kv_heads, head_dim, max_batch, max_pages, max_nodes,
                  dtype="bf16", device="cuda"):
         """An empty cache with memory of its own."""
-        import torch
-        t = torch.bfloat16 if dtype == "bf16" else torch.float32
+        t = _BF16 if dtype == "bf16" else _F32
         shape = (n_layers, n_pages, n_kv_heads, page_size, head_dim)
 
         def ints(*s):
-            return torch.zeros(s, dtype=torch.int32, device=device)
+            return torch.zeros(s, dtype=_I32, device=device)
 
         return cls(k=torch.empty(shape, dtype=t, device=device), v=torch.empty(shape, dtype=t, device=device),
                    table=ints(max_batch, max_pages) - 1, lens=ints(max_batch), held=ints(max_batch), refs=ints(n_pages),
-                   free=torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device), n_free=ints(1) + n_pages,
+                   free=torch.arange(n_pages - 1, -1, -1, dtype=_I32, device=device), n_free=ints(1) + n_pages,
                    n_q_heads=n_q_heads, max_nodes=max_nodes)
 
     def close(self):
@@ -252,7 +248,6 @@ class PagedCache:
         """Attention of q [batch][n][n_q_heads][head_dim] over the pages into out (contiguous). mask: the
         ancestor bits of tree_plan (None: node i sees nodes 0 .. i). scale: head_dim^-0.5 if None. lse: optional
         fp32 [batch][n][n_q_heads]."""
-        import torch
         if q.dim() != 4:
             raise ValueError(f"q must be [batch][n][n_q_heads][head_dim], got {list(q.shape)}")
         batch, n = q.shape[:2]
@@ -262,7 +257,7 @@ class PagedCache:
             raise ValueError(f"out must be contiguous {list(q.shape)}, got {list(out.shape)}")
         lp = None
         if lse is not None:
-            _typed("lse", lse, torch.float32)
+            _typed("lse", lse, _F32)
             if lse.numel() < batch * n * self.n_q_heads or not lse.is_contiguous():
                 raise ValueError(f"lse must be contiguous and hold {batch * n * self.n_q_heads} elements")
             lp = lse.data_ptr()
