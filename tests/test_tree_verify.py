@@ -928,3 +928,16 @@ def test_the_binding_refuses_wrong_tensors():
             call()
             pytest.fail(f"case {k} was accepted")
     assert c.error() == 0
+
+
+# ------------------------------------------------------------------------------------------ all of it together
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("plant", [0.0, 0.7])
+def test_the_example_decodes_what_plain_decoding_does(plant):
+    from examples import tree_verify as example
+    prompt = [(7 * i * i + 3) % example.VOCAB for i in range(37)]
+    out, plain, lengths = example.decode(prompt, [5, 6, 7], 8, plant)
+    assert all(o == p[:len(o)] for o, p in zip(out, plain))
+    if plant:       # the walk takes first and second choices, deep ones among them
+        assert max(map(max, lengths)) >= 4 and min(map(min, lengths)) >= 1
