@@ -54,7 +54,7 @@ struct TreeArgs {
     float2* part_ml;
     int layer, batch, n_max, words, hq, G;   // G: query heads per kv head
     uint32_t G_inv;            // 2^32 / G, rounded up (G > 1)
-    int QG, C;                 // groups of query rows, and CTAs along the keys for each
+    int QG, C;                 // groups of query rows, and CTAs that share the work (more are launched for more groups)
     float scale_log2;
 };
 

@@ -85,7 +85,6 @@ __global__ void __launch_bounds__(kMmaThreads, 2) tree_mma_kernel(const __grid_c
     __shared__ int abort_flag;
     __shared__ float2 ml[4][kRows];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int c = blockIdx.x;
     const uint32_t sb = smem_u32(smem), full = sb + LY::BARS, empty = full + 8 * kStages;
     if (tid == 0) {
         for (int i = 0; i < kStages; ++i) {
@@ -99,8 +98,8 @@ __global__ void __launch_bounds__(kMmaThreads, 2) tree_mma_kernel(const __grid_c
     if (tid < kMaxNodes / 32) odd[tid] = 0;
     pdl_wait();
     pdl_trigger();      // the joining launch reads the lengths at once: after this kernel's own wait
-    int v, v1;
-    tree_runs<kRows, kKeys, kExtra, kLeast>(a, 0, c, cum, v, v1);
+    int qg, v, v1;
+    tree_runs<kRows, kKeys, kExtra, kLeast>(a, cum, qg, v, v1);
     const int v0 = v;
     TreePair p, after;
     if (!tree_pair<kExtra>(a, cum, v, v1, p)) return;
@@ -362,7 +361,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) tree_mma_kernel(const __grid_c
                         }
                 });
             if (p.partial()) {
-                const size_t row = ((size_t)c * 2 + (p.start < v0 ? 0 : 1)) * kRows + r;
+                const size_t row = ((size_t)blockIdx.x * 2 + (p.start < v0 ? 0 : 1)) * kRows + r;
 #pragma unroll
                 for (int y = 0; y < QB; ++y)
                     *reinterpret_cast<float2*>(a.part_o + row * HD + col + y * 8) = make_float2(mine[y][2 * half], mine[y][2 * half + 1]);
@@ -412,11 +411,11 @@ __global__ void __launch_bounds__(kFThreads) tree_f32_kernel(const TreeArgs a) {
     extern __shared__ __align__(16) float fs[];
     __shared__ int32_t cum[kMaxSeqs + 1];
     float *Qs = fs + LY::Q, *Ks = fs + LY::K, *Vs = fs + LY::V, *Ps = fs + LY::P, *As = fs + LY::A;
-    const int tid = threadIdx.x, qg = blockIdx.x % a.QG, c = blockIdx.x / a.QG;
+    const int tid = threadIdx.x;
     pdl_wait();
     pdl_trigger();
-    int v, v1;
-    tree_runs<kFRows, kFKeys, kFExtra, kFLeast>(a, qg, c, cum, v, v1);
+    int qg, v, v1;
+    tree_runs<kFRows, kFKeys, kFExtra, kFLeast>(a, cum, qg, v, v1);
     const int v0 = v;
     const int ry = tid / 16, kx = tid % 16;         // scores: rows 2 ry, 2 ry + 1, keys kx, kx + 16
     const int rg = tid / DG, dg = tid % DG;         // output: rows rg RR .., head dims 4 dg ..
@@ -555,7 +554,7 @@ __global__ void __launch_bounds__(kFThreads) tree_f32_kernel(const TreeArgs a) {
             if (rr >= R) continue;
             const float mr = As[lr], sr = As[kFRows + lr];
             if (partial) {
-                const size_t row = (((size_t)c * a.QG + qg) * 2 + (it.start < v0 ? 0 : 1)) * kFRows + lr;
+                const size_t row = ((size_t)blockIdx.x * 2 + (it.start < v0 ? 0 : 1)) * kFRows + lr;
                 *reinterpret_cast<float4*>(a.part_o + row * HD + 4 * dg) = make_float4(o[r][0], o[r][1], o[r][2], o[r][3]);
                 if (dg == 0) a.part_ml[row] = make_float2(mr, sr);
             } else {
@@ -595,18 +594,32 @@ __global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(const TreeArgs 
     tree_lengths(a, tree_raw(a, b), n, ctx, keys);
     const bool some = there && node < n && keys > 0;
     const int r = node * a.G + head % a.G, qg = r / QT;
-    int before = 0, total = 0;
+    int cost = 0, groups = 0, C = max(a.C / a.QG, 1), first = qg * C, total = 0;       // the group's CTAs and list
+    const bool shares = a.QG > 1 && a.QG <= kShares;
+    if (shares) {
+        const TreeCosts costs = tree_costs<LPR>(a, l, QT, KT, extra, cost, groups);
+        tree_shares(a, costs, [&](int g, int from, int many) {
+            if (g == qg) {
+                first = from;
+                C = many;
+                total = costs.list[g];
+            }
+        });
+    }
+    int before = 0, sum_all = 0;
     for (int x = l; x < a.batch; x += LPR) {
-        const int t = tree_cost(tree_tiles(a, x, qg, QT, KT), extra);
-        total += t;
-        if (x < b) before += t;
+        if (x != l || !shares) cost = tree_cost(tree_tiles(a, x, QT, KT, groups), extra);
+        if (groups <= qg) continue;
+        sum_all += cost;
+        if (x < b) before += cost;
     }
 #pragma unroll
     for (int o = LPR / 2; o > 0; o >>= 1) {
-        total += __shfl_xor_sync(0xffffffffu, total, o);
+        if (!shares) sum_all += __shfl_xor_sync(0xffffffffu, sum_all, o);
         before += __shfl_xor_sync(0xffffffffu, before, o);
     }
-    const int per = tree_run(a, total * a.pg.hkv, least), tiles = tree_tiles(a, b, qg, QT, KT);
+    if (!shares) total = sum_all;
+    const int per = tree_run(total * a.pg.hkv, max(C, 1), least), tiles = tree_tiles(a, b, QT, KT, groups);
     const int start = before * a.pg.hkv + head / a.G * tree_cost(tiles, extra);
     const int c0 = start / per;
     int parts = some ? (start + tiles - 1) / per - c0 + 1 : 0;
@@ -617,7 +630,7 @@ __global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(const TreeArgs 
     const int most = __reduce_max_sync(0xffffffffu, parts);
     auto at = [&](int i) {
         const int c = c0 + pw + i * PW;
-        return (((size_t)c * a.QG + qg) * 2 + (start < c * per ? 0 : 1)) * QT + r % QT;
+        return ((size_t)(first + c) * 2 + (start < c * per ? 0 : 1)) * QT + r % QT;
     };
     float acc[E], x[J][E], m = -INFINITY, sum = 0.f;
 #pragma unroll
@@ -749,8 +762,8 @@ cudaError_t launch_f32(dflare_cache* c, TreeArgs a, cudaStream_t s) {
     cudaError_t e = once([] { return cudaFuncSetAttribute(tree_f32_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); });
     if (e != cudaSuccess) return e;
     a.QG = (a.n_max * a.G + kFRows - 1) / kFRows;
-    a.C = std::max(1, 2 * c->num_sms / a.QG);
-    e = launch_kernel(true, tree_f32_kernel<HD>, dim3(a.QG * a.C), dim3(kFThreads), bytes, s, a);
+    a.C = 2 * c->num_sms;
+    e = launch_kernel(true, tree_f32_kernel<HD>, dim3(std::max(a.QG, a.C)), dim3(kFThreads), bytes, s, a);
     return e == cudaSuccess ? launch_join<float, HD>(a, kFRows, kFKeys, kFExtra, kFLeast, false, s) : e;
 }
 

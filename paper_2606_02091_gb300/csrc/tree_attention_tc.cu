@@ -100,6 +100,24 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// Bounded wait, inline (a call would keep the compiler from giving the softmax threads their registers).
+__device__ __forceinline__ bool wait_inline(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t* err) {
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
+        if (mbar_try_wait(bar, parity)) return true;
+    const uint64_t t0 = globaltimer_ns();
+#pragma unroll 1
+    while (true) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if (*abort_flag) return false;
+        if (globaltimer_ns() - t0 > kTimeoutNs) {
+            *abort_flag = 1;
+            atomicOr(err, DFLARE_DEVERR_TIMEOUT);
+            return false;
+        }
+    }
+}
+
 template <int HD, int NQ>
 __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_constant__ CUtensorMap mk,
                                                               const __grid_constant__ CUtensorMap mv, const TreeArgs a) {
@@ -112,7 +130,6 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     __shared__ int odd_any, abort_flag;
     __shared__ uint32_t tmem_base;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int qg = blockIdx.x % a.QG, c = blockIdx.x / a.QG;
     const uint32_t sb = smem_u32(smem), bars = sb + LY::BARS;
     auto kfull = [&](int i) { return bars + 8u * i; };
     auto kempty = [&](int i) { return bars + 8u * (NK + i); };
@@ -157,8 +174,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     // before its own dependency wait can never hold columns that this CTA waits for. After this kernel's own
     // wait: the joining launch reads the lengths at once.
     pdl_trigger();
-    int v, v1;
-    tree_runs<QT, kKeys, kTcExtra, kTcLeast>(a, qg, c, cum, v, v1);
+    int qg, v, v1;
+    tree_runs<QT, kKeys, kTcExtra, kTcLeast>(a, cum, qg, v, v1);
     const int v0 = v;
     TreePair p, after;
     bool more = tree_pair<kTcExtra>(a, cum, v, v1, p);
@@ -187,7 +204,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                     if (i == 0 && kv == 1) asm volatile("bar.sync 2, 288;" ::: "memory");
                     const int N = kv ? NV : NK, st = i % N;
                     if (i >= N)
-                        ok = __all_sync(0xffffffffu, bar_wait(kv ? vempty(st) : kempty(st), (uint32_t)(i / N - 1) & 1u, &abort_flag, a.pg.err));
+                        ok = __all_sync(0xffffffffu, wait_inline(kv ? vempty(st) : kempty(st), (uint32_t)(i / N - 1) & 1u, &abort_flag, a.pg.err));
                     if (!ok) break;
                     const uint32_t bar = kv ? vfull(st) : kfull(st), dst = sb + (kv ? LY::V : LY::K) + st * TB;
                     if (leader) mbar_expect_tx(bar, TB);
@@ -205,8 +222,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         }
         if (!ok && leader) {   // the copies in flight land before the CTA's shared memory is given up
             volatile int never = 0;
-            for (int j = max(0, i - NK); j < i; ++j) bar_wait(kfull(j % NK), (uint32_t)(j / NK) & 1u, &never, a.pg.err);
-            for (int j = max(0, i - NV); j < i; ++j) bar_wait(vfull(j % NV), (uint32_t)(j / NV) & 1u, &never, a.pg.err);
+            for (int j = max(0, i - NK); j < i; ++j) wait_inline(kfull(j % NK), (uint32_t)(j / NK) & 1u, &never, a.pg.err);
+            for (int j = max(0, i - NV); j < i; ++j) wait_inline(vfull(j % NV), (uint32_t)(j / NV) & 1u, &never, a.pg.err);
         }
         __syncwarp();
     } else if (warp == 9) {
@@ -220,7 +237,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
             uint32_t ps0 = 0, ps1 = 0;      // P handed over by each stream
             uint32_t pair = 0;
             auto wait = [&](uint32_t bar, uint32_t parity) {
-                if (ok) ok = bar_wait(bar, parity & 1u, &abort_flag, a.pg.err);
+                if (ok) ok = wait_inline(bar, parity & 1u, &abort_flag, a.pg.err);
             };
             // S of tile x of the run by stream w (a constant where it is called)
             auto issue_s = [&](uint32_t x, int w) {
@@ -282,7 +299,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
             if (!ok) {
                 umma_commit(drain);
                 volatile int never = 0;
-                bar_wait(drain, 0, &never, a.pg.err);
+                wait_inline(drain, 0, &never, a.pg.err);
             }
         }
         __syncwarp();
@@ -297,7 +314,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         bool ok = true;
         int base = 0, ss = 0, os = 0;
         auto wait = [&](uint32_t bar, uint32_t parity) {
-            if (ok) ok = __all_sync(0xffffffffu, bar_wait(bar, parity, &abort_flag, a.pg.err));
+            if (ok) ok = __all_sync(0xffffffffu, wait_inline(bar, parity, &abort_flag, a.pg.err));
         };
         // Q of a pair, asynchronously, by `many` threads (this one the who-th) from row q0 on: pieces of eight
         // elements, swizzled; rows past R are never looked at
@@ -379,16 +396,17 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                 }
                 if (edge && warp_live) {
                     // scores of unseen keys become -inf where they are (in the loop below a branch for it costs
-                    // every tile 0.1 us)
+                    // every tile 0.1 us, a second copy of the loop as much in registers)
 #pragma unroll 1
                     for (int x = max(ctx - k0, 0) >> 5; x < 4; ++x) {
-                        const uint32_t see = seen32(a, row, p.b, node, ctx, keys, k0 + 32 * x);
-                        uint32_t s[32];
-                        tmem_ld32_async(tS(w) + lanes + 32 * x, s);
-                        tmem_wait_ld();
+                        uint32_t see = 0, s[32];
+                        if (k0 + 32 * x < keys) {
+                            see = seen32(a, row, p.b, node, ctx, keys, k0 + 32 * x);
+                            tmem_ld32_async(tS(w) + lanes + 32 * x, s);
+                            tmem_wait_ld();
+                        }
 #pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (!((see >> e) & 1u)) s[e] = 0xff800000u;
+                        for (int e = 0; e < 32; ++e) s[e] = see & (1u << e) ? s[e] : 0xff800000u;
                         tmem_st16(tS(w) + lanes + 32 * x, s);
                         tmem_st16(tS(w) + lanes + 32 * x + 16, s + 16);
                     }
@@ -431,6 +449,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                                 p0 = pow2(p0);
                                 p1 = pow2(p1);
                                 sum[e & 1] = add2(sum[e & 1], pack2(p0, p1));
+                                // (rounded to bf16, relative error 2^-8 at most; the sum is of the unrounded ones)
                                 pw[16 * x + e] = two_bf16(p0, p1);
                             }
                         }
@@ -502,7 +521,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                 }
                 uint8_t* turn = smem + LY::TURN + warp * 4096;
                 const int rows = min(32, R - (my_row - lane));
-                const size_t prow = (((size_t)c * a.QG + qg) * 2 + slot) * QT + (NQ == 2 ? 128 * w : 0) + r;
+                const size_t prow = ((size_t)blockIdx.x * 2 + slot) * QT + (NQ == 2 ? 128 * w : 0) + r;
                 const size_t orow = ((size_t)p.b * a.n_max + node) * a.hq + p.h * a.G + min(my_row, R - 1) - node * a.G;
                 constexpr int CH = NQ == 2 ? HD / 32 : HD / 64;
                 const int col0 = NQ == 2 ? 0 : w * (HD / 2);
@@ -612,8 +631,8 @@ cudaError_t launch_tc(dflare_cache* c, TreeArgs& a, cudaStream_t s) {
     });
     if (e != cudaSuccess) return e;
     a.QG = (a.n_max * a.G + 128 * NQ - 1) / (128 * NQ);
-    a.C = std::max(1, c->num_sms / a.QG);
-    return launch_kernel(true, tree_tc_kernel<HD, NQ>, dim3(a.QG * a.C), dim3(kThreads), TcLayout<HD, NQ>::BYTES, s, c->maps[0],
+    a.C = c->num_sms;
+    return launch_kernel(true, tree_tc_kernel<HD, NQ>, dim3(std::max(a.QG, a.C)), dim3(kThreads), TcLayout<HD, NQ>::BYTES, s, c->maps[0],
                          c->maps[1], a);
 }
 

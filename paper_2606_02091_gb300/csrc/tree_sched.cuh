@@ -2,10 +2,11 @@
 //
 // The query rows of one kv head are n * G (row r: node r / G, query head r % G of the group), cut into
 // groups of QT rows. For one group index qg the work is the list of all (sequence, kv head) pairs that have
-// such rows, each with ceil(keys / KT) key tiles; C CTAs take equal runs of that list, wherever they begin
-// and end, so contexts of any lengths load the CTAs evenly. A pair counts EXTRA tiles beyond its own for what
-// beginning and ending it costs. The CTAs of different qg with the same place in the list are neighbours in
-// the grid: they read the same keys at about the same time, once from HBM.
+// such rows, each with ceil(keys / KT) key tiles; the group's CTAs take equal runs of that list, wherever they
+// begin and end, so contexts of any lengths load the CTAs evenly. A pair counts EXTRA tiles beyond its own for
+// what beginning and ending it costs. The groups share the CTAs in proportion to their lists (trees of a batch
+// differ, and so does the number of sequences that reach a group); groups with equal lists read the same keys at
+// about the same time, once from HBM.
 // Rows whose keys lie in one run are written by that CTA; rows whose keys several CTAs read leave partial
 // results (at most two per CTA: of the pair it begins in and of the pair it ends in) that a second launch
 // joins in a fixed order.
@@ -29,26 +30,112 @@ __device__ __forceinline__ void tree_lengths(const TreeArgs& a, const TreeRaw& x
     ctx = min(ctx, keys);
 }
 
-// key tiles of sequence b for query group qg, and what they count in the list
-__device__ __forceinline__ int tree_tiles(const TreeArgs& a, int b, int qg, int QT, int KT) {
+// key tiles of sequence b (0: it has no query rows, or no keys) and its query groups
+__device__ __forceinline__ int tree_tiles(const TreeArgs& a, int b, int QT, int KT, int& groups) {
     int n, ctx, keys;
     tree_lengths(a, tree_raw(a, b), n, ctx, keys);
-    return n * a.G > qg * QT ? (int)(((long long)keys + KT - 1) / KT) : 0;
+    const int tiles = n ? (int)(((long long)keys + KT - 1) / KT) : 0;
+    groups = tiles ? (n * a.G + QT - 1) / QT : 0;
+    return tiles;
 }
 __device__ __forceinline__ int tree_cost(int tiles, int extra) { return tiles ? tiles + extra : 0; }
 // length of a run; below `least` it would cost more in joining than it saves
-__device__ __forceinline__ int tree_run(const TreeArgs& a, int total, int least) { return max((total + a.C - 1) / a.C, least); }
+__device__ __forceinline__ int tree_run(int total, int C, int least) { return max((total + C - 1) / C, least); }
 
-// The run [v0, v1) of this CTA, and cum[0 .. batch] (cost of one kv head before sequence b) in shared memory.
-// All threads of the CTA call it; it ends with a barrier.
+// The groups' lists and their parts of the grid. Up to kShares groups share the CTAs by their lists, one CTA for
+// every group that has rows and the others in proportion; more groups share them evenly.
+constexpr int kShares = 8;
+struct TreeCosts {
+    int list[kShares];      // of one kv head
+};
+// LANES adjacent lanes (l: this one's number) add up the groups' lists; first_cost, first_groups: those of sequence l.
+template <int LANES>
+__device__ __forceinline__ TreeCosts tree_costs(const TreeArgs& a, int l, int QT, int KT, int extra, int& first_cost, int& first_groups) {
+    TreeCosts c;
+#pragma unroll
+    for (int g = 0; g < kShares; ++g) c.list[g] = 0;
+    first_cost = first_groups = 0;
+    for (int b = l; b < a.batch; b += LANES) {
+        int groups;
+        const int cost = tree_cost(tree_tiles(a, b, QT, KT, groups), extra);
+        if (b == l) {
+            first_cost = cost;
+            first_groups = groups;
+        }
+#pragma unroll
+        for (int g = 0; g < kShares; ++g) c.list[g] += groups > g ? cost : 0;
+    }
+#pragma unroll
+    for (int g = 0; g < kShares; ++g) {
+        if (g >= a.QG) break;
+        if constexpr (LANES == 32) {
+            c.list[g] = __reduce_add_sync(0xffffffffu, c.list[g]);
+        } else {
+#pragma unroll
+            for (int o = LANES / 2; o > 0; o >>= 1) c.list[g] += __shfl_xor_sync(0xffffffffu, c.list[g], o);
+        }
+    }
+    return c;
+}
+// f(group, first CTA, CTAs) for every group, in order (up to kShares of them)
+template <class F>
+__device__ __forceinline__ void tree_shares(const TreeArgs& a, const TreeCosts& c, F f) {
+    float all = 0.f;
+    int some = 0;
+#pragma unroll
+    for (int g = 0; g < kShares; ++g) {
+        if (g >= a.QG) break;
+        all += (float)c.list[g];
+        some += c.list[g] > 0;
+    }
+    int base = 0;
+#pragma unroll
+    for (int g = 0; g < kShares; ++g) {
+        if (g >= a.QG) break;
+        // rounded down with room to spare, so that the parts never add up to more than there is
+        const int C = c.list[g] ? 1 + (int)__fmul_rn(__fmul_rn((float)max(a.C - some, 0), 0.999999f), __fdiv_rn((float)c.list[g], all)) : 0;
+        f(g, base, C);
+        base += C;
+    }
+}
+
+// The query group of this CTA, its run [v0, v1) of the group's list, and cum[0 .. batch] (cost of one kv head before
+// sequence b) in shared memory. All threads of the CTA call it; it ends with a barrier. An empty run: nothing to do.
 template <int QT, int KT, int EXTRA, int LEAST>
-__device__ __forceinline__ void tree_runs(const TreeArgs& a, int qg, int c, int32_t* cum, int& v0, int& v1) {
+__device__ __forceinline__ void tree_runs(const TreeArgs& a, int32_t* cum, int& qg, int& v0, int& v1) {
+    __shared__ int mine[3];     // group, this CTA's number in it, its CTAs
     const int tid = threadIdx.x;
     if (tid < 32) {
+        int cost, groups, g = 0, c = blockIdx.x, C = a.C;
+        if (a.QG > kShares) {
+            C = max(a.C / a.QG, 1);
+            g = blockIdx.x / C;
+            c = blockIdx.x % C;
+            if (g >= a.QG) C = 0;
+        } else if (a.QG > 1) {
+            const TreeCosts costs = tree_costs<32>(a, tid, QT, KT, EXTRA, cost, groups);
+            C = 0;
+            tree_shares(a, costs, [&](int x, int first, int many) {
+                if ((int)blockIdx.x >= first && (int)blockIdx.x < first + many) {
+                    g = x;
+                    c = blockIdx.x - first;
+                    C = many;
+                }
+            });
+        }
+        if (tid == 0) {
+            mine[0] = g;
+            mine[1] = c;
+            mine[2] = C;
+        }
         int base = 0;
         for (int b0 = 0; b0 < a.batch; b0 += 32) {
             const int b = b0 + tid;
-            int v = b < a.batch ? tree_cost(tree_tiles(a, b, qg, QT, KT), EXTRA) : 0;
+            if (b0 || a.QG == 1 || a.QG > kShares) {
+                groups = 0;
+                cost = b < a.batch ? tree_cost(tree_tiles(a, b, QT, KT, groups), EXTRA) : 0;
+            }
+            int v = groups > g ? cost : 0;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const int x = __shfl_up_sync(0xffffffffu, v, o);
@@ -60,8 +147,9 @@ __device__ __forceinline__ void tree_runs(const TreeArgs& a, int qg, int c, int3
         if (tid == 0) cum[0] = 0;
     }
     __syncthreads();
-    const int total = cum[a.batch] * a.pg.hkv, per = tree_run(a, total, LEAST);
-    v0 = (int)min((long long)c * per, (long long)total);
+    qg = mine[0];
+    const int total = mine[2] ? cum[a.batch] * a.pg.hkv : 0, per = tree_run(total, max(mine[2], 1), LEAST);
+    v0 = (int)min((long long)mine[1] * per, (long long)total);
     v1 = (int)min((long long)v0 + per, (long long)total);
 }
 
@@ -113,17 +201,20 @@ __device__ __forceinline__ TileBoxes tile_boxes(const TreeArgs& a, const TreePai
     return x;
 }
 
-// Infinite and NaN bf16 values of a 16-byte piece become 0; whether there were any.
+// Infinite and NaN bf16 values of a 16-byte piece become 0; whether there were any. (An exponent of all ones plus
+// its lowest bit carries into the sign's place.)
 __device__ __forceinline__ bool drop_odd(uint4& v) {
+    auto carry = [](uint32_t w) { return (w & 0x7f807f80u) + 0x00800080u; };
+    if (!((carry(v.x) | carry(v.y) | carry(v.z) | carry(v.w)) & 0x80008000u)) return false;
     uint32_t* e = reinterpret_cast<uint32_t*>(&v);
-    bool bad = false;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        if ((e[q] & 0x7f80u) == 0x7f80u) { e[q] &= 0xffff0000u; bad = true; }
-        if ((e[q] & 0x7f800000u) == 0x7f800000u) { e[q] &= 0xffffu; bad = true; }
+        const uint32_t c = carry(e[q]);
+        e[q] &= (c & 0x8000u ? 0xffff0000u : ~0u) & (c & 0x80000000u ? 0xffffu : ~0u);
     }
-    return bad;
+    return true;
 }
+
 // row / G for the rows of a kv head (below 2^16): a multiplication by the rounded-up reciprocal
 __device__ __forceinline__ int group_of(const TreeArgs& a, int row) { return a.G == 1 ? row : (int)__umulhi((unsigned)row, a.G_inv); }
 
@@ -169,12 +260,13 @@ __device__ __forceinline__ uint32_t seen_word(const TreeArgs& a, const SeenRow& 
     if (i >= 4 && i < a.words) v = (uint32_t)a.mask[((size_t)b * a.n_max + node) * a.words + i];
     return v;
 }
+__device__ __forceinline__ uint32_t low_bits32(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
 __device__ __forceinline__ uint32_t seen32(const TreeArgs& a, const SeenRow& r, int b, int node, int ctx, int keys, int k0) {
     const int rel = k0 - ctx;
     uint32_t v;
     if (a.mask) v = __funnelshift_r(seen_word(a, r, b, node, rel >> 5), seen_word(a, r, b, node, (rel >> 5) + 1), rel & 31);
-    else v = (uint32_t)low_bits(node + 1 - rel);
-    return (v | (uint32_t)low_bits(-rel)) & (uint32_t)low_bits(keys - k0);
+    else v = low_bits32(node + 1 - rel);
+    return (v | low_bits32(-rel)) & low_bits32(keys - k0);
 }
 
 // f(value address) for every node in odd[] (one bit per node) that `node` sees, in the layer's values of kv head h
