@@ -395,7 +395,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) tree_mma_kernel(const __grid_c
 constexpr int kFKeys = 32;
 constexpr int kFRows = 16;
 constexpr int kFThreads = 128;
-constexpr int kFExtra = 2, kFLeast = 3;
+constexpr int kFExtra = 0, kFLeast = 1;     // (a tile takes as long as beginning and ending a pair: 13.0 us with 2 and 3, three contexts up to 600)
 
 template <int HD>
 struct F32Layout {
