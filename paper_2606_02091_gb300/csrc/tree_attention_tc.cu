@@ -399,12 +399,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                     // every tile 0.1 us, a second copy of the loop as much in registers)
 #pragma unroll 1
                     for (int x = max(ctx - k0, 0) >> 5; x < 4; ++x) {
-                        uint32_t see = 0, s[32];
-                        if (k0 + 32 * x < keys) {
-                            see = seen32(a, row, p.b, node, ctx, keys, k0 + 32 * x);
-                            tmem_ld32_async(tS(w) + lanes + 32 * x, s);
-                            tmem_wait_ld();
-                        }
+                        const uint32_t see = seen32(a, row, p.b, node, ctx, keys, k0 + 32 * x);
+                        uint32_t s[32];
+                        tmem_ld32_async(tS(w) + lanes + 32 * x, s);
+                        tmem_wait_ld();
 #pragma unroll
                         for (int e = 0; e < 32; ++e) s[e] = see & (1u << e) ? s[e] : 0xff800000u;
                         tmem_st16(tS(w) + lanes + 32 * x, s);
