@@ -393,7 +393,9 @@ dflare_status dflare_argmax_noalloc(const float* logits_dev, int rows, int vocab
  *
  * These calls take no dflare_ctx. Messages of failing calls are in dflare_last_error(NULL) of the
  * calling thread. They are stream-ordered, asynchronous unless they say otherwise, allocate nothing
- * except dflare_cache_create, and may be captured into CUDA graphs.
+ * except dflare_cache_create, and may be captured into CUDA graphs. Calls on one cache share its
+ * workspace and tables: they must be ordered by a stream, or by events across streams. Those with a cache
+ * run on its device, the others on the current device.
  */
 
 /* Rotary frequencies. Pair j of rot_dim / 2 turns by inv_j = theta^(-2 j / rot_dim) radians per position;
@@ -491,8 +493,9 @@ dflare_status dflare_cache_reserve(dflare_cache* cache, const int32_t* n_new_dev
  *   depth_dev            [batch][n_max] int32: the row's position is lens[b] + depth; NULL: lens[b] + i.
  *   phase_dev ... magnitude  as in dflare_rope; rot_dim = 0 stores keys as they are.
  * Rotated keys and the values go to slot lens[b] + i; a row whose slot lies beyond the sequence's pages
- * is left out and sets DFLARE_DEVERR_CAPACITY (its query is still written). Rows from n_new[b] on are
- * neither read nor written.
+ * is left out and sets DFLARE_DEVERR_CAPACITY, one whose slot lies on a page that is still shared (no room
+ * was reserved) DFLARE_DEVERR_PAGE; its query is written all the same. Rows from n_new[b] on are neither
+ * read nor written.
  */
 dflare_status dflare_cache_append(dflare_cache* cache, int layer, const void* q_dev, long long q_row,
                                   const void* k_dev, long long k_row, const void* v_dev, long long v_row,
@@ -520,7 +523,8 @@ dflare_status dflare_cache_attend(dflare_cache* cache, int layer, const void* q_
 /* Accept nodes path[b][0 .. accept_len[b]) of each sequence's tree ([batch][path_row] int32, increasing):
  * their rows of all layers move to slots lens[b] .. lens[b] + accept_len[b] - 1, lens grows by accept_len,
  * and pages past the new length are given back (by sequence, then by position). A length or path that no
- * tree has sets DFLARE_DEVERR_TREE and commits nothing of that sequence. */
+ * tree has, or a last page that is still shared, sets DFLARE_DEVERR_TREE and commits nothing of that
+ * sequence. */
 dflare_status dflare_cache_commit(dflare_cache* cache, const int32_t* accept_len_dev, const int32_t* path_dev,
                                   int path_row, int batch, void* stream);
 

@@ -56,10 +56,15 @@ __device__ __forceinline__ int entry_owner(const int* first, int n, int e) {
 
 __device__ __forceinline__ int pages_of(int tokens, int ps) { return (tokens + ps - 1) / ps; }
 
-// Whether sequence b can commit `a` nodes of `path`: 0 <= a <= n, numbers increasing from 0 or more, and
-// all their slots on pages that it holds. The answer is the same in every lane of the calling warp.
-__device__ __forceinline__ bool path_fits(const PagesView& pg, const int32_t* path, int a, int n, int len, int held) {
-    bool ok = a >= 0 && a <= n;
+// Whether sequence b can commit `a` nodes of `path`: 0 <= a <= n, numbers increasing from 0 or more, all their slots
+// on pages that it holds, and the page with its last tokens its own (it is, once room was reserved). The answer is
+// the same in every lane of the calling warp.
+__device__ __forceinline__ bool path_fits(const PagesView& pg, int b, const int32_t* path, int a, int n, int len, int held) {
+    bool ok = len >= 0 && a >= 0 && a <= n;
+    if (ok && a > 0 && len % pg.ps && len / pg.ps < min(held, pg.max_pages)) {
+        const int page = pg.table[(size_t)b * pg.max_pages + len / pg.ps];
+        if (page < 0 || page >= pg.pages || pg.refs[page] > 1) ok = false;
+    }
     const int room = min(held, pg.max_pages) * pg.ps - len;     // slots behind len
     for (int j = threadIdx.x & 31; ok && j < a; j += 32) {
         const int x = path[j];
@@ -88,7 +93,7 @@ __global__ void __launch_bounds__(kMetaThreads) trim_kernel(const PagesView pg, 
         // the new length until the pages are counted
         for (int b = tid >> 5; b < n; b += kMetaThreads / 32) {
             const int len = pg.lens[b], a = add[b];
-            const bool fits = path_fits(pg, path + (size_t)b * path_row, a, path_row, len, pg.held[b]);
+            const bool fits = path_fits(pg, b, path + (size_t)b * path_row, a, path_row, len, pg.held[b]);
             if ((tid & 31) == 0) {
                 from[b] = fits ? len + a : len;
                 if (!fits) atomicOr(pg.err, DFLARE_DEVERR_TREE);
@@ -326,7 +331,7 @@ __global__ void __launch_bounds__(kCopyThreads) move_kernel(const PagesView pg, 
     const int len = pg.lens[b], a = accept[b], held = pg.held[b];
     if (tid < 32) {
         int count = 0;
-        if (path_fits(pg, path, a, path_row, len, held)) {
+        if (path_fits(pg, b, path, a, path_row, len, held)) {
             const int32_t* row = pg.table + (size_t)b * pg.max_pages;
             for (int j0 = 0; j0 < a; j0 += 32) {
                 const int j = j0 + tid;

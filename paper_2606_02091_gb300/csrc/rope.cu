@@ -63,12 +63,15 @@ __device__ __forceinline__ bool row_of(const RopeArgs& a, int row, long long& po
     pos = (long long)len + (a.depth ? a.depth[row] : i);
     const long long at = (long long)len + i;
     const long long room = (long long)min(a.pg.held[b], a.pg.max_pages) * a.pg.ps;
+    uint32_t err = DFLARE_DEVERR_CAPACITY;
     if (len >= 0 && at < room) {
         const int page = a.pg.table[(size_t)b * a.pg.max_pages + at / a.pg.ps];
-        if (page >= 0 && page < a.pg.pages)
+        err = DFLARE_DEVERR_PAGE;
+        // the page that holds the last tokens may still be shared where no room was reserved: it is not written
+        if (page >= 0 && page < a.pg.pages && !(at / a.pg.ps == len / a.pg.ps && len % a.pg.ps && a.pg.refs[page] > 1))
             slot = ((long long)a.layer * a.pg.pages + page) * a.pg.hkv * a.pg.ps + at % a.pg.ps;
     }
-    if (slot < 0) atomicOr(a.pg.err, DFLARE_DEVERR_CAPACITY);
+    if (slot < 0) atomicOr(a.pg.err, err);
     return true;
 }
 

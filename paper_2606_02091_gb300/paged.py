@@ -38,6 +38,12 @@ def _stream(stream):
     return _raw_stream(_device())
 
 
+def _here(name, t):
+    """Calls without a cache run on the current device; memory of another one must not reach them."""
+    if _device is not None and t.get_device() != _device():
+        raise ValueError(f"{name} must be on the current device, got {t.device}")
+
+
 def _check(status):
     if status:
         _lib.check(status, None)
@@ -116,6 +122,7 @@ def rope(x, positions, phase, out, *, layout="half", magnitude=1.0, backward=Fal
         raise ValueError(f"x must be torch.bfloat16 or torch.float32, got {dtype}")
     _typed("x", x, dtype)
     _typed("out", out, dtype)
+    _here("x", x)
     rows, heads, hd = x.shape
     x0, x1, x2 = x.stride()
     o0, o1, o2 = out.stride()
@@ -126,27 +133,31 @@ def rope(x, positions, phase, out, *, layout="half", magnitude=1.0, backward=Fal
                                    _lib.DFLARE_BF16 if dtype is _BF16 else _lib.DFLARE_F32, _stream(stream)))
 
 
-def tree_plan(parents, n_nodes, mask, depth, stream=None):
+def tree_plan(parents, n_nodes, mask, depth, error=None, stream=None):
     """Ancestor bits (int32 [batch][n][ceil(n / 32)]) and depths (int32 [batch][n]) of the trees with parent
-    numbers ``parents`` int32 [batch][n]."""
+    numbers ``parents`` int32 [batch][n]. error: optional int32 [1] that gets DEVERR_TREE for an impossible tree."""
     if parents.dim() != 2:
         raise ValueError(f"parents must be [batch][n], got {list(parents.shape)}")
     batch, n = parents.shape
-    _check(_lib.load().dflare_tree_plan(_ints("parents", parents, 0), _ints("n_nodes", n_nodes, batch), batch, n,
-                                        _ints("mask", mask, batch * n * ((n + 31) // 32)),
-                                        _ints("depth", depth, batch * n), None, _stream(stream)))
+    pp = _ints("parents", parents, 0)
+    _here("parents", parents)
+    _check(_lib.load().dflare_tree_plan(pp, _ints("n_nodes", n_nodes, batch), batch, n,
+                                        _ints("mask", mask, batch * n * ((n + 31) // 32)), _ints("depth", depth, batch * n),
+                                        None if error is None else _ints("error", error, 1), _stream(stream)))
 
 
-def tree_accept(tokens, parents, choice, n_nodes, accept_len, path, next_token, stream=None):
+def tree_accept(tokens, parents, choice, n_nodes, accept_len, path, next_token, error=None, stream=None):
     """Greedy acceptance in drafted trees: tokens, parents and choice (the target's argmax after each node)
-    int32 [batch][n]; writes accept_len [batch], path [batch][n], next_token [batch]."""
+    int32 [batch][n]; writes accept_len [batch], path [batch][n], next_token [batch]. error: as in tree_plan."""
     if parents.dim() != 2:
         raise ValueError(f"parents must be [batch][n], got {list(parents.shape)}")
     batch, n = parents.shape
+    pp = _ints("parents", parents, 0)
+    _here("parents", parents)
     _check(_lib.load().dflare_tree_accept(
-        _ints("tokens", tokens, batch * n), _ints("parents", parents, 0), _ints("choice", choice, batch * n),
-        _ints("n_nodes", n_nodes, batch), batch, n, _ints("accept_len", accept_len, batch), _ints("path", path, batch * n),
-        _ints("next_token", next_token, batch), None, _stream(stream)))
+        _ints("tokens", tokens, batch * n), pp, _ints("choice", choice, batch * n), _ints("n_nodes", n_nodes, batch), batch, n,
+        _ints("accept_len", accept_len, batch), _ints("path", path, batch * n), _ints("next_token", next_token, batch),
+        None if error is None else _ints("error", error, 1), _stream(stream)))
 
 
 class PagedCache:

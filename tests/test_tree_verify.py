@@ -511,6 +511,28 @@ def test_append_rotates_and_writes_the_pages(rot, layout, depths, dtype):
 
 
 @pytest.mark.gpu
+def test_a_page_that_is_still_shared_is_not_written():
+    """Two sequences share a partly filled page; without a reserve neither append nor commit may touch it."""
+    c = P.PagedCache.allocate(n_layers=1, n_pages=8, page_size=16, n_q_heads=1, n_kv_heads=1, head_dim=64, max_batch=2, max_pages=3, max_nodes=8)
+    c.k.zero_(), c.v.zero_()
+    c.reserve(i32([10, 0]))
+    c.commit(i32([10, 0]), i32([np.arange(10), np.arange(10)]))
+    c.fork(i32([0]), i32([1]))
+    k0, table = c.k.clone(), c.table.clone()
+    x = torch.ones((2, 3, 1, 64), dtype=c.dtype, device="cuda")
+    c.append(0, None, x, x, i32([0, 3]), None, None)
+    assert c.error() == P.DEVERR_PAGE and torch.equal(c.k, k0)
+    c.commit(i32([0, 2]), i32([[0, 1, 2], [0, 2, -1]]))
+    assert c.error() == P.DEVERR_TREE and torch.equal(c.k, k0) and c.lens.tolist() == [10, 10] and torch.equal(c.table, table)
+    c.reserve(i32([0, 3]))          # sequence 1 gets its copy, and sequence 0 keeps the page
+    c.append(0, None, x, x, i32([0, 3]), None, None)
+    c.commit(i32([0, 2]), i32([[0, 1, 2], [0, 2, -1]]))
+    assert c.error() == 0 and c.lens.tolist() == [10, 12] and torch.equal(c.k[0, table[0, 0]], k0[0, table[0, 0]])
+    c.append(0, None, x, x, i32([3, 0]), None, None)        # its own now
+    assert c.error() == 0 and (c.k[0, table[0, 0], :, 10:13] == 1).all()
+
+
+@pytest.mark.gpu
 def test_append_beyond_the_pages_is_left_out():
     rng = np.random.default_rng(1)
     p = Paged(rng, [30], [2], hq=2, hkv=2, hd=64, page=16, dtype="bf16")
@@ -793,6 +815,9 @@ def test_impossible_trees_are_reported():
         p, c = i32(parents), i32([count])
         s = torch.cuda.current_stream().cuda_stream
         assert L.dflare_tree_plan(p.data_ptr(), c.data_ptr(), 1, 3, mask.data_ptr(), depth.data_ptr(), err.data_ptr(), s) == 0
+        assert err.item() == P.DEVERR_TREE
+        err.zero_()
+        P.tree_plan(p, c, mask.view(1, 3), depth, error=err)
         assert err.item() == P.DEVERR_TREE
         err.zero_()
         acc, nxt = i32([0]), i32([0])
