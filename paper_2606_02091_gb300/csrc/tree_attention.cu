@@ -72,7 +72,8 @@ struct MmaLayout {
 // bf16, up to 16 query rows per kv head (single tokens, small trees). Four warps take 16 keys of each 64-key tile
 // each; a fifth warp streams the tiles' pages by TMA into a ring of stages. Every warp keeps its own running
 // maximum and sum; when a pair's keys are done each warp sums up a quarter of the head dims of all four.
-// HBM-bound for long contexts; for short ones by its chain of latencies (lengths, page table, keys).
+// HBM-bound for long contexts (one token over 100000 keys, 8 kv heads of 128: 71 us, 5.8 TB/s); for short ones by
+// its chain of latencies, lengths, page table, keys (2048 keys: 9.5 us).
 template <int HD>
 __global__ void __launch_bounds__(kMmaThreads, 2) tree_mma_kernel(const __grid_constant__ CUtensorMap mk,
                                                                   const __grid_constant__ CUtensorMap mv, const TreeArgs a) {
@@ -391,7 +392,8 @@ __global__ void __launch_bounds__(kMmaThreads, 2) tree_mma_kernel(const __grid_c
 }
 
 // fp32: 16 query rows per CTA, 32-key tiles by cp.async in two stages, exact fp32 products on the CUDA cores.
-// Scores: a thread takes two rows x two keys; output: (16 / RG) rows x four head dims.
+// Scores: a thread takes two rows x two keys; output: (16 / RG) rows x four head dims. Bound by the latency of its
+// steps at the sizes that fp32 models have (8 nodes over 600 keys 9 us; 16 over 2 x 1000 keys, 32 heads of 128: 45).
 constexpr int kFKeys = 32;
 constexpr int kFRows = 16;
 constexpr int kFThreads = 128;
