@@ -334,6 +334,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                                  "l"(src + (size_t)nd * a.q_row + (rr - nd * a.G) * HD) : "memory");
             }
         };
+        auto q_there = [&]() {      // this thread's part of Q is in shared memory, for the MMAs to read
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(qfull);
+        };
         TreeRaw raw{};
         int nodes = 0, ctx = 0, keys = 0;
         if (more) {
@@ -342,6 +348,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
             if (NQ == 2) load_q(p, nodes * a.G, row0 + 128 * w, r, 128);
             else load_q(p, nodes * a.G, row0, tid, 256);
             asm volatile("bar.arrive 2, 288;" ::: "memory");
+            q_there();
         }
         while (more) {
             const int n = p.hi - p.lo;
@@ -351,10 +358,6 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
             const bool warp_live = my_row - lane < R;
             const int node = group_of(a, min(my_row, R - 1));
             const SeenRow row = seen_row(a, p.b, node);
-            asm volatile("cp.async.wait_all;" ::: "memory");
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(qfull);
             more = tree_pair<kTcExtra>(a, cum, v, v1, after);
             if (more) raw = tree_raw(a, after.b);
             int nodes2 = 0, ctx2 = 0, keys2 = 0;        // the next pair's
@@ -487,7 +490,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                 __syncwarp();
                 if (lane == 0) mbar_arrive(pfull(w));
             }
-            if (more) tree_lengths(a, raw, nodes2, ctx2, keys2);    // (the stream without the last tile too)
+            if (more) {
+                tree_lengths(a, raw, nodes2, ctx2, keys2);      // (the stream without the last tile too)
+                q_there();      // the next pair's first S is computed while this one's rows are written
+            }
             if (mine > 0) wait(ofull(w), (uint32_t)os++ & 1u);
             tc_fence_after();
             // ---------------- the pair's rows. NQ = 2: a thread has its row. NQ = 1: the streams swap (m, l)
