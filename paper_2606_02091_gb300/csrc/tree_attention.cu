@@ -85,6 +85,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) tree_mma_kernel(const __grid_c
     __shared__ int odd_any;
     __shared__ int abort_flag;
     __shared__ float2 ml[4][kRows];
+    __shared__ int planes[2][32];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t sb = smem_u32(smem), full = sb + LY::BARS, empty = full + 8 * kStages;
     if (tid == 0) {
@@ -108,35 +109,30 @@ __global__ void __launch_bounds__(kMmaThreads, 2) tree_mma_kernel(const __grid_c
     if (warp == 4) {
         // ---------------- stream the tiles: a box is up to 64 tokens of a page x 64 head dims
         const int rows = min(a.pg.ps, kKeys), boxes = kKeys / rows;
-        bool ok = true, more = true;
         int i = 0;
-        TileBoxes next = tile_boxes(a, p, p.lo, kKeys, rows, lane);
-        // the first pair's queries go first: behind the ring's tiles they would arrive after all of them
-        asm volatile("bar.sync 2, 160;" ::: "memory");
-        for (int t = p.lo; more; ++i) {
-            const TileBoxes now = next;
-            if (++t == p.hi) {
-                more = tree_pair<kExtra>(a, cum, v, v1, p);
-                t = p.lo;
-            }
-            if (more) next = tile_boxes(a, p, t, kKeys, rows, lane);
-            const int st = i % kStages;
-            if (i >= kStages) ok = __all_sync(0xffffffffu, bar_wait(empty + 8 * st, (uint32_t)(i / kStages - 1) & 1u, &abort_flag, a.pg.err));
-            if (!ok) break;
-            const uint32_t bar = full + 8 * st, kd = sb + st * 2 * TB;
-            if (elect_one()) mbar_expect_tx(bar, 2 * TB);
-            for (int x = 0; x < boxes; ++x) {
-                const int z = __shfl_sync(0xffffffffu, now.plane, x);
-                const int y = (now.first_slot + x * rows) & (a.pg.ps - 1);
+        const bool ok = each_group<kExtra>(a, cum, v, v1, p, kKeys, rows, lane, planes, [&](int first, int n, const int* plane) {
+            for (int tile = first; tile < first + n; ++tile, plane += boxes) {
+                // the first pair's queries go first: behind the ring's tiles they would arrive after all of them
+                if (i == 0) asm volatile("bar.sync 2, 160;" ::: "memory");
+                const int st = i % kStages;
+                if (i >= kStages && !__all_sync(0xffffffffu, bar_wait(empty + 8 * st, (uint32_t)(i / kStages - 1) & 1u, &abort_flag, a.pg.err)))
+                    return false;
                 if (elect_one()) {
+                    const uint32_t bar = full + 8 * st, kd = sb + st * 2 * TB;
+                    mbar_expect_tx(bar, 2 * TB);
+                    for (int x = 0; x < boxes; ++x) {
+                        const int z = plane[x], y = (tile * kKeys + x * rows) & (a.pg.ps - 1);
 #pragma unroll
-                    for (int h = 0; h < HD / 64; ++h) {
-                        tma_load_3d(kd + h * 8192 + x * rows * 128, &mk, h * 64, y, z, bar);
-                        tma_load_3d(kd + TB + h * 8192 + x * rows * 128, &mv, h * 64, y, z, bar);
+                        for (int h = 0; h < HD / 64; ++h) {
+                            tma_load_3d(kd + h * 8192 + x * rows * 128, &mk, h * 64, y, z, bar);
+                            tma_load_3d(kd + TB + h * 8192 + x * rows * 128, &mv, h * 64, y, z, bar);
+                        }
                     }
                 }
+                ++i;
             }
-        }
+            return true;
+        });
         if (!ok && elect_one()) {   // the copies in flight land before the CTA's shared memory is given up
             volatile int never = 0;
             for (int j = max(0, i - kStages); j < i; ++j)
@@ -574,174 +570,201 @@ __global__ void __launch_bounds__(kFThreads) tree_f32_kernel(const TreeArgs a) {
 // Rows whose keys several CTAs read: their partial results in the order of the keys. Also the rows that no
 // CTA had anything for: no keys, or past the tree's nodes. Where rows are few, four warps share a row's parts (PW), of
 // which one long context on one kv head leaves 304; where they are many, a warp takes four rows (RW). Measured, the
-// whole attention: one token over 100000 keys on one kv head 37 us with a warp per row and 21 with four; 16 nodes over
-// four contexts (2048 rows) 20 with one and 23 with four; 33 nodes at head_dim 64 (4224 rows) 35 with a warp per row
-// and 39 with one for four rows; 64 nodes over 8 x 32768 keys (16384 rows) 217 and 205.
-constexpr int kJoinThreads = 128;      // few enough registers to be resident beside the tcgen05 kernel's CTA
-constexpr int kJoinFew = 1024, kJoinMany = 8192;    // rows below which a row takes four warps, from which on a warp takes four rows
+// whole attention: one token over 100000 keys on one kv head 37 us with a warp per row and 21 with four; 64 nodes over
+// 4096 keys (2048 rows) 18.5 with one and 21.7 with one for four rows; 33 nodes at head_dim 64 (4224 rows) 33 and 29.
+// The grid is resident at once and walks the rows: a block finds the division of the work once (2.5 us, while the last
+// CTAs of the attention still run). With a block for every four rows, and the division for each, 57 nodes over 20
+// contexts of 443 to 1112 keys took 23.5 us for 18.5.
+constexpr int kJoinThreads = 128;
+constexpr int kJoinFew = 1024, kJoinMany = 4096;    // rows below which a row takes four warps, from which on a warp takes four rows
+
+constexpr int join_blocks(int HD, int RW) { return HD == 64 ? 6 : RW == 1 ? 5 : 4; }     // on an SM, as their registers allow
 
 template <class T, int HD, int RW, int PW>
-__global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(const TreeArgs a, int QT, int KT, int extra, int least, bool blocks) {
+__global__ void __launch_bounds__(kJoinThreads, join_blocks(HD, RW))
+    tree_join_kernel(const TreeArgs a, int QT, int KT, int extra, int least, bool blocks) {
     static_assert(RW == 1 || PW == 1, "several rows per warp or several warps per row");
     constexpr int LPR = 32 / RW, E = HD / LPR, V = E < 4 ? E : 4, J = RW == 1 && PW == 1 ? 8 : 4;
     __shared__ float others[PW][HD + 2];    // of a row's warps: output, maximum, sum
+    __shared__ int tiles_of[kMaxSeqs], nodes_of[kMaxSeqs], groups_of[kMaxSeqs];
+    __shared__ int first_of[kShares], many_of[kShares];     // of the query groups
     // The kernel before this one let it start after its own dependency wait, so the lengths are final here and
     // the division of the work is found while that kernel still runs.
     // Lane l of a row has the elements (g LPR + l) V .. of its groups g; warp pw of a row the parts pw, pw + PW, ...
     const int lane = threadIdx.x & 31, l = lane % LPR, warp = threadIdx.x >> 5, pw = warp % PW;
-    const long long row = ((long long)blockIdx.x * (kJoinThreads / 32 / PW) + warp / PW) * RW + lane / LPR;
-    const bool there = row < (long long)a.batch * a.n_max * a.hq;
-    const int head = (int)(row % a.hq), node = (int)(row / a.hq % a.n_max), b = there ? (int)(row / a.hq / a.n_max) : 0;
-    int n, ctx, keys;
-    tree_lengths(a, tree_raw(a, b), n, ctx, keys);
-    const bool some = there && node < n && keys > 0;
-    const int r = node * a.G + head % a.G, qg = r / QT;
-    int cost = 0, groups = 0, C = max(a.C / a.QG, 1), first = qg * C, total = 0;       // the group's CTAs and list
+    for (int x = threadIdx.x; x < a.batch; x += kJoinThreads) {
+        const TreeRaw raw = tree_raw(a, x);
+        int n, ctx, keys, groups;
+        tree_lengths(a, raw, n, ctx, keys);
+        tiles_of[x] = tree_tiles(a, raw, QT, KT, groups);
+        nodes_of[x] = n;
+        groups_of[x] = groups;
+    }
+    __syncthreads();
     const bool shares = a.QG > 1 && a.QG <= kShares;
-    if (shares) {
-        const TreeCosts costs = tree_costs<LPR>(a, l, QT, KT, extra, cost, groups);
+    if (shares && warp == 0) {
+        const TreeCosts costs = tree_costs(a, lane, [&](int b, int& cost, int& groups) {
+            cost = tree_cost(tiles_of[b], extra);
+            groups = groups_of[b];
+        });
         tree_shares(a, costs, [&](int g, int from, int many) {
-            if (g == qg) {
-                first = from;
-                C = many;
-                total = costs.list[g];
+            if (lane == 0) {
+                first_of[g] = from;
+                many_of[g] = many;
             }
         });
     }
-    int before = 0, sum_all = 0;
-    for (int x = l; x < a.batch; x += LPR) {
-        if (x != l || !shares) cost = tree_cost(tree_tiles(a, x, QT, KT, groups), extra);
-        if (groups <= qg) continue;
-        sum_all += cost;
-        if (x < b) before += cost;
-    }
+    if (shares) __syncthreads();
+    const unsigned rows = (unsigned)a.batch * a.n_max * a.hq, step = gridDim.x * (kJoinThreads / 32 / PW) * RW;
+    unsigned row = (blockIdx.x * (kJoinThreads / 32 / PW) + warp / PW) * RW + lane / LPR;
+    for (bool begun = false; !begun || row - lane / LPR < rows; row += step) {
+        const bool there = row < rows;
+        const int head = row % a.hq, node = row / a.hq % a.n_max, b = there ? row / a.hq / a.n_max : 0;
+        const int r = node * a.G + head % a.G, qg = r / QT, tiles = tiles_of[b];
+        const bool some = there && node < nodes_of[b] && tiles;
+        int before = 0, total = 0, first, C;        // the group's list, its CTAs
+        for (int x = l; x < a.batch; x += LPR) {
+            const int cost = groups_of[x] > qg ? tree_cost(tiles_of[x], extra) : 0;
+            total += cost;
+            if (x < b) before += cost;
+        }
 #pragma unroll
-    for (int o = LPR / 2; o > 0; o >>= 1) {
-        if (!shares) sum_all += __shfl_xor_sync(0xffffffffu, sum_all, o);
-        before += __shfl_xor_sync(0xffffffffu, before, o);
-    }
-    if (!shares) total = sum_all;
-    const int per = tree_run(total * a.pg.hkv, max(C, 1), least), tiles = tree_tiles(a, b, QT, KT, groups);
-    const int start = before * a.pg.hkv + head / a.G * tree_cost(tiles, extra);
-    const int c0 = start / per;
-    int parts = some ? (start + tiles - 1) / per - c0 + 1 : 0;
-    const bool written = parts == 1;        // by the CTA that read all of the row's keys
-    parts = written ? 0 : (parts - pw + PW - 1) / PW;       // this warp's
-    // every warp waits, so this launch does not end before the one it depends on
-    pdl_wait();
-    const int most = __reduce_max_sync(0xffffffffu, parts);
-    auto at = [&](int i) {
-        const int c = c0 + pw + i * PW;
-        return ((size_t)(first + c) * 2 + (start < c * per ? 0 : 1)) * QT + r % QT;
-    };
-    float acc[E], x[J][E], m = -INFINITY, sum = 0.f;
+        for (int o = LPR / 2; o > 0; o >>= 1) {
+            total += __shfl_xor_sync(0xffffffffu, total, o);
+            before += __shfl_xor_sync(0xffffffffu, before, o);
+        }
+        if (shares) {
+            C = many_of[qg];
+            first = first_of[qg];
+        } else {
+            C = max(a.C / a.QG, 1);
+            first = qg * C;
+        }
+        const int per = tree_run(total * a.pg.hkv, max(C, 1), least);
+        const int start = before * a.pg.hkv + head / a.G * tree_cost(tiles, extra);
+        const int c0 = start / per;
+        int parts = some ? (start + tiles - 1) / per - c0 + 1 : 0;
+        const bool written = parts == 1;        // by the CTA that read all of the row's keys
+        parts = written ? 0 : (parts - pw + PW - 1) / PW;       // this warp's
+        // every warp waits, so this launch does not end before the one it depends on
+        if (!begun) pdl_wait();
+        begun = true;
+        const int most = __reduce_max_sync(0xffffffffu, parts);
+        auto at = [&](int i) {
+            const int c = c0 + pw + i * PW;
+            return ((size_t)(first + c) * 2 + (start < c * per ? 0 : 1)) * QT + r % QT;
+        };
+        float acc[E], x[J][E], m = -INFINITY, sum = 0.f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = 0.f;
-    auto load = [&](int i) {        // parts i .. i + J - 1
+        for (int e = 0; e < E; ++e) acc[e] = 0.f;
+        auto load = [&](int i) {        // parts i .. i + J - 1
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-            const size_t row = at(min(i + j, max(parts - 1, 0)));
+            for (int j = 0; j < J; ++j) {
+                const size_t row = at(min(i + j, max(parts - 1, 0)));
 #pragma unroll
-            for (int g = 0; g < E / V; ++g) {
-                const int e = (g * LPR + l) * V;
-                // the tcgen05 kernel's rows lie in blocks of 32 rows x 32 elements, 16-byte pieces swizzled
-                const float* src = a.part_o + (!blocks ? row * HD + e
-                                                       : (row & ~(size_t)31) * HD + (e >> 5) * 1024 + (row & 31) * 32 +
-                                                             ((((e & 31) >> 2) ^ (int)(row & 7)) << 2) + (e & 3));
-                if constexpr (V == 4) {
-                    const float4 v = i + j < parts ? *reinterpret_cast<const float4*>(src) : make_float4(0.f, 0.f, 0.f, 0.f);
-                    x[j][4 * g] = v.x; x[j][4 * g + 1] = v.y; x[j][4 * g + 2] = v.z; x[j][4 * g + 3] = v.w;
-                } else {
-                    const float2 v = i + j < parts ? *reinterpret_cast<const float2*>(src) : make_float2(0.f, 0.f);
-                    x[j][0] = v.x; x[j][1] = v.y;
+                for (int g = 0; g < E / V; ++g) {
+                    const int e = (g * LPR + l) * V;
+                    // the tcgen05 kernel's rows lie in blocks of 32 rows x 32 elements, 16-byte pieces swizzled
+                    const float* src = a.part_o + (!blocks ? row * HD + e
+                                                           : (row & ~(size_t)31) * HD + (e >> 5) * 1024 + (row & 31) * 32 +
+                                                                 ((((e & 31) >> 2) ^ (int)(row & 7)) << 2) + (e & 3));
+                    if constexpr (V == 4) {
+                        const float4 v = i + j < parts ? *reinterpret_cast<const float4*>(src) : make_float4(0.f, 0.f, 0.f, 0.f);
+                        x[j][4 * g] = v.x; x[j][4 * g + 1] = v.y; x[j][4 * g + 2] = v.z; x[j][4 * g + 3] = v.w;
+                    } else {
+                        const float2 v = i + j < parts ? *reinterpret_cast<const float2*>(src) : make_float2(0.f, 0.f);
+                        x[j][0] = v.x; x[j][1] = v.y;
+                    }
                 }
             }
-        }
-    };
-    // the first J parts come in together with the (m, l) that weigh them
-    load(0);
-    float2 v = l < parts ? a.part_ml[at(l)] : make_float2(-INFINITY, 0.f);
-    m = v.x;
-    for (int i = LPR + l; i < parts; i += LPR) m = fmaxf(m, a.part_ml[at(i)].x);
+        };
+        // the first J parts come in together with the (m, l) that weigh them
+        load(0);
+        float2 v = l < parts ? a.part_ml[at(l)] : make_float2(-INFINITY, 0.f);
+        m = v.x;
+        for (int i = LPR + l; i < parts; i += LPR) m = fmaxf(m, a.part_ml[at(i)].x);
 #pragma unroll
-    for (int o = LPR / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    const float ref = m == -INFINITY ? 0.f : m;
-    float w = exp2f(v.x - ref);             // 0 past the last part
-    sum = v.y * w;
-    for (int i = 0; i < most; i += J) {
-        if (i) {
-            load(i);
-            if (i % LPR == 0) {
-                v = i + l < parts ? a.part_ml[at(i + l)] : make_float2(-INFINITY, 0.f);
-                w = exp2f(v.x - ref);
-                sum = fmaf(v.y, w, sum);
+        for (int o = LPR / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        const float ref = m == -INFINITY ? 0.f : m;
+        float w = exp2f(v.x - ref);             // 0 past the last part
+        sum = v.y * w;
+        for (int i = 0; i < most; i += J) {
+            if (i) {
+                load(i);
+                if (i % LPR == 0) {
+                    v = i + l < parts ? a.part_ml[at(i + l)] : make_float2(-INFINITY, 0.f);
+                    w = exp2f(v.x - ref);
+                    sum = fmaf(v.y, w, sum);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const float wj = __shfl_sync(0xffffffffu, w, i % LPR + j, LPR);
+                if (i + j >= parts) continue;
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[e] = fmaf(wj, x[j][e], acc[e]);
             }
         }
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-            const float wj = __shfl_sync(0xffffffffu, w, i % LPR + j, LPR);
-            if (i + j >= parts) continue;
+        for (int o = LPR / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if constexpr (PW > 1) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) acc[e] = fmaf(wj, x[j][e], acc[e]);
+            for (int e = 0; e < E; ++e) others[pw][l * E + e] = acc[e];
+            if (l == 0) {
+                others[pw][HD] = m;
+                others[pw][HD + 1] = sum;
+            }
+            __syncthreads();
+            if (pw == 0) {
+                float top = m;
+#pragma unroll
+                for (int q = 1; q < PW; ++q) top = fmaxf(top, others[q][HD]);
+                const float ref = top == -INFINITY ? 0.f : top;
+                float f = exp2f(m - ref);
+                sum *= f;
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[e] *= f;
+#pragma unroll
+                for (int q = 1; q < PW; ++q) {
+                    f = exp2f(others[q][HD] - ref);
+                    sum = fmaf(others[q][HD + 1], f, sum);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) acc[e] = fmaf(others[q][l * E + e], f, acc[e]);
+                }
+                m = top;
+            }
+            __syncthreads();
         }
+        if (!there || written || pw) continue;
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        T* out = static_cast<T*>(a.out) + (size_t)row * HD;
+#pragma unroll
+        for (int g = 0; g < E / V; ++g) {
+            const int e = (g * LPR + l) * V;
+            if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                for (int y = 0; y < V; y += 2)
+                    *reinterpret_cast<uint32_t*>(out + e + y) = two_bf16(acc[g * V + y] * inv, acc[g * V + y + 1] * inv);
+            } else {
+#pragma unroll
+                for (int y = 0; y < V; ++y) out[e + y] = acc[g * V + y] * inv;
+            }
+        }
+        if (a.lse && l == 0) a.lse[row] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * 0.69314718055994531f;
     }
-#pragma unroll
-    for (int o = LPR / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if constexpr (PW > 1) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) others[pw][l * E + e] = acc[e];
-        if (l == 0) {
-            others[pw][HD] = m;
-            others[pw][HD + 1] = sum;
-        }
-        __syncthreads();
-        if (pw) return;
-        float top = m;
-#pragma unroll
-        for (int q = 1; q < PW; ++q) top = fmaxf(top, others[q][HD]);
-        const float ref = top == -INFINITY ? 0.f : top;
-        float f = exp2f(m - ref);
-        sum *= f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] *= f;
-#pragma unroll
-        for (int q = 1; q < PW; ++q) {
-            f = exp2f(others[q][HD] - ref);
-            sum = fmaf(others[q][HD + 1], f, sum);
-#pragma unroll
-            for (int e = 0; e < E; ++e) acc[e] = fmaf(others[q][l * E + e], f, acc[e]);
-        }
-        m = top;
-    }
-    if (!there || written) return;
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    T* out = static_cast<T*>(a.out) + row * HD;
-#pragma unroll
-    for (int g = 0; g < E / V; ++g) {
-        const int e = (g * LPR + l) * V;
-        if constexpr (sizeof(T) == 2) {
-#pragma unroll
-            for (int y = 0; y < V; y += 2)
-                *reinterpret_cast<uint32_t*>(out + e + y) = two_bf16(acc[g * V + y] * inv, acc[g * V + y + 1] * inv);
-        } else {
-#pragma unroll
-            for (int y = 0; y < V; ++y) out[e + y] = acc[g * V + y] * inv;
-        }
-    }
-    if (a.lse && l == 0) a.lse[row] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * 0.69314718055994531f;
 }
 
 template <class T, int HD>
-cudaError_t launch_join(const TreeArgs& a, int QT, int KT, int extra, int least, bool blocks, cudaStream_t s) {
-    const long long rows = (long long)a.batch * a.n_max * a.hq, warps = kJoinThreads / 32;
-    if (rows < kJoinFew)
-        return launch_kernel(true, tree_join_kernel<T, HD, 1, 4>, dim3((unsigned)((rows * 4 + warps - 1) / warps)), dim3(kJoinThreads), 0, s,
-                             a, QT, KT, extra, least, blocks);
-    if (rows < kJoinMany)
-        return launch_kernel(true, tree_join_kernel<T, HD, 1, 1>, dim3((unsigned)((rows + warps - 1) / warps)), dim3(kJoinThreads), 0, s, a,
-                             QT, KT, extra, least, blocks);
-    return launch_kernel(true, tree_join_kernel<T, HD, 4, 1>, dim3((unsigned)((rows + 4 * warps - 1) / (4 * warps))), dim3(kJoinThreads), 0, s,
-                         a, QT, KT, extra, least, blocks);
+cudaError_t launch_join(const dflare_cache* c, const TreeArgs& a, int QT, int KT, int extra, int least, bool blocks, cudaStream_t s) {
+    const long long rows = (long long)a.batch * a.n_max * a.hq;
+    auto go = [&](auto kernel, int RW, int PW) {
+        const long long per = kJoinThreads / 32 / PW * RW, most = (long long)c->num_sms * join_blocks(HD, RW);
+        return launch_kernel(true, kernel, dim3((unsigned)std::min((rows + per - 1) / per, most)), dim3(kJoinThreads), 0, s, a, QT, KT, extra,
+                             least, blocks);
+    };
+    if (rows < kJoinFew) return go(tree_join_kernel<T, HD, 1, 4>, 1, 4);
+    if (rows < kJoinMany) return go(tree_join_kernel<T, HD, 1, 1>, 1, 1);
+    return go(tree_join_kernel<T, HD, 4, 1>, 4, 1);
 }
 
 template <int HD>
@@ -754,7 +777,7 @@ cudaError_t launch_mma(dflare_cache* c, TreeArgs a, cudaStream_t s) {
     a.QG = 1;
     a.C = 2 * c->num_sms;
     e = launch_kernel(true, tree_mma_kernel<HD>, dim3(a.C), dim3(kMmaThreads), MmaLayout<HD>::BYTES, s, c->maps[0], c->maps[1], a);
-    return e == cudaSuccess ? launch_join<bf16, HD>(a, kRows, kKeys, kExtra, kLeast, false, s) : e;
+    return e == cudaSuccess ? launch_join<bf16, HD>(c, a, kRows, kKeys, kExtra, kLeast, false, s) : e;
 }
 
 template <int HD>
@@ -766,7 +789,7 @@ cudaError_t launch_f32(dflare_cache* c, TreeArgs a, cudaStream_t s) {
     a.QG = (a.n_max * a.G + kFRows - 1) / kFRows;
     a.C = 2 * c->num_sms;
     e = launch_kernel(true, tree_f32_kernel<HD>, dim3(std::max(a.QG, a.C)), dim3(kFThreads), bytes, s, a);
-    return e == cudaSuccess ? launch_join<float, HD>(a, kFRows, kFKeys, kFExtra, kFLeast, false, s) : e;
+    return e == cudaSuccess ? launch_join<float, HD>(c, a, kFRows, kFKeys, kFExtra, kFLeast, false, s) : e;
 }
 
 template <int HD>
@@ -776,7 +799,7 @@ cudaError_t launch_hd(dflare_cache* c, TreeArgs a, cudaStream_t s) {
     if (R <= kRows) return launch_mma<HD>(c, a, s);
     int QT;
     const cudaError_t e = launch_tree_attention_tc(c, a, &QT, s);
-    return e == cudaSuccess ? launch_join<bf16, HD>(a, QT, kTcKeys, kTcExtra, kTcLeast, true, s) : e;
+    return e == cudaSuccess ? launch_join<bf16, HD>(c, a, QT, kTcKeys, kTcExtra, kTcLeast, true, s) : e;
 }
 
 }  // namespace

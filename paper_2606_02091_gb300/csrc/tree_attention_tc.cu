@@ -30,7 +30,7 @@ namespace dfl {
 namespace {
 
 constexpr int kKeys = kTcKeys;
-constexpr int kThreads = 320;       // warps 0-3, 4-7: softmax streams; 8: TMA; 9: MMA and tensor memory
+constexpr int kThreads = 352;       // warps 0-3, 4-7: softmax streams; 8, 10: TMA of K, V; 9: MMA and tensor memory
 constexpr float kRaise = 8.0f;      // growth (log2) of a row's maximum that rescales O
 
 template <int HD, int NQ>
@@ -42,7 +42,7 @@ struct TcLayout {
     static constexpr uint32_t K = NQ * TB;                          // [NK][HD / 64][128][128 B]
     static constexpr uint32_t V = K + NK * TB;
     static constexpr uint32_t BARS = V + NV * TB;
-    static constexpr int NBARS = 2 * NK + 2 * NV + 8;
+    static constexpr int NBARS = 2 * NK + 2 * NV + 9;
     static constexpr uint32_t ML = BARS + ((NBARS * 8 + 15) & ~15);    // NQ == 1: [2][128] (m, l) of the streams
     static constexpr uint32_t END = (ML + (NQ == 1 ? 2048 : 0) + 15) & ~15u;
     static constexpr uint32_t TURN = END;                           // 4 KB for each softmax warp to turn its rows around
@@ -103,24 +103,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// Bounded wait, inline (a call would keep the compiler from giving the softmax threads their registers).
-__device__ __forceinline__ bool wait_inline(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t* err) {
-#pragma unroll 1
-    for (int i = 0; i < 64; ++i)
-        if (mbar_try_wait(bar, parity)) return true;
-    const uint64_t t0 = globaltimer_ns();
-#pragma unroll 1
-    while (true) {
-        if (mbar_try_wait(bar, parity)) return true;
-        if (*abort_flag) return false;
-        if (globaltimer_ns() - t0 > kTimeoutNs) {
-            *abort_flag = 1;
-            atomicOr(err, DFLARE_DEVERR_TIMEOUT);
-            return false;
-        }
-    }
-}
-
 template <int HD, int NQ>
 __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_constant__ CUtensorMap mk,
                                                               const __grid_constant__ CUtensorMap mv, const TreeArgs a) {
@@ -130,8 +112,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ int32_t cum[kMaxSeqs + 1];
     __shared__ uint32_t odd[kMaxNodes / 32];    // nodes with an infinite or NaN value
-    __shared__ int odd_any, abort_flag;
+    __shared__ int odd_any;
+    __shared__ volatile int abort_flag;
     __shared__ uint32_t tmem_base;
+    __shared__ int planes[2][2][32];            // of the K and of the V warp
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t sb = smem_u32(smem), bars = sb + LY::BARS;
     auto kfull = [&](int i) { return bars + 8u * i; };
@@ -142,7 +126,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     auto pfull = [&](int w) { return bars + 8u * (2 * NK + 2 * NV + 2 + w); };   // its P written, O scaled
     auto ofull = [&](int w) { return bars + 8u * (2 * NK + 2 * NV + 4 + w); };   // its last PV of a pair done
     const uint32_t qfull = bars + 8u * (2 * NK + 2 * NV + 6);                    // Q of a pair in shared memory
-    const uint32_t drain = qfull + 8u;                                           // after a wait that gave up
+    const uint32_t qsent = qfull + 8u;                                           // the first pair's Q is on its way
+    const uint32_t drain = qfull + 16u;                                          // after a wait that gave up
     if (tid == 0) {
         for (int i = 0; i < NK; ++i) {
             mbar_init(kfull(i), 1);
@@ -158,8 +143,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
             mbar_init(ofull(w), 1);
         }
         mbar_init(qfull, 8);
+        mbar_init(qsent, 8);
         mbar_init(drain, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&mk)) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&mv)) : "memory");
         abort_flag = 0;
         odd_any = 0;
     }
@@ -185,48 +173,39 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     auto tS = [&](int w) { return tmem + 128u * w; };
     auto tO = [&](int w) { return tmem + 256u + (uint32_t)HD * w; };
 
-    if (warp == 8) {
-        // ---------------- TMA: K and V tiles into their rings, a box being up to 64 tokens x 64 head dims
-        const bool leader = elect_one();
-        const int rows = min(a.pg.ps, 64), boxes = kKeys / rows;
-        bool ok = true;
+    if (warp == 8 || warp == 10) {
+        // ---------------- TMA: K tiles into their ring (warp 8) and V tiles into theirs (warp 10), a box being up to
+        // 64 tokens x 64 head dims. In one warp K(i + 1) waits for the slot of V(i), which is free a tile's time later;
+        // one thread that polls for either ring's slot slows the softmax warps (64 nodes over 8 x 32768 keys 211 us).
+        const bool vs = warp == 10;
+        const int N = vs ? NV : NK, rows = min(a.pg.ps, 64), boxes = kKeys / rows;
+        const uint32_t full = vs ? vfull(0) : kfull(0), empty = vs ? vempty(0) : kempty(0), ring = sb + (vs ? LY::V : LY::K);
+        const CUtensorMap* map = vs ? &mv : &mk;
         int i = 0;
-        if (more) {
-            TileBoxes next = tile_boxes(a, p, p.lo, kKeys, rows, lane);
-            for (int t = p.lo; more && ok; ++i) {
-                const TileBoxes now = next;
-                if (++t == p.hi) {
-                    more = tree_pair<kTcExtra>(a, cum, v, v1, p);
-                    t = p.lo;
-                }
-                if (more) next = tile_boxes(a, p, t, kKeys, rows, lane);
-#pragma unroll
-                for (int kv = 0; kv < 2 && ok; ++kv) {
-                    // After the first K tile the first pair's queries: behind the whole ring they would arrive
-                    // last (measured: 3.5 us later, the time in which 152 x 128 KB come from memory).
-                    if (i == 0 && kv == 1) asm volatile("bar.sync 2, 288;" ::: "memory");
-                    const int N = kv ? NV : NK, st = i % N;
-                    if (i >= N)
-                        ok = __all_sync(0xffffffffu, wait_inline(kv ? vempty(st) : kempty(st), (uint32_t)(i / N - 1) & 1u, &abort_flag, a.pg.err));
-                    if (!ok) break;
-                    const uint32_t bar = kv ? vfull(st) : kfull(st), dst = sb + (kv ? LY::V : LY::K) + st * TB;
-                    if (leader) mbar_expect_tx(bar, TB);
+        const bool ok = !more || each_group<kTcExtra>(a, cum, v, v1, p, kKeys, rows, lane, planes[vs], [&](int first, int n, const int* plane) {
+            bool fine = true;
+            if (elect_one()) {      // (a branch with a single active lane: copies issue from uniform registers)
+                for (int tile = first; tile < first + n; ++tile, ++i, plane += boxes) {
+                    // After the first K tile the first pair's queries: behind the whole ring they would arrive last
+                    // (measured: 3.5 us later, the time in which 152 x 128 KB come from memory).
+                    if (i == (vs ? 0 : 1)) fine = wait_inline(qsent, 0, &abort_flag, a.pg.err);
+                    const int st = i % N;
+                    if (i >= N && fine) fine = wait_inline(empty + 8 * st, (uint32_t)(i / N - 1) & 1u, &abort_flag, a.pg.err);
+                    if (!fine) break;
+                    const uint32_t bar = full + 8 * st, dst = ring + st * TB;
+                    mbar_expect_tx(bar, TB);
                     for (int x = 0; x < boxes; ++x) {
-                        const int z = __shfl_sync(0xffffffffu, now.plane, x);
-                        const int y = (now.first_slot + x * rows) & (a.pg.ps - 1);
-                        if (leader) {
+                        const int z = plane[x], y = (tile * kKeys + x * rows) & (a.pg.ps - 1);
 #pragma unroll
-                            for (int h = 0; h < HD / 64; ++h)
-                                tma_load_3d(dst + h * 16384 + x * rows * 128, kv ? &mv : &mk, h * 64, y, z, bar);
-                        }
+                        for (int h = 0; h < HD / 64; ++h) tma_load_3d(dst + h * 16384 + x * rows * 128, map, h * 64, y, z, bar);
                     }
                 }
             }
-        }
-        if (!ok && leader) {   // the copies in flight land before the CTA's shared memory is given up
+            return (bool)__all_sync(0xffffffffu, fine);
+        });
+        if (!ok) {      // the copies in flight land before the CTA's shared memory is given up (i: the issuing lane's)
             volatile int never = 0;
-            for (int j = max(0, i - NK); j < i; ++j) wait_inline(kfull(j % NK), (uint32_t)(j / NK) & 1u, &never, a.pg.err);
-            for (int j = max(0, i - NV); j < i; ++j) wait_inline(vfull(j % NV), (uint32_t)(j / NV) & 1u, &never, a.pg.err);
+            for (int j = max(0, i - N); j < i; ++j) wait_inline(full + 8 * (j % N), (uint32_t)(j / N) & 1u, &never, a.pg.err);
         }
         __syncwarp();
     } else if (warp == 9) {
@@ -347,7 +326,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
             tree_lengths(a, raw, nodes, ctx, keys);
             if (NQ == 2) load_q(p, nodes * a.G, row0 + 128 * w, r, 128);
             else load_q(p, nodes * a.G, row0, tid, 256);
-            asm volatile("bar.arrive 2, 288;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(qsent);
             q_there();
         }
         while (more) {

@@ -13,6 +13,7 @@
 #pragma once
 #include "common.cuh"
 #include "paged.h"
+#include "umma.cuh"
 
 namespace dfl {
 
@@ -30,10 +31,10 @@ __device__ __forceinline__ void tree_lengths(const TreeArgs& a, const TreeRaw& x
     ctx = min(ctx, keys);
 }
 
-// key tiles of sequence b (0: it has no query rows, or no keys) and its query groups
-__device__ __forceinline__ int tree_tiles(const TreeArgs& a, int b, int QT, int KT, int& groups) {
+// key tiles of a sequence (0: it has no query rows, or no keys) and its query groups
+__device__ __forceinline__ int tree_tiles(const TreeArgs& a, const TreeRaw& raw, int QT, int KT, int& groups) {
     int n, ctx, keys;
-    tree_lengths(a, tree_raw(a, b), n, ctx, keys);
+    tree_lengths(a, raw, n, ctx, keys);
     const int tiles = n ? (int)(((long long)keys + KT - 1) / KT) : 0;
     groups = tiles ? (n * a.G + QT - 1) / QT : 0;
     return tiles;
@@ -48,32 +49,22 @@ constexpr int kShares = 8;
 struct TreeCosts {
     int list[kShares];      // of one kv head
 };
-// LANES adjacent lanes (l: this one's number) add up the groups' lists; first_cost, first_groups: those of sequence l.
-template <int LANES>
-__device__ __forceinline__ TreeCosts tree_costs(const TreeArgs& a, int l, int QT, int KT, int extra, int& first_cost, int& first_groups) {
+// A warp adds up the groups' lists; seq(b, cost, groups) says what sequence b has.
+template <class F>
+__device__ __forceinline__ TreeCosts tree_costs(const TreeArgs& a, int lane, F seq) {
     TreeCosts c;
 #pragma unroll
     for (int g = 0; g < kShares; ++g) c.list[g] = 0;
-    first_cost = first_groups = 0;
-    for (int b = l; b < a.batch; b += LANES) {
-        int groups;
-        const int cost = tree_cost(tree_tiles(a, b, QT, KT, groups), extra);
-        if (b == l) {
-            first_cost = cost;
-            first_groups = groups;
-        }
+    for (int b = lane; b < a.batch; b += 32) {
+        int cost, groups;
+        seq(b, cost, groups);
 #pragma unroll
         for (int g = 0; g < kShares; ++g) c.list[g] += groups > g ? cost : 0;
     }
 #pragma unroll
     for (int g = 0; g < kShares; ++g) {
         if (g >= a.QG) break;
-        if constexpr (LANES == 32) {
-            c.list[g] = __reduce_add_sync(0xffffffffu, c.list[g]);
-        } else {
-#pragma unroll
-            for (int o = LANES / 2; o > 0; o >>= 1) c.list[g] += __shfl_xor_sync(0xffffffffu, c.list[g], o);
-        }
+        c.list[g] = __reduce_add_sync(0xffffffffu, c.list[g]);
     }
     return c;
 }
@@ -106,14 +97,20 @@ __device__ __forceinline__ void tree_runs(const TreeArgs& a, int32_t* cum, int& 
     __shared__ int mine[3];     // group, this CTA's number in it, its CTAs
     const int tid = threadIdx.x;
     if (tid < 32) {
-        int cost, groups, g = 0, c = blockIdx.x, C = a.C;
+        int cost = 0, groups = 0, g = 0, c = blockIdx.x, C = a.C;       // (cost, groups: of sequence tid)
         if (a.QG > kShares) {
             C = max(a.C / a.QG, 1);
             g = blockIdx.x / C;
             c = blockIdx.x % C;
             if (g >= a.QG) C = 0;
         } else if (a.QG > 1) {
-            const TreeCosts costs = tree_costs<32>(a, tid, QT, KT, EXTRA, cost, groups);
+            const TreeCosts costs = tree_costs(a, tid, [&](int b, int& x, int& many) {
+                x = tree_cost(tree_tiles(a, tree_raw(a, b), QT, KT, many), EXTRA);
+                if (b == tid) {
+                    cost = x;
+                    groups = many;
+                }
+            });
             C = 0;
             tree_shares(a, costs, [&](int x, int first, int many) {
                 if ((int)blockIdx.x >= first && (int)blockIdx.x < first + many) {
@@ -133,7 +130,7 @@ __device__ __forceinline__ void tree_runs(const TreeArgs& a, int32_t* cum, int& 
             const int b = b0 + tid;
             if (b0 || a.QG == 1 || a.QG > kShares) {
                 groups = 0;
-                cost = b < a.batch ? tree_cost(tree_tiles(a, b, QT, KT, groups), EXTRA) : 0;
+                cost = b < a.batch ? tree_cost(tree_tiles(a, tree_raw(a, b), QT, KT, groups), EXTRA) : 0;
             }
             int v = groups > g ? cost : 0;
 #pragma unroll
@@ -182,23 +179,62 @@ __device__ __forceinline__ bool tree_pair(const TreeArgs& a, const int32_t* cum,
     return false;
 }
 
-// The pages of one key tile, for the warp that streams tiles by TMA: lane x holds the tensor-map plane of the
-// tile's box x (`rows` tokens, a divisor of the tile), read by all lanes at once so that a tile costs one trip
-// to the table. Slots without a page take a plane outside the pool, which reads as zero.
-struct TileBoxes {
-    int plane, first_slot;
-};
-__device__ __forceinline__ TileBoxes tile_boxes(const TreeArgs& a, const TreePair& p, int tile, int KT, int rows, int lane) {
-    TileBoxes x;
-    x.first_slot = tile * KT;
-    x.plane = (int)min(0x7fffffffLL, (long long)a.pg.layers * a.pg.pages * a.pg.hkv);
-    const int pages = min(max(a.pg.held[p.b], 0), a.pg.max_pages);
-    const int pi = (int)(((unsigned)x.first_slot + (unsigned)(lane * rows)) / (unsigned)a.pg.ps);
-    if (lane * rows < KT && pi < pages) {
-        const int page = a.pg.table[(size_t)p.b * a.pg.max_pages + pi];
-        if (page >= 0 && page < a.pg.pages) x.plane = (a.layer * a.pg.pages + page) * a.pg.hkv + p.h;
+// Bounded wait, inline (a call would keep the compiler from giving a kernel's other threads their registers).
+__device__ __forceinline__ bool wait_inline(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t* err) {
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
+        if (mbar_try_wait(bar, parity)) return true;
+    const uint64_t t0 = globaltimer_ns();
+#pragma unroll 1
+    while (true) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if (*abort_flag) return false;
+        if (globaltimer_ns() - t0 > kTimeoutNs) {
+            *abort_flag = 1;
+            atomicOr(err, DFLARE_DEVERR_TIMEOUT);
+            return false;
+        }
     }
-    return x;
+}
+
+// Pages for the warp that streams tiles by TMA: lane x looks up the page of box x (`rows` tokens, a divisor of the tile)
+// from tile `base` of a pair on, so that one trip to the table serves 32 boxes. What memory says is looked at only when
+// the boxes are due: the first group's copies would wait for the second's pages. A slot without a page takes a plane of
+// the tensor map outside the pool, which reads as zero.
+struct BoxPage {
+    int held, page, at, h;
+};
+__device__ __forceinline__ BoxPage box_page(const TreeArgs& a, const TreePair& p, int base, int KT, int rows, int lane) {
+    const int at = (int)(((unsigned)(base * KT) + (unsigned)(lane * rows)) / (unsigned)a.pg.ps);
+    return {a.pg.held[p.b], at < a.pg.max_pages ? a.pg.table[(size_t)p.b * a.pg.max_pages + at] : -1, at, p.h};
+}
+__device__ __forceinline__ int box_plane(const TreeArgs& a, const BoxPage& x) {
+    if (x.at < x.held && x.page >= 0 && x.page < a.pg.pages) return (a.layer * a.pg.pages + x.page) * a.pg.hkv + x.h;
+    return (int)min(0x7fffffffLL, (long long)a.pg.layers * a.pg.pages * a.pg.hkv);
+}
+// f(first tile, tiles, planes of their boxes) for groups of tiles (of one pair, as many as have 32 boxes) of the run from
+// pair p on, in order, while it says true; false if it did not. The whole warp calls this and f. planes: [2][32] in
+// shared memory; a group's stay as they are until the warp is through with f for the next group.
+template <int EXTRA, class F>
+__device__ __forceinline__ bool each_group(const TreeArgs& a, const int32_t* cum, int& v, int v1, TreePair p, int KT, int rows, int lane,
+                                           int (*planes)[32], F f) {
+    const int many = 32 / (KT / rows);
+    int base = p.lo, buf = 0;
+    BoxPage found = box_page(a, p, base, KT, rows, lane);
+    bool ok = true;
+    for (bool more = true; more && ok; buf ^= 1) {
+        const int n = min(many, p.hi - base), from = base;
+        planes[buf][lane] = box_plane(a, found);
+        __syncwarp();
+        base += n;
+        if (base == p.hi) {
+            more = tree_pair<EXTRA>(a, cum, v, v1, p);
+            base = p.lo;
+        }
+        if (more) found = box_page(a, p, base, KT, rows, lane);
+        ok = f(from, n, planes[buf]);
+    }
+    return ok;
 }
 
 // Infinite and NaN bf16 values of a 16-byte piece become 0; whether there were any. (An exponent of all ones plus
