@@ -61,15 +61,14 @@ __device__ __forceinline__ int pages_of(int tokens, int ps) { return (tokens + p
 // the same in every lane of the calling warp.
 __device__ __forceinline__ bool path_fits(const PagesView& pg, int b, const int32_t* path, int a, int n, int len, int held) {
     bool ok = len >= 0 && a >= 0 && a <= n;
-    if (ok && a > 0 && len % pg.ps && len / pg.ps < min(held, pg.max_pages)) {
-        const int page = pg.table[(size_t)b * pg.max_pages + len / pg.ps];
-        if (page < 0 || page >= pg.pages || pg.refs[page] > 1) ok = false;
-    }
+    const bool tail = ok && a > 0 && len % pg.ps && len / pg.ps < min(held, pg.max_pages);
+    const int page = tail ? pg.table[(size_t)b * pg.max_pages + len / pg.ps] : 0;      // (under way with the path)
     const int room = min(held, pg.max_pages) * pg.ps - len;     // slots behind len
     for (int j = threadIdx.x & 31; ok && j < a; j += 32) {
-        const int x = path[j];
-        if (x < (j ? path[j - 1] + 1 : 0) || x >= room) ok = false;
+        const int x = path[j], before = j ? path[j - 1] : -1;
+        if (x <= before || x >= room) ok = false;
     }
+    if (tail && (page < 0 || page >= pg.pages || pg.refs[page] > 1)) ok = false;
     return __all_sync(0xffffffffu, ok);
 }
 
@@ -85,8 +84,9 @@ __global__ void __launch_bounds__(kMetaThreads) trim_kernel(const PagesView pg, 
                                                             int32_t* __restrict__ last, int n) {
     __shared__ int first[kMaxSeqs + 1], from[kMaxSeqs], tmp[32];
     const int tid = threadIdx.x;
-    pdl_wait();
-    pdl_trigger();
+    // Behind the moving launch (add), which lets this one start after its own dependency wait and writes nothing that is
+    // read here, everything is found out while it moves; only the writes wait for it.
+    if (!add) pdl_wait();
     int top = *pg.n_free;
     if (add) {
         // a path that does not fit commits nothing (the moving kernel decided the same); from[] holds
@@ -101,31 +101,36 @@ __global__ void __launch_bounds__(kMetaThreads) trim_kernel(const PagesView pg, 
         }
         __syncthreads();
     }
-    int gone = 0;
+    int gone = 0, old = 0, len = 0, keep = 0;
     if (tid < n) {
-        const int old = pg.lens[tid];
-        const int len = add ? from[tid] : min(old, max(new_len[tid], 0));
-        const int held = min(max(pg.held[tid], 0), pg.max_pages), keep = pages_of(max(len, 0), pg.ps);
-        if (len != old) pg.lens[tid] = len;
+        old = pg.lens[tid];
+        len = add ? from[tid] : min(old, max(new_len[tid], 0));
+        const int held = min(max(pg.held[tid], 0), pg.max_pages);
+        keep = pages_of(max(len, 0), pg.ps);
         gone = max(held - keep, 0);
         from[tid] = keep;
-        if (gone) pg.held[tid] = keep;
     }
     int total;
     const int upto = block_scan(gone, tmp, &total);
     if (tid < n) first[tid + 1] = upto;
     if (tid == 0) first[0] = 0;
     __syncthreads();
-    if (total == 0) return;
     auto entry = [&](int e, int* slot) {
         const int b = entry_owner(first, n, e);
         *slot = b * pg.max_pages + from[b] + e - first[b];
         const int p = pg.table[*slot];
         return p >= 0 && p < pg.pages ? p : -1;
     };
-    int slot;
+    int slot, mine = tid < total ? entry(tid, &slot) : -1;
+    if (add) pdl_wait();
+    pdl_trigger();
+    if (tid < n) {
+        if (len != old) pg.lens[tid] = len;
+        if (gone) pg.held[tid] = keep;
+    }
+    if (total == 0) return;
     for (int e = tid; e < total; e += kMetaThreads) {
-        const int p = entry(e, &slot);
+        const int p = e == tid ? mine : entry(e, &slot);
         if (p >= 0) {
             atomicSub(&pg.refs[p], 1);
             atomicMax(&last[p], e);
@@ -136,7 +141,7 @@ __global__ void __launch_bounds__(kMetaThreads) trim_kernel(const PagesView pg, 
     __syncthreads();
     for (int e0 = 0; e0 < total; e0 += kMetaThreads) {
         const int e = e0 + tid;
-        const int p = e < total ? entry(e, &slot) : -1;
+        const int p = e0 == 0 ? mine : e < total ? entry(e, &slot) : -1;
         bool push = false;
         if (p >= 0) {
             const int refs = __ldcg(&pg.refs[p]), winner = __ldcg(&last[p]);
@@ -166,6 +171,7 @@ __global__ void __launch_bounds__(kMetaThreads) trim_kernel(const PagesView pg, 
 __global__ void __launch_bounds__(kMetaThreads) reserve_kernel(const PagesView pg, const int32_t* __restrict__ n_new,
                                                                int32_t* __restrict__ copies, int n) {
     __shared__ int first[kMaxSeqs + 1], held0[kMaxSeqs], tail[kMaxSeqs], copy_of[kMaxSeqs], tmp[32], bad;
+    __shared__ int avail[kMetaThreads];     // the first free pages, looked up while the need is counted
     const int tid = threadIdx.x;
     if (tid == 0) bad = 0;
     pdl_wait();
@@ -189,6 +195,8 @@ __global__ void __launch_bounds__(kMetaThreads) reserve_kernel(const PagesView p
         tail[tid] = grow > 0 ? page : -1;
         held0[tid] = held;
     }
+    auto free_page = [&](int e) { return pg.free_pages[top - 1 - e]; };
+    avail[tid] = tid < top && top <= pg.pages ? free_page(tid) : -1;
     __syncthreads();
     if (grow < 0) bad = 1;
     bool copy = false;
@@ -218,7 +226,7 @@ __global__ void __launch_bounds__(kMetaThreads) reserve_kernel(const PagesView p
     for (int e = tid; e < total; e += kMetaThreads) {
         const int b = entry_owner(first, n, e);
         const int i = e - first[b] - copy_of[b];       // -1: the copy of the tail page
-        const int p = pg.free_pages[top - 1 - e];
+        const int p = e < kMetaThreads ? avail[e] : free_page(e);
         const bool ok = p >= 0 && p < pg.pages;
         if (!ok) atomicOr(pg.err, DFLARE_DEVERR_PAGE);
         if (i >= 0) {
@@ -227,7 +235,7 @@ __global__ void __launch_bounds__(kMetaThreads) reserve_kernel(const PagesView p
         }
     }
     if (copy) {
-        const int p = pg.free_pages[top - 1 - first[tid]];
+        const int p = first[tid] < kMetaThreads ? avail[first[tid]] : free_page(first[tid]);
         pg.table[(size_t)tid * pg.max_pages + len / pg.ps] = p;
         if (p >= 0 && p < pg.pages) pg.refs[p] = 1;
         atomicSub(&pg.refs[page], 1);
@@ -323,7 +331,7 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const PagesView pg, 
 __global__ void __launch_bounds__(kCopyThreads) move_kernel(const PagesView pg, const int32_t* __restrict__ accept,
                                                             const int32_t* __restrict__ path, int path_row,
                                                             int row_units) {
-    __shared__ int move_from[kMaxNodes], move_to[kMaxNodes];     // page * page size + offset
+    __shared__ long long move_from[kMaxNodes], move_to[kMaxNodes];   // where head 0's row lies in a layer, in units of 16 bytes
     __shared__ int n_moves;
     pdl_wait();
     pdl_trigger();
@@ -333,16 +341,19 @@ __global__ void __launch_bounds__(kCopyThreads) move_kernel(const PagesView pg, 
     const int len = pg.lens[b], a = accept[b], held = pg.held[b];
     if (tid < 32) {
         int count = 0;
+        const int32_t* row = pg.table + (size_t)b * pg.max_pages;
+        // the pages of the first 32 moves, wherever the path would read the table's row at all
+        auto in_row = [&](int x) { return x >= 0 && len >= 0 && ((unsigned)len + (unsigned)x) / (unsigned)pg.ps < (unsigned)pg.max_pages; };
+        const int pa0 = tid < a && in_row(first) ? row[(len + first) / pg.ps] : -1, pb0 = tid < a && in_row(tid) ? row[(len + tid) / pg.ps] : -1;
         if (path_fits(pg, b, path, a, path_row, len, held)) {
-            const int32_t* row = pg.table + (size_t)b * pg.max_pages;
             for (int j0 = 0; j0 < a; j0 += 32) {
                 const int j = j0 + tid;
                 const int x = j >= a ? j : j0 ? path[j] : first;
                 bool moves = x != j;
                 int pa = 0, pb = 0;
                 if (moves) {
-                    pa = row[(len + x) / pg.ps];
-                    pb = row[(len + j) / pg.ps];
+                    pa = j0 ? row[(len + x) / pg.ps] : pa0;
+                    pb = j0 ? row[(len + j) / pg.ps] : pb0;
                     if (pa < 0 || pa >= pg.pages || pb < 0 || pb >= pg.pages) {
                         atomicOr(pg.err, DFLARE_DEVERR_PAGE);
                         moves = false;
@@ -351,8 +362,8 @@ __global__ void __launch_bounds__(kCopyThreads) move_kernel(const PagesView pg, 
                 const unsigned votes = __ballot_sync(0xffffffffu, moves);
                 if (moves) {
                     const int at = count + __popc(votes & ((1u << tid) - 1u));
-                    move_from[at] = pa * pg.ps + (len + x) % pg.ps;
-                    move_to[at] = pb * pg.ps + (len + j) % pg.ps;
+                    move_from[at] = ((long long)pa * pg.hkv * pg.ps + (len + x) % pg.ps) * row_units;
+                    move_to[at] = ((long long)pb * pg.hkv * pg.ps + (len + j) % pg.ps) * row_units;
                 }
                 count += __popc(votes);
             }
@@ -366,20 +377,16 @@ __global__ void __launch_bounds__(kCopyThreads) move_kernel(const PagesView pg, 
     if (n == 0 || u >= (long long)per_layer * pg.layers) return;
     const int layer = (int)(u / per_layer), rest = (int)(u % per_layer);
     const int piece = rest % row_units, head = rest / row_units % pg.hkv;
-    uint4* pool = static_cast<uint4*>(rest / row_units >= pg.hkv ? pg.v : pg.k) +
-                  (size_t)layer * pg.pages * pg.hkv * pg.ps * row_units;
-    // slot s of the pool (page * ps + offset) holds this thread's piece here
-    auto at = [&](int s) {
-        return pool + ((size_t)(s / pg.ps) * pg.hkv + head) * pg.ps * row_units + (size_t)(s % pg.ps) * row_units + piece;
-    };
+    uint4* mine = static_cast<uint4*>(rest / row_units >= pg.hkv ? pg.v : pg.k) +
+                  ((size_t)layer * pg.pages * pg.hkv + head) * pg.ps * row_units + piece;
     for (int j0 = 0; j0 < n; j0 += 8) {
         uint4 x[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (j0 + j < n) x[j] = *at(move_from[j0 + j]);
+            if (j0 + j < n) x[j] = mine[move_from[j0 + j]];
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (j0 + j < n) *at(move_to[j0 + j]) = x[j];
+            if (j0 + j < n) mine[move_to[j0 + j]] = x[j];
     }
 }
 
