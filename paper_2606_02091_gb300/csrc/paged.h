@@ -58,8 +58,10 @@ struct TreeArgs {
     float scale_log2;
 };
 
-// the tcgen05 kernel's keys per tile, and how its work is divided (see tree_sched.cuh)
-constexpr int kTcKeys = 128, kTcExtra = 2, kTcLeast = 3;
+// The tcgen05 kernel's keys per tile, and how its work is divided (see tree_sched.cuh). Measured with 1 and 2 extra tiles
+// a pair: 16 nodes over four contexts 21.1 and 20.0 us, over eight up to 900 keys 16.5 and 14.5; with runs of at least 1
+// and 3: 171 nodes over two contexts of 142 and 96 keys 13.1 and 17.4.
+constexpr int kTcKeys = 128, kTcExtra = 2, kTcLeast = 1;
 
 cudaError_t launch_tree_attention(dflare_cache* c, TreeArgs a, cudaStream_t s);
 // tcgen05 kernel for many query rows per kv head (bf16); sets a.QG, a.C and the rows of a query group

@@ -58,7 +58,11 @@ constexpr int kKeys = 64;           // keys per tile
 constexpr int kRows = 16;
 constexpr int kStages = 2;
 constexpr int kMmaThreads = 160;
-constexpr int kExtra = 3, kLeast = 4;      // see tree_sched.cuh
+constexpr int kExtra = 3;       // see tree_sched.cuh
+// 2 tiles of head_dim 128, 4 of 64: what the stages and a trip to memory hold anyway. Measured at 128 with 1, 2 and 4: 2048
+// keys 9.5, 8.6 and 9.6 us, 300 keys 7.5, 7.5 and 9.0; at 64 with 2 and 4: 4096 keys 8.4 and 8.1.
+template <int HD>
+constexpr int kLeast = 256 / HD;
 
 template <int HD>
 struct MmaLayout {
@@ -73,7 +77,7 @@ struct MmaLayout {
 // each; a fifth warp streams the tiles' pages by TMA into a ring of stages. Every warp keeps its own running
 // maximum and sum; when a pair's keys are done each warp sums up a quarter of the head dims of all four.
 // HBM-bound for long contexts (one token over 100000 keys, 8 kv heads of 128: 71 us, 5.8 TB/s); for short ones by
-// its chain of latencies, lengths, page table, keys (2048 keys: 9.5 us).
+// its chain of latencies, lengths, page table, keys (2048 keys: 8.6 us).
 template <int HD>
 __global__ void __launch_bounds__(kMmaThreads, 2) tree_mma_kernel(const __grid_constant__ CUtensorMap mk,
                                                                   const __grid_constant__ CUtensorMap mv, const TreeArgs a) {
@@ -101,7 +105,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) tree_mma_kernel(const __grid_c
     pdl_wait();
     pdl_trigger();      // the joining launch reads the lengths at once: after this kernel's own wait
     int qg, v, v1;
-    tree_runs<kRows, kKeys, kExtra, kLeast>(a, cum, qg, v, v1);
+    tree_runs<kRows, kKeys, kExtra, kLeast<HD>>(a, cum, qg, v, v1);
     const int v0 = v;
     TreePair p, after;
     if (!tree_pair<kExtra>(a, cum, v, v1, p)) return;
@@ -777,7 +781,7 @@ cudaError_t launch_mma(dflare_cache* c, TreeArgs a, cudaStream_t s) {
     a.QG = 1;
     a.C = 2 * c->num_sms;
     e = launch_kernel(true, tree_mma_kernel<HD>, dim3(a.C), dim3(kMmaThreads), MmaLayout<HD>::BYTES, s, c->maps[0], c->maps[1], a);
-    return e == cudaSuccess ? launch_join<bf16, HD>(c, a, kRows, kKeys, kExtra, kLeast, false, s) : e;
+    return e == cudaSuccess ? launch_join<bf16, HD>(c, a, kRows, kKeys, kExtra, kLeast<HD>, false, s) : e;
 }
 
 template <int HD>
