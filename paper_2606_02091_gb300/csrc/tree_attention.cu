@@ -611,12 +611,12 @@ __global__ void __launch_bounds__(kJoinThreads, join_blocks(HD, RW))
             cost = tree_cost(tiles_of[b], extra);
             groups = groups_of[b];
         });
-        tree_shares(a, costs, [&](int g, int from, int many) {
-            if (lane == 0) {
-                first_of[g] = from;
-                many_of[g] = many;
-            }
-        });
+        int first, many;
+        tree_shares(a, costs, lane, first, many);
+        if (lane < kShares) {
+            first_of[lane] = first;
+            many_of[lane] = many;
+        }
     }
     if (shares) __syncthreads();
     const unsigned rows = (unsigned)a.batch * a.n_max * a.hq, step = gridDim.x * (kJoinThreads / 32 / PW) * RW;

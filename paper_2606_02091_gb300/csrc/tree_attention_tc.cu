@@ -361,21 +361,27 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                         // of nodes become 0
                         const int x = base + tile, st = x % NV, rows = min(kKeys, (keys - k0 + 15) & ~15);
                         wait(vfull(st), (uint32_t)(x / NV) & 1u);
-#pragma unroll 4
-                        for (int y = max(ctx - k0, 0) * (HD / 8) + r; y < rows * (HD / 8); y += 128) {
-                            const int kr = y / (HD / 8), pc = y % (HD / 8), key = k0 + kr;
+                        // (a thread's pieces lie 128 / (HD / 8) rows apart in the same place of the swizzle; four at a time)
+                        constexpr int PC = HD / 8, STEP = 128 / PC;
+                        const int pc = r % PC;
+                        for (int kr = max(ctx - k0, 0) + r / PC; kr < rows; kr += 4 * STEP) {
                             uint4* at = reinterpret_cast<uint4*>(smem + LY::V + st * TB + (pc >> 3) * 16384 + kr * 128 + (((pc & 7) ^ (kr & 7)) << 4));
-                            uint4 x = make_uint4(0u, 0u, 0u, 0u);
-                            bool bad = key >= keys;
-                            if (!bad) {
-                                x = *at;
-                                bad = drop_odd(x);
+                            uint4 x[4];
+#pragma unroll
+                            for (int u = 0; u < 4; ++u) x[u] = kr + u * STEP < rows ? at[u * STEP * 8] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+                            for (int u = 0; u < 4; ++u) {
+                                const int key = k0 + kr + u * STEP;
+                                bool bad = key >= keys;
                                 if (bad) {
+                                    x[u] = make_uint4(0u, 0u, 0u, 0u);
+                                } else if (drop_odd(x[u])) {
+                                    bad = true;
                                     atomicOr(&odd[(key - ctx) >> 5], 1u << ((key - ctx) & 31));
                                     odd_any = 1;
                                 }
+                                if (bad && kr + u * STEP < rows) at[u * STEP * 8] = x[u];
                             }
-                            if (bad) *at = x;
                         }
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     }

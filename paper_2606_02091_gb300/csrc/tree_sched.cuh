@@ -68,26 +68,26 @@ __device__ __forceinline__ TreeCosts tree_costs(const TreeArgs& a, int lane, F s
     }
     return c;
 }
-// f(group, first CTA, CTAs) for every group, in order (up to kShares of them)
-template <class F>
-__device__ __forceinline__ void tree_shares(const TreeArgs& a, const TreeCosts& c, F f) {
-    float all = 0.f;
+// Lane g of the warp gets group g's first CTA and how many it has (up to kShares groups).
+__device__ __forceinline__ void tree_shares(const TreeArgs& a, const TreeCosts& c, int lane, int& first, int& many) {
+    float all = 0.f, own = 0.f;
     int some = 0;
 #pragma unroll
     for (int g = 0; g < kShares; ++g) {
         if (g >= a.QG) break;
         all += (float)c.list[g];
         some += c.list[g] > 0;
+        if (lane == g) own = (float)c.list[g];
     }
-    int base = 0;
+    // rounded down with room to spare, so that the parts never add up to more than there is
+    many = own > 0.f ? 1 + (int)__fmul_rn(__fmul_rn((float)max(a.C - some, 0), 0.999999f), __fdiv_rn(own, all)) : 0;
+    first = many;
 #pragma unroll
-    for (int g = 0; g < kShares; ++g) {
-        if (g >= a.QG) break;
-        // rounded down with room to spare, so that the parts never add up to more than there is
-        const int C = c.list[g] ? 1 + (int)__fmul_rn(__fmul_rn((float)max(a.C - some, 0), 0.999999f), __fdiv_rn((float)c.list[g], all)) : 0;
-        f(g, base, C);
-        base += C;
+    for (int o = 1; o < kShares; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, first, o);
+        if (lane >= o) first += x;
     }
+    first -= many;
 }
 
 // The query group of this CTA, its run [v0, v1) of the group's list, and cum[0 .. batch] (cost of one kv head before
@@ -111,14 +111,12 @@ __device__ __forceinline__ void tree_runs(const TreeArgs& a, int32_t* cum, int& 
                     groups = many;
                 }
             });
-            C = 0;
-            tree_shares(a, costs, [&](int x, int first, int many) {
-                if ((int)blockIdx.x >= first && (int)blockIdx.x < first + many) {
-                    g = x;
-                    c = blockIdx.x - first;
-                    C = many;
-                }
-            });
+            int first, many;
+            tree_shares(a, costs, tid, first, many);
+            const unsigned here = __ballot_sync(0xffffffffu, (int)blockIdx.x >= first && (int)blockIdx.x < first + many);
+            g = here ? __ffs(here) - 1 : 0;
+            c -= __shfl_sync(0xffffffffu, first, g);
+            C = here ? __shfl_sync(0xffffffffu, many, g) : 0;
         }
         if (tid == 0) {
             mine[0] = g;
