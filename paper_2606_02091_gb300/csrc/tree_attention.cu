@@ -76,7 +76,7 @@ struct MmaLayout {
 // bf16, up to 16 query rows per kv head (single tokens, small trees). Four warps take 16 keys of each 64-key tile
 // each; a fifth warp streams the tiles' pages by TMA into a ring of stages. Every warp keeps its own running
 // maximum and sum; when a pair's keys are done each warp sums up a quarter of the head dims of all four.
-// HBM-bound for long contexts (one token over 100000 keys, 8 kv heads of 128: 71 us, 5.8 TB/s); for short ones by
+// HBM-bound for long contexts (one token over 100000 keys, 8 kv heads of 128: 70 us, 5.9 TB/s); for short ones by
 // its chain of latencies, lengths, page table, keys (2048 keys: 8.6 us).
 template <int HD>
 __global__ void __launch_bounds__(kMmaThreads, 2) tree_mma_kernel(const __grid_constant__ CUtensorMap mk,

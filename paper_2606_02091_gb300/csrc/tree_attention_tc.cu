@@ -13,8 +13,8 @@
 // m is raised (and O scaled) only when a tile's maximum exceeds it by 2^8: P <= 2^8 carries the same relative
 // precision, and O / l does not depend on m.
 // Bound by the chain of hand-offs between softmax and MMA (1.7 us per tile of 256 rows against 1.46 us of HBM time):
-// measured, 64 nodes over 8 x 32768 keys, 32/8 heads of 128: 205 us, 5.3 TB/s and 1340 TFLOP/s at once; for short
-// contexts by latency, 16 nodes over contexts of 1355 to 3853 keys 20 us.
+// measured, 64 nodes over 8 x 32768 keys, 32/8 heads of 128: 201 us, 5.4 TB/s and 1370 TFLOP/s at once; for short
+// contexts by latency, 16 nodes over contexts of 1355 to 3853 keys 19.7 us.
 // One thread issues all MMAs in the order PV(i), S(i + 2): MMAs of one thread complete in order, so S(i + 2) may
 // overwrite the columns of P(i) without a wait, and the barrier of S(i + 2) also says that PV(i) is done.
 #include <math.h>
