@@ -58,10 +58,11 @@ struct TreeArgs {
     float scale_log2;
 };
 
-// The tcgen05 kernel's keys per tile, and how its work is divided (see tree_sched.cuh). Measured with 1 and 2 extra tiles
-// a pair: 16 nodes over four contexts 21.1 and 20.0 us, over eight up to 900 keys 16.5 and 14.5; with runs of at least 1
-// and 3: 171 nodes over two contexts of 142 and 96 keys 13.1 and 17.4.
-constexpr int kTcKeys = 128, kTcExtra = 2, kTcLeast = 1;
+// The tcgen05 kernel's keys per tile, and how its work is divided (see tree_sched.cuh). Measured with 1, 2, 3 and 4 extra
+// tiles a pair: 33 nodes at head_dim 64 over 2 x 8192 keys 27.5, 29.3, 27.9 and 29.0 us, 16 nodes over four contexts 21.1, 19.5,
+// 19.5 and 19.8, over eight up to 900 keys 16.5, 14.2, 14.8 and 14.8, 90 over three up to 3000 keys 29.8, 27.9, 26.5 and 28.1;
+// with runs of at least 1 and 3: 171 nodes over two contexts of 142 and 96 keys 13.1 and 17.4.
+constexpr int kTcKeys = 128, kTcExtra = 3, kTcLeast = 1;
 
 cudaError_t launch_tree_attention(dflare_cache* c, TreeArgs a, cudaStream_t s);
 // tcgen05 kernel for many query rows per kv head (bf16); sets a.QG, a.C and the rows of a query group
