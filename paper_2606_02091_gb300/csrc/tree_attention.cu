@@ -397,6 +397,9 @@ __global__ void __launch_bounds__(kMmaThreads, 2) tree_mma_kernel(const __grid_c
 constexpr int kFKeys = 32;
 constexpr int kFRows = 16;
 constexpr int kFThreads = 128;
+// CTAs on an SM, as their shared memory allows. Measured at head_dim 64 with 2 and 5: 60 nodes of 16/8 heads over 1000 and 2000
+// keys 79 and 53 us, 150 nodes over 40 contexts up to 100 keys 478 and 300, 8 nodes over 600 keys 8.3 and 8.5.
+constexpr int f32_ctas(int HD) { return HD == 64 ? 5 : 2; }
 constexpr int kFExtra = 0, kFLeast = 1;     // (a tile takes as long as beginning and ending a pair: 13.0 us with 2 and 3, three contexts up to 600)
 
 template <int HD>
@@ -791,7 +794,7 @@ cudaError_t launch_f32(dflare_cache* c, TreeArgs a, cudaStream_t s) {
     cudaError_t e = once([] { return cudaFuncSetAttribute(tree_f32_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); });
     if (e != cudaSuccess) return e;
     a.QG = (a.n_max * a.G + kFRows - 1) / kFRows;
-    a.C = 2 * c->num_sms;
+    a.C = f32_ctas(HD) * c->num_sms;
     e = launch_kernel(true, tree_f32_kernel<HD>, dim3(std::max(a.QG, a.C)), dim3(kFThreads), bytes, s, a);
     return e == cudaSuccess ? launch_join<float, HD>(c, a, kFRows, kFKeys, kFExtra, kFLeast, false, s) : e;
 }
@@ -809,9 +812,10 @@ cudaError_t launch_hd(dflare_cache* c, TreeArgs a, cudaStream_t s) {
 }  // namespace
 
 size_t tree_partial_rows(const dflare_cache_config& g, int num_sms) {
-    // two partial results per CTA: two CTAs per SM of 16 rows, or one of up to 256 rows
+    // two partial results per CTA: of 16 rows with several CTAs per SM, or of up to 256 rows with one
     const int R = g.max_nodes * (g.n_q_heads / g.n_kv_heads);
-    return (size_t)num_sms * 2 * (g.dtype == DFLARE_F32 || R <= 16 ? 2 * kFRows : R <= 128 ? 128 : 256);
+    const int rows = g.dtype == DFLARE_F32 ? f32_ctas(g.head_dim) * kFRows : R <= kRows ? 2 * kRows : R <= 128 ? 128 : 256;
+    return (size_t)num_sms * 2 * rows;
 }
 
 cudaError_t launch_tree_attention(dflare_cache* c, TreeArgs a, cudaStream_t s) {
