@@ -252,6 +252,20 @@ def test_runs_that_cross_from_pair_to_pair(nodes, hq, hkv, hd, batch, top, dtype
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nodes,hq,hd,batch", [(31, 32, 128, 1), (60, 32, 128, 2), (64, 64, 128, 3), (120, 64, 64, 2)])
+def test_more_rows_than_the_joining_launch_holds_at_once(nodes, hq, hd, batch, dtype):
+    """Few enough (sequence, kv head) pairs that CTAs share their keys, so many rows that each of the join's forms walks
+    them: 992, 3840, 12288 and 15360. One sequence has fewer nodes, one no key but its own nodes'."""
+    rng = np.random.default_rng(nodes)
+    lens, counts = [450, 0, 301][:batch], [nodes, nodes, nodes // 3][:batch]
+    p = Paged(rng, lens, counts, hq=hq, hkv=4, hd=hd, page=64, dtype=dtype)
+    q = queries(rng, p, batch, nodes)
+    mask, seen = tree_masks(rng, lens, counts, nodes)
+    check_attend(p, q, seen, mask)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("nodes", [4, 40])
 def test_rows_that_see_nothing_are_zero(dtype, nodes):
     rng = np.random.default_rng(3)
@@ -700,6 +714,22 @@ def test_pages_follow_the_model_through_random_calls(page, dtype, seed):
         assert c.error() == 0
         check_pages(c, m)
     assert full or page > 16
+
+
+@pytest.mark.gpu
+def test_pages_by_the_thousand():
+    """More pages in one call than a CTA has threads: taken, given back in order, taken again."""
+    c = P.PagedCache.allocate(n_layers=1, n_pages=3000, page_size=16, n_q_heads=1, n_kv_heads=1, head_dim=64, max_batch=3, max_pages=1300,
+                              max_nodes=1, dtype="f32")
+    m = Model(3, 3000, 16)
+    for n in ([20000, 5, 17000], [0, 20800, 9000], [16, 16, 20001]):
+        c.reserve(i32(n))
+        assert m.reserve(n) and c.error() == 0
+        check_pages(c, m)
+        c.truncate(i32([0, 0, 0]))
+        m.truncate([0, 0, 0])
+        assert c.error() == 0
+        check_pages(c, m)
 
 
 @pytest.mark.gpu
