@@ -481,7 +481,8 @@ dflare_status dflare_cache_error(dflare_cache* cache, uint32_t* bits_host, void*
  * the free stack, by sequence and then by position. A sequence with n_new > 0 whose last, partly filled
  * page is shared first gets a copy of that page's tokens (over all layers) as its own; the last sharer
  * keeps the page. All sequences get their room or, when pages or table columns do not suffice or an
- * n_new is negative, none does and DFLARE_DEVERR_CAPACITY is set. */
+ * n_new is negative, none does and DFLARE_DEVERR_CAPACITY is set; DFLARE_DEVERR_PAGE, and nothing taken as well,
+ * where *n_free or the page numbers that would be taken cannot be. */
 dflare_status dflare_cache_reserve(dflare_cache* cache, const int32_t* n_new_dev, int batch, void* stream);
 
 /*
@@ -529,7 +530,8 @@ dflare_status dflare_cache_commit(dflare_cache* cache, const int32_t* accept_len
                                   int path_row, int batch, void* stream);
 
 /* lens[b] = min(lens[b], max(new_len[b], 0)) for b < batch; pages past that, reserved ones among them, are
- * given back: a page is free once the last sequence that holds it lets go. */
+ * given back: a page is free once the last sequence that holds it lets go. Here and in a commit an *n_free
+ * outside [0, n_pages] sets DFLARE_DEVERR_PAGE and counts as the nearer of the two. */
 dflare_status dflare_cache_truncate(dflare_cache* cache, const int32_t* new_len_dev, int batch, void* stream);
 
 /* Sequence dst_dev[i] (which must hold no pages) becomes a copy of sequence src_dev[i], i < n <= max_batch,

@@ -87,7 +87,10 @@ __global__ void __launch_bounds__(kMetaThreads) trim_kernel(const PagesView pg, 
     // Behind the moving launch (add), which lets this one start after its own dependency wait and writes nothing that is
     // read here, everything is found out while it moves; only the writes wait for it.
     if (!add) pdl_wait();
-    int top = *pg.n_free;
+    // a count that no stack of `pages` entries has is reported, and taken as empty or full: pushes stay in the array
+    const int told = *pg.n_free;
+    int top = min(max(told, 0), pg.pages);
+    if (told != top && tid == 0) atomicOr(pg.err, DFLARE_DEVERR_PAGE);
     if (add) {
         // a path that does not fit commits nothing (the moving kernel decided the same); from[] holds
         // the new length until the pages are counted
@@ -167,7 +170,8 @@ __global__ void __launch_bounds__(kMetaThreads) trim_kernel(const PagesView pg, 
 
 // Room for n_new tokens. Thread b counts sequence b's pages; "shared at its turn": refs minus the
 // sequences before it that share its partly filled page and write to it too is above one (each of those
-// has taken a copy by then). The copies go to a list that copy_kernel works off.
+// has taken a copy by then). The copies go to a list that copy_kernel works off. Nothing is written before the free
+// stack is known to hold what is taken: a count that it cannot have, or a page number that does not exist, takes nothing.
 __global__ void __launch_bounds__(kMetaThreads) reserve_kernel(const PagesView pg, const int32_t* __restrict__ n_new,
                                                                int32_t* __restrict__ copies, int n) {
     __shared__ int first[kMaxSeqs + 1], held0[kMaxSeqs], tail[kMaxSeqs], copy_of[kMaxSeqs], tmp[32], bad;
@@ -177,6 +181,7 @@ __global__ void __launch_bounds__(kMetaThreads) reserve_kernel(const PagesView p
     pdl_wait();
     pdl_trigger();
     const int top = *pg.n_free;
+    const bool stack_ok = top >= 0 && top <= pg.pages;
     int grow = 0, len = 0, held = 0, fresh = 0, page = -1;
     if (tid < n) {
         grow = n_new[tid];
@@ -196,7 +201,7 @@ __global__ void __launch_bounds__(kMetaThreads) reserve_kernel(const PagesView p
         held0[tid] = held;
     }
     auto free_page = [&](int e) { return pg.free_pages[top - 1 - e]; };
-    avail[tid] = tid < top && top <= pg.pages ? free_page(tid) : -1;
+    avail[tid] = stack_ok && tid < top ? free_page(tid) : -1;
     __syncthreads();
     if (grow < 0) bad = 1;
     bool copy = false;
@@ -214,10 +219,21 @@ __global__ void __launch_bounds__(kMetaThreads) reserve_kernel(const PagesView p
     }
     if (tid == 0) first[0] = 0;
     __syncthreads();
-    if (bad || total > top || total < 0) {     // (a total past 2^31 would need more columns than tables have)
+    auto taken = [&](int e) { return e < kMetaThreads ? avail[e] : free_page(e); };
+    // (a total past 2^31 would need more columns than tables have)
+    uint32_t err = !stack_ok ? DFLARE_DEVERR_PAGE : bad || total > top || total < 0 ? DFLARE_DEVERR_CAPACITY : 0u;
+    if (!err) {
+        bool odd = false;
+        for (int e = tid; e < total; e += kMetaThreads) {
+            const int p = taken(e);
+            odd |= p < 0 || p >= pg.pages;
+        }
+        if (__syncthreads_or(odd)) err = DFLARE_DEVERR_PAGE;
+    }
+    if (err) {
         if (tid == 0) {
             copies[0] = 0;
-            atomicOr(pg.err, DFLARE_DEVERR_CAPACITY);
+            atomicOr(pg.err, err);
         }
         return;
     }
@@ -226,18 +242,16 @@ __global__ void __launch_bounds__(kMetaThreads) reserve_kernel(const PagesView p
     for (int e = tid; e < total; e += kMetaThreads) {
         const int b = entry_owner(first, n, e);
         const int i = e - first[b] - copy_of[b];       // -1: the copy of the tail page
-        const int p = e < kMetaThreads ? avail[e] : free_page(e);
-        const bool ok = p >= 0 && p < pg.pages;
-        if (!ok) atomicOr(pg.err, DFLARE_DEVERR_PAGE);
+        const int p = taken(e);
         if (i >= 0) {
             pg.table[(size_t)b * pg.max_pages + held0[b] + i] = p;
-            if (ok) pg.refs[p] = 1;
+            pg.refs[p] = 1;
         }
     }
     if (copy) {
-        const int p = first[tid] < kMetaThreads ? avail[first[tid]] : free_page(first[tid]);
+        const int p = taken(first[tid]);
         pg.table[(size_t)tid * pg.max_pages + len / pg.ps] = p;
-        if (p >= 0 && p < pg.pages) pg.refs[p] = 1;
+        pg.refs[p] = 1;
         atomicSub(&pg.refs[page], 1);
         copies[1 + 3 * c] = page;
         copies[2 + 3 * c] = p;

@@ -783,6 +783,45 @@ def test_page_calls_report_what_cannot_be():
     check_pages(c, m)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("told", [-1, -1500, 2001, 4000])
+def test_a_free_count_that_cannot_be_stays_inside_the_stack(told):
+    """*n_free below zero or above the pool: reported, nothing taken, and nothing written outside the stack (which
+    lies between values that would do as page numbers)."""
+    pages = 2000
+    around = torch.full((3 * pages,), 5, dtype=torch.int32, device="cuda")
+    free = around[pages:2 * pages]
+    free.copy_(torch.arange(pages - 1, -1, -1, dtype=torch.int32))
+    pool = [torch.zeros((1, pages, 1, 16, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    c = P.PagedCache(k=pool[0], v=pool[1], table=i32(np.full((2, pages), -1)), lens=i32([0, 0]), held=i32([0, 0]), refs=i32([0] * pages),
+                     free=free, n_free=i32([pages]), n_q_heads=1, max_nodes=1)
+    c.reserve(i32([1300 * 16, 5]))
+    assert c.error() == 0
+    before = [t.clone() for t in (c.table, c.held, c.refs, around)]
+    c.n_free.fill_(told)
+    c.reserve(i32([0, 1200 * 16]))
+    assert c.error() == P.DEVERR_PAGE and int(c.n_free) == told
+    assert all(torch.equal(a, b) for a, b in zip((c.table, c.held, c.refs, around), before))
+    c.truncate(i32([0, 0]))             # 1301 pages come back: to an empty stack, or to one that is full
+    assert c.error() == P.DEVERR_PAGE and int(c.n_free) == (1301 if told < 0 else pages)
+    assert (around[:pages] == 5).all() and (around[2 * pages:] == 5).all()
+    assert not c.refs.any() and (c.table == -1).all() and c.held.tolist() == [0, 0]
+    if told < 0:
+        assert free[:1301].tolist() == list(range(1301))      # as they were taken
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("at,number", [(0, -1), (0, 1 << 20), (1100, -7), (1100, 2000)])
+def test_free_pages_that_do_not_exist_are_not_taken(at, number):
+    c = P.PagedCache.allocate(n_layers=1, n_pages=2000, page_size=16, n_q_heads=1, n_kv_heads=1, head_dim=64, max_batch=2, max_pages=1300,
+                              max_nodes=1)
+    c.free[2000 - 1 - at] = number      # the one that would be taken at-th
+    before = [t.clone() for t in (c.table, c.held, c.refs, c.free, c.n_free)]
+    c.reserve(i32([7, 1200 * 16]))
+    assert c.error() == P.DEVERR_PAGE
+    assert all(torch.equal(a, b) for a, b in zip((c.table, c.held, c.refs, c.free, c.n_free), before))
+
+
 # ------------------------------------------------------------------------------------------ trees
 
 @pytest.mark.gpu
