@@ -101,6 +101,13 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     asm("max.f32 %0, %1, %2, %3;" : "=f"(v) : "f"(a), "f"(b), "f"(c));
     return v;
 }
+// The softmax streams meet. What either has waited for in tensor memory (O after its last PV) or read there is in order with
+// what the other does there next: tcgen05 operations keep the order of a barrier only between its two fences.
+__device__ __forceinline__ void streams_meet() {
+    tc_fence_before();
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+    tc_fence_after();
+}
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 template <int HD, int NQ>
@@ -491,7 +498,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
             if (NQ == 1) {
                 float2* ml = reinterpret_cast<float2*>(smem + LY::ML);
                 ml[w * 128 + r] = make_float2(m, l);
-                asm volatile("bar.sync 1, 256;" ::: "memory");
+                streams_meet();     // (with it, each reads the O that the other has waited for)
                 const float2 x = ml[r], y = ml[128 + r];
                 M = fmaxf(x.x, y.x);
                 const float ref = M == -INFINITY ? 0.f : M;
@@ -499,7 +506,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                 w1 = pow2(y.x - ref);
                 L = x.y * w0 + y.y * w1;
             } else {
-                asm volatile("bar.sync 1, 256;" ::: "memory");     // odd nodes noted by stream 0
+                streams_meet();     // odd nodes noted by stream 0
             }
             const bool odds = odd_any != 0;
             if (warp_live) {
@@ -590,15 +597,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                     else if (a.lse) a.lse[orow] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
                 }
             }
-            tc_fence_before();
             // O, the (m, l) exchange and the odd nodes are free for the next pair
-            asm volatile("bar.sync 1, 256;" ::: "memory");
+            streams_meet();
             if (odds) {
                 if (tid < kMaxNodes / 32) odd[tid] = 0;
                 if (tid == 0) odd_any = 0;
-                asm volatile("bar.sync 1, 256;" ::: "memory");
+                streams_meet();
             }
-            tc_fence_after();
             base += n;
             p = after;
             nodes = nodes2;

@@ -325,6 +325,34 @@ def test_attend_is_the_same_on_every_run(nodes):
         assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
 
 
+def test_the_softmax_streams_meet_between_tensor_memory_fences():
+    """With up to 128 query rows a stream reads the output that the other one has waited for. The memory model orders
+    that only where a barrier stands between a fence before it and one after it; no run can show one that is missing, so
+    this reads the source: every barrier of the two streams is the one that has both."""
+    import os
+    import re
+    src = open(os.path.join(os.path.dirname(P.__file__), "csrc", "tree_attention_tc.cu")).read()
+    src = re.sub(r"//[^\n]*", "", src)
+    barriers = [m.start() for m in re.finditer(r"bar\.(sync|arrive)", src)]
+    fenced = re.search(r'tc_fence_before\(\);\s*asm volatile\("bar\.sync 1, 256;" ::: "memory"\);\s*tc_fence_after\(\);', src)
+    assert len(barriers) == 1 and fenced and fenced.start() < barriers[0] < fenced.end()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("lens", [[0, 1], [129, 300], [40000, 511], [70000, 70000]])
+def test_the_streams_join_over_runs_of_any_length(lens, hd):
+    """Up to 128 query rows per kv head: runs of one tile (a single stream), of two, and of many."""
+    rng = np.random.default_rng(lens[0] + hd)
+    p = Paged(rng, lens, [20, 17], hq=4, hkv=1, hd=hd, page=128, dtype="bf16")
+    q = queries(rng, p, 2, 20)
+    mask, seen = tree_masks(rng, lens, [20, 17], 20)
+    check_attend(p, q, seen, mask)
+    first, _ = run_attend(p, q, mask)
+    for _ in range(20):
+        assert torch.equal(run_attend(p, q, mask)[0], first)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("nodes", [2, 40])
 def test_attend_reaches_past_32_bit_offsets(nodes):
