@@ -1052,6 +1052,106 @@ def test_the_binding_refuses_wrong_tensors():
     assert c.error() == 0
 
 
+class Elsewhere:
+    """A tensor as the binding sees one, on a device of one's choice; its memory is never looked at."""
+
+    is_cuda = True
+
+    def __init__(self, shape, dtype, index):
+        self.shape, self.dtype, self.device = torch.Size(shape), dtype, f"cuda:{index}"
+        self._index, self._plain = index, torch.empty(shape, dtype=dtype, device="meta")
+
+    def get_device(self):
+        return self._index
+
+    def data_ptr(self):
+        return 4096
+
+    def __getattr__(self, name):        # dim, numel, stride, is_contiguous
+        return getattr(self._plain, name)
+
+
+def there(shape, dtype, index):
+    return Elsewhere(shape, getattr(torch, dtype), index)
+
+
+class Taken:
+    """The library's calls, taken down."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        if not name.startswith("dflare_"):
+            raise AttributeError(name)
+        return lambda *a: self.calls.append((name, a)) or 0
+
+
+DEVICE_CALLS = {
+    # the tensors of a call, and the call; b, n, hq, hkv, hd = 2, 3, 4, 2, 64
+    "reserve": (dict(n_new=((2,), "int32")), lambda c, t, s: c.reserve(**t, stream=s)),
+    "truncate": (dict(new_len=((2,), "int32")), lambda c, t, s: c.truncate(**t, stream=s)),
+    "fork": (dict(src=((2,), "int32"), dst=((2,), "int32")), lambda c, t, s: c.fork(**t, stream=s)),
+    "copy_pages": (dict(src=((2,), "int32"), dst=((2,), "int32")), lambda c, t, s: c.copy_pages(**t, stream=s)),
+    "commit": (dict(accept_len=((2,), "int32"), path=((2, 3), "int32")), lambda c, t, s: c.commit(**t, stream=s)),
+    "append": (dict(q=((2, 3, 4, 64), "bfloat16"), k=((2, 3, 2, 64), "bfloat16"), v=((2, 3, 2, 64), "bfloat16"), n_new=((2,), "int32"),
+                    phase=((32,), "int64"), q_out=((2, 3, 4, 64), "bfloat16"), depth=((2, 3), "int32")), lambda c, t, s: c.append(0, **t, stream=s)),
+    "attend": (dict(q=((2, 3, 4, 64), "bfloat16"), n_nodes=((2,), "int32"), out=((2, 3, 4, 64), "bfloat16"), mask=((2, 3, 1), "int32"),
+                    lse=((2, 3, 4), "float32")), lambda c, t, s: c.attend(0, **t, stream=s)),
+    "rope": (dict(x=((6, 4, 64), "bfloat16"), positions=((6,), "int32"), phase=((32,), "int64"), out=((6, 4, 64), "bfloat16")),
+             lambda c, t, s: P.rope(**t, stream=s)),
+    "tree_plan": (dict(parents=((2, 3), "int32"), n_nodes=((2,), "int32"), mask=((2, 3, 1), "int32"), depth=((2, 3), "int32"),
+                       error=((1,), "int32")), lambda c, t, s: P.tree_plan(**t, stream=s)),
+    "tree_accept": (dict(tokens=((2, 3), "int32"), parents=((2, 3), "int32"), choice=((2, 3), "int32"), n_nodes=((2,), "int32"),
+                         accept_len=((2,), "int32"), path=((2, 3), "int32"), next_token=((2,), "int32"), error=((1,), "int32")),
+                    lambda c, t, s: P.tree_accept(**t, stream=s)),
+}
+
+
+@pytest.mark.parametrize("name", sorted(DEVICE_CALLS))
+def test_the_binding_keeps_to_one_device(name, monkeypatch):
+    """A cache's calls run on its device and that device's current stream, whatever the current device is; the other
+    calls on the current device. Any tensor or stream of another device is refused before the library is called."""
+    from types import SimpleNamespace
+    from paper_2606_02091_gb300 import paged
+    lib = Taken()
+    monkeypatch.setattr(_lib, "load", lambda: lib)
+    monkeypatch.setattr(paged, "_device", lambda: 0)
+    monkeypatch.setattr(paged, "_raw_stream", lambda device: 1000 + device)
+    home = 0 if name in ("rope", "tree_plan", "tree_accept") else 1
+    c = object.__new__(P.PagedCache)
+    c.__dict__.update(_cache=ctypes.c_void_p(), _L=lib, device_index=1, n_layers=1, n_pages=8, n_kv_heads=2, page_size=16, head_dim=64,
+                      max_batch=2, max_pages=3, n_q_heads=4, max_nodes=8, dtype=torch.bfloat16)
+    shapes, call = DEVICE_CALLS[name]
+    call(c, {x: there(*y, home) for x, y in shapes.items()}, None)
+    assert len(lib.calls) == 1 and lib.calls[0][1][-1] == 1000 + home
+    call(c, {x: there(*y, home) for x, y in shapes.items()}, SimpleNamespace(device_index=home, cuda_stream=77))
+    assert len(lib.calls) == 2 and lib.calls[1][1][-1] == 77
+    with pytest.raises(ValueError, match="stream"):
+        call(c, {x: there(*y, home) for x, y in shapes.items()}, SimpleNamespace(device_index=1 - home, cuda_stream=77))
+    for away in shapes:
+        tensors = {x: there(*y, 1 - home if x == away else home) for x, y in shapes.items()}
+        with pytest.raises(ValueError, match=f"cuda:{home}"):
+            call(c, tensors, None)
+    assert len(lib.calls) == 2
+    if home:
+        c.error()
+        assert lib.calls[2][1][-1] == 1001
+
+
+def test_a_cache_has_its_memory_on_one_device(monkeypatch):
+    lib = Taken()
+    monkeypatch.setattr(_lib, "load", lambda: lib)
+    shapes = dict(k=((1, 8, 2, 16, 64), "bfloat16"), v=((1, 8, 2, 16, 64), "bfloat16"), table=((2, 3), "int32"), lens=((2,), "int32"),
+                  held=((2,), "int32"), refs=((8,), "int32"), free=((8,), "int32"), n_free=((1,), "int32"))
+    for away in shapes:
+        with pytest.raises(ValueError, match="cuda:"):
+            P.PagedCache(**{x: there(*y, 1 if x == away else 0) for x, y in shapes.items()}, n_q_heads=4, max_nodes=8)
+    with pytest.raises(ValueError, match="CUDA tensor"):
+        P.PagedCache(**{x: torch.zeros(y[0], dtype=getattr(torch, y[1])) for x, y in shapes.items()}, n_q_heads=4, max_nodes=8)
+    assert not lib.calls
+
+
 # ------------------------------------------------------------------------------------------ all of it together
 
 @pytest.mark.gpu
