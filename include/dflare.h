@@ -402,9 +402,11 @@ dflare_status dflare_argmax_noalloc(const float* logits_dev, int rows, int vocab
  * scaled for contexts of `factor` (>= 1) times the trained length:
  *   DFLARE_ROPE_LINEAR  inv_j / factor (position interpolation)
  *   DFLARE_ROPE_NTK     theta multiplied by factor^(rot_dim / (rot_dim - 2)); needs rot_dim > 2
- *   DFLARE_ROPE_YARN    pairs that turn more than beta_fast times within `trained` positions keep inv_j,
- *                       those under beta_slow turns take inv_j / factor, those between a mix linear in
- *                       j; values are multiplied by 0.1 ln(factor) + 1 */
+ *   DFLARE_ROPE_YARN    pairs that turn beta_fast times or more within `trained` positions keep inv_j,
+ *                       those of beta_slow turns or fewer take inv_j / factor, those between a mix linear
+ *                       in j, from the last of the former to the first of the latter (j counted on past
+ *                       the head's pairs where they lie beyond); values are multiplied by
+ *                       0.1 ln(factor) + 1 */
 typedef enum { DFLARE_ROPE_PLAIN = 0, DFLARE_ROPE_LINEAR = 1, DFLARE_ROPE_NTK = 2, DFLARE_ROPE_YARN = 3 } dflare_rope_scaling;
 typedef struct {
     int rot_dim;          /* rotated elements of each head, even, 2..1024 */

@@ -285,18 +285,20 @@ dflare_status dflare_rope_phases(const dflare_rope_config* g, uint64_t* phase_ho
     const int half = g->rot_dim / 2;
     double theta = g->theta;
     if (g->scaling == DFLARE_ROPE_NTK) theta *= std::pow(g->factor, g->rot_dim / (g->rot_dim - 2.0));
-    // YARN: the (fractional) pair that turns `beta` times within the trained positions
+    // YARN: the (fractional) pair that turns `beta` times within the trained positions. The mix runs from the last pair with
+    // beta_fast turns or more to the first with beta_slow or fewer, either of which may lie beyond the head's pairs: ends
+    // drawn in to pairs that the head has would change the frequencies of the pairs between.
     auto pair_at = [&](double beta) { return g->rot_dim * std::log(g->trained / (beta * two_pi)) / (2.0 * std::log(theta)); };
     double lo = 0, hi = 0;
     if (g->scaling == DFLARE_ROPE_YARN) {
-        lo = std::max(std::floor(pair_at(g->beta_fast)), 0.0);
-        hi = std::min(std::ceil(pair_at(g->beta_slow)), (double)(half - 1));
+        lo = std::floor(pair_at(g->beta_fast));
+        hi = std::ceil(pair_at(g->beta_slow));
     }
     for (int j = 0; j < half; ++j) {
         double inv = std::pow(theta, -2.0 * j / g->rot_dim);
         if (g->scaling == DFLARE_ROPE_LINEAR) inv /= g->factor;
         if (g->scaling == DFLARE_ROPE_YARN) {
-            const double mix = std::min(std::max((j - lo) / std::max(hi - lo, 1e-3), 0.0), 1.0);
+            const double mix = std::min(std::max((j - lo) / std::max(hi - lo, 1.0), 0.0), 1.0);
             inv = inv * (1.0 - mix) + inv / g->factor * mix;
         }
         phase_host[j] = (uint64_t)std::ldexp(inv / two_pi, 64);    // below 2^64 / 6: inv <= 1

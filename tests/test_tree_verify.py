@@ -506,6 +506,37 @@ def test_rope_phases_are_the_frequencies(scaling):
     assert np.all(np.abs(got - inv) <= 1e-14 * inv + 2.0 ** -60) and abs(m - magnitude) < 1e-6
 
 
+@pytest.mark.parametrize("rot,theta,trained,factor,fast,slow", [
+    (128, 1e4, 131072, 4.0, 32.0, 1.0),     # the last pair still turns twice: the mix ends beyond it
+    (64, 1e4, 10 ** 7, 16.0, 32.0, 1.0),    # every pair turns 32 times: all keep their frequency
+    (64, 1e4, 100, 2.0, 32.0, 1.0),         # the first pair turns 16 times: the mix begins before it
+    (64, 1e6, 3, 8.0, 32.0, 1.0),           # no pair turns once: all stretch
+    (4, 1e4, 4096, 4.0, 32.0, 1.0),         # two pairs, neither at an end
+    (128, 1e6, 32768, 4.0, 32.0, 1.0),
+    (2, 1e4, 4096, 4.0, 32.0, 1.0),
+])
+def test_yarn_goes_by_the_turns_of_each_pair(raw, rot, theta, trained, factor, fast, slow):
+    """Frequencies from the turns that pairs make within the trained positions, pairs counted past the head's at both ends."""
+    def turns(j):
+        return trained * theta ** (-2.0 * j / rot) / (2 * math.pi)
+
+    lo = next(j for j in range(4 * rot, -4 * rot, -1) if turns(j) >= fast)
+    hi = next(j for j in range(-4 * rot, 4 * rot) if turns(j) <= slow)
+    assert lo < hi
+    phase, m = P.rope_phases(rot, theta, "yarn", factor, trained, fast, slow, device="cpu")
+    got = phase.numpy().astype(np.float64) / 2.0 ** 64 * 2 * math.pi
+    for j in range(rot // 2):
+        inv = theta ** (-2.0 * j / rot)
+        stretch = (j - lo) / (hi - lo) if lo < j < hi else float(turns(j) < fast)
+        want = inv * (1 - stretch) + inv / factor * stretch
+        assert abs(got[j] - want) <= 1e-13 * want + 2.0 ** -60
+        if turns(j) >= fast:
+            assert abs(got[j] - inv) <= 1e-13 * inv + 2.0 ** -60
+        if turns(j) <= slow:
+            assert abs(got[j] - inv / factor) <= 1e-13 * inv + 2.0 ** -60
+    assert abs(m - (0.1 * math.log(factor) + 1.0)) < 1e-6
+
+
 # ------------------------------------------------------------------------------------------ append
 
 @pytest.mark.gpu
