@@ -517,7 +517,10 @@ dflare_status dflare_cache_append(dflare_cache* cache, int layer, const void* q_
  *   out_dev   [batch][n_max][n_q_heads][head_dim] T, 16-byte aligned.
  *   lse_dev   optional [batch][n_max][n_q_heads] fp32: natural logarithm of the row's sum of exp(score).
  * Rows that see nothing, and rows from n_nodes[b] on, are zero with lse = -inf. What lies in a row's
- * unseen slots (any bits, infinities and NaN included) does not reach its result.
+ * unseen slots (any bits, infinities and NaN included) does not reach its result. A held page whose number
+ * does not exist sets DFLARE_DEVERR_PAGE, and its keys and values read as zeros. Counts outside [0, n_max]
+ * and keys past the sequence's pages are cut off without a report (dflare_cache_append and _reserve report
+ * what does not fit).
  */
 dflare_status dflare_cache_attend(dflare_cache* cache, int layer, const void* q_dev, long long q_row,
                                   const int32_t* mask_dev, const int32_t* n_nodes_dev, int batch, int n_max,

@@ -436,6 +436,7 @@ __global__ void __launch_bounds__(kFThreads) tree_f32_kernel(const TreeArgs a) {
                 const int r = x / DG, d = x % DG * 4, key = k0 + r;
                 const int page = key < keys ? table[key / a.pg.ps] : -1;
                 const bool there = page >= 0 && page < a.pg.pages;
+                if (key < keys && !there) atomicOr(a.pg.err, DFLARE_DEVERR_PAGE);
                 const size_t at = there ? ((((size_t)a.layer * a.pg.pages + page) * a.pg.hkv + it.h) * a.pg.ps + key % a.pg.ps) * HD + d : 0;
                 const int bytes = there ? 16 : 0;       // 0: the 16 bytes become zero
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(Ks + (st * kFKeys + r) * LD + d)),

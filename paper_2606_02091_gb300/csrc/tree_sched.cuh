@@ -198,7 +198,8 @@ __device__ __forceinline__ bool wait_inline(uint32_t bar, uint32_t parity, volat
 // Pages for the warp that streams tiles by TMA: lane x looks up the page of box x (`rows` tokens, a divisor of the tile)
 // from tile `base` of a pair on, so that one trip to the table serves 32 boxes. What memory says is looked at only when
 // the boxes are due: the first group's copies would wait for the second's pages. A slot without a page takes a plane of
-// the tensor map outside the pool, which reads as zero.
+// the tensor map outside the pool, which reads as zero: boxes past the pages held, and, reported, those of a held page
+// whose number does not exist.
 struct BoxPage {
     int held, page, at, h;
 };
@@ -208,6 +209,7 @@ __device__ __forceinline__ BoxPage box_page(const TreeArgs& a, const TreePair& p
 }
 __device__ __forceinline__ int box_plane(const TreeArgs& a, const BoxPage& x) {
     if (x.at < x.held && x.page >= 0 && x.page < a.pg.pages) return (a.layer * a.pg.pages + x.page) * a.pg.hkv + x.h;
+    if (x.at < x.held) atomicOr(a.pg.err, DFLARE_DEVERR_PAGE);
     return (int)min(0x7fffffffLL, (long long)a.pg.layers * a.pg.pages * a.pg.hkv);
 }
 // f(first tile, tiles, planes of their boxes) for groups of tiles (of one pair, as many as have 32 boxes) of the run from

@@ -424,6 +424,46 @@ def test_attend_stays_within_the_pages_a_sequence_holds():
         assert not out[0].any() and torch.isneginf(lse[0]).all()
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nodes", [1, 4, 30, 70])
+@pytest.mark.parametrize("number", [-1, 10 ** 6])
+def test_attend_reports_pages_that_do_not_exist(nodes, number, dtype):
+    """A page number in the table that no page has: reported, its keys and values read as zeros, other sequences as ever."""
+    rng = np.random.default_rng(nodes)
+    lens = [100, 60]
+    p = Paged(rng, lens, [nodes, nodes], hq=8, hkv=2, hd=64, page=16, dtype=dtype)
+    q = queries(rng, p, 2, nodes)
+    mask, seen = tree_masks(rng, lens, [nodes, nodes], nodes)
+    check_attend(p, q, seen, mask)
+    p.k[0, p.table[0, 2]] = 0
+    p.v[0, p.table[0, 2]] = 0
+    want, want_lse = run_attend(p, q, mask)
+    p.cache.table[0, 2] = number
+    out, lse = torch.empty_like(want), torch.empty_like(want_lse)
+    p.cache.attend(0, q, i32([nodes, nodes]), out, mask=mask, lse=lse)
+    assert p.cache.error() == P.DEVERR_PAGE
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    p.cache.table[0, 2] = int(p.table[0, 2])
+    out, _ = run_attend(p, q, mask)
+    assert torch.equal(out, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nodes", [8, 24, 72])
+def test_attend_over_a_length_beyond_the_pages_sees_the_keys_that_exist(nodes, dtype):
+    rng = np.random.default_rng(nodes)
+    held = up(40 + nodes, 16)
+    p = Paged(rng, [40, 20], [16 * held - 40, nodes], hq=4, hkv=2, hd=64, page=16, dtype=dtype, nodes=nodes)
+    q = queries(rng, p, 2, nodes)
+    p.cache.lens.copy_(i32([40000, 20]))
+    mask, seen = tree_masks(rng, [16 * held, 20], [0, nodes], nodes)
+    out, lse = run_attend(p, q, mask, counts=[nodes, nodes])
+    want, wlse, bound, lbound = attend_reference(p, host(q), seen, 64 ** -0.5)
+    assert np.all(np.abs(host(out) - want) <= bound) and np.all(np.abs(host(lse) - wlse) <= lbound)
+
+
 # ------------------------------------------------------------------------------------------ rotary positions
 
 ROPE = [
