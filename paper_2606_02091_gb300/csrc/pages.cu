@@ -432,13 +432,14 @@ bool check_cache_config(const dflare_cache_config* g, std::string* why) {
     if (g->max_nodes < 1 || g->max_nodes > kMaxNodes) return bad("max_nodes must be in [1, 1024]");
     if (g->dtype != DFLARE_BF16 && g->dtype != DFLARE_F32) return bad("dtype must be DFLARE_BF16 or DFLARE_F32");
     // numbers that kernels hold in 32 bits: token slots of a sequence and of the pool, boxes of the tensor
-    // maps, and the attention's 32-key tiles over all sequences and heads
+    // maps, and the attention's 32-key tiles over all sequences and heads (with the CTAs they are divided among: the
+    // division rounds up, and the run of the last CTA may end that much later)
     if ((long long)g->max_pages * g->page_size > 0x7fffffffLL) return bad("max_pages * page_size must be below 2^31");
     if ((long long)g->n_pages * g->page_size > 0x7fffffffLL) return bad("n_pages * page_size must be below 2^31");
     if ((long long)g->n_layers * g->n_pages * g->n_kv_heads > 0x7fffffffLL)
         return bad("n_layers * n_pages * n_kv_heads must be below 2^31");
-    if ((long long)g->max_batch * g->n_kv_heads * ((long long)g->max_pages * g->page_size / 32 + 1) > 0x7fffffffLL)
-        return bad("max_batch * n_kv_heads * max_pages * page_size / 32 must be below 2^31");
+    if ((long long)g->max_batch * g->n_kv_heads * ((long long)g->max_pages * g->page_size / 32 + 1) > 0x7fffffffLL - 4096)
+        return bad("max_batch * n_kv_heads * (max_pages * page_size / 32 + 1) must be below 2^31 - 4096");
     if ((long long)g->max_batch * g->max_pages > 0x7fffffffLL) return bad("max_batch * max_pages must be below 2^31");
     return true;
 }

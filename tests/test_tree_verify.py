@@ -1023,6 +1023,18 @@ def test_cache_create_refuses_bad_configs(raw, field, value):
     assert not out and raw.dflare_last_error(None).startswith(b"invalid cache config")
 
 
+def test_cache_create_leaves_room_for_the_division_of_the_work(raw):
+    """The key tiles of all sequences and heads, divided among up to 760 CTAs and rounded up, stay below 2^31."""
+    out = ctypes.c_void_p()
+    for batch, hkv, max_pages, fits in ((256, 8, 1048573, False), (256, 8, 1048572, True), (255, 8, 1048573, True)):
+        tiles = batch * hkv * (max_pages + 1)
+        assert tiles < 2 ** 31 and fits == (tiles <= 2 ** 31 - 1 - 4096)
+        g = cache_config(max_batch=batch, n_kv_heads=hkv, n_q_heads=hkv, max_pages=max_pages, page_size=32)
+        # (no buffers: what fits is refused for those)
+        assert raw.dflare_cache_create(ctypes.byref(g), None, ctypes.byref(out)) == _lib.DFLARE_EINVAL
+        assert raw.dflare_last_error(None).startswith(b"dflare_cache_create: a buffer" if fits else b"invalid cache config")
+
+
 def test_cache_create_refuses_bad_buffers(raw):
     out = ctypes.c_void_p()
     g = cache_config()
