@@ -420,7 +420,9 @@ typedef struct {
 
 /* Host only: phase_host[rot_dim / 2] = inv_j / (2 pi) in units of 2^-64 turns, and the factor on the
  * rotated values. The phases are what the rotary calls read from device memory: position * phase modulo
- * 2^64 is the angle modulo one turn, to position * 2^-65 turns, for every int32 position. */
+ * 2^64 is the angle modulo one turn for every int32 position, without a rounding of its own. The phases are
+ * computed in double precision, within 2^-50 of themselves and one unit: the angle is off by at most
+ * position * 2^-52 turns (2^-21 at the last position), and by fp32's rounding of the fraction, 2^-26. */
 dflare_status dflare_rope_phases(const dflare_rope_config* cfg, uint64_t* phase_host, float* magnitude_host);
 
 typedef enum { DFLARE_ROPE_HALF = 0, DFLARE_ROPE_INTERLEAVED = 1 } dflare_rope_layout;

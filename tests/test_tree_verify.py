@@ -546,6 +546,29 @@ def test_rope_phases_are_the_frequencies(scaling):
     assert np.all(np.abs(got - inv) <= 1e-14 * inv + 2.0 ** -60) and abs(m - magnitude) < 1e-6
 
 
+@pytest.mark.parametrize("rot,theta,scaling,factor", [(128, 1e6, "none", 1.0), (64, 1e4, "linear", 3.0), (128, 1e4, "ntk", 16.0), (128, 5e5, "yarn", 7.0)])
+def test_rope_phases_are_as_exact_as_stated(raw, rot, theta, scaling, factor):
+    """Every phase within 2^-50 of itself and one unit: an angle within position x 2^-52 turns, at int32's ends 2^-21."""
+    from decimal import Decimal, getcontext
+    getcontext().prec = 60
+    pi = Decimal("3.14159265358979323846264338327950288419716939937510582097494459")
+    base, f = Decimal(theta), Decimal(factor)
+    if scaling == "ntk":
+        base *= f ** (Decimal(rot) / (rot - 2))
+    exact = [base ** (Decimal(-2 * j) / rot) for j in range(rot // 2)]
+    if scaling == "linear":
+        exact = [x / f for x in exact]
+    if scaling == "yarn":
+        at = [rot * (Decimal(4096) / (t * 2 * pi)).ln() / (2 * base.ln()) for t in (32, 1)]
+        lo, hi = math.floor(at[0]), math.ceil(at[1])
+        mix = [min(max(Decimal(j - lo) / (hi - lo), Decimal(0)), Decimal(1)) for j in range(rot // 2)]
+        exact = [x * (1 - m) + x / f * m for x, m in zip(exact, mix)]
+    phase, _ = P.rope_phases(rot, theta, scaling, factor, device="cpu")
+    off = [abs(Decimal(p) - x / (2 * pi) * 2 ** 64) for p, x in zip(phase.tolist(), exact)]
+    assert all(o <= x / (2 * pi) * 2 ** 14 + 1 for o, x in zip(off, exact))
+    assert max(off) * 2 ** 31 / 2 ** 64 <= Decimal(2) ** -21
+
+
 @pytest.mark.parametrize("rot,theta,trained,factor,fast,slow", [
     (128, 1e4, 131072, 4.0, 32.0, 1.0),     # the last pair still turns twice: the mix ends beyond it
     (64, 1e4, 10 ** 7, 16.0, 32.0, 1.0),    # every pair turns 32 times: all keep their frequency
