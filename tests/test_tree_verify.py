@@ -2,6 +2,7 @@
 bits and acceptance, each against a plain implementation in 64 bits (or of whole numbers), and their refusals."""
 import ctypes
 import math
+import types
 
 import numpy as np
 import pytest
@@ -309,6 +310,67 @@ def test_unseen_infinities_and_nans_stay_out(dtype, nodes, hq, hkv):
     out, lse = run_attend(p, q, mask)
     assert np.array_equal(host(out)[~sees], c[~sees]) and np.array_equal(host(lse)[~sees], host(clean_lse)[~sees])
     assert np.isnan(host(out)[sees]).all() and np.isnan(host(lse)[sees]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nodes,hq,hkv", [(3, 4, 2), (16, 8, 1), (70, 8, 2)])
+def test_unseen_infinities_and_nans_stay_out_of_wide_heads(dtype, nodes, hq, hkv):
+    """The same at head_dim 128, where a tile's rows lie in two parts: odd values in both, at their ends."""
+    rng = np.random.default_rng(nodes)
+    lens, counts = [117, 64], [nodes, nodes - 2]
+    p = Paged(rng, lens, counts, hq=hq, hkv=hkv, hd=128, page=32, dtype=dtype)
+    q = queries(rng, p, 2, nodes)
+    mask, seen = tree_masks(rng, lens, counts, nodes)
+    clean, clean_lse = run_attend(p, q, mask)
+    for b, x in enumerate(lens):        # a node in the middle
+        node = (counts[b] - 1) // 2
+        page, off = p.table[b, (x + node) // 32], (x + node) % 32
+        for e, value in ((0, math.inf), (63, math.nan), (64, -math.inf), (70, math.nan), (127, math.inf)):
+            p.v[0, page, :, off, e] = value
+    out, lse = run_attend(p, q, mask)
+    sees = np.stack([s[:, x + (c - 1) // 2] & (np.arange(nodes) < c) for s, x, c in zip(seen, lens, counts)])
+    o, c = host(out), host(clean)
+    assert np.array_equal(o[~sees], c[~sees]) and np.array_equal(host(lse), host(clean_lse))
+    assert sees.any() and np.isposinf(o[sees][..., [0, 127]]).all() and np.isneginf(o[sees][..., 64]).all()
+    assert np.isnan(o[sees][..., [63, 70]]).all()
+    rest = [e for e in range(128) if e not in (0, 63, 64, 70, 127)]
+    assert np.array_equal(o[sees][..., rest], c[sees][..., rest])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,nodes,hq,hkv,hd,batch,keys", [("bf16", 9, 32, 8, 128, 12, 4000), ("bf16", 40, 64, 8, 64, 6, 1500), ("bf16", 70, 32, 8, 128, 6, 1500),
+                                                              ("bf16", 3, 16, 8, 128, 20, 900), ("f32", 5, 8, 4, 64, 12, 1500)])
+def test_scores_that_go_on_growing(dtype, nodes, hq, hkv, hd, batch, keys):
+    """Scores spread over tens of powers of two, in runs of several tiles: rows whose maximum is raised long after
+    their first keys, when their output has to be scaled down where it is."""
+    rng = np.random.default_rng(nodes)
+    lens, counts = [keys - 37 * b for b in range(batch)], [nodes - b % 2 for b in range(batch)]
+    p = Paged(rng, lens, counts, hq=hq, hkv=hkv, hd=hd, page=64, dtype=dtype, scale=20.0)
+    q = queries(rng, p, batch, nodes)
+    late = 0
+    for b in range(batch):          # rows with a tile 2^8 above the four before it
+        k = p.rows(p.k, b)[:lens[b] // 128 * 128]
+        z = np.einsum("hgd,khd->hgk", host(q)[b, 0].reshape(hkv, hq // hkv, hd), k) * hd ** -0.5 / math.log(2)
+        top = z.reshape(hq, -1, 128).max(-1)
+        late += sum(any(row[t] > row[t - 4:t].max() + 8 for t in range(4, len(row))) for row in top)
+    assert late > hq * batch // 10
+    mask, seen = tree_masks(rng, lens, counts, nodes)
+    check_attend(p, q, seen, mask)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("nodes,hq,hkv,hd,lens", [(1024, 8, 2, 128, [300, 0]), (1000, 12, 4, 64, [33]), (1024, 64, 1, 64, [70]), (600, 8, 2, 128, [2000])])
+def test_chunks_of_many_query_groups(nodes, hq, hkv, hd, lens):
+    """Chunks of a prompt with more than 2048 query rows per kv head, up to more groups of them than the GPU has SMs:
+    chains and trees."""
+    rng = np.random.default_rng(nodes + hq)
+    counts = [nodes - 3 * b for b in range(len(lens))]
+    p = Paged(rng, lens, counts, hq=hq, hkv=hkv, hd=hd, page=64, dtype="bf16")
+    q = queries(rng, p, len(lens), nodes)
+    check_attend(p, q, chain_seen(lens, counts, nodes), None)
+    mask, seen = tree_masks(rng, lens, counts, nodes)
+    check_attend(p, q, seen, mask)
 
 
 @pytest.mark.gpu
@@ -1015,6 +1077,75 @@ def test_impossible_trees_are_reported():
         assert L.dflare_tree_accept(z.data_ptr(), p.data_ptr(), z.data_ptr(), c.data_ptr(), 1, 3, acc.data_ptr(), depth.data_ptr(),
                                     nxt.data_ptr(), err.data_ptr(), s) == 0
         assert err.item() == P.DEVERR_TREE
+
+
+# ------------------------------------------------------------------------------------------ steps
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv,hd,page,n", [(4, 2, 64, 16, 7), (8, 2, 128, 32, 20), (16, 2, 64, 16, 40)])
+def test_steps_of_a_server(hq, hkv, hd, page, n, dtype):
+    """A prompt read in two chunks and forked, then steps of plan, reserve, append and attend per layer, accept and
+    commit: every attention against the definition over the rows in the pages, and the rows against a list of what
+    was accepted."""
+    rng = np.random.default_rng(n)
+    batch, layers, prompt = 3, 2, 45
+    c = P.PagedCache.allocate(n_layers=layers, n_pages=60, page_size=page, n_q_heads=hq, n_kv_heads=hkv, head_dim=hd, max_batch=batch,
+                              max_pages=16, max_nodes=max(n, 30), dtype=dtype)
+    for t in (c.k, c.v):
+        t.fill_(math.nan)
+    phase, magnitude = P.rope_phases(hd, 1e4)
+    view = object.__new__(Paged)
+    view.t, view.page, view.hq, view.hkv, view.hd, view.k, view.v = c.dtype, page, hq, hkv, hd, c.k, c.v
+    kept = [[[np.zeros((0, hkv, hd)), np.zeros((0, hkv, hd))] for _ in range(layers)] for _ in range(batch)]
+
+    def one_pass(counts, width, depth, mask, seen):
+        """A layer at a time; returns the nodes' rows as they lie in the pages."""
+        view.table, view.lens, view.counts = c.table.cpu().numpy(), c.lens.tolist(), counts
+        rows = [[None] * layers for _ in range(batch)]
+        for layer in range(layers):
+            qkv = torch.from_numpy(rng.standard_normal((batch, width, hq + 2 * hkv, hd)).astype(np.float32)).to(c.dtype).cuda()
+            q, k, v = qkv[:, :, :hq], qkv[:, :, hq:hq + hkv], qkv[:, :, hq + hkv:]
+            c.append(layer, q, k, v, i32(counts), phase, q, depth=depth, magnitude=magnitude)
+            check_attend(types.SimpleNamespace(**view.__dict__, cache=c, rows=view.rows), q, seen, mask, layer=layer)
+            for b in range(batch):
+                for i, pool in enumerate((c.k, c.v)):
+                    got = view.rows(pool, b, layer)
+                    assert np.array_equal(got[:view.lens[b]], kept[b][layer][i])
+                rows[b][layer] = [view.rows(pool, b, layer)[view.lens[b]:] for pool in (c.k, c.v)]
+        return rows
+
+    def accept(rows, paths):
+        for b in range(batch):
+            for layer in range(layers):
+                kept[b][layer] = [np.concatenate([old, new[paths[b]]]) for old, new in zip(kept[b][layer], rows[b][layer])]
+
+    for chunk in (30, prompt - 30):
+        counts = [chunk, 0, 0]
+        c.reserve(i32(counts))
+        rows = one_pass(counts, chunk, None, None, chain_seen(c.lens.tolist(), counts, chunk))
+        c.commit(i32(counts), i32(np.tile(np.arange(chunk), (batch, 1))))
+        accept(rows, [list(range(chunk)), [], []])
+    c.fork(i32([0, 0]), i32([1, 2]))
+    kept[1], kept[2] = ([list(x) for x in kept[0]] for _ in range(2))
+    for step in range(3):
+        counts = [n, max(n - 3, 1), n // 2]
+        parents = np.stack([random_parents(rng, n) for _ in range(batch)])
+        tokens, choice = rng.integers(0, 2, (batch, n)), rng.integers(0, 2, (batch, n))
+        mask, depth = torch.zeros((batch, n, up(n, 32)), dtype=torch.int32, device="cuda"), torch.zeros((batch, n), dtype=torch.int32, device="cuda")
+        acc, nxt, path = i32([0] * batch), i32([0] * batch), torch.zeros_like(depth)
+        P.tree_plan(i32(parents), i32(counts), mask, depth)
+        c.reserve(i32(counts))
+        above = np.zeros((batch, n, n), bool)
+        for b, x in enumerate(counts):
+            above[b, :x, :x] = ancestors(parents[b, :x])
+        seen = [np.concatenate([np.ones((n, x), bool), above[b, :, :counts[b]]], 1) for b, x in enumerate(c.lens.tolist())]
+        rows = one_pass(counts, n, depth, mask, seen)
+        P.tree_accept(i32(tokens), i32(parents), i32(choice), i32(counts), acc, path, nxt)
+        c.commit(acc, path)
+        accept(rows, [path[b, :x].tolist() for b, x in enumerate(acc.tolist())])
+        assert c.error() == 0 and c.lens.tolist() == [len(kept[b][0][0]) for b in range(batch)]
+    assert min(c.lens.tolist()) > prompt
 
 
 # ------------------------------------------------------------------------------------------ refusals (host)
