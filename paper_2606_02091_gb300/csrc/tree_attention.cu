@@ -1,5 +1,5 @@
-// Attention of a tree of nodes (or one token, or a chunk of a prompt) over a paged cache, for up to 64
-// query rows per kv head in bf16, and for any number in fp32; many rows in bf16 go to tree_attention_tc.cu.
+// Attention of a tree of nodes (or one token, or a chunk of a prompt) over a paged cache, for up to 16
+// query rows per kv head in bf16, and for any number in fp32; more rows in bf16 go to tree_attention_tc.cu.
 // How the keys are divided among the CTAs: tree_sched.cuh.
 //
 // One pass over the keys with the running maximum m and sum l of the softmax, in log2 units:
@@ -35,16 +35,6 @@ __device__ __forceinline__ void mma_bf16(float* c, const uint32_t* a, uint32_t b
         "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-// 2^x, relative error about 2^-22; 2^-inf = 0
-__device__ __forceinline__ float pow2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
-    __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<uint32_t*>(&h);
 }
 // byte offset of 16-byte piece c of row r in a tile of 64 rows stored as [hd / 64][64][128 bytes], swizzled
 __device__ __forceinline__ uint32_t tile_at(int r, int c) {

@@ -49,15 +49,6 @@ struct TcLayout {
     static constexpr uint32_t BYTES = END + 32768;
 };
 
-__device__ __forceinline__ float pow2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
-    __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<uint32_t*>(&h);
-}
 // MN-major operand (V): 64-element swizzle atoms along N `atom` bytes apart, 8-key groups 1024 bytes apart
 __device__ __forceinline__ uint64_t smem_desc_mn(uint32_t saddr, uint32_t atom) {
     return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(atom >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) |

@@ -17,6 +17,17 @@
 
 namespace dfl {
 
+// 2^x, relative error about 2^-22; 2^-inf = 0
+__device__ __forceinline__ float pow2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
+    __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<uint32_t*>(&h);
+}
+
 // What memory says of sequence b, and what follows: nodes, tokens, and keys that exist (tokens and nodes as
 // far as the sequence's pages reach). In two steps, so that the loads can be under way long before their use.
 struct TreeRaw {
