@@ -435,7 +435,7 @@ typedef enum { DFLARE_ROPE_HALF = 0, DFLARE_ROPE_INTERLEAVED = 1 } dflare_rope_l
  * gradient with respect to y.
  *   x_row, x_head, out_row, out_head   strides in elements between rows and between heads (elements of
  *                                      a head are adjacent); out may be x itself with the same strides.
- * Fast where the pointers are 16-byte aligned, strides and rot_dim and head_dim multiples of 16.
+ * Fast where the pointers are 16-byte aligned, strides multiples of 8, rot_dim and head_dim multiples of 16.
  */
 dflare_status dflare_rope(const void* x_dev, long long x_row, long long x_head, void* out_dev,
                           long long out_row, long long out_head, const int32_t* positions_dev,
@@ -472,8 +472,9 @@ typedef struct {
 typedef struct dflare_cache dflare_cache;
 
 /* Validate (host only: DFLARE_EINVAL without touching the GPU), then make the cache's handle on the
- * current device; it owns an error word and the attention's workspace, of at most 100 MB. The pages'
- * contents need no initialisation: nothing is read that was not written. */
+ * current device. It owns an error word, 4 bytes per page, a list of 3 KB and the attention's workspace, at most
+ * 512 rows of head_dim + 2 fp32 values per SM (41 MB on 152 SMs). The pages' contents need no initialisation:
+ * nothing is read that was not written. */
 dflare_status dflare_cache_create(const dflare_cache_config* cfg, const dflare_cache_buffers* buffers,
                                   dflare_cache** out);
 /* Free what dflare_cache_create allocated (synchronises the device first). NULL is a no-op. */
@@ -492,7 +493,8 @@ dflare_status dflare_cache_reserve(dflare_cache* cache, const int32_t* n_new_dev
 /*
  * The new tokens of one layer: rows i < n_new[b] of sequence b (b < batch).
  *   q_dev, k_dev, v_dev  [batch][n_max][heads][head_dim] T with `*_row` elements between rows (heads
- *                        adjacent): three parts of one projection's rows will do.
+ *                        adjacent): three parts of one projection's rows will do. Sequence b's rows begin
+ *                        n_max rows behind sequence b - 1's.
  *   q_out_dev            [batch][n_max][n_q_heads][head_dim] T, rotated queries; q_dev itself (with
  *                        out_row = q_row) rotates in place. NULL (with q_dev NULL) leaves queries out.
  *   depth_dev            [batch][n_max] int32: the row's position is lens[b] + depth; NULL: lens[b] + i.
@@ -515,9 +517,12 @@ dflare_status dflare_cache_append(dflare_cache* cache, int layer, const void* q_
  *   q_dev     [batch][n_max][n_q_heads][head_dim] T, `q_row` elements between rows; 16-byte aligned,
  *             q_row a multiple of 8. Query head h reads kv head h / (n_q_heads / n_kv_heads).
  *   mask_dev  [batch][n_max][(n_max + 31) / 32] int32, of dflare_tree_plan.
- *   scale     on the scores; finite.
+ *   scale     on the scores; positive and finite.
  *   out_dev   [batch][n_max][n_q_heads][head_dim] T, 16-byte aligned.
  *   lse_dev   optional [batch][n_max][n_q_heads] fp32: natural logarithm of the row's sum of exp(score).
+ * Scores, maxima, sums and outputs are held in fp32. In bf16 the softmax weights are rounded to bf16 for their
+ * product with the values (the tensor cores' operand type; the sum that divides is of the unrounded ones) and the
+ * result once more: each by 2^-8 of itself at most. In fp32 products are exact fp32 ones.
  * Rows that see nothing, and rows from n_nodes[b] on, are zero with lse = -inf. What lies in a row's
  * unseen slots (any bits, infinities and NaN included) does not reach its result. A held page whose number
  * does not exist sets DFLARE_DEVERR_PAGE, and its keys and values read as zeros. Counts outside [0, n_max]
@@ -532,7 +537,7 @@ dflare_status dflare_cache_attend(dflare_cache* cache, int layer, const void* q_
  * their rows of all layers move to slots lens[b] .. lens[b] + accept_len[b] - 1, lens grows by accept_len,
  * and pages past the new length are given back (by sequence, then by position). A length or path that no
  * tree has, or a last page that is still shared, sets DFLARE_DEVERR_TREE and commits nothing of that
- * sequence. */
+ * sequence, whose reserved pages are given back all the same. */
 dflare_status dflare_cache_commit(dflare_cache* cache, const int32_t* accept_len_dev, const int32_t* path_dev,
                                   int path_row, int batch, void* stream);
 

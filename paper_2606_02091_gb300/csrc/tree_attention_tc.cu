@@ -13,7 +13,8 @@
 // m is raised (and O scaled) only when a tile's maximum exceeds it by 2^8: P <= 2^8 carries the same relative
 // precision, and O / l does not depend on m.
 // Bound by the chain of hand-offs between softmax and MMA (1.7 us per tile of 256 rows against 1.46 us of HBM time):
-// measured, 64 nodes over 8 x 32768 keys, 32/8 heads of 128: 201 us, 5.4 TB/s and 1370 TFLOP/s at once; for short
+// measured, 64 nodes over 8 x 32768 keys, 32/8 heads of 128: 200 us in runs of 4 ms, 5.4 TB/s and 1370 TFLOP/s at once;
+// 224 us for seconds on end, 4.8 TB/s and 1230 TFLOP/s, under the power cap (1.37 kW) at a median of 1590 MHz. For short
 // contexts by latency, 16 nodes over contexts of 1355 to 3853 keys 19.7 us.
 // One thread issues all MMAs in the order PV(i), S(i + 2): MMAs of one thread complete in order, so S(i + 2) may
 // overwrite the columns of P(i) without a wait, and the barrier of S(i + 2) also says that PV(i) is done.
@@ -437,7 +438,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                                 p0 = pow2(p0);
                                 p1 = pow2(p1);
                                 sum[e & 1] = add2(sum[e & 1], pack2(p0, p1));
-                                // (rounded to bf16, relative error 2^-8 at most; the sum is of the unrounded ones)
+                                // (rounded to bf16, relative error 2^-8 at most: the operand type that goes with bf16
+                                // values; the sum is of the unrounded ones)
                                 pw[16 * x + e] = two_bf16(p0, p1);
                             }
                         }

@@ -1,5 +1,5 @@
 // mbarrier, TMA and tcgen05 helpers of the projection GEMMs (sm_103a inline PTX); the attention uses its thread
-// election and asynchronous tensor-memory loads, the context-fill fusion its election.
+// election and asynchronous tensor-memory loads, the context-fill fusion its election, the paged attention all of it.
 #pragma once
 #include <cuda.h>
 
