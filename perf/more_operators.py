@@ -244,7 +244,7 @@ def prepare(case, seed):
         s["lib"] = lib
         if "table" in s:
             _handle(case, s, min(case["nodes"], 1024))
-            if s["kind"] == "shared":
+            if s["kind"] == "shared":       # the division of the work and partial results
                 s["work"] = s["cache"].shared_work(s["q"].shape[1], s["q"].shape[2])
         elif s["kind"] == "norm":
             s["work"] = lib.qk_norm_rope_work(case["hd"])
@@ -298,7 +298,7 @@ def _prepare_shared(c, r):
     common = [p // page * page for p in prefixes]
     s.update(lens=_i32(lens), counts=_i32(counts), q=r.normal("q", (c["layers"], batch, n, c["hq"], c["hd"]), t, 1.5), ways=ways, common=_i32(common),
              longest=max(common), widest=max(lens[b] + counts[b] - common[b // ways] for b in range(batch)),
-             out=torch.zeros((c["layers"], batch, n, c["hq"], c["hd"]), dtype=t, device="cuda"), plan=_i32(np.zeros((batch, 2))))
+             out=torch.zeros((c["layers"], batch, n, c["hq"], c["hd"]), dtype=t, device="cuda"))
     s["mask"] = None if c["chain"] else _i32(_words(_ancestors(_parents(r.host("tree"), batch, n))))
     return s
 
@@ -372,9 +372,10 @@ def _own_norm(s):
 
 
 def _own_shared(s):
-    s["cache"].share_plan(s["plan"])
-    for layer in range(s["q"].shape[0]):
-        s["cache"].attend_shared(layer, s["q"][layer], s["counts"], s["out"][layer], s["plan"], s["work"], mask=s["mask"])
+    layers, _, n = s["q"].shape[:3]
+    s["cache"].share_plan(s["counts"], n, s["work"])        # once for all layers of a step
+    for layer in range(layers):
+        s["cache"].attend_shared(layer, s["q"][layer], s["out"][layer], s["work"], mask=s["mask"])
     return s["out"]
 
 
