@@ -442,6 +442,44 @@ dflare_status dflare_rope(const void* x_dev, long long x_row, long long x_head, 
                           const uint64_t* phase_dev, int rows, int heads, int head_dim, int rot_dim,
                           int layout, float magnitude, int backward, int dtype, void* stream);
 
+/* The query or key heads of dflare_qk_norm_rope and its backward. Strides in elements between rows and between heads; the
+ * elements of a head are adjacent. */
+typedef struct {
+    const void* x;              /* [rows][heads][head_dim] T: the heads before their norm */
+    long long x_row, x_head;
+    const void* dy;             /* backward only: the gradient with respect to the results */
+    long long dy_row, dy_head;
+    void* out;                  /* the results; backward: the gradient with respect to x. x or dy itself with the same strides will do */
+    long long out_row, out_head;
+    const void* gain;           /* [head_dim] T */
+    float* dgain;               /* backward only: [head_dim] fp32, written: the sum over rows and heads */
+    int heads;                  /* 1..4096 */
+} dflare_qk_heads;
+
+/* Rows of dflare_qk_norm_rope_backward's workspace. */
+#define DFLARE_QK_NORM_WORK_ROWS 1024
+
+/*
+ * The root-mean-square norm of every head with the rotary embedding in the same pass: z = gain x / sqrt(mean(x^2) + eps)
+ * over a head's elements, then the pairs of its first rot_dim elements turned and scaled as in dflare_rope (rot_dim = 0:
+ * none; phase_dev and positions_dev may then be NULL). In fp32, rounded once.
+ *   q, k      the query heads, and the key heads or NULL: one call for both, each with its own gain.
+ *   head_dim  2..1024; eps at least 0.
+ * Fast where pointers are 16-byte aligned, strides multiples of 8, rot_dim and head_dim multiples of 16 and head_dim
+ * at most 512.
+ */
+dflare_status dflare_qk_norm_rope(const dflare_qk_heads* q, const dflare_qk_heads* k, const int32_t* positions_dev,
+                                  const uint64_t* phase_dev, int rows, int head_dim, int rot_dim, int layout,
+                                  float magnitude, float eps, int dtype, void* stream);
+
+/* The gradients of the same with respect to x (into out) and the gains, from x and dy. work_dev: fp32
+ * [DFLARE_QK_NORM_WORK_ROWS][head_dim], for this call alone until it is done. The gains' gradients are summed in the same
+ * order on every run on one kind of GPU. */
+dflare_status dflare_qk_norm_rope_backward(const dflare_qk_heads* q, const dflare_qk_heads* k,
+                                           const int32_t* positions_dev, const uint64_t* phase_dev, int rows,
+                                           int head_dim, int rot_dim, int layout, float magnitude, float eps,
+                                           float* work_dev, int dtype, void* stream);
+
 /* A paged cache of one model's keys and values. */
 typedef struct {
     int n_layers;         /* layers of the model, 1..256 */
@@ -510,6 +548,15 @@ dflare_status dflare_cache_append(dflare_cache* cache, int layer, const void* q_
                                   const int32_t* n_new_dev, int batch, int n_max,
                                   const uint64_t* phase_dev, int rot_dim, int layout, float magnitude,
                                   void* stream);
+
+/* dflare_cache_append with the norm of dflare_qk_norm_rope on queries and keys before they turn: q_gain_dev (with
+ * queries) and k_gain_dev [head_dim] T, eps at least 0. Values are stored as they are. */
+dflare_status dflare_cache_append_normed(dflare_cache* cache, int layer, const void* q_dev, long long q_row,
+                                         const void* k_dev, long long k_row, const void* v_dev, long long v_row,
+                                         void* q_out_dev, long long out_row, const void* q_gain_dev,
+                                         const void* k_gain_dev, float eps, const int32_t* depth_dev,
+                                         const int32_t* n_new_dev, int batch, int n_max, const uint64_t* phase_dev,
+                                         int rot_dim, int layout, float magnitude, void* stream);
 
 /*
  * Attention of one layer: node i < n_nodes[b] of sequence b sees the sequence's lens[b] tokens and those
@@ -580,6 +627,34 @@ dflare_status dflare_tree_plan(const int32_t* parents_dev, const int32_t* n_node
  */
 dflare_status dflare_tree_accept(const int32_t* tokens_dev, const int32_t* parents_dev, const int32_t* choice_dev,
                                  const int32_t* n_nodes_dev, int batch, int n_max, int32_t* accept_len_dev,
+                                 int32_t* path_dev, int32_t* next_token_dev, uint32_t* err_dev, void* stream);
+
+/*
+ * Sampled acceptance in drafted trees from given probabilities and random numbers (dflare_verify_sampled does the same for the
+ * blocks of a context, with random numbers of its own). From node 0 on, the children of the current node, with tokens x, are
+ * asked in the order of their numbers. Before the first F = 0, W = Q = 1; then, with p the target's row of the current node
+ * and q the draft's,
+ *   child i is kept where u[i] (q[x] / Q) W < max(0, p[x] - F q[x]), and the walk goes on from it;
+ *   otherwise F grows by W / Q, W becomes the sum of max(0, p - F q) over the vocabulary, and, with `distinct`, Q loses q[x]
+ *   (where Q is not above 0, q[x] / Q counts as 0 and F stays).
+ * Where no child is kept, the next token is the lowest id whose running sum of max(0, p - F q) exceeds u[0] times the whole
+ * sum; of p, where that sum is not above 0. So every token has the target's distribution, whatever the draft.
+ *   tokens_dev, parents_dev, n_nodes_dev, accept_len_dev, path_dev, next_token_dev, err_dev  as in dflare_tree_accept.
+ *   target_dev  [batch][n_max][vocab] fp32: the target's probabilities after each node.
+ *   draft_dev   [batch][draft_rows][vocab] fp32, draft_rows at least n_max - 1 (the last node has no children): the
+ *               distributions that the children of each node were drawn from; with replacement (distinct = 0), or without
+ *               (distinct = 1, siblings' tokens differ). NULL: drafts were picked, not drawn; with W = 1 before the first,
+ *               child i is kept where u[i] W < p[x] (0 if a sibling before had the same token), otherwise W loses p[x]; the next
+ *               token is drawn from p without the children's tokens.
+ *   u_dev       [batch][n_max] fp32, uniform in [0, 1); other values count as the nearest number of that range, NaN as 0.
+ *   vocab       1..2^28.
+ * Sums over the vocabulary are good to 2^-40 of themselves, in the same order on every run. Probabilities that are negative or
+ * not finite weigh nothing in them. A token outside [0, vocab) is not kept and sets DFLARE_DEVERR_TOKEN; a row that weighs nothing
+ * gives token 0 and sets it too.
+ */
+dflare_status dflare_tree_sample(const int32_t* tokens_dev, const int32_t* parents_dev, const int32_t* n_nodes_dev,
+                                 const float* target_dev, const float* draft_dev, int draft_rows, const float* u_dev,
+                                 int batch, int n_max, int vocab, int distinct, int32_t* accept_len_dev,
                                  int32_t* path_dev, int32_t* next_token_dev, uint32_t* err_dev, void* stream);
 
 #ifdef __cplusplus

@@ -1,0 +1,587 @@
+// Root-mean-square norm of query and key heads with the rotary positions in the same pass: forward, backward, and on
+// a step's new tokens on their way into the pages of a cache.
+//
+// Of one head x with gain g:  r = 1 / sqrt(mean(x^2) + eps),  z = g x r,  y = R z  (R turns the pairs of the rotated
+// elements by position * phase and scales them; the other elements stay).
+// Backward, from dy:  dz = R^T dy,  a = g dz,  dx = r (a - x r^2 mean(a x)),  dg = sum over rows and heads of dz x r.
+// All of it in fp32, y and dx rounded once.
+//
+// Work: as in rope.cu a thread has 16 elements of a head, the head's threads (a power of two of them, neighbours in a
+// warp) add up their squares by shuffles, and a thread walks over several heads of one row, which share its cosines. A
+// thread has heads of queries or of keys, so that it needs one gain.
+#include <math.h>
+
+#include <algorithm>
+#include <cmath>
+#include <string>
+
+#include "common.cuh"
+#include "paged.h"
+#include "rope.cuh"
+
+namespace dfl {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kBatch = 4;               // heads whose loads are in flight together
+constexpr int kWorkRows = DFLARE_QK_NORM_WORK_ROWS;     // CTAs that may leave a sum of gain gradients
+
+// queries, keys, values (values in an append only: copied)
+struct Part {
+    const void* x;
+    long long x_row, x_head;
+    const void* dy;                     // backward
+    long long dy_row, dy_head;
+    void* out;                          // y or dx; keys and values of an append go to the pages
+    long long out_row, out_head;
+    const void* gain;
+    float* dgain;                       // backward, [hd]
+    int heads;
+    int slots;                          // threads that share one row's 16 elements of these heads
+    int blocks;                         // backward: CTAs
+};
+struct NormArgs {
+    Part part[3];
+    const int32_t* positions;
+    const uint64_t* phase;
+    float* work;                        // backward: [CTAs][hd]
+    int rows, hd, rot;
+    int lanes;                          // threads of a head: the power of two from hd / 16 on
+    int per;                            // heads that a thread walks over, at most
+    float magnitude, eps;
+    PagesView pg;
+    AppendRows rows_of;
+};
+
+template <class T>
+__device__ __forceinline__ const T* head_at(const void* base, long long row, long long row_stride, int h, long long head_stride) {
+    return static_cast<const T*>(base) + row * row_stride + h * head_stride;
+}
+// where head h of a part's row goes; null: nowhere
+template <class T, bool APPEND>
+__device__ __forceinline__ T* out_at(const NormArgs& a, const Part& p, int part, long long row, int h, long long slot) {
+    if (!APPEND || part == 0) return static_cast<T*>(p.out) + row * p.out_row + h * p.out_head;
+    return slot < 0 ? nullptr : static_cast<T*>(part == 2 ? a.pg.v : a.pg.k) + (slot + (long long)h * a.pg.ps) * a.hd;
+}
+// element 0 and 1 of pair j of a unit, numbered within its 16 elements (two runs of eight)
+template <bool INTER> __device__ __forceinline__ constexpr int first_of(int j) { return INTER ? 2 * j : j; }
+template <bool INTER> __device__ __forceinline__ constexpr int second_of(int j) { return INTER ? 2 * j + 1 : 8 + j; }
+
+template <class T>
+__device__ __forceinline__ void values(const Unit<T>& u, float* v) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float2 f = get2(u, i);
+        v[2 * i] = f.x;
+        v[2 * i + 1] = f.y;
+    }
+}
+__device__ __forceinline__ float head_sum(float v, int lanes) {
+    for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// Vector form: rot and hd multiples of 16, hd up to 512, everything 16-byte aligned.
+template <class T, bool INTER, bool APPEND>
+__global__ void __launch_bounds__(kThreads, 2) qk_norm_kernel(const NormArgs a) {
+    pdl_wait();
+    pdl_trigger();
+    const int total = a.part[0].slots + a.part[1].slots + a.part[2].slots;
+    const long long t = (long long)blockIdx.x * kThreads + threadIdx.x;
+    const int u = (int)(t & (a.lanes - 1));
+    const long long g = t / a.lanes;
+    const long long row = g / total;
+    int s = (int)(g - row * total), part = 0;
+    if (s >= a.part[0].slots) {
+        s -= a.part[0].slots;
+        part = 1;
+        if (APPEND && s >= a.part[1].slots) {
+            s -= a.part[1].slots;
+            part = 2;
+        }
+    }
+    const Part& p = a.part[part];
+    // threads without work stay for the shuffles
+    long long pos = 0, slot = -1;
+    bool live = row < a.rows;
+    if (live) {
+        if (APPEND) live = append_row(a.pg, a.rows_of, (int)row, pos, slot);
+        else pos = a.positions ? a.positions[row] : 0;
+    }
+    live = live && u < a.hd / 16;
+    const bool rotates = u < a.rot / 16;
+    const int e0 = rotates && !INTER ? u * 8 : u * 16, e1 = rotates && !INTER ? a.rot / 2 + u * 8 : u * 16 + 8;
+    Unit<T> gain{};
+    if (live && part < 2) load_unit(gain, static_cast<const T*>(p.gain) + e0, static_cast<const T*>(p.gain) + e1);
+    float c[8], sn[8];
+    for (int i0 = 0; i0 < a.per; i0 += kBatch) {
+        Unit<T> x[kBatch];
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            const int h = s + (i0 + k) * p.slots;
+            x[k] = Unit<T>{};
+            if (live && h < p.heads) {
+                const T* from = head_at<T>(p.x, row, p.x_row, h, p.x_head);
+                load_unit(x[k], from + e0, from + e1);
+            }
+        }
+        if (i0 == 0 && rotates && live) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) pair_turn(pos, a.phase[u * 8 + j], 1.f, a.magnitude, c[j], sn[j]);
+        }
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            const int h = s + (i0 + k) * p.slots;
+            float v[16];
+            values(x[k], v);
+            float sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sum = fmaf(v[e], v[e], sum);
+            sum = head_sum(sum, a.lanes);
+            if (!live || h >= p.heads) continue;
+            T* to = out_at<T, APPEND>(a, p, part, row, h, slot);
+            if (APPEND && !to) continue;
+            if (!APPEND || part < 2) {
+                const float r = inv_rms(sum, a.hd, a.eps);
+                float w[16];
+                values(gain, w);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) v[e] = v[e] * r * w[e];
+                if (rotates) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float v0 = v[first_of<INTER>(j)], v1 = v[second_of<INTER>(j)];
+                        v[first_of<INTER>(j)] = v0 * c[j] - v1 * sn[j];
+                        v[second_of<INTER>(j)] = v1 * c[j] + v0 * sn[j];
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) set2(x[k], i, v[2 * i], v[2 * i + 1]);
+            }
+            store_unit(x[k], to + e0, to + e1);
+        }
+    }
+}
+
+// Any hd up to 1024, rot, strides and alignment: a warp per head, which a lane reads twice.
+template <class T, bool INTER, bool APPEND>
+__global__ void __launch_bounds__(kThreads) qk_norm_any_kernel(const NormArgs a) {
+    pdl_wait();
+    pdl_trigger();
+    const int total = a.part[0].heads + a.part[1].heads + a.part[2].heads, lane = threadIdx.x & 31;
+    const long long g = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+    const long long row = g / total;
+    int h = (int)(g - row * total), part = 0;
+    if (row >= a.rows) return;
+    while (h >= a.part[part].heads) h -= a.part[part++].heads;
+    const Part& p = a.part[part];
+    long long pos = 0, slot = -1;
+    if (APPEND) {
+        if (!append_row(a.pg, a.rows_of, (int)row, pos, slot)) return;
+    } else if (a.positions) {
+        pos = a.positions[row];
+    }
+    const T* x = head_at<T>(p.x, row, p.x_row, h, p.x_head);
+    T* to = out_at<T, APPEND>(a, p, part, row, h, slot);
+    if (APPEND && !to) return;
+    float sum = 0.f;
+    for (int e = lane; e < a.hd; e += 32) sum = fmaf(to_f(x[e]), to_f(x[e]), sum);
+    const float r = inv_rms(warp_sum(sum), a.hd, a.eps);      // (every lane has read before any lane writes)
+    const T* gain = static_cast<const T*>(p.gain);
+    const int half = a.rot / 2;
+    if (APPEND && part == 2) {
+        for (int e = lane; e < a.hd; e += 32) to[e] = x[e];
+        return;
+    }
+    for (int j = lane; j < half; j += 32) {
+        const int i0 = INTER ? 2 * j : j, i1 = INTER ? 2 * j + 1 : half + j;
+        float c, s;
+        pair_turn(pos, a.phase[j], 1.f, a.magnitude, c, s);
+        const float z0 = to_f(x[i0]) * r * to_f(gain[i0]), z1 = to_f(x[i1]) * r * to_f(gain[i1]);
+        to[i0] = from_f<T>(z0 * c - z1 * s);
+        to[i1] = from_f<T>(z1 * c + z0 * s);
+    }
+    for (int e = a.rot + lane; e < a.hd; e += 32) to[e] = from_f<T>(to_f(x[e]) * r * to_f(gain[e]));
+}
+
+// Backward. A CTA has heads of one part and goes through rows a grid's width apart; every thread keeps the gain
+// gradients of its 16 elements, which the CTA adds up at the end in a fixed order and leaves in its row of `work`.
+template <class T, bool INTER>
+__global__ void __launch_bounds__(kThreads, 2) qk_norm_backward_kernel(const NormArgs a) {
+    constexpr int B = sizeof(T) == 2 ? 2 : 1;       // heads in flight
+    extern __shared__ float sums[];                 // [groups][hd]
+    pdl_wait();
+    pdl_trigger();
+    const int part = (int)blockIdx.x >= a.part[0].blocks;
+    const Part& p = a.part[part];
+    const int bid = blockIdx.x - (part ? a.part[0].blocks : 0), groups = kThreads / a.lanes;
+    const int u = threadIdx.x & (a.lanes - 1), group = threadIdx.x / a.lanes;
+    const bool mine = u < a.hd / 16, rotates = u < a.rot / 16;
+    const int e0 = rotates && !INTER ? u * 8 : u * 16, e1 = rotates && !INTER ? a.rot / 2 + u * 8 : u * 16 + 8;
+    Unit<T> gain{};
+    if (mine) load_unit(gain, static_cast<const T*>(p.gain) + e0, static_cast<const T*>(p.gain) + e1);
+    float acc[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+    const float inv_hd = 1.f / (float)a.hd;
+    const long long items = (long long)a.rows * p.slots;
+    for (long long base = (long long)bid * groups; base < items; base += (long long)p.blocks * groups) {
+        const long long item = base + group;
+        const long long row = item / p.slots;
+        const int s = (int)(item - row * p.slots);
+        const bool live = item < items && mine;
+        const long long pos = live && a.positions ? a.positions[row] : 0;
+        float c[8], sn[8];
+        for (int i0 = 0; i0 < a.per; i0 += B) {
+            Unit<T> x[B], d[B];
+#pragma unroll
+            for (int k = 0; k < B; ++k) {
+                const int h = s + (i0 + k) * p.slots;
+                x[k] = d[k] = Unit<T>{};
+                if (live && h < p.heads) {
+                    const T* from = head_at<T>(p.x, row, p.x_row, h, p.x_head);
+                    load_unit(x[k], from + e0, from + e1);
+                    from = head_at<T>(p.dy, row, p.dy_row, h, p.dy_head);
+                    load_unit(d[k], from + e0, from + e1);
+                }
+            }
+            if (i0 == 0 && rotates && live) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) pair_turn(pos, a.phase[u * 8 + j], 1.f, a.magnitude, c[j], sn[j]);
+            }
+#pragma unroll
+            for (int k = 0; k < B; ++k) {
+                const int h = s + (i0 + k) * p.slots;
+                float v[16], z[16], w[16];
+                values(x[k], v);
+                values(d[k], z);
+                values(gain, w);
+                if (rotates && live) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float z0 = z[first_of<INTER>(j)], z1 = z[second_of<INTER>(j)];
+                        z[first_of<INTER>(j)] = z0 * c[j] + z1 * sn[j];
+                        z[second_of<INTER>(j)] = z1 * c[j] - z0 * sn[j];
+                    }
+                }
+                float sq = 0.f, ax = 0.f;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    sq = fmaf(v[e], v[e], sq);
+                    ax = fmaf(z[e] * w[e], v[e], ax);
+                }
+                sq = head_sum(sq, a.lanes);
+                ax = head_sum(ax, a.lanes);
+                if (!live || h >= p.heads) continue;
+                const float r = inv_rms(sq, a.hd, a.eps), f = r * r * ax * inv_hd;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    acc[e] = fmaf(z[e], v[e] * r, acc[e]);
+                    v[e] = r * (z[e] * w[e] - v[e] * f);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) set2(x[k], i, v[2 * i], v[2 * i + 1]);
+                T* to = static_cast<T*>(p.out) + row * p.out_row + h * p.out_head;
+                store_unit(x[k], to + e0, to + e1);
+            }
+        }
+    }
+    if (mine) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sums[group * a.hd + (e < 8 ? e0 + e : e1 + e - 8)] = acc[e];
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.hd; e += kThreads) {
+        float v = 0.f;
+        for (int g = 0; g < groups; ++g) v += sums[g * a.hd + e];
+        a.work[(size_t)blockIdx.x * a.hd + e] = v;
+    }
+}
+
+// The same for any hd up to 1024, rot, strides and alignment: a warp per head, its gain gradients in shared memory (a
+// lane's elements are its own).
+template <class T, bool INTER>
+__global__ void __launch_bounds__(kThreads) qk_norm_backward_any_kernel(const NormArgs a) {
+    extern __shared__ float sums[];                 // [warps][hd]
+    pdl_wait();
+    pdl_trigger();
+    const int part = (int)blockIdx.x >= a.part[0].blocks;
+    const Part& p = a.part[part];
+    const int bid = blockIdx.x - (part ? a.part[0].blocks : 0), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    constexpr int warps = kThreads / 32;
+    float* acc = sums + warp * a.hd;
+    for (int e = lane; e < a.hd; e += 32) acc[e] = 0.f;
+    __syncwarp();
+    const T* gain = static_cast<const T*>(p.gain);
+    const int half = a.rot / 2;
+    const long long items = (long long)a.rows * p.heads;
+    for (long long item = (long long)bid * warps + warp; item < items; item += (long long)p.blocks * warps) {
+        const long long row = item / p.heads;
+        const int h = (int)(item - row * p.heads);
+        const T* x = head_at<T>(p.x, row, p.x_row, h, p.x_head);
+        const T* dy = head_at<T>(p.dy, row, p.dy_row, h, p.dy_head);
+        T* to = static_cast<T*>(p.out) + row * p.out_row + h * p.out_head;
+        const long long pos = a.positions ? a.positions[row] : 0;
+        auto turned = [&](int j, float& z0, float& z1, int& i0, int& i1) {      // pair j of dz
+            i0 = INTER ? 2 * j : j;
+            i1 = INTER ? 2 * j + 1 : half + j;
+            float c, s;
+            pair_turn(pos, a.phase[j], 1.f, a.magnitude, c, s);
+            const float d0 = to_f(dy[i0]), d1 = to_f(dy[i1]);
+            z0 = d0 * c + d1 * s;
+            z1 = d1 * c - d0 * s;
+        };
+        float sq = 0.f, ax = 0.f;
+        for (int j = lane; j < half; j += 32) {
+            float z0, z1;
+            int i0, i1;
+            turned(j, z0, z1, i0, i1);
+            const float x0 = to_f(x[i0]), x1 = to_f(x[i1]);
+            sq = fmaf(x0, x0, fmaf(x1, x1, sq));
+            ax = fmaf(z0 * to_f(gain[i0]), x0, fmaf(z1 * to_f(gain[i1]), x1, ax));
+        }
+        for (int e = a.rot + lane; e < a.hd; e += 32) {
+            const float v = to_f(x[e]);
+            sq = fmaf(v, v, sq);
+            ax = fmaf(to_f(dy[e]) * to_f(gain[e]), v, ax);
+        }
+        const float r = inv_rms(warp_sum(sq), a.hd, a.eps), f = r * r * warp_sum(ax) / (float)a.hd;
+        auto put = [&](int e, float z) {
+            const float v = to_f(x[e]);
+            acc[e] = fmaf(z, v * r, acc[e]);
+            to[e] = from_f<T>(r * (z * to_f(gain[e]) - v * f));
+        };
+        for (int j = lane; j < half; j += 32) {
+            float z0, z1;
+            int i0, i1;
+            turned(j, z0, z1, i0, i1);
+            put(i0, z0);
+            put(i1, z1);
+        }
+        for (int e = a.rot + lane; e < a.hd; e += 32) put(e, to_f(dy[e]));
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < a.hd; e += kThreads) {
+        float v = 0.f;
+        for (int g = 0; g < warps; ++g) v += sums[g * a.hd + e];
+        a.work[(size_t)blockIdx.x * a.hd + e] = v;
+    }
+}
+
+// The CTAs' sums of a part's gain gradients, in their order: 32 elements per CTA, eight warps of which each adds up
+// every eighth row.
+__global__ void __launch_bounds__(kThreads) qk_norm_gain_kernel(const NormArgs a) {
+    __shared__ float sums[kThreads / 32][32];
+    pdl_wait();
+    pdl_trigger();
+    const Part& p = a.part[blockIdx.y];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = blockIdx.x * 32 + lane;
+    const float* rows = a.work + (size_t)(blockIdx.y ? a.part[0].blocks : 0) * a.hd;
+    float v = 0.f;
+    if (e < a.hd) {
+#pragma unroll 8
+        for (int i = warp; i < p.blocks; i += kThreads / 32) v += rows[(size_t)i * a.hd + e];
+    }
+    sums[warp][lane] = v;
+    __syncthreads();
+    if (warp == 0 && e < a.hd) {
+        v = 0.f;
+        for (int w = 0; w < kThreads / 32; ++w) v += sums[w][lane];
+        p.dgain[e] = v;
+    }
+}
+
+dflare_status refuse(dflare_status st, const std::string& m) {
+    noalloc_set_error(m);
+    return st;
+}
+
+// Threads of a head, and heads of a part that a thread walks over: one while all threads still fit the GPU at once, up
+// to eight where rows are many and a cosine should serve several heads.
+void plan_threads(NormArgs& a, int num_sms) {
+    a.lanes = 1;
+    while (a.lanes < a.hd / 16) a.lanes *= 2;
+    int heads = 0;
+    for (const Part& p : a.part) heads += p.heads;
+    const long long fit = std::max<long long>(1, (long long)a.rows * heads * a.lanes / ((long long)num_sms * 2048));
+    const int walk = (int)std::min<long long>(fit, 8);
+    a.per = 1;
+    for (Part& p : a.part) {
+        p.slots = (p.heads + walk - 1) / walk;
+        if (p.slots) a.per = std::max(a.per, (p.heads + p.slots - 1) / p.slots);
+    }
+}
+
+template <class T, bool INTER, bool APPEND>
+cudaError_t launch_forward(NormArgs& a, bool vec, int num_sms, cudaStream_t s) {
+    plan_threads(a, num_sms);
+    if (vec) {
+        const long long threads = (long long)a.rows * (a.part[0].slots + a.part[1].slots + a.part[2].slots) * a.lanes;
+        return launch_kernel(true, qk_norm_kernel<T, INTER, APPEND>, dim3((unsigned)((threads + kThreads - 1) / kThreads)), dim3(kThreads), 0,
+                             s, a);
+    }
+    const long long warps = (long long)a.rows * (a.part[0].heads + a.part[1].heads + a.part[2].heads);
+    return launch_kernel(true, qk_norm_any_kernel<T, INTER, APPEND>, dim3((unsigned)((warps + kThreads / 32 - 1) / (kThreads / 32))),
+                         dim3(kThreads), 0, s, a);
+}
+template <bool APPEND>
+cudaError_t forward(NormArgs& a, int dtype, int layout, bool vec, int num_sms, cudaStream_t s) {
+    if (dtype == DFLARE_BF16)
+        return layout == DFLARE_ROPE_INTERLEAVED ? launch_forward<bf16, true, APPEND>(a, vec, num_sms, s)
+                                                 : launch_forward<bf16, false, APPEND>(a, vec, num_sms, s);
+    return layout == DFLARE_ROPE_INTERLEAVED ? launch_forward<float, true, APPEND>(a, vec, num_sms, s)
+                                             : launch_forward<float, false, APPEND>(a, vec, num_sms, s);
+}
+
+template <class T, bool INTER>
+cudaError_t launch_backward(NormArgs& a, bool vec, int num_sms, cudaStream_t s) {
+    plan_threads(a, num_sms);
+    const int groups = vec ? kThreads / a.lanes : kThreads / 32;
+    long long need[2];
+    for (int i = 0; i < 2; ++i) need[i] = ((long long)a.rows * (vec ? a.part[i].slots : a.part[i].heads) + groups - 1) / groups;
+    // CTAs that are resident at once, shared by the parts' heads; a part with heads has one at least
+    const long long most = std::min(2 * num_sms, kWorkRows), all = std::max<long long>(need[0] + need[1], 1);
+    const bool fits = all <= most;
+    for (int i = 0; i < 2; ++i)
+        a.part[i].blocks = (int)(fits ? need[i] : need[i] ? std::max<long long>(1, (most - 1) * need[i] / all) : 0);
+    const dim3 grid(a.part[0].blocks + a.part[1].blocks);
+    const size_t bytes = (size_t)groups * a.hd * sizeof(float);     // 16 KB at most; 32 KB for the other kernel
+    cudaError_t e = vec ? launch_kernel(true, qk_norm_backward_kernel<T, INTER>, grid, dim3(kThreads), bytes, s, a)
+                        : launch_kernel(true, qk_norm_backward_any_kernel<T, INTER>, grid, dim3(kThreads), bytes, s, a);
+    if (e != cudaSuccess) return e;
+    return launch_kernel(true, qk_norm_gain_kernel, dim3((a.hd + 31) / 32, a.part[1].heads ? 2 : 1), dim3(kThreads), 0, s, a);
+}
+
+// What both directions ask of their arguments; nullptr: nothing is wrong.
+const char* check_call(const dflare_qk_heads* q, const dflare_qk_heads* k, const int32_t* positions, const uint64_t* phase, int rows,
+                       int head_dim, int rot_dim, int layout, float magnitude, float eps, int dtype, bool backward) {
+    if (!q) return "NULL argument";
+    if (rot_dim && (!positions || !phase)) return "positions and phases go with a rotation";
+    if (rows < 1 || rows > (1 << 24) || head_dim < 2 || head_dim > 1024) return "rows must be in [1, 2^24], head_dim in [2, 1024]";
+    if (rot_dim < 0 || rot_dim > head_dim || rot_dim % 2) return "rot_dim must be even, in [0, head_dim]";
+    if (layout != DFLARE_ROPE_HALF && layout != DFLARE_ROPE_INTERLEAVED) return "unknown layout";
+    if (dtype != DFLARE_BF16 && dtype != DFLARE_F32) return "unknown dtype";
+    if (!std::isfinite(magnitude)) return "magnitude must be finite";
+    if (!(eps >= 0.f) || !std::isfinite(eps)) return "eps must be finite and not negative";
+    long long heads = 0;
+    for (const dflare_qk_heads* p : {q, k}) {
+        if (!p) continue;
+        if (p->heads < 1 || p->heads > 4096) return "heads must be in [1, 4096]";
+        if (!p->x || !p->out || !p->gain || (backward && (!p->dy || !p->dgain))) return "NULL argument";
+        if (p->x_row < 0 || p->x_head < 0 || p->out_row < 0 || p->out_head < 0 || (backward && (p->dy_row < 0 || p->dy_head < 0)) ||
+            (rows > 1 && p->out_row < head_dim) || (p->heads > 1 && p->out_head < head_dim))
+            return "strides must not be negative, nor overlap in out";
+        if (p->x == p->out && (p->x_row != p->out_row || p->x_head != p->out_head)) return "in place needs equal strides";
+        if (backward && p->dy == p->out && (p->dy_row != p->out_row || p->dy_head != p->out_head)) return "in place needs equal strides";
+        heads += p->heads;
+    }
+    if ((long long)rows * heads * 32 / kThreads > 0x7ffffff0LL) return "too many heads";
+    return nullptr;
+}
+
+Part part_of(const dflare_qk_heads* p) {
+    if (!p) return Part{};
+    return Part{p->x, p->x_row, p->x_head, p->dy, p->dy_row, p->dy_head, p->out, p->out_row, p->out_head, p->gain, p->dgain, p->heads, 0, 0};
+}
+bool part_vec(const Part& p, bool backward) {
+    if (!p.heads) return true;
+    return aligned16(p.x) && even8(p.x_row) && even8(p.x_head) && aligned16(p.out) && even8(p.out_row) && even8(p.out_head) && aligned16(p.gain) &&
+           (!backward || (aligned16(p.dy) && even8(p.dy_row) && even8(p.dy_head)));
+}
+bool dims_vec(int head_dim, int rot_dim) { return head_dim % 16 == 0 && head_dim <= 512 && rot_dim % 16 == 0; }
+
+}  // namespace
+}  // namespace dfl
+
+using namespace dfl;
+
+extern "C" {
+
+dflare_status dflare_qk_norm_rope(const dflare_qk_heads* q, const dflare_qk_heads* k, const int32_t* positions_dev,
+                                  const uint64_t* phase_dev, int rows, int head_dim, int rot_dim, int layout, float magnitude, float eps,
+                                  int dtype, void* stream) {
+    if (const char* m = check_call(q, k, positions_dev, phase_dev, rows, head_dim, rot_dim, layout, magnitude, eps, dtype, false))
+        return refuse(DFLARE_EINVAL, std::string("dflare_qk_norm_rope: ") + m);
+    NormArgs a{};
+    a.part[0] = part_of(q);
+    a.part[1] = part_of(k);
+    a.positions = positions_dev;
+    a.phase = phase_dev;
+    a.rows = rows;
+    a.hd = head_dim;
+    a.rot = rot_dim;
+    a.magnitude = magnitude;
+    a.eps = eps;
+    const bool vec = dims_vec(head_dim, rot_dim) && part_vec(a.part[0], false) && part_vec(a.part[1], false);
+    const cudaError_t e = forward<false>(a, dtype, layout, vec, std::max(sms_of_current_device(), 1), static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? DFLARE_OK : refuse(DFLARE_ECUDA, std::string("dflare_qk_norm_rope: ") + cudaGetErrorString(e));
+}
+
+dflare_status dflare_qk_norm_rope_backward(const dflare_qk_heads* q, const dflare_qk_heads* k, const int32_t* positions_dev,
+                                           const uint64_t* phase_dev, int rows, int head_dim, int rot_dim, int layout, float magnitude,
+                                           float eps, float* work_dev, int dtype, void* stream) {
+    const char* m = check_call(q, k, positions_dev, phase_dev, rows, head_dim, rot_dim, layout, magnitude, eps, dtype, true);
+    if (!m && !work_dev) m = "NULL argument";
+    if (m) return refuse(DFLARE_EINVAL, std::string("dflare_qk_norm_rope_backward: ") + m);
+    NormArgs a{};
+    a.part[0] = part_of(q);
+    a.part[1] = part_of(k);
+    a.positions = positions_dev;
+    a.phase = phase_dev;
+    a.work = work_dev;
+    a.rows = rows;
+    a.hd = head_dim;
+    a.rot = rot_dim;
+    a.magnitude = magnitude;
+    a.eps = eps;
+    const bool vec = dims_vec(head_dim, rot_dim) && part_vec(a.part[0], true) && part_vec(a.part[1], true);
+    const int sms = std::max(sms_of_current_device(), 1);
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const bool inter = layout == DFLARE_ROPE_INTERLEAVED;
+    const cudaError_t e = dtype == DFLARE_BF16 ? (inter ? launch_backward<bf16, true>(a, vec, sms, s) : launch_backward<bf16, false>(a, vec, sms, s))
+                                               : (inter ? launch_backward<float, true>(a, vec, sms, s) : launch_backward<float, false>(a, vec, sms, s));
+    return e == cudaSuccess ? DFLARE_OK : refuse(DFLARE_ECUDA, std::string("dflare_qk_norm_rope_backward: ") + cudaGetErrorString(e));
+}
+
+dflare_status dflare_cache_append_normed(dflare_cache* c, int layer, const void* q_dev, long long q_row, const void* k_dev,
+                                         long long k_row, const void* v_dev, long long v_row, void* q_out_dev, long long out_row,
+                                         const void* q_gain_dev, const void* k_gain_dev, float eps, const int32_t* depth_dev,
+                                         const int32_t* n_new_dev, int batch, int n_max, const uint64_t* phase_dev, int rot_dim, int layout,
+                                         float magnitude, void* stream) {
+    auto bad = [](const char* m) { return refuse(DFLARE_EINVAL, std::string("dflare_cache_append_normed: ") + m); };
+    if (!c || !k_dev || !v_dev || !n_new_dev || !k_gain_dev) return bad("NULL argument");
+    if (!q_dev != !q_out_dev) return bad("q and q_out go together");
+    if (q_dev && !q_gain_dev) return bad("queries need their gain");
+    const dflare_cache_config& g = c->cfg;
+    if (layer < 0 || layer >= g.n_layers) return bad("layer out of range");
+    if (batch < 1 || batch > g.max_batch) return bad("batch must be in [1, max_batch]");
+    if (n_max < 1 || n_max > (1 << 20)) return bad("n_max must be in [1, 2^20]");
+    if (rot_dim < 0 || rot_dim > g.head_dim || rot_dim % 2 || (rot_dim && !phase_dev))
+        return bad("rot_dim must be even, in [0, head_dim], with phases where it is not 0");
+    if (layout != DFLARE_ROPE_HALF && layout != DFLARE_ROPE_INTERLEAVED) return bad("unknown layout");
+    if (!std::isfinite(magnitude)) return bad("magnitude must be finite");
+    if (!(eps >= 0.f) || !std::isfinite(eps)) return bad("eps must be finite and not negative");
+    const long long kv = (long long)g.n_kv_heads * g.head_dim, qw = (long long)g.n_q_heads * g.head_dim;
+    if (k_row < kv || v_row < kv || (q_dev && (q_row < qw || out_row < qw))) return bad("a row stride is below a row's heads");
+    if (q_dev && q_dev == q_out_dev && q_row != out_row) return bad("in place needs equal strides");
+    const int hd = g.head_dim;
+    if ((long long)batch * n_max * ((q_dev ? g.n_q_heads : 0) + 2 * g.n_kv_heads) * 32 / kThreads > 0x7ffffff0LL) return bad("too many heads");
+    NormArgs a{};
+    if (q_dev) a.part[0] = Part{q_dev, q_row, hd, nullptr, 0, 0, q_out_dev, out_row, hd, q_gain_dev, nullptr, g.n_q_heads, 0, 0};
+    a.part[1] = Part{k_dev, k_row, hd, nullptr, 0, 0, nullptr, 0, 0, k_gain_dev, nullptr, g.n_kv_heads, 0, 0};
+    a.part[2] = Part{v_dev, v_row, hd, nullptr, 0, 0, nullptr, 0, 0, nullptr, nullptr, g.n_kv_heads, 0, 0};
+    a.phase = phase_dev;
+    a.rows = batch * n_max;
+    a.hd = hd;
+    a.rot = rot_dim;
+    a.magnitude = magnitude;
+    a.eps = eps;
+    a.pg = c->view;
+    a.rows_of = AppendRows{depth_dev, n_new_dev, layer, n_max};
+    const bool vec = rot_dim % 16 == 0 && part_vec(a.part[0], false) && part_vec(a.part[1], false) && part_vec(a.part[2], false);
+    DeviceGuard guard(c->device);
+    const cudaError_t e = forward<true>(a, g.dtype, layout, vec, c->num_sms, static_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? DFLARE_OK : refuse(DFLARE_ECUDA, std::string("dflare_cache_append_normed: ") + cudaGetErrorString(e));
+}
+
+}  // extern "C"

@@ -18,6 +18,7 @@
 
 #include "common.cuh"
 #include "paged.h"
+#include "rope.cuh"
 
 namespace dfl {
 namespace {
@@ -37,43 +38,16 @@ struct RopeArgs {
     float magnitude, sign;
     // dflare_cache_append
     PagesView pg;
-    const int32_t* depth;
-    const int32_t* n_new;
-    int layer, n_max;
+    AppendRows rows_of;
     int slots;                 // threads that share one row's unit
 };
-
-__device__ __forceinline__ void pair_turn(long long pos, uint64_t phase, float sign, float magnitude, float& c, float& s) {
-    // [-1/2, 1/2) turns; sincospi of twice that
-    const float turns = (float)(long long)((uint64_t)pos * phase) * 5.4210108624275222e-20f;
-    sincospif(2.0f * turns, &s, &c);
-    c *= magnitude;
-    s *= magnitude * sign;
-}
 
 // row -> position, and whether there is anything to do; slot: where its key and value go (-1: nowhere)
 template <bool APPEND>
 __device__ __forceinline__ bool row_of(const RopeArgs& a, int row, long long& pos, long long& slot) {
+    if (APPEND) return append_row(a.pg, a.rows_of, row, pos, slot);
     slot = -1;
-    if (!APPEND) {
-        pos = a.positions[row];
-        return true;
-    }
-    const int b = row / a.n_max, i = row - b * a.n_max;
-    if (i >= a.n_new[b]) return false;
-    const int len = a.pg.lens[b];
-    pos = (long long)len + (a.depth ? a.depth[row] : i);
-    const long long at = (long long)len + i;
-    const long long room = (long long)min(a.pg.held[b], a.pg.max_pages) * a.pg.ps;
-    uint32_t err = DFLARE_DEVERR_CAPACITY;
-    if (len >= 0 && at < room) {
-        const int page = a.pg.table[(size_t)b * a.pg.max_pages + at / a.pg.ps];
-        err = DFLARE_DEVERR_PAGE;
-        // the page that holds the last tokens may still be shared where no room was reserved: it is not written
-        if (page >= 0 && page < a.pg.pages && !(at / a.pg.ps == len / a.pg.ps && len % a.pg.ps && a.pg.refs[page] > 1))
-            slot = ((long long)a.layer * a.pg.pages + page) * a.pg.hkv * a.pg.ps + at % a.pg.ps;
-    }
-    if (slot < 0) atomicOr(a.pg.err, err);
+    pos = a.positions[row];
     return true;
 }
 
@@ -94,31 +68,6 @@ __device__ __forceinline__ bool place_of(const RopeArgs& a, int row, int h, long
     turn = !is_v;
     return slot >= 0;
 }
-
-// 16 elements of storage in two runs of eight, as loaded; and their values
-template <class T> struct Unit { uint4 v[sizeof(T)]; };      // bf16: one 16-byte piece per run, fp32: two
-template <class T>
-__device__ __forceinline__ void load_unit(Unit<T>& x, const T* p0, const T* p1) {
-    constexpr int H = sizeof(T) / 2;
-#pragma unroll
-    for (int i = 0; i < H; ++i) {
-        x.v[i] = reinterpret_cast<const uint4*>(p0)[i];
-        x.v[H + i] = reinterpret_cast<const uint4*>(p1)[i];
-    }
-}
-template <class T>
-__device__ __forceinline__ void store_unit(const Unit<T>& x, T* p0, T* p1) {
-    constexpr int H = sizeof(T) / 2;
-#pragma unroll
-    for (int i = 0; i < H; ++i) {
-        reinterpret_cast<uint4*>(p0)[i] = x.v[i];
-        reinterpret_cast<uint4*>(p1)[i] = x.v[H + i];
-    }
-}
-__device__ __forceinline__ float2 get2(const Unit<bf16>& x, int i) { return __bfloat1622float2(reinterpret_cast<const __nv_bfloat162*>(x.v)[i]); }
-__device__ __forceinline__ float2 get2(const Unit<float>& x, int i) { return reinterpret_cast<const float2*>(x.v)[i]; }
-__device__ __forceinline__ void set2(Unit<bf16>& x, int i, float a, float b) { reinterpret_cast<__nv_bfloat162*>(x.v)[i] = __floats2bfloat162_rn(a, b); }
-__device__ __forceinline__ void set2(Unit<float>& x, int i, float a, float b) { reinterpret_cast<float2*>(x.v)[i] = make_float2(a, b); }
 
 // Vector form: rot and hd multiples of 16, everything 16-byte aligned. A thread's first heads are on their way
 // before it works out its cosines, and stay as they were stored until they are turned.
@@ -248,20 +197,6 @@ cudaError_t launch_rope(RopeArgs& a, int dtype, int layout, bool vec, int num_sm
                                              : launch_typed<float, false, APPEND>(a, vec, num_sms, s);
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-// elements that keep 16-byte alignment for either type
-bool even8(long long n) { return n % 8 == 0; }
-
-int sms_of_current_device() {
-    static std::atomic<int> known[64];
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
-    int n = known[dev & 63].load(std::memory_order_relaxed);
-    if (n == 0 && cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess)
-        known[dev & 63].store(n, std::memory_order_relaxed);
-    return n;
-}
-
 }  // namespace
 }  // namespace dfl
 
@@ -380,10 +315,7 @@ dflare_status dflare_cache_append(dflare_cache* c, int layer, const void* q_dev,
     a.magnitude = magnitude;
     a.sign = 1.f;
     a.pg = c->view;
-    a.depth = depth_dev;
-    a.n_new = n_new_dev;
-    a.layer = layer;
-    a.n_max = n_max;
+    a.rows_of = AppendRows{depth_dev, n_new_dev, layer, n_max};
     DeviceGuard guard(c->device);
     const bool vec = rot_dim % 16 == 0 && aligned16(k_dev) && aligned16(v_dev) && even8(k_row) && even8(v_row) &&
                      (!q_dev || (aligned16(q_dev) && aligned16(q_out_dev) && even8(q_row) && even8(out_row)));
