@@ -112,6 +112,7 @@ typedef enum { DFLARE_BF16 = 0, DFLARE_F32 = 1 } dflare_dtype;
 #define DFLARE_DEVERR_PAGE      0x8u    /* a sequence or page number out of range, a fork into a sequence
                                            that holds pages, or a page table that contradicts itself */
 #define DFLARE_DEVERR_TREE      0x10u   /* a node count, parent, accepted length or path that no tree has */
+#define DFLARE_DEVERR_PLAN      0x20u   /* dflare_cache_attend_shared: the workspace holds no plan for the call's sizes */
 
 typedef struct {
     int d;                /* hidden size; multiple of 64 */
@@ -641,9 +642,9 @@ dflare_status dflare_tree_accept(const int32_t* tokens_dev, const int32_t* paren
  * sum; of p, where that sum is not above 0. So every token has the target's distribution, whatever the draft.
  *   tokens_dev, parents_dev, n_nodes_dev, accept_len_dev, path_dev, next_token_dev, err_dev  as in dflare_tree_accept.
  *   target_dev  [batch][n_max][vocab] fp32: the target's probabilities after each node.
- *   draft_dev   [batch][draft_rows][vocab] fp32, draft_rows at least n_max - 1 (the last node has no children): the
- *               distributions that the children of each node were drawn from; with replacement (distinct = 0), or without
- *               (distinct = 1, siblings' tokens differ). NULL: drafts were picked, not drawn; with W = 1 before the first,
+ *   draft_dev   [batch][draft_rows][vocab] fp32, draft_rows at least n_max - 1 (the last node has no children; only the first
+ *               n_max - 1 rows are read): the distributions that the children of each node were drawn from; with replacement
+ *               (distinct = 0), or without (distinct = 1, siblings' tokens differ). NULL: drafts were picked, not drawn; with W = 1 before the first,
  *               child i is kept where u[i] W < p[x] (0 if a sibling before had the same token), otherwise W loses p[x]; the next
  *               token is drawn from p without the children's tokens.
  *   u_dev       [batch][n_max] fp32, uniform in [0, 1); other values count as the nearest number of that range, NaN as 0.

@@ -14,7 +14,7 @@ from ._lib import (  # noqa: F401
     DFlareError, DFLARE_BF16, DFLARE_F32, FLAG_NO_BLOCK_ROPE, FLAG_RAW_FUSION, FLAG_SIMT_GEMM,
     FLAG_SERIAL_LAUNCH, FLAG_SHARED_KV, FLAG_FUSION_FC, FLAG_DFLASH_FC, FLAG_DETERMINISTIC,
     FLAG_MMA_SYNC_ATTENTION,
-    DEVERR_TOKEN, DEVERR_CAPACITY, DEVERR_TIMEOUT, DEVERR_PAGE, DEVERR_TREE, EXPORTS, WEIGHT_FIELDS,
+    DEVERR_TOKEN, DEVERR_CAPACITY, DEVERR_TIMEOUT, DEVERR_PAGE, DEVERR_TREE, DEVERR_PLAN, EXPORTS, WEIGHT_FIELDS,
     NOALLOC_MAX_ROWS, load,
 )
 
@@ -259,7 +259,8 @@ def synthetic_target(draft_tokens, u, r, last, step, threshold, batch, block, ta
 
 # The paged cache's binding works with torch at module level, so it is imported when one of its names is first asked for
 # (importing the package alone, as a build does, does not load torch).
-_PAGED = ("PagedCache", "rope", "rope_phases", "tree_accept", "tree_plan")
+_PAGED = ("PagedCache", "qk_norm_rope", "qk_norm_rope_backward", "qk_norm_rope_work", "rope", "rope_phases", "tree_accept",
+          "tree_plan", "tree_sample")
 
 
 def __getattr__(name):

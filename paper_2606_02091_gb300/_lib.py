@@ -25,7 +25,7 @@ FLAG_FUSION_FC = 0x20
 FLAG_DFLASH_FC = 0x40
 FLAG_DETERMINISTIC = 0x80
 FLAG_MMA_SYNC_ATTENTION = 0x100
-DEVERR_TOKEN, DEVERR_CAPACITY, DEVERR_TIMEOUT, DEVERR_PAGE, DEVERR_TREE = 0x1, 0x2, 0x4, 0x8, 0x10
+DEVERR_TOKEN, DEVERR_CAPACITY, DEVERR_TIMEOUT, DEVERR_PAGE, DEVERR_TREE, DEVERR_PLAN = 0x1, 0x2, 0x4, 0x8, 0x10, 0x20
 ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 
@@ -42,9 +42,11 @@ EXPORTS = ("dflare_create", "dflare_destroy", "dflare_set_weights", "dflare_rese
            "dflare_argmax_noalloc", "dflare_rope_phases", "dflare_rope", "dflare_cache_create",
            "dflare_cache_destroy", "dflare_cache_error", "dflare_cache_reserve", "dflare_cache_append",
            "dflare_cache_attend", "dflare_cache_commit", "dflare_cache_truncate", "dflare_cache_fork",
-           "dflare_cache_copy_pages", "dflare_tree_plan", "dflare_tree_accept")
+           "dflare_cache_copy_pages", "dflare_tree_plan", "dflare_tree_accept", "dflare_qk_norm_rope",
+           "dflare_qk_norm_rope_backward", "dflare_cache_append_normed", "dflare_tree_sample")
 
 NOALLOC_MAX_ROWS = 4096
+QK_NORM_WORK_ROWS = 1024
 
 TRACE_FN = ctypes.CFUNCTYPE(None, ctypes.c_void_p, ctypes.c_char_p, ctypes.c_int, ctypes.c_void_p)
 
@@ -72,6 +74,13 @@ class RopeConfig(ctypes.Structure):
     _fields_ = [("rot_dim", ctypes.c_int), ("scaling", ctypes.c_int), ("theta", ctypes.c_double),
                 ("factor", ctypes.c_double), ("trained", ctypes.c_double),
                 ("beta_fast", ctypes.c_double), ("beta_slow", ctypes.c_double)]
+
+
+class QkHeads(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("x_row", ctypes.c_longlong), ("x_head", ctypes.c_longlong),
+                ("dy", ctypes.c_void_p), ("dy_row", ctypes.c_longlong), ("dy_head", ctypes.c_longlong),
+                ("out", ctypes.c_void_p), ("out_row", ctypes.c_longlong), ("out_head", ctypes.c_longlong),
+                ("gain", ctypes.c_void_p), ("dgain", ctypes.c_void_p), ("heads", ctypes.c_int)]
 
 
 class CacheConfig(ctypes.Structure):
@@ -125,11 +134,15 @@ def load():
         "dflare_argmax_noalloc": [vp, i32, i32, vp, vp],
         "dflare_rope_phases": [P(RopeConfig), vp, P(f32)],
         "dflare_rope": [vp, i64, i64, vp, i64, i64, vp, vp, i32, i32, i32, i32, i32, f32, i32, i32, vp],
+        "dflare_qk_norm_rope": [P(QkHeads), P(QkHeads), vp, vp, i32, i32, i32, i32, f32, f32, i32, vp],
+        "dflare_qk_norm_rope_backward": [P(QkHeads), P(QkHeads), vp, vp, i32, i32, i32, i32, f32, f32, vp, i32, vp],
+        "dflare_tree_sample": [vp, vp, vp, vp, vp, i32, vp, i32, i32, i32, i32, vp, vp, vp, vp, vp],
         "dflare_cache_create": [P(CacheConfig), P(CacheBuffers), P(vp)],
         "dflare_cache_destroy": [vp],
         "dflare_cache_error": [vp, P(u32), vp],
         "dflare_cache_reserve": [vp, vp, i32, vp],
         "dflare_cache_append": [vp, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, i32, i32, vp, i32, i32, f32, vp],
+        "dflare_cache_append_normed": [vp, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, f32, vp, vp, i32, i32, vp, i32, i32, f32, vp],
         "dflare_cache_attend": [vp, i32, vp, i64, vp, vp, i32, i32, f32, vp, vp, vp],
         "dflare_cache_commit": [vp, vp, vp, i32, i32, vp],
         "dflare_cache_truncate": [vp, vp, i32, vp],

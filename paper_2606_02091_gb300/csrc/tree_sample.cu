@@ -1,0 +1,421 @@
+// Sampled acceptance in drafted trees: the target's probabilities p and the drafter's q decide, by given random numbers,
+// which drafted child of a node is kept, and what follows where none is.
+//
+// At a node the walk holds a residual w = max(0, p - F q) with F = 0, its sum W = 1, and the mass Q = 1 that the drafter's
+// next draw is from. Child i with token x is kept where u_i (q_x / Q) W < w_x. If it is not, the residual loses the
+// drafter's share: w <- max(0, w - (W / Q) q). As q and the shares are not negative, clamping after every step is clamping
+// once, so F <- F + W / Q says it all, and only W = sum w needs another look at the rows. Drawn without replacement,
+// Q <- Q - q_x. Where no child is left, the next token is the first whose running sum of w exceeds u_0 sum w.
+// Drafts that were picked and not drawn (no q) have the residual p without the picked tokens before.
+//
+// Decisions hang on sums over the vocabulary: fp32 sums of 150000 terms would move them for one call in a hundred.
+// They are held as pairs of fp32 numbers (Knuth's two-sum, products by a fused multiply-add: 2^-46), as 64-bit
+// arithmetic has 1/64 of the fp32 rate on this GPU.
+//
+// A cluster of CTAs per tree, each with a part of the vocabulary; all of them walk the same tree in step. What a walk asks
+// of a node whose children before it were not asked (u q_x < p_x) is found for all nodes at once while their numbers come
+// in. A residual's sum is one pass over the rows by the whole cluster; its parts meet through distributed shared memory.
+#include <math.h>
+
+#include <algorithm>
+#include <string>
+
+#include "common.cuh"
+#include "paged.h"
+
+namespace dfl {
+namespace {
+
+constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kMaxCluster = 16;
+
+struct SampleArgs {
+    const int32_t* tokens;
+    const int32_t* parents;
+    const int32_t* n_nodes;
+    const float* target;        // [batch][n_max][vocab]
+    const float* draft;         // [batch][draft_rows][vocab], or null
+    const float* u;             // [batch][n_max]
+    int32_t* accept_len;
+    int32_t* path;
+    int32_t* next_token;
+    uint32_t* err;
+    int n_max, draft_rows, vocab, distinct;
+    int part;                   // elements of a warp, a multiple of 4
+};
+
+// A sum as two fp32 numbers. `l` takes up what `h` could not hold.
+struct Sum {
+    float h, l;
+};
+__device__ __forceinline__ void add(Sum& s, float x, float low) {
+    const float t = __fadd_rn(s.h, x), b = __fsub_rn(t, s.h);
+    s.l = __fadd_rn(s.l, __fadd_rn(__fadd_rn(__fsub_rn(s.h, __fsub_rn(t, b)), __fsub_rn(x, b)), low));
+    s.h = t;
+}
+__device__ __forceinline__ Sum shuffled(const Sum& s, int o) { return {__shfl_xor_sync(0xffffffffu, s.h, o), __shfl_xor_sync(0xffffffffu, s.l, o)}; }
+__device__ __forceinline__ Sum warp_total(Sum s) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const Sum x = shuffled(s, o);
+        // (the lower lane's first: both lanes have the same bits)
+        Sum a = threadIdx.x & o ? x : s, b = threadIdx.x & o ? s : x;
+        add(a, b.h, b.l);
+        s = a;
+    }
+    return s;
+}
+// inclusive sums over the lanes
+__device__ __forceinline__ Sum warp_upto(Sum s) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        Sum x = {__shfl_up_sync(0xffffffffu, s.h, o), __shfl_up_sync(0xffffffffu, s.l, o)};
+        if ((threadIdx.x & 31) >= o) {
+            add(x, s.h, s.l);
+            s = x;
+        }
+    }
+    return s;
+}
+__device__ __forceinline__ double value(const Sum& s) { return (double)s.h + (double)s.l; }
+
+// The residual that the cluster sums up: of node `at`; F as two numbers; gone: picked tokens that are out of it.
+struct Residual {
+    const float* p;
+    const float* q;             // null: F = 0
+    float fh, fl;
+    const int32_t* gone;
+    int n_gone;
+};
+// w = max(0, p - F q) as two numbers added to s; not finite or negative: nothing
+__device__ __forceinline__ void add_weight(Sum& s, const Residual& r, float p, float q) {
+    const float ph = __fmul_rn(r.fh, q), pl = __fmaf_rn(r.fl, q, __fmaf_rn(r.fh, q, -ph));
+    const float d = __fsub_rn(p, ph), b = __fsub_rn(d, p);
+    const float low = __fsub_rn(__fsub_rn(__fsub_rn(p, __fsub_rn(d, b)), __fadd_rn(ph, b)), pl);
+    if (__fadd_rn(d, low) > 0.f) add(s, d, low);
+}
+__device__ __forceinline__ bool is_gone(const Residual& r, int e) {
+    for (int g = 0; g < r.n_gone; ++g)
+        if (r.gone[g] == e) return true;
+    return false;
+}
+// The sum of the calling warp over elements [e0, e1). vec: the rows are 16-byte aligned, and e0 a multiple of 4.
+__device__ __forceinline__ Sum part_sum(const Residual& r, int e0, int e1, bool vec) {
+    constexpr int U = 4;
+    const int lane = threadIdx.x & 31;
+    Sum s[U] = {};
+    bool drops = false;
+    for (int g = lane; g < r.n_gone; g += 32) drops |= r.gone[g] >= e0 && r.gone[g] < e1;
+    drops = __any_sync(0xffffffffu, drops);
+    if (vec && !drops) {
+        for (int e = e0 + lane * 4; e < e1; e += U * 128) {
+            float4 p[U], q[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                // (a row's end is a multiple of 4 where rows are aligned)
+                const bool there = e + k * 128 < e1;
+                p[k] = there ? __ldg(reinterpret_cast<const float4*>(r.p + e + k * 128)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                q[k] = there && r.q ? __ldg(reinterpret_cast<const float4*>(r.q + e + k * 128)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                add_weight(s[k], r, p[k].x, q[k].x);
+                add_weight(s[k], r, p[k].y, q[k].y);
+                add_weight(s[k], r, p[k].z, q[k].z);
+                add_weight(s[k], r, p[k].w, q[k].w);
+            }
+        }
+    } else {
+        constexpr int N = 8;
+        for (int e = e0 + lane; e < e1; e += N * 32) {
+            float p[N], q[N];
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const bool there = e + k * 32 < e1;
+                p[k] = there ? __ldg(r.p + e + k * 32) : 0.f;
+                q[k] = there && r.q ? __ldg(r.q + e + k * 32) : 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+                if (!drops || !is_gone(r, e + k * 32)) add_weight(s[k % U], r, p[k], q[k]);
+        }
+    }
+#pragma unroll
+    for (int k = 1; k < U; ++k) add(s[0], s[k].h, s[k].l);
+    return warp_total(s[0]);
+}
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// the Sum at address `p` of this CTA's shared memory, as CTA `rank` of the cluster has it
+__device__ __forceinline__ Sum sum_of(const Sum* p, uint32_t rank) {
+    uint32_t at;
+    Sum s;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(s.h), "=f"(s.l) : "r"(at) : "memory");
+    return s;
+}
+
+enum { kSum, kLast, kNone };    // what warp 0 asks of the CTA: a residual's sum; the last one, with the token; nothing more
+
+__global__ void __launch_bounds__(kThreads, 2) tree_sample_kernel(const SampleArgs a) {
+    __shared__ int32_t up[kMaxNodes], tok[kMaxNodes], first[kMaxNodes], list[kMaxNodes];
+    __shared__ float u[kMaxNodes], px[kMaxNodes], qx[kMaxNodes];
+    __shared__ Sum of_warp[2][kWarps];
+    __shared__ __align__(8) Sum of_cta[2];
+    __shared__ Residual todo;
+    __shared__ int what, steps;
+    pdl_wait();
+    pdl_trigger();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t rank = cluster_rank(), ctas = cluster_size();
+    const int b = blockIdx.x / ctas;
+    const int told = a.n_nodes[b], n = min(max(told, 0), a.n_max);
+    const float* target = a.target + (size_t)b * a.n_max * a.vocab;
+    const float* draft = a.draft ? a.draft + (size_t)b * a.draft_rows * a.vocab : nullptr;
+    bool bad = told != n, odd = false;
+    for (int i = tid; i < n; i += kThreads) first[i] = n;
+    __syncthreads();
+    for (int i = tid; i < n; i += kThreads) {
+        int p = a.parents[(size_t)b * a.n_max + i];
+        if (i == 0 ? p != -1 : (p < -1 || p >= i)) {
+            bad = true;
+            p = -1;
+        }
+        const int x = a.tokens[(size_t)b * a.n_max + i];
+        const float r = a.u[(size_t)b * a.n_max + i];
+        const bool in = x >= 0 && x < a.vocab;
+        odd |= i > 0 && !in;
+        up[i] = p;
+        tok[i] = in ? x : -1;
+        u[i] = r > 0.f ? fminf(r, 0x1.fffffep-1f) : 0.f;
+        px[i] = p >= 0 && in ? target[(size_t)p * a.vocab + x] : 0.f;
+        qx[i] = p >= 0 && in && draft ? draft[(size_t)p * a.vocab + x] : 0.f;
+        if (p >= 0) atomicMin(&first[p], i);
+    }
+    if (bad && rank == 0 && a.err) atomicOr(a.err, DFLARE_DEVERR_TREE);
+    if (odd && rank == 0 && a.err) atomicOr(a.err, DFLARE_DEVERR_TOKEN);
+    if (n == 0) {       // (the same in every CTA of the cluster)
+        if (rank == 0) {
+            if (tid == 0) {
+                a.accept_len[b] = 0;
+                a.next_token[b] = -1;
+            }
+            for (int i = tid; i < a.n_max; i += kThreads) a.path[(size_t)b * a.n_max + i] = -1;
+        }
+        return;
+    }
+    __syncthreads();
+
+    // ---------------- warp 0 walks; the others sum what it asks for. Every CTA of the cluster finds the same.
+    int at = 0, i = first[0], walked = 1, turn = 0;
+    double F = 0.0, W = 1.0, Q = 1.0;
+    bool again = false;         // the last residual was empty: p instead
+    if (tid == 0 && rank == 0) a.path[(size_t)b * a.n_max] = 0;
+    for (;; ++turn) {
+        if (warp == 0) {
+            int ask = again ? kLast : kNone;
+            while (ask == kNone) {
+                if (i >= n) {
+                    ask = kLast;
+                    break;
+                }
+                bool keep;
+                double w = 0.0;
+                if (i == first[at]) {
+                    // u q < p, or u < p where drafts were picked: the sign of an fp32 fused product is exact
+                    keep = draft ? fmaf(u[i], qx[i], -px[i]) < 0.f : u[i] < px[i];
+                    w = px[i];
+                } else if (draft) {
+                    const double share = Q > 0.0 ? (double)qx[i] / Q : 0.0;
+                    keep = (double)u[i] * share * W < fmax((double)px[i] - F * (double)qx[i], 0.0);
+                } else {
+                    bool before = false;        // the same token was picked before
+                    for (int j = at + 1 + lane; j < i; j += 32) before |= up[j] == at && tok[j] == tok[i];
+                    w = __any_sync(0xffffffffu, before) ? 0.0 : (double)px[i];
+                    keep = (double)u[i] * W < w;
+                }
+                if (keep) {
+                    at = i;
+                    i = first[at];
+                    if (lane == 0 && rank == 0) a.path[(size_t)b * a.n_max + walked] = at;
+                    ++walked;
+                    F = 0.0;
+                    W = Q = 1.0;
+                    continue;
+                }
+                int j = n;      // the next child
+                for (int j0 = i + 1; j0 < n && j == n; j0 += 32) {
+                    const unsigned hit = __ballot_sync(0xffffffffu, j0 + lane < n && up[j0 + lane] == at);
+                    if (hit) j = j0 + __ffs(hit) - 1;
+                }
+                if (draft) {
+                    if (Q > 0.0) F += W / Q;
+                    if (a.distinct) Q -= (double)qx[i];
+                    if (j < n) ask = kSum;
+                } else {
+                    W -= w;
+                }
+                i = j;
+            }
+            int gone = 0;
+            if (!draft && ask == kLast && !again && first[at] < n) {        // the picked tokens
+                for (int j0 = at + 1; j0 < n; j0 += 32) {
+                    const bool mine = j0 + lane < n && up[j0 + lane] == at;
+                    const unsigned hit = __ballot_sync(0xffffffffu, mine);
+                    if (mine) list[gone + __popc(hit & ((1u << lane) - 1u))] = tok[j0 + lane];
+                    gone += __popc(hit);
+                }
+            }
+            if (lane == 0) {
+                const bool less = draft && F > 0.0 && !again;
+                const double f = fmin(F, 3e38);
+                todo.p = target + (size_t)at * a.vocab;
+                todo.q = less ? draft + (size_t)at * a.vocab : nullptr;
+                todo.fh = less ? (float)f : 0.f;
+                todo.fl = less ? (float)(f - (double)(float)f) : 0.f;
+                todo.gone = list;
+                todo.n_gone = gone;
+                what = ask;
+                steps = walked;
+            }
+        }
+        __syncthreads();
+        const Residual r = todo;
+        const bool last = what == kLast;
+        const bool vec = a.vocab % 4 == 0 && ((reinterpret_cast<uintptr_t>(r.p) | reinterpret_cast<uintptr_t>(r.q)) & 15u) == 0;
+        const long long from = ((long long)rank * kWarps + warp) * a.part;
+        const int e0 = (int)min(from, (long long)a.vocab), e1 = (int)min(from + a.part, (long long)a.vocab);
+        const Sum mine = part_sum(r, e0, e1, vec);
+        if (lane == 0) of_warp[turn & 1][warp] = mine;
+        __syncthreads();
+        if (warp == 0) {
+            const Sum s = warp_total(lane < kWarps ? of_warp[turn & 1][lane] : Sum{0.f, 0.f});
+            if (lane == 0) of_cta[turn & 1] = s;
+        }
+        cluster_arrive();
+        cluster_wait();
+        bool done = false;
+        if (warp == 0) {
+            const Sum part = lane < (int)ctas ? sum_of(&of_cta[turn & 1], lane) : Sum{0.f, 0.f};
+            const Sum upto = warp_upto(part);
+            const Sum all = {__shfl_sync(0xffffffffu, upto.h, 31), __shfl_sync(0xffffffffu, upto.l, 31)};
+            W = value(all);
+            if (last) {
+                if (!(W > 0.0) && !again && (r.q || r.n_gone)) {
+                    again = true;
+                } else {
+                    done = true;
+                    // the CTA, the warp of it, the lane's elements of that, and the element at which the running sum passes
+                    const double goal = (double)u[0] * W;
+                    unsigned past = __ballot_sync(0xffffffffu, lane < (int)ctas && value(upto) > goal);
+                    const int cta = past ? __ffs(past) - 1 : -1;
+                    if (cta < 0 && rank == 0) {         // no weight at all
+                        if (lane == 0) {
+                            a.next_token[b] = 0;
+                            if (a.err) atomicOr(a.err, DFLARE_DEVERR_TOKEN);
+                        }
+                    } else if (cta == (int)rank) {
+                        Sum base = {0.f, 0.f};
+                        const Sum before = {__shfl_sync(0xffffffffu, upto.h, max(cta - 1, 0)), __shfl_sync(0xffffffffu, upto.l, max(cta - 1, 0))};
+                        if (cta) base = before;
+                        const Sum ws = warp_upto(lane < kWarps ? of_warp[turn & 1][lane] : Sum{0.f, 0.f});
+                        Sum x = base;
+                        add(x, ws.h, ws.l);
+                        past = __ballot_sync(0xffffffffu, lane < kWarps && value(x) > goal);
+                        // (rounding: the last warp with any weight)
+                        const unsigned some = __ballot_sync(0xffffffffu, lane < kWarps && of_warp[turn & 1][min(lane, kWarps - 1)].h > 0.f);
+                        const int w = past ? __ffs(past) - 1 : 31 - __clz(some);
+                        const Sum wb = {__shfl_sync(0xffffffffu, x.h, max(w - 1, 0)), __shfl_sync(0xffffffffu, x.l, max(w - 1, 0))};
+                        if (w) base = wb;
+                        const long long f0 = ((long long)rank * kWarps + w) * a.part;
+                        const int s0 = (int)min(f0, (long long)a.vocab), s1 = (int)min(f0 + a.part, (long long)a.vocab);
+                        const int each = (s1 - s0 + 31) / 32, l0 = min(s0 + lane * each, s1), l1 = min(l0 + each, s1);
+                        auto weigh = [&](Sum& s, int e) {
+                            if (!is_gone(r, e)) add_weight(s, r, __ldg(r.p + e), r.q ? __ldg(r.q + e) : 0.f);
+                        };
+                        Sum own = {0.f, 0.f};
+#pragma unroll 8
+                        for (int e = l0; e < l1; ++e) weigh(own, e);
+                        const Sum lanes = warp_upto(own);
+                        x = base;
+                        add(x, lanes.h, lanes.l);
+                        past = __ballot_sync(0xffffffffu, value(x) > goal);
+                        const unsigned any = __ballot_sync(0xffffffffu, own.h > 0.f);
+                        const int l = past ? __ffs(past) - 1 : 31 - __clz(any);
+                        const Sum lb = {__shfl_sync(0xffffffffu, x.h, max(l - 1, 0)), __shfl_sync(0xffffffffu, x.l, max(l - 1, 0))};
+                        if (lane == l) {
+                            Sum s = l ? lb : base;
+                            int token = 0;
+                            for (int e = l0; e < l1; ++e) {
+                                Sum before = s;
+                                weigh(s, e);
+                                if (s.h != before.h || s.l != before.l) token = e;
+                                if (value(s) > goal) break;
+                            }
+                            a.next_token[b] = token;
+                        }
+                    }
+                }
+            }
+            if (lane == 0) what = done;
+        }
+        __syncthreads();
+        if (last && what) break;
+        __syncthreads();
+    }
+    if (rank == 0) {
+        if (tid == 0) a.accept_len[b] = steps;
+        for (int x = steps + tid; x < a.n_max; x += kThreads) a.path[(size_t)b * a.n_max + x] = -1;
+    }
+    // no CTA ends while another may still read its sums
+    cluster_arrive();
+    cluster_wait();
+}
+
+dflare_status refuse(dflare_status st, const std::string& m) {
+    noalloc_set_error(m);
+    return st;
+}
+
+}  // namespace
+}  // namespace dfl
+
+using namespace dfl;
+
+extern "C" dflare_status dflare_tree_sample(const int32_t* tokens_dev, const int32_t* parents_dev, const int32_t* n_nodes_dev,
+                                            const float* target_dev, const float* draft_dev, int draft_rows, const float* u_dev,
+                                            int batch, int n_max, int vocab, int distinct, int32_t* accept_len_dev, int32_t* path_dev,
+                                            int32_t* next_token_dev, uint32_t* err_dev, void* stream) {
+    auto bad = [](const char* m) { return refuse(DFLARE_EINVAL, std::string("dflare_tree_sample: ") + m); };
+    if (!tokens_dev || !parents_dev || !n_nodes_dev || !target_dev || !u_dev || !accept_len_dev || !path_dev || !next_token_dev)
+        return bad("NULL argument");
+    if (batch < 1 || batch > 65535 || n_max < 1 || n_max > kMaxNodes) return bad("batch must be in [1, 65535], n_max in [1, 1024]");
+    if (vocab < 1 || vocab > (1 << 28)) return bad("vocab must be in [1, 2^28]");
+    if (draft_dev && draft_rows < n_max - 1) return bad("every node but the last needs a row of the draft's probabilities");
+    if (distinct != 0 && distinct != 1) return bad("distinct must be 0 or 1");
+    static PerDeviceOnce once;
+    cudaError_t e = once([] { return cudaFuncSetAttribute(tree_sample_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1); });
+    int dev = 0, sms = 0;
+    if (e == cudaSuccess) e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return refuse(DFLARE_ECUDA, std::string("dflare_tree_sample: ") + cudaGetErrorString(e));
+    // as many CTAs per tree as the GPU holds at once, none with less than a load per thread
+    int ctas = kMaxCluster;
+    while (ctas > 1 && ((long long)batch * ctas > 2LL * sms || (long long)vocab < (long long)ctas * kThreads * 4)) ctas /= 2;
+    SampleArgs a{tokens_dev, parents_dev, n_nodes_dev, target_dev, draft_dev, u_dev, accept_len_dev, path_dev, next_token_dev, err_dev,
+                 n_max, draft_rows, vocab, distinct, 0};
+    a.part = ((vocab + ctas * kWarps - 1) / (ctas * kWarps) + 3) / 4 * 4;
+    e = launch_cluster(true, ctas, tree_sample_kernel, dim3((unsigned)(batch * ctas)), dim3(kThreads), 0, static_cast<cudaStream_t>(stream), a);
+    return e == cudaSuccess ? DFLARE_OK : refuse(DFLARE_ECUDA, std::string("dflare_tree_sample: ") + cudaGetErrorString(e));
+}

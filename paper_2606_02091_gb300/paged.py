@@ -138,6 +138,83 @@ def rope(x, positions, phase, out, *, layout="half", magnitude=1.0, backward=Fal
                                    _lib.DFLARE_BF16 if dtype is _BF16 else _lib.DFLARE_F32, _stream(stream, dev)))
 
 
+def _qk_part(name, x, dy, out, gain, dgain, rows, hd, dtype, device):
+    """The struct of one call's queries or keys: [rows][heads][head_dim] tensors and their gain."""
+    g = _lib.QkHeads()
+    if x.dim() != 3 or x.shape[0] != rows or x.shape[2] != hd:
+        raise ValueError(f"{name} must be [{rows}][heads][{hd}], got {list(x.shape)}")
+    for field, t in (("x", x), ("out", out), ("dy", dy)):
+        if t is None:
+            continue
+        what = name if field == "x" else f"{name}'s " + ("result" if field == "out" else "gradient")
+        _typed(what, t, dtype, device)
+        if t.shape != x.shape:
+            raise ValueError(f"{what} must be {list(x.shape)}, got {list(t.shape)}")
+        row, head, one = t.stride()
+        if one != 1 and hd > 1:
+            raise ValueError("the elements of a head must be adjacent")
+        setattr(g, field, t.data_ptr())
+        setattr(g, field + "_row", row)
+        setattr(g, field + "_head", head)
+    g.gain = _line(f"{name}'s gain", gain, dtype, hd, device)
+    if dgain is not None:
+        g.dgain = _line(f"{name}'s gain gradient", dgain, _F32, hd, device)
+    g.heads = x.shape[1]
+    return g
+
+
+def _line(name, t, dtype, numel, device):
+    """A tensor of `numel` elements without gaps; its address."""
+    _typed(name, t, dtype, device)
+    if t.numel() != numel or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous and hold {numel} elements, got {list(t.shape)}")
+    return t.data_ptr()
+
+
+def _qk_call(q, k, positions, phase, layout, dev):
+    """What both directions pass on: rows, head_dim, rot_dim, positions, phases, layout, dtype."""
+    if q.dim() != 3:
+        raise ValueError(f"q must be [rows][heads][head_dim], got {list(q.shape)}")
+    if q.dtype is not _BF16 and q.dtype is not _F32:
+        raise ValueError(f"q must be torch.bfloat16 or torch.float32, got {q.dtype}")
+    rows, _, hd = q.shape
+    if (phase is None) != (positions is None):
+        raise ValueError("positions and phase go together")
+    pos = None if phase is None else _ints("positions", positions, rows, dev)
+    return (pos, None if phase is None else _phase(phase, dev), rows, hd, 0 if phase is None else 2 * phase.numel(), _layout(layout))
+
+
+def qk_norm_rope(q, k, positions, phase, q_gain, k_gain, q_out, k_out, *, eps=1e-6, layout="half", magnitude=1.0, stream=None):
+    """The norm of each query head of q [rows][heads][head_dim] and key head of k (None, with k_gain and k_out: queries
+    only) and its rotary embedding at int32 positions [rows], into q_out and k_out (q and k themselves: in place). Gains
+    [head_dim] have q's type. phase and positions None: no rotation."""
+    dev = _current()
+    pos, ph, rows, hd, rot, lay = _qk_call(q, k, positions, phase, layout, dev)
+    qs = _qk_part("q", q, None, q_out, q_gain, None, rows, hd, q.dtype, dev)
+    ks = None if k is None else _qk_part("k", k, None, k_out, k_gain, None, rows, hd, q.dtype, dev)
+    _check(_lib.load().dflare_qk_norm_rope(ctypes.byref(qs), None if ks is None else ctypes.byref(ks), pos, ph, rows, hd, rot, lay, magnitude,
+                                           eps, _lib.DFLARE_BF16 if q.dtype is _BF16 else _lib.DFLARE_F32, _stream(stream, dev)))
+
+
+def qk_norm_rope_work(head_dim, device="cuda"):
+    """A workspace of qk_norm_rope_backward, for one call at a time."""
+    return torch.empty(_lib.QK_NORM_WORK_ROWS * head_dim, dtype=_F32, device=device)
+
+
+def qk_norm_rope_backward(q, k, dq_out, dk_out, positions, phase, q_gain, k_gain, dq, dk, dq_gain, dk_gain, work, *, eps=1e-6,
+                          layout="half", magnitude=1.0, stream=None):
+    """The gradients of qk_norm_rope from its arguments q and k and the gradients dq_out and dk_out of its results: dq
+    and dk (dq_out and dk_out themselves: in place), and dq_gain and dk_gain (fp32 [head_dim], overwritten)."""
+    dev = _current()
+    pos, ph, rows, hd, rot, lay = _qk_call(q, k, positions, phase, layout, dev)
+    qs = _qk_part("q", q, dq_out, dq, q_gain, dq_gain, rows, hd, q.dtype, dev)
+    ks = None if k is None else _qk_part("k", k, dk_out, dk, k_gain, dk_gain, rows, hd, q.dtype, dev)
+    _check(_lib.load().dflare_qk_norm_rope_backward(
+        ctypes.byref(qs), None if ks is None else ctypes.byref(ks), pos, ph, rows, hd, rot, lay, magnitude, eps,
+        _line("work", work, _F32, _lib.QK_NORM_WORK_ROWS * hd, dev), _lib.DFLARE_BF16 if q.dtype is _BF16 else _lib.DFLARE_F32,
+        _stream(stream, dev)))
+
+
 def tree_plan(parents, n_nodes, mask, depth, error=None, stream=None):
     """Ancestor bits (int32 [batch][n][ceil(n / 32)]) and depths (int32 [batch][n]) of the trees with parent
     numbers ``parents`` int32 [batch][n]. error: optional int32 [1] that gets DEVERR_TREE for an impossible tree."""
@@ -163,6 +240,40 @@ def tree_accept(tokens, parents, choice, n_nodes, accept_len, path, next_token, 
         _ints("tokens", tokens, batch * n, dev), pp, _ints("choice", choice, batch * n, dev), _ints("n_nodes", n_nodes, batch, dev), batch, n,
         _ints("accept_len", accept_len, batch, dev), _ints("path", path, batch * n, dev), _ints("next_token", next_token, batch, dev),
         None if error is None else _ints("error", error, 1, dev), _stream(stream, dev)))
+
+
+def _grid(name, t, dtype, shape, device):
+    """A contiguous tensor of a shape; its address."""
+    _typed(name, t, dtype, device)
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous {list(shape)}, got {list(t.shape)}")
+    return t.data_ptr()
+
+
+def tree_sample(tokens, parents, n_nodes, target, draft, u, accept_len, path, next_token, *, distinct=False, error=None, stream=None):
+    """Sampled acceptance in drafted trees: target [batch][n][vocab] and draft [batch][n - 1 or more][vocab] fp32
+    probabilities after each node (a part of a tensor with more rows will do for draft; None: drafts were picked, not drawn), u fp32 [batch][n] uniform numbers in [0, 1).
+    distinct: siblings were drawn without replacement. The others as in tree_accept; error gets DEVERR_TREE, DEVERR_TOKEN."""
+    if parents.dim() != 2 or target.dim() != 3:
+        raise ValueError(f"parents must be [batch][n] and target [batch][n][vocab], got {list(parents.shape)} and {list(target.shape)}")
+    batch, n = parents.shape
+    vocab = target.shape[2]
+    dev = _current()
+    pp = _ints("parents", parents, 0, dev)
+    tp = _grid("target", target, _F32, (batch, n, vocab), dev)
+    dp, rows = None, 0
+    if draft is not None:
+        _typed("draft", draft, _F32, dev)
+        if draft.dim() != 3 or draft.shape[0] != batch or draft.shape[1] < n - 1 or draft.shape[2] != vocab:
+            raise ValueError(f"draft must be [{batch}][{n - 1} or more][{vocab}], got {list(draft.shape)}")
+        rows = draft.stride(0) // vocab if batch > 1 else max(n - 1, 1)
+        if draft.stride(2) != 1 or (draft.shape[1] > 1 and draft.stride(1) != vocab) or (batch > 1 and draft.stride(0) != rows * vocab):
+            raise ValueError(f"draft's rows must be adjacent and sequences whole rows apart, got strides {list(draft.stride())}")
+        dp = draft.data_ptr()
+    _check(_lib.load().dflare_tree_sample(
+        _ints("tokens", tokens, batch * n, dev), pp, _ints("n_nodes", n_nodes, batch, dev), tp, dp, rows, _grid("u", u, _F32, (batch, n), dev),
+        batch, n, vocab, 1 if distinct else 0, _ints("accept_len", accept_len, batch, dev), _ints("path", path, batch * n, dev),
+        _ints("next_token", next_token, batch, dev), None if error is None else _ints("error", error, 1, dev), _stream(stream, dev)))
 
 
 class PagedCache:
@@ -242,10 +353,12 @@ class PagedCache:
         dev = self.device_index
         _check(self._L.dflare_cache_reserve(self._cache, _ints("n_new", n_new, 1, dev), n_new.numel(), _stream(stream, dev)))
 
-    def append(self, layer, q, k, v, n_new, phase, q_out, *, depth=None, layout="half", magnitude=1.0, stream=None):
+    def append(self, layer, q, k, v, n_new, phase, q_out, *, depth=None, layout="half", magnitude=1.0, q_gain=None, k_gain=None,
+               eps=1e-6, stream=None):
         """A layer's new tokens: q [batch][n][n_q_heads][head_dim] rotated into q_out (q itself: in place), k
         and v [batch][n][n_kv_heads][head_dim] into the pages. q and q_out None: keys and values only. phase
-        None: no rotation. depth int32 [batch][n]: positions relative to lens (None: 0, 1, 2, ...)."""
+        None: no rotation. depth int32 [batch][n]: positions relative to lens (None: 0, 1, 2, ...). k_gain (and
+        q_gain, with queries) [head_dim]: every key and query head is normed first, as in qk_norm_rope."""
         dev = self.device_index
         batch, n = k.shape[:2]
         kv = (batch, n, self.n_kv_heads, self.head_dim)
@@ -259,6 +372,17 @@ class PagedCache:
             shape = (batch, n, self.n_q_heads, self.head_dim)
             qp, qs = _rows("q", q, self.dtype, shape, dev)
             op, os_ = (qp, qs) if q_out is q else _rows("q_out", q_out, self.dtype, shape, dev)
+        if q_gain is not None or k_gain is not None:
+            if k_gain is None or (q_gain is None) != (q is None):
+                raise ValueError("keys and, where there are queries, queries have a gain, or neither has")
+            _check(self._L.dflare_cache_append_normed(
+                self._cache, layer, qp, qs, kp, ks, vp, vs, op, os_,
+                None if q_gain is None else _line("q_gain", q_gain, self.dtype, self.head_dim, dev),
+                _line("k_gain", k_gain, self.dtype, self.head_dim, dev), eps,
+                None if depth is None else _ints("depth", depth, batch * n, dev), _ints("n_new", n_new, batch, dev), batch, n,
+                None if phase is None else _phase(phase, dev), 0 if phase is None else 2 * phase.numel(), _layout(layout), magnitude,
+                _stream(stream, dev)))
+            return
         _check(self._L.dflare_cache_append(
             self._cache, layer, qp, qs, kp, ks, vp, vs, op, os_,
             None if depth is None else _ints("depth", depth, batch * n, dev), _ints("n_new", n_new, batch, dev), batch, n,
