@@ -581,6 +581,30 @@ dflare_status dflare_cache_attend(dflare_cache* cache, int layer, const void* q_
                                   const int32_t* mask_dev, const int32_t* n_nodes_dev, int batch, int n_max,
                                   float scale, void* out_dev, float* lse_dev, void* stream);
 
+/*
+ * dflare_cache_attend for a batch whose sequences share their leading pages (dflare_cache_fork, or tables that name the same
+ * pages): keys on shared pages are read once for all rows of a group. The same result for a row, up to the rounding of sums.
+ * Once per step, after dflare_cache_reserve:
+ *   dflare_cache_share_plan     n_nodes_dev as in dflare_cache_attend. Finds the groups, sequences that are neighbours
+ *                               (those without nodes left out) and hold the same pages in the same places, full of
+ *                               context, and divides the work among the CTAs, into work_dev. Neighbours are grouped where that
+ *                               saves reading, by a rule on the lengths alone. groups_dev: optional [batch][2] int32, the
+ *                               first sequence of b's group (b: none) and the pages that it shares.
+ * then, per layer, with the same batch and n_max:
+ *   dflare_cache_attend_shared  as dflare_cache_attend, with the node counts and lengths of the plan.
+ * A plan holds until the lengths, the pages or the node counts change; what a call with an older one computes is that of
+ * the plan's lengths over the pages that the tables then name. A workspace without a plan for the call's batch and n_max sets
+ * DFLARE_DEVERR_PLAN, and nothing is written.
+ *   work_dev  dflare_cache_shared_bytes bytes, 128-byte aligned, zero before its first plan; for one plan and the calls that
+ *             follow it at a time. Calls with a batch, n_max and cache so large that the list of work would not fit 31 bits are refused.
+ */
+dflare_status dflare_cache_shared_bytes(dflare_cache* cache, int batch, int n_max, size_t* bytes);
+dflare_status dflare_cache_share_plan(dflare_cache* cache, const int32_t* n_nodes_dev, int batch, int n_max,
+                                      void* work_dev, int32_t* groups_dev, void* stream);
+dflare_status dflare_cache_attend_shared(dflare_cache* cache, int layer, const void* q_dev, long long q_row,
+                                         const int32_t* mask_dev, int batch, int n_max, float scale, void* out_dev,
+                                         float* lse_dev, void* work_dev, void* stream);
+
 /* Accept nodes path[b][0 .. accept_len[b]) of each sequence's tree ([batch][path_row] int32, increasing):
  * their rows of all layers move to slots lens[b] .. lens[b] + accept_len[b] - 1, lens grows by accept_len,
  * and pages past the new length are given back (by sequence, then by position). A length or path that no

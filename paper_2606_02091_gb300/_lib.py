@@ -43,7 +43,8 @@ EXPORTS = ("dflare_create", "dflare_destroy", "dflare_set_weights", "dflare_rese
            "dflare_cache_destroy", "dflare_cache_error", "dflare_cache_reserve", "dflare_cache_append",
            "dflare_cache_attend", "dflare_cache_commit", "dflare_cache_truncate", "dflare_cache_fork",
            "dflare_cache_copy_pages", "dflare_tree_plan", "dflare_tree_accept", "dflare_qk_norm_rope",
-           "dflare_qk_norm_rope_backward", "dflare_cache_append_normed", "dflare_tree_sample")
+           "dflare_qk_norm_rope_backward", "dflare_cache_append_normed", "dflare_tree_sample",
+           "dflare_cache_shared_bytes", "dflare_cache_share_plan", "dflare_cache_attend_shared")
 
 NOALLOC_MAX_ROWS = 4096
 QK_NORM_WORK_ROWS = 1024
@@ -144,6 +145,9 @@ def load():
         "dflare_cache_append": [vp, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, i32, i32, vp, i32, i32, f32, vp],
         "dflare_cache_append_normed": [vp, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, f32, vp, vp, i32, i32, vp, i32, i32, f32, vp],
         "dflare_cache_attend": [vp, i32, vp, i64, vp, vp, i32, i32, f32, vp, vp, vp],
+        "dflare_cache_shared_bytes": [vp, i32, i32, P(ctypes.c_size_t)],
+        "dflare_cache_share_plan": [vp, vp, i32, i32, vp, vp, vp],
+        "dflare_cache_attend_shared": [vp, i32, vp, i64, vp, i32, i32, f32, vp, vp, vp, vp],
         "dflare_cache_commit": [vp, vp, vp, i32, i32, vp],
         "dflare_cache_truncate": [vp, vp, i32, vp],
         "dflare_cache_fork": [vp, vp, vp, i32, vp],

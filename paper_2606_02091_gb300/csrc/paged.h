@@ -41,6 +41,35 @@ struct dflare_cache {
 
 namespace dfl {
 
+// Attention over shared pages (tree_shared.cu): one CTA's part of one unit of work, which is a block of query rows of one kv
+// head against a sequence's own keys, or a group's rows against the keys that the group shares.
+struct __align__(16) TreeItem {
+    int b;               // the table's row
+    int h;               // kv head
+    int lo, hi;          // key tiles [lo, hi) of the unit's
+    int page0, held;     // the first page of the unit's keys in the table's row, and how many count from there
+    int ctx, keys;       // of them: tokens, and tokens and nodes (the same number for a group's)
+    int nodes;           // whose rows these are: node i's query row is first + i, or map[~first + i] of a group
+    int first;
+    int row0;            // the block's first row
+    int dst;             // its first row among the partial results, or -1: the result itself
+};
+// What the joining launch has to know of a sequence.
+struct __align__(16) TreeSeq {
+    int n;               // nodes
+    int start, tiles, blocks;                   // own units: the first one's place in the list, tiles of each, blocks of rows
+    int lead_start, lead_tiles, lead_blocks;    // its group's (tiles 0: none)
+    int node0;           // its first node among the group's
+    int row, lead_row;   // rows of whole units among the partial results: of kv head 0 (lead_row: of the group's row 0)
+    int pad[2];
+};
+// The head of an attend_shared workspace.
+struct SharedHead {
+    int batch, n_max, per, ok;
+    int groups[2 * kMaxSeqs];       // [batch][2]: the sequence that leads b's group (b: none), shared pages
+    int same[kMaxSeqs];             // pages that b shares with the sequence before it that has nodes
+};
+
 // one launch of the paged attention
 struct TreeArgs {
     PagesView pg;
@@ -56,6 +85,13 @@ struct TreeArgs {
     uint32_t G_inv;            // 2^32 / G, rounded up (G > 1)
     int QG, C;                 // groups of query rows, and CTAs that share the work (more are launched for more groups)
     float scale_log2;
+    // attend_shared
+    const SharedHead* head;
+    const int2* runs;          // [C]: the first and the last item of a CTA, plus one
+    const TreeItem* items;
+    const int32_t* map;        // query rows of the groups' nodes
+    const TreeSeq* seqs;
+    int own_rows, lead_rows;   // rows among the partial results between kv heads
 };
 
 // The tcgen05 kernel's keys per tile, and how its work is divided (see tree_sched.cuh). Measured with 1, 2, 3 and 4 extra
@@ -64,9 +100,16 @@ struct TreeArgs {
 // with runs of at least 1 and 3: 171 nodes over two contexts of 142 and 96 keys 13.1 and 17.4.
 constexpr int kTcKeys = 128, kTcExtra = 3, kTcLeast = 1;
 
+// The fp32 kernel's: a tile takes as long as beginning and ending a pair: 13.0 us with 2 and 3, three contexts up to 600.
+constexpr int kFKeys = 32, kFRows = 16, kFExtra = 0, kFLeast = 1;
+
 cudaError_t launch_tree_attention(dflare_cache* c, TreeArgs a, cudaStream_t s);
 // tcgen05 kernel for many query rows per kv head (bf16); sets a.QG, a.C and the rows of a query group
 cudaError_t launch_tree_attention_tc(dflare_cache* c, TreeArgs& a, int* QT, cudaStream_t s);
+// the same kernels over a plan's items, with QT (tcgen05: 128 or 256; fp32: kFRows) rows in a block
+cudaError_t launch_shared_tc(dflare_cache* c, const TreeArgs& a, int QT, cudaStream_t s);
+cudaError_t launch_shared_f32(dflare_cache* c, const TreeArgs& a, cudaStream_t s);
+int f32_ctas_per_sm(int head_dim);
 // rows of the partial buffers that any launch of a cache may use
 size_t tree_partial_rows(const dflare_cache_config& g, int num_sms);
 

@@ -13,6 +13,7 @@
 #include <algorithm>
 #include <cmath>
 #include <string>
+#include <type_traits>
 
 #include "common.cuh"
 #include "paged.h"
@@ -385,13 +386,10 @@ __global__ void __launch_bounds__(kMmaThreads, 2) tree_mma_kernel(const __grid_c
 // fp32: 16 query rows per CTA, 32-key tiles by cp.async in two stages, exact fp32 products on the CUDA cores.
 // Scores: a thread takes two rows x two keys; output: (16 / RG) rows x four head dims. Bound by the latency of its
 // steps at the sizes that fp32 models have (8 nodes over 600 keys 9 us; 16 over 2 x 1000 keys, 32 heads of 128: 45).
-constexpr int kFKeys = 32;
-constexpr int kFRows = 16;
 constexpr int kFThreads = 128;
 // CTAs on an SM, as their shared memory allows. Measured at head_dim 64 with 2 and 5: 60 nodes of 16/8 heads over 1000 and 2000
 // keys 79 and 53 us, 150 nodes over 40 contexts up to 100 keys 478 and 300, 8 nodes over 600 keys 8.3 and 8.5.
 constexpr int f32_ctas(int HD) { return HD == 64 ? 5 : 2; }
-constexpr int kFExtra = 0, kFLeast = 1;     // (a tile takes as long as beginning and ending a pair: 13.0 us with 2 and 3, three contexts up to 600)
 
 template <int HD>
 struct F32Layout {
@@ -400,7 +398,8 @@ struct F32Layout {
     static constexpr int FLOATS = A + 2 * kFRows;
 };
 
-template <int HD>
+// SHARED: over the items of a plan (tree_shared.cu).
+template <int HD, bool SHARED>
 __global__ void __launch_bounds__(kFThreads) tree_f32_kernel(const TreeArgs a) {
     using LY = F32Layout<HD>;
     constexpr int LD = LY::LD, PL = kFKeys + 4, DG = HD / 4, RG = kFThreads / DG, RR = kFRows / RG;
@@ -410,17 +409,20 @@ __global__ void __launch_bounds__(kFThreads) tree_f32_kernel(const TreeArgs a) {
     const int tid = threadIdx.x;
     pdl_wait();
     pdl_trigger();
-    int qg, v, v1;
-    tree_runs<kFRows, kFKeys, kFExtra, kFLeast>(a, cum, qg, v, v1);
+    int qg = 0, v, v1;
+    if constexpr (SHARED) tree_items(a, v, v1);
+    else tree_runs<kFRows, kFKeys, kFExtra, kFLeast>(a, cum, qg, v, v1);
     const int v0 = v;
     const int ry = tid / 16, kx = tid % 16;         // scores: rows 2 ry, 2 ry + 1, keys kx, kx + 16
     const int rg = tid / DG, dg = tid % DG;         // output: rows rg RR .., head dims 4 dg ..
-    TreePair it;
+    std::conditional_t<SHARED, TreeItem, TreePair> it;
     while (tree_pair<kFExtra>(a, cum, v, v1, it)) {
         int n, ctx, keys;
-        tree_lengths(a, tree_raw(a, it.b), n, ctx, keys);
-        const int R = n * a.G, base = qg * kFRows;
-        const int32_t* table = a.pg.table + (size_t)it.b * a.pg.max_pages;
+        pair_lengths<SHARED>(a, pair_raw(a, it), n, ctx, keys);
+        int base = qg * kFRows;
+        if constexpr (SHARED) base = it.row0;
+        const int R = n * a.G;
+        const int32_t* table = a.pg.table + (size_t)it.b * a.pg.max_pages + first_page(it);
         auto load = [&](int tile, int st) {
             const int k0 = tile * kFKeys;
             for (int x = tid; x < kFKeys * DG; x += kFThreads) {
@@ -442,12 +444,12 @@ __global__ void __launch_bounds__(kFThreads) tree_f32_kernel(const TreeArgs a) {
             const int r = x / DG, d = x % DG * 4, rr = base + r;
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
             if (rr < R)
-                v = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + ((size_t)it.b * a.n_max + rr / a.G) * a.q_row +
+                v = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + query_row(a, it, rr / a.G) * a.q_row +
                                                      (size_t)(it.h * a.G + rr % a.G) * HD + d);
             *reinterpret_cast<float4*>(Qs + r * LD + d) = v;
         }
         int node[2];
-        for (int i = 0; i < 2; ++i) node[i] = min(base + 2 * ry + i, R - 1) / a.G;
+        for (int i = 0; i < 2; ++i) node[i] = mask_node(it, min(base + 2 * ry + i, R - 1) / a.G);
         float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, o[RR][4];
 #pragma unroll
         for (int r = 0; r < RR; ++r) o[r][0] = o[r][1] = o[r][2] = o[r][3] = 0.f;
@@ -544,14 +546,22 @@ __global__ void __launch_bounds__(kFThreads) tree_f32_kernel(const TreeArgs a) {
                 As[kFRows + 2 * ry + i] = l[i];
             }
         __syncthreads();
-        const bool partial = it.partial();
+        bool partial;
+        size_t part0;
+        if constexpr (SHARED) {
+            partial = it.dst >= 0;
+            part0 = (size_t)max(it.dst, 0);
+        } else {
+            partial = it.partial();
+            part0 = ((size_t)blockIdx.x * 2 + (it.start < v0 ? 0 : 1)) * kFRows;
+        }
 #pragma unroll
         for (int r = 0; r < RR; ++r) {
             const int lr = rg * RR + r, rr = base + lr;
             if (rr >= R) continue;
             const float mr = As[lr], sr = As[kFRows + lr];
             if (partial) {
-                const size_t row = ((size_t)blockIdx.x * 2 + (it.start < v0 ? 0 : 1)) * kFRows + lr;
+                const size_t row = part0 + lr;
                 *reinterpret_cast<float4*>(a.part_o + row * HD + 4 * dg) = make_float4(o[r][0], o[r][1], o[r][2], o[r][3]);
                 if (dg == 0) a.part_ml[row] = make_float2(mr, sr);
             } else {
@@ -783,12 +793,22 @@ template <int HD>
 cudaError_t launch_f32(dflare_cache* c, TreeArgs a, cudaStream_t s) {
     static PerDeviceOnce once;
     constexpr int bytes = F32Layout<HD>::FLOATS * 4;
-    cudaError_t e = once([] { return cudaFuncSetAttribute(tree_f32_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); });
+    auto kernel = tree_f32_kernel<HD, false>;
+    cudaError_t e = once([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); });
     if (e != cudaSuccess) return e;
     a.QG = (a.n_max * a.G + kFRows - 1) / kFRows;
     a.C = f32_ctas(HD) * c->num_sms;
-    e = launch_kernel(true, tree_f32_kernel<HD>, dim3(std::max(a.QG, a.C)), dim3(kFThreads), bytes, s, a);
+    e = launch_kernel(true, kernel, dim3(std::max(a.QG, a.C)), dim3(kFThreads), bytes, s, a);
     return e == cudaSuccess ? launch_join<float, HD>(c, a, kFRows, kFKeys, kFExtra, kFLeast, false, s) : e;
+}
+
+template <int HD>
+cudaError_t launch_f32_items(const TreeArgs& a, cudaStream_t s) {
+    static PerDeviceOnce once;
+    constexpr int bytes = F32Layout<HD>::FLOATS * 4;
+    auto kernel = tree_f32_kernel<HD, true>;
+    cudaError_t e = once([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); });
+    return e == cudaSuccess ? launch_kernel(true, kernel, dim3(a.C), dim3(kFThreads), bytes, s, a) : e;
 }
 
 template <int HD>
@@ -805,6 +825,11 @@ cudaError_t launch_hd(dflare_cache* c, TreeArgs a, cudaStream_t s) {
 }
 
 }  // namespace
+
+cudaError_t launch_shared_f32(dflare_cache* c, const TreeArgs& a, cudaStream_t s) {
+    return c->cfg.head_dim == 128 ? launch_f32_items<128>(a, s) : launch_f32_items<64>(a, s);
+}
+int f32_ctas_per_sm(int head_dim) { return f32_ctas(head_dim); }
 
 size_t tree_partial_rows(const dflare_cache_config& g, int num_sms) {
     // two partial results per CTA: of 16 rows with several CTAs per SM, or of up to 256 rows with one

@@ -21,6 +21,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "common.cuh"
 #include "paged.h"
@@ -102,10 +103,12 @@ __device__ __forceinline__ void streams_meet() {
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-template <int HD, int NQ>
+// SHARED: over the items of a plan (tree_shared.cu) instead of the batch's sequences and kv heads.
+template <int HD, int NQ, bool SHARED>
 __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_constant__ CUtensorMap mk,
                                                               const __grid_constant__ CUtensorMap mv, const TreeArgs a) {
     using LY = TcLayout<HD, NQ>;
+    using Pair = std::conditional_t<SHARED, TreeItem, TreePair>;
     constexpr int NK = LY::NK, NV = LY::NV, QT = 128 * NQ;
     constexpr uint32_t TB = LY::TB;
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -164,10 +167,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     // before its own dependency wait can never hold columns that this CTA waits for. After this kernel's own
     // wait: the joining launch reads the lengths at once.
     pdl_trigger();
-    int qg, v, v1;
-    tree_runs<QT, kKeys, kTcExtra, kTcLeast>(a, cum, qg, v, v1);
+    int qg = 0, v, v1;
+    if constexpr (SHARED) tree_items(a, v, v1);
+    else tree_runs<QT, kKeys, kTcExtra, kTcLeast>(a, cum, qg, v, v1);
     const int v0 = v;
-    TreePair p, after;
+    Pair p, after;
     bool more = tree_pair<kTcExtra>(a, cum, v, v1, p);
     auto tS = [&](int w) { return tmem + 128u * w; };
     auto tO = [&](int w) { return tmem + 256u + (uint32_t)HD * w; };
@@ -236,13 +240,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                 umma_commit(sfull(w));
                 if (NQ == 1 || w == 1) umma_commit(kempty(st));
             };
-            TreeRaw raw = more ? tree_raw(a, p.b) : TreeRaw{};
+            TreeRaw raw = more ? pair_raw(a, p) : TreeRaw{};
             for (; more; ++pair) {
                 const int n = p.hi - p.lo;
                 int nodes, ctx, keys;
-                tree_lengths(a, raw, nodes, ctx, keys);
+                pair_lengths<SHARED>(a, raw, nodes, ctx, keys);
                 const bool next = tree_pair<kTcExtra>(a, cum, v, v1, after);
-                if (next) raw = tree_raw(a, after.b);
+                if (next) raw = pair_raw(a, after);
                 // PV of tile j of the pair by stream w, then the stream's next S
                 auto step = [&](int j, int w) {
                     constexpr int stride = NQ == 1 ? 2 : 1;
@@ -291,25 +295,28 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         // microseconds too.
         const int w = warp >> 2, r = tid & 127;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const int row0 = qg * QT;
+        auto row0_of = [&](const Pair& p) {     // the first row of the block
+            if constexpr (SHARED) return p.row0;
+            else return qg * QT;
+        };
         bool ok = true;
         int base = 0, ss = 0, os = 0;
         auto wait = [&](uint32_t bar, uint32_t parity) {
             if (ok) ok = __all_sync(0xffffffffu, wait_inline(bar, parity, &abort_flag, a.pg.err));
         };
-        // Q of a pair, asynchronously, by `many` threads (this one the who-th) from row q0 on: pieces of eight
-        // elements, swizzled; rows past R are never looked at
-        auto load_q = [&](const TreePair& p, int R, int q0, int who, int many) {
+        // Q of a pair, asynchronously, by `many` threads (this one the who-th), 128 rows from the block's row 128 x half
+        // on: pieces of eight elements, swizzled; rows past R are never looked at
+        auto load_q = [&](const Pair& p, int R, int half, int who, int many) {
             constexpr int PC = HD / 8;
-            const int pc = who % PC;
-            const uint32_t dst = sb + LY::Q + (uint32_t)((q0 - row0) >> 7) * TB + (pc >> 3) * 16384;
-            const bf16* src = static_cast<const bf16*>(a.q) + (size_t)p.b * a.n_max * a.q_row + (size_t)(p.h * a.G) * HD + pc * 8;
+            const int pc = who % PC, q0 = row0_of(p) + 128 * half;
+            const uint32_t dst = sb + LY::Q + (uint32_t)half * TB + (pc >> 3) * 16384;
+            const bf16* src = static_cast<const bf16*>(a.q) + (SHARED ? 0 : (size_t)p.b * a.n_max * a.q_row) + (size_t)(p.h * a.G) * HD + pc * 8;
 #pragma unroll 4
             for (int lr = who / PC; lr < 128; lr += many / PC) {
                 const int rr = q0 + lr, nd = group_of(a, rr);
                 if (rr < R)
                     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + lr * 128 + (((pc & 7) ^ (lr & 7)) << 4)),
-                                 "l"(src + (size_t)nd * a.q_row + (rr - nd * a.G) * HD) : "memory");
+                                 "l"(src + (SHARED ? query_row(a, p, nd) : (size_t)nd) * a.q_row + (rr - nd * a.G) * HD) : "memory");
             }
         };
         auto q_there = [&]() {      // this thread's part of Q is in shared memory, for the MMAs to read
@@ -321,10 +328,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         TreeRaw raw{};
         int nodes = 0, ctx = 0, keys = 0;
         if (more) {
-            raw = tree_raw(a, p.b);
-            tree_lengths(a, raw, nodes, ctx, keys);
-            if (NQ == 2) load_q(p, nodes * a.G, row0 + 128 * w, r, 128);
-            else load_q(p, nodes * a.G, row0, tid, 256);
+            raw = pair_raw(a, p);
+            pair_lengths<SHARED>(a, raw, nodes, ctx, keys);
+            if (NQ == 2) load_q(p, nodes * a.G, w, r, 128);
+            else load_q(p, nodes * a.G, 0, tid, 256);
             __syncwarp();
             if (lane == 0) mbar_arrive(qsent);
             q_there();
@@ -332,13 +339,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         while (more) {
             const int n = p.hi - p.lo;
             const int R = nodes * a.G;
-            const int my_row = row0 + (NQ == 2 ? 128 * w : 0) + r;
+            const int my_row = row0_of(p) + (NQ == 2 ? 128 * w : 0) + r;
             const bool live = my_row < R;
             const bool warp_live = my_row - lane < R;
-            const int node = group_of(a, min(my_row, R - 1));
+            const int node = mask_node(p, group_of(a, min(my_row, R - 1)));
             const SeenRow row = seen_row(a, p.b, node);
             more = tree_pair<kTcExtra>(a, cum, v, v1, after);
-            if (more) raw = tree_raw(a, after.b);
+            if (more) raw = pair_raw(a, after);
             int nodes2 = 0, ctx2 = 0, keys2 = 0;        // the next pair's
             float m = -INFINITY, l = 0.f;
             const int mine = NQ == 2 ? n : (n + 1 - w) / 2;      // tiles of this stream
@@ -349,8 +356,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                 tc_fence_after();
                 // every S of the pair (of this stream, with NQ = 2) has been computed: the next pair's Q
                 if (tile == n - 1 && more) {
-                    tree_lengths(a, raw, nodes2, ctx2, keys2);
-                    load_q(after, nodes2 * a.G, row0 + (NQ == 2 ? 128 * w : 0), r, 128);
+                    pair_lengths<SHARED>(a, raw, nodes2, ctx2, keys2);
+                    load_q(after, nodes2 * a.G, NQ == 2 ? w : 0, r, 128);
                 }
                 const bool edge = k0 + kKeys > ctx;
                 if (edge) {
@@ -477,15 +484,22 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                 if (lane == 0) mbar_arrive(pfull(w));
             }
             if (more) {
-                tree_lengths(a, raw, nodes2, ctx2, keys2);      // (the stream without the last tile too)
+                pair_lengths<SHARED>(a, raw, nodes2, ctx2, keys2);      // (the stream without the last tile too)
                 q_there();      // the next pair's first S is computed while this one's rows are written
             }
             if (mine > 0) wait(ofull(w), (uint32_t)os++ & 1u);
             tc_fence_after();
             // ---------------- the pair's rows. NQ = 2: a thread has its row. NQ = 1: the streams swap (m, l)
             // and each joins one half of the head dims of both.
-            const bool partial = p.partial();
-            const int slot = p.start < v0 ? 0 : 1;
+            bool partial;
+            size_t part0;       // the block's first row among the partial results
+            if constexpr (SHARED) {
+                partial = p.dst >= 0;
+                part0 = (size_t)max(p.dst, 0);
+            } else {
+                partial = p.partial();
+                part0 = ((size_t)blockIdx.x * 2 + (p.start < v0 ? 0 : 1)) * QT;
+            }
             float M = m, L = l, w0 = 1.f, w1 = 0.f;
             const bool two = NQ == 1 && n > 1;
             if (NQ == 1) {
@@ -514,7 +528,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                 }
                 uint8_t* turn = smem + LY::TURN + warp * 4096;
                 const int rows = min(32, R - (my_row - lane));
-                const size_t prow = ((size_t)blockIdx.x * 2 + slot) * QT + (NQ == 2 ? 128 * w : 0) + r;
+                const size_t prow = part0 + (NQ == 2 ? 128 * w : 0) + r;
                 const size_t orow = ((size_t)p.b * a.n_max + node) * a.hq + p.h * a.G + min(my_row, R - 1) - node * a.G;
                 constexpr int CH = NQ == 2 ? HD / 32 : HD / 64;
                 const int col0 = NQ == 2 ? 0 : w * (HD / 2);
@@ -617,14 +631,21 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
 template <int HD, int NQ>
 cudaError_t launch_tc(dflare_cache* c, TreeArgs& a, cudaStream_t s) {
     static PerDeviceOnce once;
-    cudaError_t e = once([] {
-        return cudaFuncSetAttribute(tree_tc_kernel<HD, NQ>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TcLayout<HD, NQ>::BYTES);
-    });
+    auto kernel = tree_tc_kernel<HD, NQ, false>;
+    cudaError_t e = once([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TcLayout<HD, NQ>::BYTES); });
     if (e != cudaSuccess) return e;
     a.QG = (a.n_max * a.G + 128 * NQ - 1) / (128 * NQ);
     a.C = c->num_sms;
-    return launch_kernel(true, tree_tc_kernel<HD, NQ>, dim3(std::max(a.QG, a.C)), dim3(kThreads), TcLayout<HD, NQ>::BYTES, s, c->maps[0],
-                         c->maps[1], a);
+    return launch_kernel(true, kernel, dim3(std::max(a.QG, a.C)), dim3(kThreads), TcLayout<HD, NQ>::BYTES, s, c->maps[0], c->maps[1], a);
+}
+
+template <int HD, int NQ>
+cudaError_t launch_items(dflare_cache* c, const TreeArgs& a, cudaStream_t s) {
+    static PerDeviceOnce once;
+    auto kernel = tree_tc_kernel<HD, NQ, true>;
+    cudaError_t e = once([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TcLayout<HD, NQ>::BYTES); });
+    if (e != cudaSuccess) return e;
+    return launch_kernel(true, kernel, dim3(a.C), dim3(kThreads), TcLayout<HD, NQ>::BYTES, s, c->maps[0], c->maps[1], a);
 }
 
 }  // namespace
@@ -634,6 +655,11 @@ cudaError_t launch_tree_attention_tc(dflare_cache* c, TreeArgs& a, int* QT, cuda
     *QT = one ? 128 : 256;
     if (c->cfg.head_dim == 128) return one ? launch_tc<128, 1>(c, a, s) : launch_tc<128, 2>(c, a, s);
     return one ? launch_tc<64, 1>(c, a, s) : launch_tc<64, 2>(c, a, s);
+}
+
+cudaError_t launch_shared_tc(dflare_cache* c, const TreeArgs& a, int QT, cudaStream_t s) {
+    if (c->cfg.head_dim == 128) return QT == 128 ? launch_items<128, 1>(c, a, s) : launch_items<128, 2>(c, a, s);
+    return QT == 128 ? launch_items<64, 1>(c, a, s) : launch_items<64, 2>(c, a, s);
 }
 
 }  // namespace dfl

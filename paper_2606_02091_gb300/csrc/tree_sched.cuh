@@ -188,6 +188,49 @@ __device__ __forceinline__ bool tree_pair(const TreeArgs& a, const int32_t* cum,
     return false;
 }
 
+// The same from a plan's items: v counts them, cum is not looked at.
+template <int EXTRA>
+__device__ __forceinline__ bool tree_pair(const TreeArgs& a, const int32_t*, int& v, int v1, TreeItem& p) {
+    if (v >= v1) return false;
+    const int4* from = reinterpret_cast<const int4*>(a.items + v++);
+    int4* to = reinterpret_cast<int4*>(&p);
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(TreeItem) / 16); ++i) to[i] = __ldg(from + i);
+    return true;
+}
+// This CTA's items; false (and reported) where the workspace does not hold a plan for this call.
+__device__ __forceinline__ bool tree_items(const TreeArgs& a, int& v, int& v1) {
+    const int2 run = a.runs[blockIdx.x];
+    const bool ok = a.head->batch == a.batch && a.head->n_max == a.n_max && a.head->ok;
+    v = ok ? run.x : 0;
+    v1 = ok ? run.y : 0;
+    if (!ok && threadIdx.x == 0 && blockIdx.x == 0) atomicOr(a.pg.err, DFLARE_DEVERR_PLAN);
+    return ok;
+}
+// Lengths of a pair: what memory has to say of it, and what follows
+__device__ __forceinline__ TreeRaw pair_raw(const TreeArgs& a, const TreePair& p) { return tree_raw(a, p.b); }
+__device__ __forceinline__ TreeRaw pair_raw(const TreeArgs&, const TreeItem& p) { return {p.nodes, p.keys, p.ctx}; }
+template <bool SHARED>
+__device__ __forceinline__ void pair_lengths(const TreeArgs& a, const TreeRaw& x, int& n, int& ctx, int& keys) {
+    if constexpr (SHARED) {
+        n = x.n;
+        keys = x.held;
+        ctx = x.len;
+    } else {
+        tree_lengths(a, x, n, ctx, keys);
+    }
+}
+// the query row of a pair's node, in rows of q
+__device__ __forceinline__ size_t query_row(const TreeArgs& a, const TreePair& p, int node) { return (size_t)p.b * a.n_max + node; }
+__device__ __forceinline__ size_t query_row(const TreeArgs& a, const TreeItem& p, int node) {
+    return (size_t)(p.first >= 0 ? p.first + node : __ldg(a.map + ~p.first + node));
+}
+// the node that a row's mask goes by (a group's rows have none: all of its keys are context)
+__device__ __forceinline__ int mask_node(const TreePair&, int node) { return node; }
+__device__ __forceinline__ int mask_node(const TreeItem& p, int node) { return p.first >= 0 ? node : 0; }
+__device__ __forceinline__ int first_page(const TreePair&) { return 0; }
+__device__ __forceinline__ int first_page(const TreeItem& p) { return p.page0; }
+
 // Bounded wait, inline (a call would keep the compiler from giving a kernel's other threads their registers).
 __device__ __forceinline__ bool wait_inline(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t* err) {
 #pragma unroll 1
@@ -218,6 +261,10 @@ __device__ __forceinline__ BoxPage box_page(const TreeArgs& a, const TreePair& p
     const int at = (int)(((unsigned)(base * KT) + (unsigned)(lane * rows)) / (unsigned)a.pg.ps);
     return {a.pg.held[p.b], at < a.pg.max_pages ? a.pg.table[(size_t)p.b * a.pg.max_pages + at] : -1, at, p.h};
 }
+__device__ __forceinline__ BoxPage box_page(const TreeArgs& a, const TreeItem& p, int base, int KT, int rows, int lane) {
+    const int at = (int)(((unsigned)(base * KT) + (unsigned)(lane * rows)) / (unsigned)a.pg.ps);
+    return {p.held, at < p.held ? a.pg.table[(size_t)p.b * a.pg.max_pages + p.page0 + at] : -1, at, p.h};
+}
 __device__ __forceinline__ int box_plane(const TreeArgs& a, const BoxPage& x) {
     if (x.at < x.held && x.page >= 0 && x.page < a.pg.pages) return (a.layer * a.pg.pages + x.page) * a.pg.hkv + x.h;
     if (x.at < x.held) atomicOr(a.pg.err, DFLARE_DEVERR_PAGE);
@@ -226,8 +273,8 @@ __device__ __forceinline__ int box_plane(const TreeArgs& a, const BoxPage& x) {
 // f(first tile, tiles, planes of their boxes) for groups of tiles (of one pair, as many as have 32 boxes) of the run from
 // pair p on, in order, while it says true; false if it did not. The whole warp calls this and f. planes: [2][32] in
 // shared memory; a group's stay as they are until the warp is through with f for the next group.
-template <int EXTRA, class F>
-__device__ __forceinline__ bool each_group(const TreeArgs& a, const int32_t* cum, int& v, int v1, TreePair p, int KT, int rows, int lane,
+template <int EXTRA, class P, class F>
+__device__ __forceinline__ bool each_group(const TreeArgs& a, const int32_t* cum, int& v, int v1, P p, int KT, int rows, int lane,
                                            int (*planes)[32], F f) {
     const int many = 32 / (KT / rows);
     int base = p.lo, buf = 0;
@@ -262,7 +309,7 @@ __device__ __forceinline__ bool drop_odd(uint4& v) {
     return true;
 }
 
-// row / G for the rows of a kv head (below 2^16): a multiplication by the rounded-up reciprocal
+// row / G for the rows of a kv head (below 2^24, as G <= 64): a multiplication by the rounded-up reciprocal
 __device__ __forceinline__ int group_of(const TreeArgs& a, int row) { return a.G == 1 ? row : (int)__umulhi((unsigned)row, a.G_inv); }
 
 // 64 bits of a node's mask row from bit x >= 0 on
@@ -317,15 +364,15 @@ __device__ __forceinline__ uint32_t seen32(const TreeArgs& a, const SeenRow& r, 
 }
 
 // f(value address) for every node in odd[] (one bit per node) that `node` sees, in the layer's values of kv head h
-template <class F>
-__device__ __forceinline__ void each_odd(const TreeArgs& a, const uint32_t* odd, const TreePair& p, int node, int ctx, int keys, F f) {
+template <class P, class F>
+__device__ __forceinline__ void each_odd(const TreeArgs& a, const uint32_t* odd, const P& p, int node, int ctx, int keys, F f) {
     for (int word = 0; word < a.words; ++word) {
         uint32_t bits = odd[word];
         while (bits) {
             const int key = ctx + word * 32 + __ffs(bits) - 1;
             bits &= bits - 1;
             if (!(tree_seen(a, p.b, node, ctx, keys, key) & 1)) continue;
-            const int page = a.pg.table[(size_t)p.b * a.pg.max_pages + key / a.pg.ps];
+            const int page = a.pg.table[(size_t)p.b * a.pg.max_pages + first_page(p) + key / a.pg.ps];
             f(((((size_t)a.layer * a.pg.pages + page) * a.pg.hkv + p.h) * a.pg.ps + key % a.pg.ps) * a.pg.hd);
         }
     }

@@ -13,6 +13,13 @@ A block step of a target model:
         cache.attend(layer, q, n_nodes, out, mask=mask)
     tree_accept(tokens, parents, choice, n_nodes, accept_len, path, next_token)
     cache.commit(accept_len, path)
+
+A server that samples several continuations of one prompt (cache.fork) from a model that norms its heads:
+
+    cache.share_plan(n_nodes, n, work)                                    # behind reserve, once for all layers
+        cache.append(layer, q, k, v, n_nodes, phase, q, depth=depth, q_gain=q_gain, k_gain=k_gain)
+        cache.attend_shared(layer, q, out, work, mask=mask)
+    tree_sample(tokens, parents, n_nodes, target, draft, u, accept_len, path, next_token)
 """
 from __future__ import annotations
 
@@ -286,6 +293,7 @@ class PagedCache:
 
     def __init__(self, *, k, v, table, lens, held, refs, free, n_free, n_q_heads, max_nodes):
         self._cache = ctypes.c_void_p()
+        self._sizes = {}        # bytes of attend_shared's workspace by batch and n
         if not k.is_cuda:
             raise ValueError("k must be a CUDA tensor")
         self.device_index = dev = k.get_device()
@@ -394,6 +402,12 @@ class PagedCache:
         ancestor bits of tree_plan (None: node i sees nodes 0 .. i). scale: head_dim^-0.5 if None. lse: optional
         fp32 [batch][n][n_q_heads]."""
         dev = self.device_index
+        batch, n, qp, qs, op, lp = self._attend_args(q, out, lse, dev)
+        _check(self._L.dflare_cache_attend(
+            self._cache, layer, qp, qs, None if mask is None else _ints("mask", mask, batch * n * ((n + 31) // 32), dev),
+            _ints("n_nodes", n_nodes, batch, dev), batch, n, self.head_dim ** -0.5 if scale is None else scale, op, lp, _stream(stream, dev)))
+
+    def _attend_args(self, q, out, lse, dev):
         if q.dim() != 4:
             raise ValueError(f"q must be [batch][n][n_q_heads][head_dim], got {list(q.shape)}")
         batch, n = q.shape[:2]
@@ -407,10 +421,43 @@ class PagedCache:
             if lse.numel() < batch * n * self.n_q_heads or not lse.is_contiguous():
                 raise ValueError(f"lse must be contiguous and hold {batch * n * self.n_q_heads} elements")
             lp = lse.data_ptr()
-        _check(self._L.dflare_cache_attend(
-            self._cache, layer, qp, qs, None if mask is None else _ints("mask", mask, batch * n * ((n + 31) // 32), dev),
-            _ints("n_nodes", n_nodes, batch, dev), batch, n, self.head_dim ** -0.5 if scale is None else scale, out.data_ptr(), lp,
-            _stream(stream, dev)))
+        return batch, n, qp, qs, out.data_ptr(), lp
+
+    def _shared_bytes(self, batch, n):
+        size = self._sizes.get((batch, n))
+        if size is None:
+            got = ctypes.c_size_t(0)
+            _check(self._L.dflare_cache_shared_bytes(self._cache, batch, n, ctypes.byref(got)))
+            size = self._sizes[batch, n] = got.value
+        return size
+
+    def shared_work(self, batch, n):
+        """A workspace of share_plan and attend_shared for a batch with up to n nodes each; for one plan at a time."""
+        return torch.zeros(self._shared_bytes(batch, n), dtype=torch.uint8, device=self.k.device)
+
+    def _work(self, work, batch, n, dev):
+        _typed("work", work, torch.uint8, dev)
+        need = self._shared_bytes(batch, n)
+        if work.numel() < need or not work.is_contiguous():
+            raise ValueError(f"work must be contiguous and hold {need} bytes for this batch and n, got {work.numel()}")
+        return work.data_ptr()
+
+    def share_plan(self, n_nodes, n, work, *, groups=None, stream=None):
+        """Find which neighbouring sequences share their leading pages and divide the attention of one step's trees with
+        n_nodes [batch] of up to n nodes, for attend_shared with every layer. groups: optional int32 [batch][2], the first
+        sequence of the group that each is in and the pages that it shares."""
+        dev = self.device_index
+        batch = n_nodes.numel()
+        _check(self._L.dflare_cache_share_plan(self._cache, _ints("n_nodes", n_nodes, 1, dev), batch, n, self._work(work, batch, n, dev),
+                                               None if groups is None else _ints("groups", groups, 2 * batch, dev), _stream(stream, dev)))
+
+    def attend_shared(self, layer, q, out, work, *, mask=None, scale=None, lse=None, stream=None):
+        """attend for the node counts and lengths of the plan in work, with shared pages read once for a whole group."""
+        dev = self.device_index
+        batch, n, qp, qs, op, lp = self._attend_args(q, out, lse, dev)
+        _check(self._L.dflare_cache_attend_shared(
+            self._cache, layer, qp, qs, None if mask is None else _ints("mask", mask, batch * n * ((n + 31) // 32), dev), batch, n,
+            self.head_dim ** -0.5 if scale is None else scale, op, lp, self._work(work, batch, n, dev), _stream(stream, dev)))
 
     def commit(self, accept_len, path, stream=None):
         """Keep the nodes path[b][: accept_len[b]] (int32 [batch], [batch][n]) behind every length, moved
