@@ -24,6 +24,8 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kBatch = 4;               // heads whose loads are in flight together
+constexpr int kForwardCtas = 2, kBackwardCtas = 2;
+template <class T> constexpr int kStreamCtas = 2;      // CTAs on an SM, as their registers and rings allow
 constexpr int kWorkRows = DFLARE_QK_NORM_WORK_ROWS;     // CTAs that may leave a sum of gain gradients
 
 // queries, keys, values (values in an append only: copied)
@@ -63,27 +65,79 @@ __device__ __forceinline__ T* out_at(const NormArgs& a, const Part& p, int part,
     if (!APPEND || part == 0) return static_cast<T*>(p.out) + row * p.out_row + h * p.out_head;
     return slot < 0 ? nullptr : static_cast<T*>(part == 2 ? a.pg.v : a.pg.k) + (slot + (long long)h * a.pg.ps) * a.hd;
 }
-// element 0 and 1 of pair j of a unit, numbered within its 16 elements (two runs of eight)
-template <bool INTER> __device__ __forceinline__ constexpr int first_of(int j) { return INTER ? 2 * j : j; }
-template <bool INTER> __device__ __forceinline__ constexpr int second_of(int j) { return INTER ? 2 * j + 1 : 8 + j; }
-
+// A unit's values as eight packed pairs: of neighbours, so that halves turn (0..3 with 4..7) in packed operations, and
+// interleaved pairs turn with their own exchange.
 template <class T>
-__device__ __forceinline__ void values(const Unit<T>& u, float* v) {
+__device__ __forceinline__ void values(const Unit<T>& u, uint64_t* v) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float2 f = get2(u, i);
-        v[2 * i] = f.x;
-        v[2 * i + 1] = f.y;
+        v[i] = pack2(f.x, f.y);
     }
+}
+template <class T>
+__device__ __forceinline__ void put(Unit<T>& u, const uint64_t* v) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float a, b;
+        unpack2(v[i], a, b);
+        set2(u, i, a, b);
+    }
+}
+__device__ __forceinline__ uint64_t swapped(uint64_t v) {
+    float a, b;
+    unpack2(v, a, b);
+    return pack2(b, a);
+}
+__device__ __forceinline__ uint64_t both(float v) { return pack2(v, v); }
+__device__ __forceinline__ float sum2(uint64_t v) {
+    float a, b;
+    unpack2(v, a, b);
+    return a + b;
 }
 __device__ __forceinline__ float head_sum(float v, int lanes) {
     for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
+// 1 / sqrt(mean + eps), rounded once more than its argument
+__device__ __forceinline__ float inverse_rms(float sum_sq, float inv_hd, float eps) { return __frsqrt_rn(fmaf(sum_sq, inv_hd, eps)); }
+
+// What turns a unit: y_i = r (x_i A_i + x_partner(i) B_i), with the gain in it; or y_i = r x_i A_i where nothing turns.
+struct Turn {
+    uint64_t a[8], b[8];
+};
+// c, s of the unit's eight pairs; gain
+template <bool INTER>
+__device__ __forceinline__ void make_turn(Turn& t, bool rotates, const float* c, const float* s, const uint64_t* gain) {
+    if (!rotates) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            t.a[i] = gain[i];
+            t.b[i] = 0ull;
+        }
+    } else if (INTER) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            t.a[i] = mul2(both(c[i]), gain[i]);
+            t.b[i] = mul2(pack2(-s[i], s[i]), swapped(gain[i]));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint64_t cc = pack2(c[2 * i], c[2 * i + 1]), ss = pack2(s[2 * i], s[2 * i + 1]);
+            t.a[i] = mul2(cc, gain[i]);
+            t.a[4 + i] = mul2(cc, gain[4 + i]);
+            t.b[i] = mul2(pack2(-s[2 * i], -s[2 * i + 1]), gain[4 + i]);
+            t.b[4 + i] = mul2(ss, gain[i]);
+        }
+    }
+}
+template <bool INTER>
+__device__ __forceinline__ uint64_t partner(const uint64_t* v, int i) { return INTER ? swapped(v[i]) : v[i ^ 4]; }
 
 // Vector form: rot and hd multiples of 16, hd up to 512, everything 16-byte aligned.
 template <class T, bool INTER, bool APPEND>
-__global__ void __launch_bounds__(kThreads, 2) qk_norm_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(kThreads, kForwardCtas) qk_norm_kernel(const NormArgs a) {
     pdl_wait();
     pdl_trigger();
     const int total = a.part[0].slots + a.part[1].slots + a.part[2].slots;
@@ -111,56 +165,344 @@ __global__ void __launch_bounds__(kThreads, 2) qk_norm_kernel(const NormArgs a) 
     live = live && u < a.hd / 16;
     const bool rotates = u < a.rot / 16;
     const int e0 = rotates && !INTER ? u * 8 : u * 16, e1 = rotates && !INTER ? a.rot / 2 + u * 8 : u * 16 + 8;
-    Unit<T> gain{};
-    if (live && part < 2) load_unit(gain, static_cast<const T*>(p.gain) + e0, static_cast<const T*>(p.gain) + e1);
-    float c[8], sn[8];
+    const float inv_hd = 1.f / (float)a.hd;
+    const T* from = static_cast<const T*>(p.x) + row * p.x_row;
+    Turn turn;
     for (int i0 = 0; i0 < a.per; i0 += kBatch) {
         Unit<T> x[kBatch];
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
             const int h = s + (i0 + k) * p.slots;
             x[k] = Unit<T>{};
-            if (live && h < p.heads) {
-                const T* from = head_at<T>(p.x, row, p.x_row, h, p.x_head);
-                load_unit(x[k], from + e0, from + e1);
-            }
+            if (live && h < p.heads) load_unit(x[k], from + h * p.x_head + e0, from + h * p.x_head + e1);
         }
-        if (i0 == 0 && rotates && live) {
+        if (i0 == 0 && live && part < 2) {
+            Unit<T> g;
+            load_unit(g, static_cast<const T*>(p.gain) + e0, static_cast<const T*>(p.gain) + e1);
+            float c[8], sn[8];
+            if (rotates) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) pair_turn(pos, a.phase[u * 8 + j], 1.f, a.magnitude, c[j], sn[j]);
+                for (int j = 0; j < 8; ++j) pair_turn(pos, a.phase[u * 8 + j], 1.f, a.magnitude, c[j], sn[j]);
+            }
+            uint64_t gain[8];
+            values(g, gain);
+            make_turn<INTER>(turn, rotates, c, sn, gain);
         }
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
             const int h = s + (i0 + k) * p.slots;
-            float v[16];
+            uint64_t v[8], sq = 0ull;
             values(x[k], v);
-            float sum = 0.f;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) sum = fmaf(v[e], v[e], sum);
-            sum = head_sum(sum, a.lanes);
+            for (int i = 0; i < 8; ++i) sq = fma2(v[i], v[i], sq);
+            const float sum = head_sum(sum2(sq), a.lanes);
             if (!live || h >= p.heads) continue;
             T* to = out_at<T, APPEND>(a, p, part, row, h, slot);
             if (APPEND && !to) continue;
             if (!APPEND || part < 2) {
-                const float r = inv_rms(sum, a.hd, a.eps);
-                float w[16];
-                values(gain, w);
+                const uint64_t r = both(inverse_rms(sum, inv_hd, a.eps));
+                uint64_t y[8];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) v[e] = v[e] * r * w[e];
+                for (int i = 0; i < 8; ++i) y[i] = mul2(v[i], turn.a[i]);
                 if (rotates) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float v0 = v[first_of<INTER>(j)], v1 = v[second_of<INTER>(j)];
-                        v[first_of<INTER>(j)] = v0 * c[j] - v1 * sn[j];
-                        v[second_of<INTER>(j)] = v1 * c[j] + v0 * sn[j];
-                    }
+                    for (int i = 0; i < 8; ++i) y[i] = fma2(partner<INTER>(v, i), turn.b[i], y[i]);
                 }
 #pragma unroll
-                for (int i = 0; i < 8; ++i) set2(x[k], i, v[2 * i], v[2 * i + 1]);
+                for (int i = 0; i < 8; ++i) y[i] = mul2(y[i], r);
+                put(x[k], y);
             }
             store_unit(x[k], to + e0, to + e1);
         }
     }
+}
+
+// Sums of gain gradients: a thread's pairs to their places in its group's row; the groups' rows added up in order
+__device__ __forceinline__ void leave(float* row, const uint64_t* acc, int e0, int e1) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float lo, hi;
+        unpack2(acc[i], lo, hi);
+        const int e = i < 4 ? e0 + 2 * i : e1 + 2 * i - 8;
+        row[e] = lo;
+        row[e + 1] = hi;
+    }
+}
+__device__ __forceinline__ void add_up(const float* sums, int groups, const NormArgs& a) {
+    for (int e = threadIdx.x; e < a.hd; e += kThreads) {
+        float v = 0.f;
+        for (int g = 0; g < groups; ++g) v += sums[g * a.hd + e];
+        a.work[(size_t)blockIdx.x * a.hd + e] = v;
+    }
+}
+
+// ---------------- many rows
+// A warp has the heads of one part of a row after the other, 32 / LANES heads at a time, and copies its units ahead into shared memory, kStages
+// deep and across rows, so that as much as a load's latency asks for is always under way; a thread reads only what it
+// copied itself, so its own wait is enough. A row's cosines are worked out once per warp: a unit's eight pairs are shared out
+// among the threads that have the same unit of different heads.
+constexpr int kStages = 4;
+constexpr int kStreamLeast = 8;         // iterations of a warp per CTA of an SM
+
+__device__ __forceinline__ void copy16(uint32_t to, const void* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// One thread's ring of units: NA arrays (x, or x and dy), kStages deep; pieces of 16 bytes, a warp's side by side.
+template <class T, int NA>
+struct Ring {
+    static constexpr int P = sizeof(T);             // pieces of a unit
+    static constexpr uint32_t BYTES = kStages * NA * P * 512;      // of a warp
+    uint32_t base;                                  // this thread's first piece
+    __device__ __forceinline__ void copy(int stage, int array, const T* p0, const T* p1) const {
+        const uint32_t to = base + (stage * NA + array) * (P * 512);
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+            copy16(to + i * 512, reinterpret_cast<const char*>(i < P / 2 ? p0 : p1) + (i % (P / 2)) * 16);
+    }
+    __device__ __forceinline__ void read(int stage, int array, Unit<T>& u) const {
+        const uint32_t at = base + (stage * NA + array) * (P * 512);
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(u.v[i].x), "=r"(u.v[i].y), "=r"(u.v[i].z), "=r"(u.v[i].w) : "r"(at + i * 512) : "memory");
+    }
+};
+
+// Cosines and sines of the eight pairs of a thread's unit at `pos`: the G threads that have the unit work out 8 / G each.
+template <int LANES>
+struct Pairs {
+    static constexpr int G = 32 / LANES, M = G >= 8 ? 1 : 8 / G;
+    uint64_t phase[M];
+    __device__ __forceinline__ void load(const uint64_t* all, int u, int group, bool rotates) {
+#pragma unroll
+        for (int m = 0; m < M; ++m) phase[m] = rotates ? all[u * 8 + (m * G + group) % 8] : 0ull;
+    }
+    __device__ __forceinline__ void at(long long pos, float magnitude, int u, float* c, float* s) const {
+        float cm[M], sm[M];
+#pragma unroll
+        for (int m = 0; m < M; ++m) pair_turn(pos, phase[m], 1.f, magnitude, cm[m], sm[m]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int from = u + LANES * (j % G);
+            c[j] = __shfl_sync(0xffffffffu, cm[j / G], from);
+            s[j] = __shfl_sync(0xffffffffu, sm[j / G], from);
+        }
+    }
+};
+template <int LANES>
+__device__ __forceinline__ float sum_of_head(float v) {
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// f(row, head of this thread, whether it is there, stage, issue) for the warp's part of the list of all (row, 32 / LANES heads),
+// which the part's warps share evenly; next(row) before the first of a row. NA arrays, whose units begin at elements e0 and e1.
+template <class T, int NA, int LANES, class Next, class F>
+__device__ __forceinline__ void each_unit(const NormArgs& a, const Part& p, int wid, int warps, const Ring<T, NA>& ring, int group, bool mine, int e0, int e1,
+                                          Next next, F f) {
+    constexpr int G = 32 / LANES;
+    const int iters = (p.heads + G - 1) / G;
+    const long long all = (long long)a.rows * iters;
+    const long long n0 = all * wid / warps;
+    int left_i = (int)(all * (wid + 1) / warps - n0), left = left_i;
+    int row = (int)(n0 / iters), h = (int)(n0 - (long long)row * iters) * G + group;
+    int row_i = row, h_i = h, stage_i = 0, stage = 0;
+    auto issue = [&]() {
+        if (left_i > 0) {
+            --left_i;
+            if (mine && h_i < p.heads) {
+                const T* x = head_at<T>(p.x, row_i, p.x_row, h_i, p.x_head);
+                ring.copy(stage_i, 0, x + e0, x + e1);
+                if constexpr (NA == 2) {
+                    const T* d = head_at<T>(p.dy, row_i, p.dy_row, h_i, p.dy_head);
+                    ring.copy(stage_i, 1, d + e0, d + e1);
+                }
+            }
+            h_i += G;
+            if (h_i - group >= p.heads) {
+                h_i = group;
+                ++row_i;
+            }
+        }
+        copies_commit();
+        stage_i = stage_i + 1 == kStages ? 0 : stage_i + 1;
+    };
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i) issue();
+    for (; left > 0; ++row, h = group) {
+        next(row);
+        for (; h - group < p.heads && left > 0; h += G, --left) {
+            copies_wait<kStages - 2>();
+            f(row, h, mine && h < p.heads, stage, issue);
+            stage = stage + 1 == kStages ? 0 : stage + 1;
+        }
+    }
+    copies_wait<0>();
+}
+
+// CTAs of a part, its number among them, and what a thread has of its heads.
+struct StreamPlace {
+    int part, wid, warps, u, group, e0, e1;
+    bool mine, rotates;
+};
+template <int LANES, bool INTER>
+__device__ __forceinline__ StreamPlace stream_place(const NormArgs& a) {
+    StreamPlace y;
+    y.part = (int)blockIdx.x >= a.part[0].blocks;
+    const int lane = threadIdx.x & 31;
+    y.wid = ((int)blockIdx.x - (y.part ? a.part[0].blocks : 0)) * (kThreads / 32) + (threadIdx.x >> 5);
+    y.warps = a.part[y.part].blocks * (kThreads / 32);
+    y.u = lane % LANES;
+    y.group = lane / LANES;
+    y.mine = y.u < a.hd / 16;
+    y.rotates = y.u < a.rot / 16;
+    y.e0 = y.rotates && !INTER ? y.u * 8 : y.u * 16;
+    y.e1 = y.rotates && !INTER ? a.rot / 2 + y.u * 8 : y.u * 16 + 8;
+    return y;
+}
+
+template <class T, bool INTER, int LANES>
+__global__ void __launch_bounds__(kThreads, kStreamCtas<T>) qk_norm_stream_kernel(const NormArgs a) {
+    extern __shared__ __align__(16) uint8_t smem[];
+    pdl_wait();
+    pdl_trigger();
+    const StreamPlace y = stream_place<LANES, INTER>(a);
+    const Part& p = a.part[y.part];
+    const Ring<T, 1> ring{(uint32_t)__cvta_generic_to_shared(smem) + (threadIdx.x >> 5) * Ring<T, 1>::BYTES + (threadIdx.x & 31) * 16};
+    Unit<T> gain{};
+    if (y.mine) load_unit(gain, static_cast<const T*>(p.gain) + y.e0, static_cast<const T*>(p.gain) + y.e1);
+    Pairs<LANES> pairs;
+    pairs.load(a.phase, y.u, y.group, y.rotates);
+    const float inv_hd = 1.f / (float)a.hd;
+    int pos = 0;
+    bool begun = false;
+    Turn turn;
+    each_unit<T, 1, LANES>(a, p, y.wid, y.warps, ring, y.group, y.mine, y.e0, y.e1,
+        [&](int row) {
+            uint64_t g[8];
+            float c[8], s[8];
+            if (a.positions) {
+                if (!begun) pos = a.positions[row];
+                begun = true;
+            }
+            pairs.at(pos, a.magnitude, y.u, c, s);
+            if (a.positions && row + 1 < a.rows) pos = a.positions[row + 1];     // (a row ahead)
+            values(gain, g);
+            make_turn<INTER>(turn, y.rotates, c, s, g);
+        },
+        [&](int row, int h, bool there, int stage, auto issue) {
+            Unit<T> x{};
+            if (there) ring.read(stage, 0, x);
+            issue();
+            uint64_t v[8], sq = 0ull;
+            values(x, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sq = fma2(v[i], v[i], sq);
+            const uint64_t r = both(inverse_rms(sum_of_head<LANES>(sum2(sq)), inv_hd, a.eps));
+            uint64_t out[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) out[i] = mul2(v[i], turn.a[i]);
+            if (y.rotates) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) out[i] = fma2(partner<INTER>(v, i), turn.b[i], out[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) out[i] = mul2(out[i], r);
+            put(x, out);
+            T* to = static_cast<T*>(p.out) + row * p.out_row + h * p.out_head;
+            if (there) store_unit(x, to + y.e0, to + y.e1);
+        });
+}
+
+// R^T of a unit's pairs: y_i = z_i C_i + z_partner(i) S_i
+template <bool INTER>
+__device__ __forceinline__ void turn_back(uint64_t* z, const float* c, const float* s) {
+    if (INTER) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] = fma2(swapped(z[i]), pack2(s[i], -s[i]), mul2(z[i], both(c[i])));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint64_t cc = pack2(c[2 * i], c[2 * i + 1]), ss = pack2(s[2 * i], s[2 * i + 1]), ns = pack2(-s[2 * i], -s[2 * i + 1]);
+            const uint64_t z0 = z[i], z1 = z[4 + i];
+            z[i] = fma2(z1, ss, mul2(z0, cc));
+            z[4 + i] = fma2(z0, ns, mul2(z1, cc));
+        }
+    }
+}
+
+template <class T, bool INTER, int LANES>
+__global__ void __launch_bounds__(kThreads, kBackwardCtas) qk_norm_backward_stream_kernel(const NormArgs a) {
+    extern __shared__ __align__(16) uint8_t smem[];
+    pdl_wait();
+    pdl_trigger();
+    const StreamPlace y = stream_place<LANES, INTER>(a);
+    const Part& p = a.part[y.part];
+    const Ring<T, 2> ring{(uint32_t)__cvta_generic_to_shared(smem) + (threadIdx.x >> 5) * Ring<T, 2>::BYTES + (threadIdx.x & 31) * 16};
+    uint64_t w[8], acc[8];
+    {
+        Unit<T> g{};
+        if (y.mine) load_unit(g, static_cast<const T*>(p.gain) + y.e0, static_cast<const T*>(p.gain) + y.e1);
+        values(g, w);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i] = 0ull;
+    Pairs<LANES> pairs;
+    pairs.load(a.phase, y.u, y.group, y.rotates);
+    const float inv_hd = 1.f / (float)a.hd;
+    int pos = 0;
+    bool begun = false;
+    float c[8], s[8];
+    each_unit<T, 2, LANES>(a, p, y.wid, y.warps, ring, y.group, y.mine, y.e0, y.e1,
+        [&](int row) {
+            if (a.positions) {
+                if (!begun) pos = a.positions[row];
+                begun = true;
+            }
+            pairs.at(pos, a.magnitude, y.u, c, s);
+            if (a.positions && row + 1 < a.rows) pos = a.positions[row + 1];     // (a row ahead)
+        },
+        [&](int row, int h, bool there, int stage, auto issue) {
+            Unit<T> x{}, d{};
+            if (there) {
+                ring.read(stage, 0, x);
+                ring.read(stage, 1, d);
+            }
+            issue();
+            uint64_t v[8], z[8], sq = 0ull, ax = 0ull;
+            values(x, v);
+            values(d, z);
+            if (y.rotates) turn_back<INTER>(z, c, s);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                sq = fma2(v[i], v[i], sq);
+                ax = fma2(mul2(z[i], w[i]), v[i], ax);
+            }
+            const float all = sum_of_head<LANES>(sum2(sq)), dot = sum_of_head<LANES>(sum2(ax));
+            if (!there) return;
+            const float r = inverse_rms(all, inv_hd, a.eps);
+            const uint64_t rr = both(r), f = both(-(r * r * (dot * inv_hd)));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint64_t n = mul2(v[i], rr);      // x r
+                acc[i] = fma2(z[i], n, acc[i]);
+                v[i] = fma2(n, f, mul2(mul2(z[i], w[i]), rr));
+            }
+            put(x, v);
+            T* to = static_cast<T*>(p.out) + row * p.out_row + h * p.out_head;
+            store_unit(x, to + y.e0, to + y.e1);
+        });
+    // the CTA's sums in the order of its warps and their groups, over the rings (whose copies have all landed)
+    constexpr int groups = kThreads / LANES;
+    float* sums = reinterpret_cast<float*>(smem);
+    __syncthreads();
+    if (y.mine) leave(sums + (threadIdx.x / LANES) * a.hd, acc, y.e0, y.e1);
+    __syncthreads();
+    add_up(sums, groups, a);
 }
 
 // Any hd up to 1024, rot, strides and alignment: a warp per head, which a lane reads twice.
@@ -207,7 +549,7 @@ __global__ void __launch_bounds__(kThreads) qk_norm_any_kernel(const NormArgs a)
 // Backward. A CTA has heads of one part and goes through rows a grid's width apart; every thread keeps the gain
 // gradients of its 16 elements, which the CTA adds up at the end in a fixed order and leaves in its row of `work`.
 template <class T, bool INTER>
-__global__ void __launch_bounds__(kThreads, 2) qk_norm_backward_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(kThreads, kBackwardCtas) qk_norm_backward_kernel(const NormArgs a) {
     constexpr int B = sizeof(T) == 2 ? 2 : 1;       // heads in flight
     extern __shared__ float sums[];                 // [groups][hd]
     pdl_wait();
@@ -218,11 +560,14 @@ __global__ void __launch_bounds__(kThreads, 2) qk_norm_backward_kernel(const Nor
     const int u = threadIdx.x & (a.lanes - 1), group = threadIdx.x / a.lanes;
     const bool mine = u < a.hd / 16, rotates = u < a.rot / 16;
     const int e0 = rotates && !INTER ? u * 8 : u * 16, e1 = rotates && !INTER ? a.rot / 2 + u * 8 : u * 16 + 8;
-    Unit<T> gain{};
-    if (mine) load_unit(gain, static_cast<const T*>(p.gain) + e0, static_cast<const T*>(p.gain) + e1);
-    float acc[16];
+    uint64_t w[8], acc[8];
+    {
+        Unit<T> g{};
+        if (mine) load_unit(g, static_cast<const T*>(p.gain) + e0, static_cast<const T*>(p.gain) + e1);
+        values(g, w);
+    }
 #pragma unroll
-    for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+    for (int i = 0; i < 8; ++i) acc[i] = 0ull;
     const float inv_hd = 1.f / (float)a.hd;
     const long long items = (long long)a.rows * p.slots;
     for (long long base = (long long)bid * groups; base < items; base += (long long)p.blocks * groups) {
@@ -231,7 +576,8 @@ __global__ void __launch_bounds__(kThreads, 2) qk_norm_backward_kernel(const Nor
         const int s = (int)(item - row * p.slots);
         const bool live = item < items && mine;
         const long long pos = live && a.positions ? a.positions[row] : 0;
-        float c[8], sn[8];
+        // of the unit's pairs: cosines, and sines with the sign that each element's partner has in R^T
+        uint64_t c[INTER ? 8 : 4], sn[INTER ? 8 : 4];
         for (int i0 = 0; i0 < a.per; i0 += B) {
             Unit<T> x[B], d[B];
 #pragma unroll
@@ -246,56 +592,58 @@ __global__ void __launch_bounds__(kThreads, 2) qk_norm_backward_kernel(const Nor
                 }
             }
             if (i0 == 0 && rotates && live) {
+                float cf[8], sf[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) pair_turn(pos, a.phase[u * 8 + j], 1.f, a.magnitude, c[j], sn[j]);
+                for (int j = 0; j < 8; ++j) pair_turn(pos, a.phase[u * 8 + j], 1.f, a.magnitude, cf[j], sf[j]);
+#pragma unroll
+                for (int j = 0; j < (INTER ? 8 : 4); ++j) {
+                    c[j] = INTER ? both(cf[j]) : pack2(cf[2 * j], cf[2 * j + 1]);
+                    sn[j] = INTER ? pack2(sf[j], -sf[j]) : pack2(sf[2 * j], sf[2 * j + 1]);
+                }
             }
 #pragma unroll
             for (int k = 0; k < B; ++k) {
                 const int h = s + (i0 + k) * p.slots;
-                float v[16], z[16], w[16];
+                uint64_t v[8], z[8], sq = 0ull, ax = 0ull;
                 values(x[k], v);
                 values(d[k], z);
-                values(gain, w);
                 if (rotates && live) {
+                    if (INTER) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float z0 = z[first_of<INTER>(j)], z1 = z[second_of<INTER>(j)];
-                        z[first_of<INTER>(j)] = z0 * c[j] + z1 * sn[j];
-                        z[second_of<INTER>(j)] = z1 * c[j] - z0 * sn[j];
+                        for (int i = 0; i < 8; ++i) z[i] = fma2(swapped(z[i]), sn[i], mul2(z[i], c[i]));
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const uint64_t z0 = z[i], z1 = z[4 + i];
+                            z[i] = fma2(z1, sn[i], mul2(z0, c[i]));
+                            z[4 + i] = fma2(z1, c[i], mul2(z0, mul2(sn[i], both(-1.f))));
+                        }
                     }
                 }
-                float sq = 0.f, ax = 0.f;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    sq = fmaf(v[e], v[e], sq);
-                    ax = fmaf(z[e] * w[e], v[e], ax);
+                for (int i = 0; i < 8; ++i) {
+                    sq = fma2(v[i], v[i], sq);
+                    ax = fma2(mul2(z[i], w[i]), v[i], ax);
                 }
-                sq = head_sum(sq, a.lanes);
-                ax = head_sum(ax, a.lanes);
+                const float all = head_sum(sum2(sq), a.lanes), dot = head_sum(sum2(ax), a.lanes);
                 if (!live || h >= p.heads) continue;
-                const float r = inv_rms(sq, a.hd, a.eps), f = r * r * ax * inv_hd;
+                const float r = inverse_rms(all, inv_hd, a.eps);
+                const uint64_t rr = both(r), f = both(-(r * r * (dot * inv_hd)));
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    acc[e] = fmaf(z[e], v[e] * r, acc[e]);
-                    v[e] = r * (z[e] * w[e] - v[e] * f);
+                for (int i = 0; i < 8; ++i) {
+                    const uint64_t n = mul2(v[i], rr);      // x r
+                    acc[i] = fma2(z[i], n, acc[i]);
+                    v[i] = fma2(n, f, mul2(mul2(z[i], w[i]), rr));
                 }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) set2(x[k], i, v[2 * i], v[2 * i + 1]);
+                put(x[k], v);
                 T* to = static_cast<T*>(p.out) + row * p.out_row + h * p.out_head;
                 store_unit(x[k], to + e0, to + e1);
             }
         }
     }
-    if (mine) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) sums[group * a.hd + (e < 8 ? e0 + e : e1 + e - 8)] = acc[e];
-    }
+    if (mine) leave(sums + group * a.hd, acc, e0, e1);
     __syncthreads();
-    for (int e = threadIdx.x; e < a.hd; e += kThreads) {
-        float v = 0.f;
-        for (int g = 0; g < groups; ++g) v += sums[g * a.hd + e];
-        a.work[(size_t)blockIdx.x * a.hd + e] = v;
-    }
+    add_up(sums, groups, a);
 }
 
 // The same for any hd up to 1024, rot, strides and alignment: a warp per head, its gain gradients in shared memory (a
@@ -361,17 +709,14 @@ __global__ void __launch_bounds__(kThreads) qk_norm_backward_any_kernel(const No
         for (int e = a.rot + lane; e < a.hd; e += 32) put(e, to_f(dy[e]));
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < a.hd; e += kThreads) {
-        float v = 0.f;
-        for (int g = 0; g < warps; ++g) v += sums[g * a.hd + e];
-        a.work[(size_t)blockIdx.x * a.hd + e] = v;
-    }
+    add_up(sums, warps, a);
 }
 
-// The CTAs' sums of a part's gain gradients, in their order: 32 elements per CTA, eight warps of which each adds up
-// every eighth row.
-__global__ void __launch_bounds__(kThreads) qk_norm_gain_kernel(const NormArgs a) {
-    __shared__ float sums[kThreads / 32][32];
+// The CTAs' sums of a part's gain gradients, in their order: 32 elements per CTA, 32 warps of which each adds up every 32nd
+// row, ten at most at a time (with eight warps 3 us more for 302 rows).
+constexpr int kGainThreads = 1024;
+__global__ void __launch_bounds__(kGainThreads) qk_norm_gain_kernel(const NormArgs a) {
+    __shared__ float sums[kGainThreads / 32][32];
     pdl_wait();
     pdl_trigger();
     const Part& p = a.part[blockIdx.y];
@@ -379,14 +724,14 @@ __global__ void __launch_bounds__(kThreads) qk_norm_gain_kernel(const NormArgs a
     const float* rows = a.work + (size_t)(blockIdx.y ? a.part[0].blocks : 0) * a.hd;
     float v = 0.f;
     if (e < a.hd) {
-#pragma unroll 8
-        for (int i = warp; i < p.blocks; i += kThreads / 32) v += rows[(size_t)i * a.hd + e];
+#pragma unroll 10
+        for (int i = warp; i < p.blocks; i += kGainThreads / 32) v += rows[(size_t)i * a.hd + e];
     }
     sums[warp][lane] = v;
     __syncthreads();
     if (warp == 0 && e < a.hd) {
         v = 0.f;
-        for (int w = 0; w < kThreads / 32; ++w) v += sums[w][lane];
+        for (int w = 0; w < kGainThreads / 32; ++w) v += sums[w][lane];
         p.dgain[e] = v;
     }
 }
@@ -412,8 +757,50 @@ void plan_threads(NormArgs& a, int num_sms) {
     }
 }
 
+// Whether the kernels for many rows take a call: every warp that the GPU holds has some iterations of 32 / lanes heads.
+bool streams(const NormArgs& a, bool vec, int num_sms) {
+    if (!vec || a.hd <= 32 || a.hd > 256) return false;
+    const int lanes = a.hd <= 64 ? 4 : a.hd <= 128 ? 8 : 16, many = 32 / lanes;
+    const long long work = (long long)a.rows * ((a.part[0].heads + many - 1) / many + (a.part[1].heads + many - 1) / many);
+    return work >= (long long)kStreamLeast * num_sms * (kThreads / 32);
+}
+// CTAs of the parts, in proportion to their work, of `most`
+void share_blocks(NormArgs& a, const long long* need, long long most) {
+    const long long all = std::max<long long>(need[0] + need[1], 1);
+    for (int i = 0; i < 2; ++i)
+        a.part[i].blocks = (int)(all <= most ? need[i] : need[i] ? std::max<long long>(1, (most - 1) * need[i] / all) : 0);
+}
+template <class T, bool INTER, int LANES>
+cudaError_t launch_stream(NormArgs& a, bool backward, int num_sms, cudaStream_t s) {
+    static PerDeviceOnce once;
+    auto fwd = qk_norm_stream_kernel<T, INTER, LANES>;
+    auto bwd = qk_norm_backward_stream_kernel<T, INTER, LANES>;
+    constexpr int warps = kThreads / 32, bytes1 = warps * Ring<T, 1>::BYTES, ring2 = warps * Ring<T, 2>::BYTES;
+    constexpr int sums = kThreads / LANES * LANES * 16 * 4, bytes2 = ring2 > sums ? ring2 : sums;
+    cudaError_t e = once([&] {
+        cudaError_t e = cudaFuncSetAttribute(fwd, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes1);
+        return e == cudaSuccess ? cudaFuncSetAttribute(bwd, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes2) : e;
+    });
+    if (e != cudaSuccess) return e;
+    constexpr int many = 32 / LANES;
+    long long need[2];
+    // iterations, and one for a row's cosines; CTAs by their shares
+    for (int i = 0; i < 2; ++i) need[i] = a.part[i].heads ? (long long)a.rows * ((a.part[i].heads + many - 1) / many + 1) : 0;
+    const int most = std::min((backward ? kBackwardCtas : kStreamCtas<T>) * num_sms, kWorkRows);
+    share_blocks(a, need, most);
+    const dim3 grid(a.part[0].blocks + a.part[1].blocks);
+    return backward ? launch_kernel(true, bwd, grid, dim3(kThreads), bytes2, s, a) : launch_kernel(true, fwd, grid, dim3(kThreads), bytes1, s, a);
+}
+template <class T, bool INTER>
+cudaError_t stream_rows(NormArgs& a, bool backward, int num_sms, cudaStream_t s) {
+    if (a.hd <= 64) return launch_stream<T, INTER, 4>(a, backward, num_sms, s);
+    return a.hd <= 128 ? launch_stream<T, INTER, 8>(a, backward, num_sms, s) : launch_stream<T, INTER, 16>(a, backward, num_sms, s);
+}
+
 template <class T, bool INTER, bool APPEND>
 cudaError_t launch_forward(NormArgs& a, bool vec, int num_sms, cudaStream_t s) {
+    if constexpr (!APPEND)
+        if (streams(a, vec, num_sms)) return stream_rows<T, INTER>(a, false, num_sms, s);
     plan_threads(a, num_sms);
     if (vec) {
         const long long threads = (long long)a.rows * (a.part[0].slots + a.part[1].slots + a.part[2].slots) * a.lanes;
@@ -435,21 +822,23 @@ cudaError_t forward(NormArgs& a, int dtype, int layout, bool vec, int num_sms, c
 
 template <class T, bool INTER>
 cudaError_t launch_backward(NormArgs& a, bool vec, int num_sms, cudaStream_t s) {
+    cudaError_t e;
+    const dim3 join((a.hd + 31) / 32, a.part[1].heads ? 2 : 1);
+    if (streams(a, vec, num_sms)) {
+        e = stream_rows<T, INTER>(a, true, num_sms, s);
+        return e == cudaSuccess ? launch_kernel(true, qk_norm_gain_kernel, join, dim3(kGainThreads), 0, s, a) : e;
+    }
     plan_threads(a, num_sms);
     const int groups = vec ? kThreads / a.lanes : kThreads / 32;
     long long need[2];
     for (int i = 0; i < 2; ++i) need[i] = ((long long)a.rows * (vec ? a.part[i].slots : a.part[i].heads) + groups - 1) / groups;
-    // CTAs that are resident at once, shared by the parts' heads; a part with heads has one at least
-    const long long most = std::min(2 * num_sms, kWorkRows), all = std::max<long long>(need[0] + need[1], 1);
-    const bool fits = all <= most;
-    for (int i = 0; i < 2; ++i)
-        a.part[i].blocks = (int)(fits ? need[i] : need[i] ? std::max<long long>(1, (most - 1) * need[i] / all) : 0);
+    share_blocks(a, need, std::min(kBackwardCtas * num_sms, kWorkRows));     // CTAs that are resident at once
     const dim3 grid(a.part[0].blocks + a.part[1].blocks);
     const size_t bytes = (size_t)groups * a.hd * sizeof(float);     // 16 KB at most; 32 KB for the other kernel
-    cudaError_t e = vec ? launch_kernel(true, qk_norm_backward_kernel<T, INTER>, grid, dim3(kThreads), bytes, s, a)
+    e = vec ? launch_kernel(true, qk_norm_backward_kernel<T, INTER>, grid, dim3(kThreads), bytes, s, a)
                         : launch_kernel(true, qk_norm_backward_any_kernel<T, INTER>, grid, dim3(kThreads), bytes, s, a);
     if (e != cudaSuccess) return e;
-    return launch_kernel(true, qk_norm_gain_kernel, dim3((a.hd + 31) / 32, a.part[1].heads ? 2 : 1), dim3(kThreads), 0, s, a);
+    return launch_kernel(true, qk_norm_gain_kernel, join, dim3(kGainThreads), 0, s, a);
 }
 
 // What both directions ask of their arguments; nullptr: nothing is wrong.

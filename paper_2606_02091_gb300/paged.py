@@ -145,34 +145,32 @@ def rope(x, positions, phase, out, *, layout="half", magnitude=1.0, backward=Fal
                                    _lib.DFLARE_BF16 if dtype is _BF16 else _lib.DFLARE_F32, _stream(stream, dev)))
 
 
+def _heads(name, t, shape, dtype, device):
+    """Address and strides of [rows][heads][head_dim] heads."""
+    if t.dtype is not dtype or t.get_device() != device:
+        _typed(name, t, dtype, device)
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    row, head, one = t.stride()
+    if one != 1 and shape[2] > 1:
+        raise ValueError(f"{name}: the elements of a head must be adjacent")
+    return t.data_ptr(), row, head
+
+
 def _qk_part(name, x, dy, out, gain, dgain, rows, hd, dtype, device):
     """The struct of one call's queries or keys: [rows][heads][head_dim] tensors and their gain."""
-    g = _lib.QkHeads()
-    if x.dim() != 3 or x.shape[0] != rows or x.shape[2] != hd:
-        raise ValueError(f"{name} must be [{rows}][heads][{hd}], got {list(x.shape)}")
-    for field, t in (("x", x), ("out", out), ("dy", dy)):
-        if t is None:
-            continue
-        what = name if field == "x" else f"{name}'s " + ("result" if field == "out" else "gradient")
-        _typed(what, t, dtype, device)
-        if t.shape != x.shape:
-            raise ValueError(f"{what} must be {list(x.shape)}, got {list(t.shape)}")
-        row, head, one = t.stride()
-        if one != 1 and hd > 1:
-            raise ValueError("the elements of a head must be adjacent")
-        setattr(g, field, t.data_ptr())
-        setattr(g, field + "_row", row)
-        setattr(g, field + "_head", head)
-    g.gain = _line(f"{name}'s gain", gain, dtype, hd, device)
-    if dgain is not None:
-        g.dgain = _line(f"{name}'s gain gradient", dgain, _F32, hd, device)
-    g.heads = x.shape[1]
-    return g
+    shape = x.shape
+    if x.dim() != 3 or shape[0] != rows or shape[2] != hd:
+        raise ValueError(f"{name} must be [{rows}][heads][{hd}], got {list(shape)}")
+    return _lib.QkHeads(*_heads(name, x, shape, dtype, device), *((None, 0, 0) if dy is None else _heads(name + "'s gradient", dy, shape, dtype, device)),
+                        *_heads(name + "'s result", out, shape, dtype, device), _line(name + "'s gain", gain, dtype, hd, device),
+                        None if dgain is None else _line(name + "'s gain gradient", dgain, _F32, hd, device), shape[1])
 
 
 def _line(name, t, dtype, numel, device):
     """A tensor of `numel` elements without gaps; its address."""
-    _typed(name, t, dtype, device)
+    if t.dtype is not dtype or t.get_device() != device:
+        _typed(name, t, dtype, device)
     if t.numel() != numel or not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous and hold {numel} elements, got {list(t.shape)}")
     return t.data_ptr()
