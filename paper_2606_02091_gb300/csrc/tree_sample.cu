@@ -78,6 +78,22 @@ __device__ __forceinline__ Sum warp_upto(Sum s) {
     return s;
 }
 __device__ __forceinline__ double value(const Sum& s) { return (double)s.h + (double)s.l; }
+__device__ __forceinline__ Sum split(double v) { return {(float)v, (float)(v - (double)(float)v)}; }
+__device__ __forceinline__ bool above(const Sum& a, const Sum& b) { return __fadd_rn(__fsub_rn(a.h, b.h), __fsub_rn(a.l, b.l)) > 0.f; }
+__device__ __forceinline__ Sum from_lane(const Sum& s, int lane) { return {__shfl_sync(0xffffffffu, s.h, lane), __shfl_sync(0xffffffffu, s.l, lane)}; }
+// Of parts that lie one after another behind `base`, one per lane of the first `many`: the first at which the running sum passes
+// goal (where rounding hides it, the last with any weight), and base is moved up to it.
+__device__ __forceinline__ int part_of(const Sum& part, int many, const Sum& goal, Sum& base) {
+    const int lane = threadIdx.x & 31;
+    const Sum upto = warp_upto(part);
+    Sum x = base;
+    add(x, upto.h, upto.l);
+    const unsigned past = __ballot_sync(0xffffffffu, lane < many && above(x, goal)), some = __ballot_sync(0xffffffffu, lane < many && part.h > 0.f);
+    const int at = past ? __ffs(past) - 1 : max(31 - __clz(some), 0);
+    const Sum before = from_lane(x, max(at - 1, 0));
+    if (at) base = before;
+    return at;
+}
 
 // The residual that the cluster sums up: of node `at`; F as two numbers; gone: picked tokens that are out of it.
 struct Residual {
@@ -167,6 +183,49 @@ __device__ __forceinline__ Sum sum_of(const Sum* p, uint32_t rank) {
 }
 
 enum { kSum, kLast, kNone };    // what warp 0 asks of the CTA: a residual's sum; the last one, with the token; nothing more
+enum { kGoOn, kSearch, kDone };     // what it found after the cluster's sum: the token is in this CTA's part; nothing more to do
+
+// The token at which the running sum passes goal, in warp w's part [s0, s1) behind base: the CTA's warps sum up sixteenths, and
+// warp 0 goes through one of them, 32 elements at a time.
+__device__ __forceinline__ void find_token(const Residual& r, int s0, int s1, Sum base, const Sum& goal, Sum* of_warp, int32_t* token) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int each = (s1 - s0 + kWarps - 1) / kWarps;
+    const Sum mine = part_sum(r, min(s0 + warp * each, s1), min(s0 + (warp + 1) * each, s1), false);
+    if (lane == 0) of_warp[warp] = mine;
+    __syncthreads();
+    if (warp) return;
+    const int k = part_of(lane < kWarps ? of_warp[lane] : Sum{0.f, 0.f}, kWarps, goal, base);
+    const int end = min(s0 + (k + 1) * each, s1);
+    int found = -1;
+    for (int e0 = min(s0 + k * each, s1); e0 < end; e0 += 128) {
+        float p[4], q[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int e = e0 + i * 32 + lane;
+            p[i] = e < end ? __ldg(r.p + e) : 0.f;
+            q[i] = e < end && r.q ? __ldg(r.q + e) : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int e = e0 + i * 32 + lane;
+            Sum w = {0.f, 0.f};
+            if (e < end && !is_gone(r, e)) add_weight(w, r, p[i], q[i]);
+            const unsigned some = __ballot_sync(0xffffffffu, w.h > 0.f);
+            if (!some) continue;
+            const Sum upto = warp_upto(w);
+            Sum x = base;
+            add(x, upto.h, upto.l);
+            const unsigned past = __ballot_sync(0xffffffffu, above(x, goal)) & some;
+            found = e0 + i * 32 + (past ? __ffs(past) - 1 : 31 - __clz(some));
+            if (past) {
+                if (lane == 0) *token = found;
+                return;
+            }
+            base = from_lane(x, 31);
+        }
+    }
+    if (lane == 0) *token = max(found, 0);
+}
 
 __global__ void __launch_bounds__(kThreads, 2) tree_sample_kernel(const SampleArgs a) {
     __shared__ int32_t up[kMaxNodes], tok[kMaxNodes], first[kMaxNodes], list[kMaxNodes];
@@ -174,35 +233,39 @@ __global__ void __launch_bounds__(kThreads, 2) tree_sample_kernel(const SampleAr
     __shared__ Sum of_warp[2][kWarps];
     __shared__ __align__(8) Sum of_cta[2];
     __shared__ Residual todo;
-    __shared__ int what, steps;
+    __shared__ int what, steps, found, from_warp;
+    __shared__ Sum from_base, goal;
     pdl_wait();
     pdl_trigger();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t rank = cluster_rank(), ctas = cluster_size();
     const int b = blockIdx.x / ctas;
-    const int told = a.n_nodes[b], n = min(max(told, 0), a.n_max);
     const float* target = a.target + (size_t)b * a.n_max * a.vocab;
     const float* draft = a.draft ? a.draft + (size_t)b * a.draft_rows * a.vocab : nullptr;
-    bool bad = told != n, odd = false;
-    for (int i = tid; i < n; i += kThreads) first[i] = n;
+    // (rows past the tree's nodes are fetched with the others, and stay without effect: two trips to memory, not three)
+    const int told = a.n_nodes[b];
+    for (int i = tid; i < a.n_max; i += kThreads) first[i] = a.n_max;
     __syncthreads();
-    for (int i = tid; i < n; i += kThreads) {
+    bool odd = false, twisted = false;
+    for (int i = tid; i < a.n_max; i += kThreads) {
         int p = a.parents[(size_t)b * a.n_max + i];
-        if (i == 0 ? p != -1 : (p < -1 || p >= i)) {
-            bad = true;
-            p = -1;
-        }
         const int x = a.tokens[(size_t)b * a.n_max + i];
         const float r = a.u[(size_t)b * a.n_max + i];
-        const bool in = x >= 0 && x < a.vocab;
-        odd |= i > 0 && !in;
-        up[i] = p;
-        tok[i] = in ? x : -1;
-        u[i] = r > 0.f ? fminf(r, 0x1.fffffep-1f) : 0.f;
+        const bool in = x >= 0 && x < a.vocab, wrong = i == 0 ? p != -1 : (p < -1 || p >= i);
+        if (wrong) p = -1;
         px[i] = p >= 0 && in ? target[(size_t)p * a.vocab + x] : 0.f;
         qx[i] = p >= 0 && in && draft ? draft[(size_t)p * a.vocab + x] : 0.f;
-        if (p >= 0) atomicMin(&first[p], i);
+        up[i] = i < told ? p : -1;
+        tok[i] = in ? x : -1;
+        u[i] = r > 0.f ? fminf(r, 0x1.fffffep-1f) : 0.f;
+        if (i < told) {
+            odd |= i > 0 && !in;
+            twisted |= wrong;
+            if (p >= 0) atomicMin(&first[p], i);
+        }
     }
+    const int n = min(max(told, 0), a.n_max);
+    const bool bad = told != n || twisted;
     if (bad && rank == 0 && a.err) atomicOr(a.err, DFLARE_DEVERR_TREE);
     if (odd && rank == 0 && a.err) atomicOr(a.err, DFLARE_DEVERR_TOKEN);
     if (n == 0) {       // (the same in every CTA of the cluster)
@@ -305,74 +368,42 @@ __global__ void __launch_bounds__(kThreads, 2) tree_sample_kernel(const SampleAr
         }
         cluster_arrive();
         cluster_wait();
-        bool done = false;
         if (warp == 0) {
             const Sum part = lane < (int)ctas ? sum_of(&of_cta[turn & 1], lane) : Sum{0.f, 0.f};
             const Sum upto = warp_upto(part);
-            const Sum all = {__shfl_sync(0xffffffffu, upto.h, 31), __shfl_sync(0xffffffffu, upto.l, 31)};
-            W = value(all);
+            W = value(from_lane(upto, 31));
+            int next = kGoOn;
             if (last) {
                 if (!(W > 0.0) && !again && (r.q || r.n_gone)) {
                     again = true;
+                } else if (!(W > 0.0)) {
+                    next = kDone;
+                    if (rank == 0 && lane == 0) {       // no weight at all
+                        a.next_token[b] = 0;
+                        if (a.err) atomicOr(a.err, DFLARE_DEVERR_TOKEN);
+                    }
                 } else {
-                    done = true;
-                    // the CTA, the warp of it, the lane's elements of that, and the element at which the running sum passes
-                    const double goal = (double)u[0] * W;
-                    unsigned past = __ballot_sync(0xffffffffu, lane < (int)ctas && value(upto) > goal);
-                    const int cta = past ? __ffs(past) - 1 : -1;
-                    if (cta < 0 && rank == 0) {         // no weight at all
+                    const Sum g = split((double)u[0] * W);
+                    Sum base = {0.f, 0.f};
+                    next = part_of(part, (int)ctas, g, base) == (int)rank ? kSearch : kDone;
+                    if (next == kSearch) {
+                        const int w = part_of(lane < kWarps ? of_warp[turn & 1][lane] : Sum{0.f, 0.f}, kWarps, g, base);
                         if (lane == 0) {
-                            a.next_token[b] = 0;
-                            if (a.err) atomicOr(a.err, DFLARE_DEVERR_TOKEN);
-                        }
-                    } else if (cta == (int)rank) {
-                        Sum base = {0.f, 0.f};
-                        const Sum before = {__shfl_sync(0xffffffffu, upto.h, max(cta - 1, 0)), __shfl_sync(0xffffffffu, upto.l, max(cta - 1, 0))};
-                        if (cta) base = before;
-                        const Sum ws = warp_upto(lane < kWarps ? of_warp[turn & 1][lane] : Sum{0.f, 0.f});
-                        Sum x = base;
-                        add(x, ws.h, ws.l);
-                        past = __ballot_sync(0xffffffffu, lane < kWarps && value(x) > goal);
-                        // (rounding: the last warp with any weight)
-                        const unsigned some = __ballot_sync(0xffffffffu, lane < kWarps && of_warp[turn & 1][min(lane, kWarps - 1)].h > 0.f);
-                        const int w = past ? __ffs(past) - 1 : 31 - __clz(some);
-                        const Sum wb = {__shfl_sync(0xffffffffu, x.h, max(w - 1, 0)), __shfl_sync(0xffffffffu, x.l, max(w - 1, 0))};
-                        if (w) base = wb;
-                        const long long f0 = ((long long)rank * kWarps + w) * a.part;
-                        const int s0 = (int)min(f0, (long long)a.vocab), s1 = (int)min(f0 + a.part, (long long)a.vocab);
-                        const int each = (s1 - s0 + 31) / 32, l0 = min(s0 + lane * each, s1), l1 = min(l0 + each, s1);
-                        auto weigh = [&](Sum& s, int e) {
-                            if (!is_gone(r, e)) add_weight(s, r, __ldg(r.p + e), r.q ? __ldg(r.q + e) : 0.f);
-                        };
-                        Sum own = {0.f, 0.f};
-#pragma unroll 8
-                        for (int e = l0; e < l1; ++e) weigh(own, e);
-                        const Sum lanes = warp_upto(own);
-                        x = base;
-                        add(x, lanes.h, lanes.l);
-                        past = __ballot_sync(0xffffffffu, value(x) > goal);
-                        const unsigned any = __ballot_sync(0xffffffffu, own.h > 0.f);
-                        const int l = past ? __ffs(past) - 1 : 31 - __clz(any);
-                        const Sum lb = {__shfl_sync(0xffffffffu, x.h, max(l - 1, 0)), __shfl_sync(0xffffffffu, x.l, max(l - 1, 0))};
-                        if (lane == l) {
-                            Sum s = l ? lb : base;
-                            int token = 0;
-                            for (int e = l0; e < l1; ++e) {
-                                Sum before = s;
-                                weigh(s, e);
-                                if (s.h != before.h || s.l != before.l) token = e;
-                                if (value(s) > goal) break;
-                            }
-                            a.next_token[b] = token;
+                            from_warp = w;
+                            from_base = base;
+                            goal = g;
                         }
                     }
                 }
             }
-            if (lane == 0) what = done;
+            if (lane == 0) found = next;
         }
         __syncthreads();
-        if (last && what) break;
-        __syncthreads();
+        if (found == kSearch) {
+            const long long f0 = ((long long)rank * kWarps + from_warp) * a.part;
+            find_token(r, (int)min(f0, (long long)a.vocab), (int)min(f0 + a.part, (long long)a.vocab), from_base, goal, of_warp[(turn & 1) ^ 1], a.next_token + b);
+        }
+        if (found != kGoOn) break;
     }
     if (rank == 0) {
         if (tid == 0) a.accept_len[b] = steps;
