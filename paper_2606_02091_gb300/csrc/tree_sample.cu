@@ -9,8 +9,9 @@
 // Drafts that were picked and not drawn (no q) have the residual p without the picked tokens before.
 //
 // Decisions hang on sums over the vocabulary: fp32 sums of 150000 terms would move them for one call in a hundred.
-// They are held as pairs of fp32 numbers (Knuth's two-sum, products by a fused multiply-add: 2^-46), as 64-bit
-// arithmetic has 1/64 of the fp32 rate on this GPU.
+// They are held as pairs of fp32 numbers (Knuth's two-sum, products by a fused multiply-add: 2^-46), and so is what the
+// walk holds: 64-bit arithmetic has 1/64 of the fp32 rate on this GPU (64 blocks of 16 over 151936 tokens 54.5 us with it in the last
+// search, 23.7 without).
 //
 // A cluster of CTAs per tree, each with a part of the vocabulary; all of them walk the same tree in step. What a walk asks
 // of a node whose children before it were not asked (u q_x < p_x) is found for all nodes at once while their numbers come
@@ -77,8 +78,20 @@ __device__ __forceinline__ Sum warp_upto(Sum s) {
     }
     return s;
 }
-__device__ __forceinline__ double value(const Sum& s) { return (double)s.h + (double)s.l; }
-__device__ __forceinline__ Sum split(double v) { return {(float)v, (float)(v - (double)(float)v)}; }
+// products and quotients of such numbers, to 2^-44
+__device__ __forceinline__ Sum settled(float h, float l) {
+    const float t = __fadd_rn(h, l);
+    return {t, __fsub_rn(l, __fsub_rn(t, h))};
+}
+__device__ __forceinline__ Sum times(const Sum& a, const Sum& b) {
+    const float p = __fmul_rn(a.h, b.h);
+    return settled(p, __fmaf_rn(a.h, b.l, __fmaf_rn(a.l, b.h, __fmaf_rn(a.h, b.h, -p))));
+}
+__device__ __forceinline__ Sum over(const Sum& a, const Sum& b) {
+    const float q = __fdiv_rn(a.h, b.h);
+    const float rest = __fadd_rn(__fmaf_rn(-q, b.h, a.h), __fmaf_rn(-q, b.l, a.l));
+    return settled(q, __fdiv_rn(rest, b.h));
+}
 __device__ __forceinline__ bool above(const Sum& a, const Sum& b) { return __fadd_rn(__fsub_rn(a.h, b.h), __fsub_rn(a.l, b.l)) > 0.f; }
 __device__ __forceinline__ Sum from_lane(const Sum& s, int lane) { return {__shfl_sync(0xffffffffu, s.h, lane), __shfl_sync(0xffffffffu, s.l, lane)}; }
 // Of parts that lie one after another behind `base`, one per lane of the first `many`: the first at which the running sum passes
@@ -103,12 +116,16 @@ struct Residual {
     const int32_t* gone;
     int n_gone;
 };
-// w = max(0, p - F q) as two numbers added to s; not finite or negative: nothing
-__device__ __forceinline__ void add_weight(Sum& s, const Residual& r, float p, float q) {
-    const float ph = __fmul_rn(r.fh, q), pl = __fmaf_rn(r.fl, q, __fmaf_rn(r.fh, q, -ph));
+// p - F q as two numbers
+__device__ __forceinline__ Sum left_of(float p, float q, float fh, float fl) {
+    const float ph = __fmul_rn(fh, q), pl = __fmaf_rn(fl, q, __fmaf_rn(fh, q, -ph));
     const float d = __fsub_rn(p, ph), b = __fsub_rn(d, p);
-    const float low = __fsub_rn(__fsub_rn(__fsub_rn(p, __fsub_rn(d, b)), __fadd_rn(ph, b)), pl);
-    if (__fadd_rn(d, low) > 0.f) add(s, d, low);
+    return {d, __fsub_rn(__fsub_rn(__fsub_rn(p, __fsub_rn(d, b)), __fadd_rn(ph, b)), pl)};
+}
+// w = max(0, p - F q) added to s; not finite or negative: nothing
+__device__ __forceinline__ void add_weight(Sum& s, const Residual& r, float p, float q) {
+    const Sum w = left_of(p, q, r.fh, r.fl);
+    if (__fadd_rn(w.h, w.l) > 0.f) add(s, w.h, w.l);
 }
 __device__ __forceinline__ bool is_gone(const Residual& r, int e) {
     for (int g = 0; g < r.n_gone; ++g)
@@ -282,7 +299,8 @@ __global__ void __launch_bounds__(kThreads, 2) tree_sample_kernel(const SampleAr
 
     // ---------------- warp 0 walks; the others sum what it asks for. Every CTA of the cluster finds the same.
     int at = 0, i = first[0], walked = 1, turn = 0;
-    double F = 0.0, W = 1.0, Q = 1.0;
+    const Sum one = {1.f, 0.f}, zero = {0.f, 0.f};
+    Sum F = zero, W = one, Q = one;
     bool again = false;         // the last residual was empty: p instead
     if (tid == 0 && rank == 0) a.path[(size_t)b * a.n_max] = 0;
     for (;; ++turn) {
@@ -294,27 +312,30 @@ __global__ void __launch_bounds__(kThreads, 2) tree_sample_kernel(const SampleAr
                     break;
                 }
                 bool keep;
-                double w = 0.0;
+                float w = 0.f;
                 if (i == first[at]) {
                     // u q < p, or u < p where drafts were picked: the sign of an fp32 fused product is exact
                     keep = draft ? fmaf(u[i], qx[i], -px[i]) < 0.f : u[i] < px[i];
                     w = px[i];
                 } else if (draft) {
-                    const double share = Q > 0.0 ? (double)qx[i] / Q : 0.0;
-                    keep = (double)u[i] * share * W < fmax((double)px[i] - F * (double)qx[i], 0.0);
+                    // u (q / Q) W < p - F q, times Q
+                    const Sum rest = left_of(px[i], qx[i], F.h, F.l);
+                    const float uq = __fmul_rn(u[i], qx[i]);
+                    keep = __fadd_rn(rest.h, rest.l) > 0.f;
+                    if (keep && Q.h > 0.f) keep = above(times(settled(rest.h, rest.l), Q), times({uq, __fmaf_rn(u[i], qx[i], -uq)}, W));
                 } else {
                     bool before = false;        // the same token was picked before
                     for (int j = at + 1 + lane; j < i; j += 32) before |= up[j] == at && tok[j] == tok[i];
-                    w = __any_sync(0xffffffffu, before) ? 0.0 : (double)px[i];
-                    keep = (double)u[i] * W < w;
+                    w = __any_sync(0xffffffffu, before) ? 0.f : px[i];
+                    keep = above({w, 0.f}, times(W, {u[i], 0.f}));
                 }
                 if (keep) {
                     at = i;
                     i = first[at];
                     if (lane == 0 && rank == 0) a.path[(size_t)b * a.n_max + walked] = at;
                     ++walked;
-                    F = 0.0;
-                    W = Q = 1.0;
+                    F = zero;
+                    W = Q = one;
                     continue;
                 }
                 int j = n;      // the next child
@@ -323,11 +344,19 @@ __global__ void __launch_bounds__(kThreads, 2) tree_sample_kernel(const SampleAr
                     if (hit) j = j0 + __ffs(hit) - 1;
                 }
                 if (draft) {
-                    if (Q > 0.0) F += W / Q;
-                    if (a.distinct) Q -= (double)qx[i];
+                    if (Q.h > 0.f) {
+                        const Sum more = over(W, Q);
+                        add(F, more.h, more.l);
+                        F = F.h < 3e38f ? settled(F.h, F.l) : Sum{3e38f, 0.f};
+                    }
+                    if (a.distinct) {
+                        add(Q, -qx[i], 0.f);
+                        Q = settled(Q.h, Q.l);
+                    }
                     if (j < n) ask = kSum;
                 } else {
-                    W -= w;
+                    add(W, -w, 0.f);
+                    W = settled(W.h, W.l);
                 }
                 i = j;
             }
@@ -341,12 +370,11 @@ __global__ void __launch_bounds__(kThreads, 2) tree_sample_kernel(const SampleAr
                 }
             }
             if (lane == 0) {
-                const bool less = draft && F > 0.0 && !again;
-                const double f = fmin(F, 3e38);
+                const bool less = draft && F.h > 0.f && !again;
                 todo.p = target + (size_t)at * a.vocab;
                 todo.q = less ? draft + (size_t)at * a.vocab : nullptr;
-                todo.fh = less ? (float)f : 0.f;
-                todo.fl = less ? (float)(f - (double)(float)f) : 0.f;
+                todo.fh = less ? F.h : 0.f;
+                todo.fl = less ? F.l : 0.f;
                 todo.gone = list;
                 todo.n_gone = gone;
                 what = ask;
@@ -371,19 +399,20 @@ __global__ void __launch_bounds__(kThreads, 2) tree_sample_kernel(const SampleAr
         if (warp == 0) {
             const Sum part = lane < (int)ctas ? sum_of(&of_cta[turn & 1], lane) : Sum{0.f, 0.f};
             const Sum upto = warp_upto(part);
-            W = value(from_lane(upto, 31));
+            W = from_lane(upto, 31);
+            W = settled(W.h, W.l);
             int next = kGoOn;
             if (last) {
-                if (!(W > 0.0) && !again && (r.q || r.n_gone)) {
+                if (!(W.h > 0.f) && !again && (r.q || r.n_gone)) {
                     again = true;
-                } else if (!(W > 0.0)) {
+                } else if (!(W.h > 0.f)) {
                     next = kDone;
                     if (rank == 0 && lane == 0) {       // no weight at all
                         a.next_token[b] = 0;
                         if (a.err) atomicOr(a.err, DFLARE_DEVERR_TOKEN);
                     }
                 } else {
-                    const Sum g = split((double)u[0] * W);
+                    const Sum g = times(W, {u[0], 0.f});
                     Sum base = {0.f, 0.f};
                     next = part_of(part, (int)ctas, g, base) == (int)rank ? kSearch : kDone;
                     if (next == kSearch) {
