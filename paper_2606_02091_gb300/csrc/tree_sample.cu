@@ -19,6 +19,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <atomic>
 #include <string>
 
 #include "common.cuh"
@@ -116,17 +117,18 @@ struct Residual {
     const int32_t* gone;
     int n_gone;
 };
-// p - F q as two numbers
+// p - F q as two numbers where it is positive: there p >= F q in fp32 too, so that the difference's rounding is two subtractions
 __device__ __forceinline__ Sum left_of(float p, float q, float fh, float fl) {
     const float ph = __fmul_rn(fh, q), pl = __fmaf_rn(fl, q, __fmaf_rn(fh, q, -ph));
-    const float d = __fsub_rn(p, ph), b = __fsub_rn(d, p);
-    return {d, __fsub_rn(__fsub_rn(__fsub_rn(p, __fsub_rn(d, b)), __fadd_rn(ph, b)), pl)};
+    const float d = __fsub_rn(p, ph);
+    return {d, __fsub_rn(__fsub_rn(__fsub_rn(p, d), ph), pl)};
 }
 // w = max(0, p - F q) added to s; not finite or negative: nothing
 __device__ __forceinline__ void add_weight(Sum& s, const Residual& r, float p, float q) {
     const Sum w = left_of(p, q, r.fh, r.fl);
     if (__fadd_rn(w.h, w.l) > 0.f) add(s, w.h, w.l);
 }
+__device__ __forceinline__ void add_plain(Sum& s, float p) { add(s, p > 0.f && p < INFINITY ? p : 0.f, 0.f); }
 __device__ __forceinline__ bool is_gone(const Residual& r, int e) {
     for (int g = 0; g < r.n_gone; ++g)
         if (r.gone[g] == e) return true;
@@ -149,6 +151,16 @@ __device__ __forceinline__ Sum part_sum(const Residual& r, int e0, int e1, bool 
                 const bool there = e + k * 128 < e1;
                 p[k] = there ? __ldg(reinterpret_cast<const float4*>(r.p + e + k * 128)) : make_float4(0.f, 0.f, 0.f, 0.f);
                 q[k] = there && r.q ? __ldg(reinterpret_cast<const float4*>(r.q + e + k * 128)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+            if (!r.q) {
+#pragma unroll
+                for (int k = 0; k < U; ++k) {
+                    add_plain(s[k], p[k].x);
+                    add_plain(s[k], p[k].y);
+                    add_plain(s[k], p[k].z);
+                    add_plain(s[k], p[k].w);
+                }
+                continue;
             }
 #pragma unroll
             for (int k = 0; k < U; ++k) {
@@ -443,6 +455,43 @@ __global__ void __launch_bounds__(kThreads, 2) tree_sample_kernel(const SampleAr
     cluster_wait();
 }
 
+// CTAs per tree: those that take the least time by a model of it, waves of clusters x (what a tree costs beside its rows, in elements of a
+// row's part, and the part). How many clusters the GPU holds at once depends on its clusters of SMs: of 16 CTAs 14, not
+// 304 / 16 (16 trees in clusters of 16 then go in two waves).
+constexpr int kTreeCost = 20000;
+cudaError_t cluster_for(int batch, int vocab, int* ctas) {
+    static std::atomic<int> known[64][kMaxCluster + 1];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    double best = 0.0;
+    for (int c = 1; c <= kMaxCluster; ++c) {
+        if (c > 1 && vocab < c * kThreads * 4) break;      // less than a load for every thread
+        int active = known[dev & 63][c].load(std::memory_order_relaxed);
+        if (active == 0) {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(c);
+            cfg.blockDim = dim3(kThreads);
+            cudaLaunchAttribute attr[1];
+            attr[0].id = cudaLaunchAttributeClusterDimension;
+            attr[0].val.clusterDim.x = c;
+            attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+            cfg.attrs = attr;
+            cfg.numAttrs = 1;
+            e = cudaOccupancyMaxActiveClusters(&active, tree_sample_kernel, &cfg);
+            if (e != cudaSuccess) return e;
+            active = std::max(active, 1);
+            known[dev & 63][c].store(active, std::memory_order_relaxed);
+        }
+        const double cost = (double)((batch + active - 1) / active) * (kTreeCost + (double)vocab / c);
+        if (c == 1 || cost < best) {
+            best = cost;
+            *ctas = c;
+        }
+    }
+    return cudaSuccess;
+}
+
 dflare_status refuse(dflare_status st, const std::string& m) {
     noalloc_set_error(m);
     return st;
@@ -466,13 +515,9 @@ extern "C" dflare_status dflare_tree_sample(const int32_t* tokens_dev, const int
     if (distinct != 0 && distinct != 1) return bad("distinct must be 0 or 1");
     static PerDeviceOnce once;
     cudaError_t e = once([] { return cudaFuncSetAttribute(tree_sample_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1); });
-    int dev = 0, sms = 0;
-    if (e == cudaSuccess) e = cudaGetDevice(&dev);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    int ctas = 1;
+    if (e == cudaSuccess) e = cluster_for(batch, vocab, &ctas);
     if (e != cudaSuccess) return refuse(DFLARE_ECUDA, std::string("dflare_tree_sample: ") + cudaGetErrorString(e));
-    // as many CTAs per tree as the GPU holds at once, none with less than a load per thread
-    int ctas = kMaxCluster;
-    while (ctas > 1 && ((long long)batch * ctas > 2LL * sms || (long long)vocab < (long long)ctas * kThreads * 4)) ctas /= 2;
     SampleArgs a{tokens_dev, parents_dev, n_nodes_dev, target_dev, draft_dev, u_dev, accept_len_dev, path_dev, next_token_dev, err_dev,
                  n_max, draft_rows, vocab, distinct, 0};
     a.part = ((vocab + ctas * kWarps - 1) / (ctas * kWarps) + 3) / 4 * 4;
