@@ -9,7 +9,9 @@
 // Two streams, each a softmax warpgroup with its own S/P and O columns and its own (m, l), keep the tensor pipe
 // busy while the other's scores are turned into weights. With 128 rows or fewer (NQ = 1) the streams take
 // alternate key tiles of the same rows and are joined per row at the end; with more (NQ = 2) each has 128 rows
-// of its own and both read every tile, so 256 rows cost one pass over the keys.
+// of its own and both read every tile, so 256 rows cost one pass over the keys. Over a plan's items a kernel with NQ = 2 does
+// either, unit by unit (64 sequences of 4 nodes, their own 1150 keys and four shared contexts of 32768: 187 us with one stream
+// idle in units of few rows, 151 so).
 // m is raised (and O scaled) only when a tile's maximum exceeds it by 2^8: P <= 2^8 carries the same relative
 // precision, and O / l does not depend on m.
 // Bound by the chain of hand-offs between softmax and MMA (1.7 us per tile of 256 rows against 1.46 us of HBM time):
@@ -155,6 +157,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     if constexpr (SHARED) tree_items(a, v, v1);
     else tree_runs<QT, kKeys, kTcExtra, kTcLeast>(a, cum, qg, v, v1);
     const int v0 = v;
+    // Whether the streams take alternate tiles of the same 128 rows: always (NQ = 1), or, from a plan, where a unit has no more.
+    auto alternate = [&](const Pair& p) {
+        if constexpr (SHARED && NQ == 2) return p.nodes * a.G - p.row0 <= 128;
+        else return NQ == 1;
+    };
     Pair p, after;
     bool more = tree_pair<kTcExtra>(a, cum, v, v1, p);
     auto tS = [&](int w) { return tmem + 128u * w; };
@@ -208,13 +215,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
             auto wait = [&](uint32_t bar, uint32_t parity) {
                 if (ok) ok = wait_inline(bar, parity & 1u, &abort_flag, a.pg.err);
             };
-            // S of tile x of the run by stream w (a constant where it is called)
-            auto issue_s = [&](uint32_t x, int w) {
+            // S of tile x of the run by stream w (a constant where it is called, as alt is but for SHARED)
+            auto issue_s = [&](uint32_t x, int w, bool alt) {
                 const uint32_t st = x % NK;
-                if (NQ == 1 || w == 0) wait(kfull(st), x / NK);
+                if (alt || w == 0) wait(kfull(st), x / NK);
                 if (!ok) return;
                 tc_fence_after();
-                const uint64_t dq = smem_desc(sb + LY::Q + (NQ == 2 ? w * TB : 0));
+                const uint64_t dq = smem_desc(sb + LY::Q + (alt ? 0 : w * TB));
                 const uint64_t dk = smem_desc(sb + LY::K + st * TB);
 #pragma unroll
                 for (int kk = 0; kk < HD / 16; ++kk) {
@@ -222,7 +229,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                     umma_bf16(tS(w), dq + at, dk + at, kIdS, kk > 0 ? 1u : 0u);
                 }
                 umma_commit(sfull(w));
-                if (NQ == 1 || w == 1) umma_commit(kempty(st));
+                if (alt || w == 1) umma_commit(kempty(st));
             };
             TreeRaw raw = more ? pair_raw(a, p) : TreeRaw{};
             for (; more; ++pair) {
@@ -232,10 +239,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                 const bool next = tree_pair<kTcExtra>(a, cum, v, v1, after);
                 if (next) raw = pair_raw(a, after);
                 // PV of tile j of the pair by stream w, then the stream's next S
+                const bool alt = alternate(p);
+                const int stride = alt ? 2 : 1;
                 auto step = [&](int j, int w) {
-                    constexpr int stride = NQ == 1 ? 2 : 1;
                     const uint32_t x = base + j, st = x % NV;
-                    if (NQ == 1 || w == 0) wait(vfull(st), x / NV);
+                    if (alt || w == 0) wait(vfull(st), x / NV);
                     wait(pfull(w), w ? ps1++ : ps0++);
                     if (!ok) return;
                     tc_fence_after();
@@ -245,18 +253,18 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
 #pragma unroll
                     for (int kk = 0; kk < kKeys / 16; ++kk)
                         if (kk < ks) umma_bf16_ts(tO(w), tS(w) + kk * 8, dv + (uint64_t)(kk * 128), kIdO, (j >= stride || kk > 0) ? 1u : 0u);
-                    if (NQ == 1 || w == 1) umma_commit(vempty(st));
-                    if (j + stride < n) issue_s(x + stride, w);
+                    if (alt || w == 1) umma_commit(vempty(st));
+                    if (j + stride < n) issue_s(x + stride, w, alt);
                     else umma_commit(ofull(w));
                 };
                 wait(qfull, pair);
                 if (ok) tc_fence_after();
-                issue_s(base, 0);
-                if (NQ == 2) issue_s(base, 1);
-                else if (n > 1) issue_s(base + 1, 1);
-                for (int j = 0; j < n && ok; j += NQ == 1 ? 2 : 1) {
+                issue_s(base, 0, alt);
+                if (!alt) issue_s(base, 1, alt);
+                else if (n > 1) issue_s(base + 1, 1, alt);
+                for (int j = 0; j < n && ok; j += stride) {
                     step(j, 0);
-                    if (NQ == 2 || j + 1 < n) step(NQ == 2 ? j : j + 1, 1);
+                    if (!alt || j + 1 < n) step(alt ? j + 1 : j, 1);
                 }
                 if (!ok) break;
                 base += n;
@@ -314,7 +322,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         if (more) {
             raw = pair_raw(a, p);
             pair_lengths<SHARED>(a, raw, nodes, ctx, keys);
-            if (NQ == 2) load_q(p, nodes * a.G, w, r, 128);
+            if (!alternate(p)) load_q(p, nodes * a.G, w, r, 128);
             else load_q(p, nodes * a.G, 0, tid, 256);
             __syncwarp();
             if (lane == 0) mbar_arrive(qsent);
@@ -323,7 +331,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         while (more) {
             const int n = p.hi - p.lo;
             const int R = nodes * a.G;
-            const int my_row = row0_of(p) + (NQ == 2 ? 128 * w : 0) + r;
+            const bool alt = alternate(p);
+            const int my_row = row0_of(p) + (alt ? 0 : 128 * w) + r;
             const bool live = my_row < R;
             const bool warp_live = my_row - lane < R;
             const int node = mask_node(p, group_of(a, min(my_row, R - 1)));
@@ -332,21 +341,32 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
             if (more) raw = pair_raw(a, after);
             int nodes2 = 0, ctx2 = 0, keys2 = 0;        // the next pair's
             float m = -INFINITY, l = 0.f;
-            const int mine = NQ == 2 ? n : (n + 1 - w) / 2;      // tiles of this stream
+            const int mine = alt ? (n + 1 - w) / 2 : n;      // tiles of this stream
             for (int j = 0; j < mine; ++j, ++ss) {
-                const int tile = NQ == 2 ? j : 2 * j + w;       // of the pair's run
+                const int tile = alt ? 2 * j + w : j;       // of the pair's run
                 const int k0 = (p.lo + tile) * kKeys;
                 wait(sfull(w), (uint32_t)ss & 1u);
                 tc_fence_after();
-                // every S of the pair (of this stream, with NQ = 2) has been computed: the next pair's Q
+                // every S of the pair (of this stream, where each has rows of its own) has been computed: the next pair's Q
                 if (tile == n - 1 && more) {
                     pair_lengths<SHARED>(a, raw, nodes2, ctx2, keys2);
-                    load_q(after, nodes2 * a.G, NQ == 2 ? w : 0, r, 128);
+                    if constexpr (SHARED && NQ == 2) {
+                        if (alt == alternate(after)) {
+                            load_q(after, nodes2 * a.G, alt ? 0 : w, r, 128);
+                        } else if (alt) {       // (this stream had the last S that reads either half)
+                            load_q(after, nodes2 * a.G, 0, r, 128);
+                            load_q(after, nodes2 * a.G, 1, r, 128);
+                        } else if (w == 0) {
+                            load_q(after, nodes2 * a.G, 0, r, 128);
+                        }
+                    } else {
+                        load_q(after, nodes2 * a.G, NQ == 2 ? w : 0, r, 128);
+                    }
                 }
                 const bool edge = k0 + kKeys > ctx;
                 if (edge) {
                     // nodes of the tree, or slots past the last key
-                    if (NQ == 1 || w == 0) {
+                    if (alt || w == 0) {
                         // values: slots past the last key (of those that are multiplied) and infinite or NaN values
                         // of nodes become 0
                         const int x = base + tile, st = x % NV, rows = min(kKeys, (keys - k0 + 15) & ~15);
@@ -485,17 +505,25 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                 part0 = ((size_t)blockIdx.x * 2 + (p.start < v0 ? 0 : 1)) * QT;
             }
             float M = m, L = l, w0 = 1.f, w1 = 0.f;
-            const bool two = NQ == 1 && n > 1;
-            if (NQ == 1) {
-                float2* ml = reinterpret_cast<float2*>(smem + LY::ML);
-                ml[w * 128 + r] = make_float2(m, l);
+            const bool two = alt && n > 1;
+            if (alt) {
+                // (with NQ = 2 there is room for it only where the warps turn their rows around)
+                float2 *mine = reinterpret_cast<float2*>(smem + LY::ML) + w * 128 + r, *other = reinterpret_cast<float2*>(smem + LY::ML) + (w ^ 1) * 128 + r;
+                if constexpr (NQ == 2) {
+                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                    __syncwarp();
+                    mine = reinterpret_cast<float2*>(smem + LY::TURN + warp * 4096) + lane;
+                    other = reinterpret_cast<float2*>(smem + LY::TURN + (warp ^ 4) * 4096) + lane;
+                }
+                *mine = make_float2(m, l);
                 streams_meet();     // (with it, each reads the O that the other has waited for)
-                const float2 x = ml[r], y = ml[128 + r];
+                const float2 own = make_float2(m, l), there = *other, x = w ? there : own, y = w ? own : there;
                 M = fmaxf(x.x, y.x);
                 const float ref = M == -INFINITY ? 0.f : M;
                 w0 = pow2(x.x - ref);
                 w1 = pow2(y.x - ref);
                 L = x.y * w0 + y.y * w1;
+                if constexpr (NQ == 2) streams_meet();      // both have read
             } else {
                 streams_meet();     // odd nodes noted by stream 0
             }
@@ -504,7 +532,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                 // Each warp turns its 32 rows around in shared memory, 128 bytes of every row at a time, so that
                 // global stores are whole lines.
                 const float inv = partial ? 1.f : L == 0.f ? 0.f : 1.f / L;
-                if (NQ == 1) {
+                if (alt) {
                     w0 *= inv;
                     w1 *= inv;
                 } else {
@@ -512,16 +540,16 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                 }
                 uint8_t* turn = smem + LY::TURN + warp * 4096;
                 const int rows = min(32, R - (my_row - lane));
-                const size_t prow = part0 + (NQ == 2 ? 128 * w : 0) + r;
+                const size_t prow = part0 + (alt ? 0 : 128 * w) + r;
                 const size_t orow = ((size_t)p.b * a.n_max + node) * a.hq + p.h * a.G + min(my_row, R - 1) - node * a.G;
-                constexpr int CH = NQ == 2 ? HD / 32 : HD / 64;
-                const int col0 = NQ == 2 ? 0 : w * (HD / 2);
+                const int CH = alt ? HD / 64 : HD / 32;
+                const int col0 = alt ? w * (HD / 2) : 0;
 #pragma unroll 1
                 for (int x = 0; x < CH; ++x) {
                     const int col = col0 + 32 * x;
                     uint32_t v0[32];
                     float o[32];
-                    tmem_ld32_async(tO(NQ == 2 ? w : 0) + lanes + col, v0);
+                    tmem_ld32_async(tO(alt ? 0 : w) + lanes + col, v0);
                     tmem_wait_ld();
 #pragma unroll
                     for (int e = 0; e < 32; ++e) o[e] = __uint_as_float(v0[e]) * w0;
@@ -569,10 +597,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                             *reinterpret_cast<uint4*>(turn + lane * 128 + (((4 * upper + e) ^ (lane & 7)) << 4)) = u;
                         }
                         if (upper || CH == 1) {
-                            constexpr int pieces = CH > 1 ? 8 : 4;
+                            const int pieces = CH > 1 ? 8 : 4;
                             __syncwarp();
 #pragma unroll
-                            for (int y = 0; y < pieces; ++y) {
+                            for (int y = 0; y < 8; ++y) {
+                                if (y == pieces) break;
                                 const int lr = (32 / pieces) * y + lane / pieces, pc = lane % pieces;
                                 const uint4 v = *reinterpret_cast<const uint4*>(turn + lr * 128 + ((pc ^ (lr & 7)) << 4));
                                 const size_t to = __shfl_sync(0xffffffffu, orow, lr);
@@ -583,7 +612,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                         }
                     }
                 }
-                if (live && (NQ == 2 || w == 0)) {
+                if (live && (!alt || w == 0)) {
                     if (partial) a.part_ml[prow] = make_float2(M, L);
                     else if (a.lse) a.lse[orow] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
                 }
