@@ -61,13 +61,11 @@ struct __align__(16) TreeSeq {
     int lead_start, lead_tiles, lead_blocks;    // its group's (tiles 0: none)
     int node0;           // its first node among the group's
     int row, lead_row;   // rows of whole units among the partial results: of kv head 0 (lead_row: of the group's row 0)
-    int pad[2];
+    int weight, lead_weight;    // cost of a tile
 };
 // The head of an attend_shared workspace.
 struct SharedHead {
-    int batch, n_max, per, ok;
-    int groups[2 * kMaxSeqs];       // [batch][2]: the sequence that leads b's group (b: none), shared pages
-    int same[kMaxSeqs];             // pages that b shares with the sequence before it that has nodes
+    int batch, n_max, per, ok;      // per: length of a CTA's run
 };
 
 // one launch of the paged attention

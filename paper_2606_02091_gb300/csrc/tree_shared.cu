@@ -8,7 +8,7 @@
 // more "sequence" (without a mask: shared pages hold context only), and each sequence keeps the keys behind those.
 //
 // A plan, made once per step for all layers, lists this work: units (sequence or group, kv head, block of query rows), each
-// with its key tiles and kExtra more for beginning and ending it. The CTAs take equal runs of the list. A unit that lies in one run is
+// with what its key tiles cost and what beginning and ending it does. The CTAs take equal runs of the list. A unit that lies in one run is
 // one item; others are cut where a run ends. Partial rows lie in the workspace: two blocks per CTA (of the units cut
 // at its run's ends), and one row per query row and part for units that are whole but not all of the row's keys.
 //
@@ -28,13 +28,16 @@
 namespace dfl {
 namespace {
 
-constexpr int kSameThreads = 256;
 constexpr int kPlanThreads = 1024;
+
+// Costs of the tcgen05 kernel's work.
+constexpr int kTileCost = 4, kWideTileCost = 6, kUnitCost = 14;
 
 // What a plan and the launches that follow it agree on, from the call's sizes alone.
 struct Layout {
     bool ok;                    // everything fits its numbers
-    int QT, KT, extra, least, C;
+    int QT, KT, C;
+    int weight1, weight2, extra, least;     // cost of a tile of up to 128 rows and of more, of a unit beside its tiles; the shortest run
     int own_rows, lead_rows;    // rows of one kv head among the whole units' partial results
     size_t runs, items, map, seqs, ml, o, bytes;    // offsets
 };
@@ -44,13 +47,13 @@ Layout layout_of(const dflare_cache* c, int batch, int n_max) {
     Layout y{};
     const long long rows = (long long)batch * n_max * G;
     if (g.dtype == DFLARE_F32) {
-        y.QT = kFRows, y.KT = kFKeys, y.extra = kFExtra, y.least = kFLeast, y.C = f32_ctas_per_sm(g.head_dim) * c->num_sms;
+        y.QT = kFRows, y.KT = kFKeys, y.weight1 = y.weight2 = 1, y.extra = kFExtra, y.least = kFLeast, y.C = f32_ctas_per_sm(g.head_dim) * c->num_sms;
     } else {
         // (blocks of 128 rows where no group can have more)
-        y.QT = rows <= 128 ? 128 : 256, y.KT = kTcKeys, y.extra = kTcExtra, y.least = kTcLeast, y.C = c->num_sms;
+        y.QT = rows <= 128 ? 128 : 256, y.KT = kTcKeys, y.weight1 = kTileCost, y.weight2 = kWideTileCost, y.extra = kUnitCost, y.least = kWideTileCost, y.C = c->num_sms;
     }
     const long long own = (long long)batch * (((long long)n_max * G + y.QT - 1) / y.QT), lead = (rows + y.QT - 1) / y.QT + batch / 2;
-    const long long units = (own + lead) * g.n_kv_heads, tiles = ((long long)g.max_pages * g.page_size + y.KT - 1) / y.KT + y.extra;
+    const long long units = (own + lead) * g.n_kv_heads, tiles = ((long long)g.max_pages * g.page_size + y.KT - 1) / y.KT * y.weight2 + y.extra;
     const long long own_rows = ((long long)n_max * G + 31) / 32 * 32, lead_rows = (rows / 32 + batch + 1) * 32;
     const long long part = 2LL * y.C * y.QT + (batch * own_rows + lead_rows) * g.n_kv_heads;
     const long long most = 0x7fffffffLL - 4096;
@@ -82,9 +85,14 @@ struct PlanArgs {
     int32_t* map;
     TreeSeq* seqs;
     int32_t* groups;            // optional output
-    int batch, n_max, G, QT, KT, extra, least, C, own_rows, lead_rows;
+    int batch, n_max, G, qt, kt, weight1, weight2, extra, least, C, own_rows, lead_rows;
 };
 
+// Rows among the partial results: 2 C blocks of the CTAs, then of whole units the sequences' own, then the groups'.
+__device__ __forceinline__ int own_row(const PlanArgs& a, int b) { return (2 * a.C << a.qt) + b * a.pg.hkv * a.own_rows; }
+__device__ __forceinline__ int lead_row(const PlanArgs& a, int b, int node0) {
+    return own_row(a, a.batch) + (int)((long long)node0 * a.G / 32 + b) * 32;
+}
 __device__ __forceinline__ void lengths_of(const PlanArgs& a, int b, int& n, int& held, int& ctx, int& keys) {
     n = min(max(a.n_nodes[b], 0), a.n_max);
     held = min(max(a.pg.held[b], 0), a.pg.max_pages);
@@ -94,292 +102,385 @@ __device__ __forceinline__ void lengths_of(const PlanArgs& a, int b, int& n, int
     ctx = min(len, keys);
 }
 
-// Pages that sequence b (a CTA each) and the one before it that has nodes both hold in the same places, full of context.
-__global__ void __launch_bounds__(kSameThreads) tree_same_kernel(const PlanArgs a) {
-    __shared__ int before;
-    pdl_wait();
-    pdl_trigger();
-    const int b = blockIdx.x, tid = threadIdx.x;
-    if (tid == 0) before = -1;
-    __syncthreads();
-    int n, held, ctx, keys, same = 0;
-    lengths_of(a, b, n, held, ctx, keys);
-    if (tid < b && a.n_nodes[tid] > 0) atomicMax(&before, tid);
-    __syncthreads();
-    const int p = before;
-    if (p >= 0 && n > 0) {
-        int n2, held2, ctx2, keys2;
-        lengths_of(a, p, n2, held2, ctx2, keys2);
-        const int most = min(ctx, ctx2) / a.pg.ps;
-        const int32_t *x = a.pg.table + (size_t)p * a.pg.max_pages, *y = a.pg.table + (size_t)b * a.pg.max_pages;
-        constexpr int U = 4;
-        for (;;) {      // U x 256 pages at a time, up to the first that differs
-            int u = U * kSameThreads;
-#pragma unroll
-            for (int k = U - 1; k >= 0; --k) {
-                const int i = same + k * kSameThreads + tid;
-                const bool equal = i < most && x[i] == y[i] && x[i] >= 0 && x[i] < a.pg.pages;
-                if (!equal) u = k * kSameThreads + tid;
-            }
-            __shared__ int least;
-            if (tid == 0) least = U * kSameThreads;
-            __syncthreads();
-            u = __reduce_min_sync(0xffffffffu, u);
-            if ((tid & 31) == 0) atomicMin(&least, u);
-            __syncthreads();
-            u = least;
-            __syncthreads();
-            same += u;
-            if (u < U * kSameThreads) break;
-        }
-    }
-    if (tid == 0) a.head->same[b] = same;
-}
-
-// inclusive sums over a CTA of kPlanThreads; tmp holds 32 ints
-__device__ __forceinline__ int plan_scan(int v, int* tmp, int* total) {
+// The first kMaxSeqs threads, which have a sequence each.
+__device__ __forceinline__ void seq_barrier() { asm volatile("bar.sync 1, %0;" ::"n"(kMaxSeqs) : "memory"); }
+// Inclusive sums over them, of two numbers at once; tmp holds 8 pairs.
+__device__ __forceinline__ int2 plan_scan(int2 v, int2* tmp, int2* total) {
+    constexpr int W = kMaxSeqs / 32;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int x = __shfl_up_sync(0xffffffffu, v, o);
-        if (lane >= o) v += x;
+        const int x = __shfl_up_sync(0xffffffffu, v.x, o), y = __shfl_up_sync(0xffffffffu, v.y, o);
+        if (lane >= o) {
+            v.x += x;
+            v.y += y;
+        }
     }
-    __syncthreads();
+    seq_barrier();
     if (lane == 31) tmp[warp] = v;
-    __syncthreads();
-    int t = tmp[lane];
+    seq_barrier();
+    *total = make_int2(0, 0);
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int x = __shfl_up_sync(0xffffffffu, t, o);
-        if (lane >= o) t += x;
+    for (int w = 0; w < W; ++w) {
+        const int2 t = tmp[w];
+        if (w < warp) {
+            v.x += t.x;
+            v.y += t.y;
+        }
+        total->x += t.x;
+        total->y += t.y;
     }
-    *total = __shfl_sync(0xffffffffu, t, 31);
-    const int base = __shfl_sync(0xffffffffu, t, max(warp - 1, 0));
-    return v + (warp ? base : 0);
+    return v;
 }
 
-// What a group of `many` that shares `pages` saves, in keys: less what one more unit and the joining of its rows cost, in keys
+// Pages that sequence b and the one before it that has nodes both hold in the same places, full of context (a warp; the same in
+// every lane). One trip to memory where that is sequence b - 1 and they are up to 512.
+__device__ __forceinline__ int pages_shared(const PlanArgs& a, int b) {
+    constexpr int U = 16;
+    const int lane = threadIdx.x & 31;
+    const int32_t *x = a.pg.table + (size_t)max(b - 1, 0) * a.pg.max_pages, *y = a.pg.table + (size_t)b * a.pg.max_pages;
+    int v[U], w[U];
+    auto load = [&](int at) {
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int i = at + k * 32 + lane;
+            v[k] = i < a.pg.max_pages ? x[i] : -1;
+            w[k] = i < a.pg.max_pages ? y[i] : -1;
+        }
+    };
+    load(0);
+    int n, held, ctx, keys, n2, held2, ctx2, keys2, p = -1;
+    lengths_of(a, b, n, held, ctx, keys);
+    lengths_of(a, max(b - 1, 0), n2, held2, ctx2, keys2);
+    for (int top = b - 1; top >= 0 && p < 0; top -= 32) {
+        const unsigned has = __ballot_sync(0xffffffffu, top - lane >= 0 && a.n_nodes[max(top - lane, 0)] > 0);
+        if (has) p = top - (__ffs(has) - 1);
+    }
+    if (p < 0 || n == 0) return 0;
+    if (p != b - 1) {
+        lengths_of(a, p, n2, held2, ctx2, keys2);
+        x = a.pg.table + (size_t)p * a.pg.max_pages;
+        load(0);
+    }
+    const int most = min(ctx, ctx2) / a.pg.ps;
+    for (int at = 0;;) {       // up to the first that differs
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const int i = at + k * 32 + lane;
+            const unsigned differ = __ballot_sync(0xffffffffu, i >= most || v[k] != w[k] || v[k] < 0 || v[k] >= a.pg.pages);
+            if (differ) return at + k * 32 + __ffs(differ) - 1;
+        }
+        at += U * 32;
+        load(at);
+    }
+}
+
+// What a group of `many` saves that shares `tokens`, in keys: less what one more unit and the joining of its rows cost, in keys
 // that could be read meanwhile.
-constexpr int kGroupCost = 512, kMemberCost = 64;
-__device__ __forceinline__ float saving(const PlanArgs& a, int many, int pages) {
-    return fmaxf((float)(many - 1) * (float)pages * (float)a.pg.ps - (float)(kGroupCost + kMemberCost * many), 0.f);
-}
+constexpr float kGroupCost = 512.f, kMemberCost = 64.f;
+__device__ __forceinline__ float saving(float many, float tokens) { return fmaxf(fmaf(many - 1.f, tokens, -fmaf(kMemberCost, many, kGroupCost)), 0.f); }
 
-// One CTA. Segment 2 b is sequence b's own keys, 2 b + 1 the keys shared by the group that b leads.
-__global__ void __launch_bounds__(kPlanThreads) tree_shared_plan_kernel(const PlanArgs a) {
-    __shared__ int active[kMaxSeqs], share[kMaxSeqs], from[kMaxSeqs + 1], shared_by[kMaxSeqs + 1], nodes_of[kMaxSeqs];
-    __shared__ float best[kMaxSeqs + 1];
-    __shared__ int pages_of[kMaxSeqs], node0[kMaxSeqs + 1], members[kMaxSeqs];
-    __shared__ int seg_start[2 * kMaxSeqs], seg_unit[2 * kMaxSeqs], seg_tiles[2 * kMaxSeqs], seg_blocks[2 * kMaxSeqs];
-    __shared__ int tmp[32];
-    pdl_wait();
-    pdl_trigger();
-    const int tid = threadIdx.x, lane = tid & 31;
-    int n = 0, held = 0, ctx = 0, keys = 0, total;
-    if (tid < a.batch) {
-        lengths_of(a, tid, n, held, ctx, keys);
-        pages_of[tid] = 0;
-        members[tid] = 0;
+// The places s .. e - 1 are one group that shares `pages`, or one by itself (a warp).
+struct Groups {
+    int *first, *members, *pages;       // by place: of its group, the first place, how many (at the first), what they share
+    __device__ __forceinline__ void put(int s, int e, int shared) const {
+        const int lane = threadIdx.x & 31;
+        for (int i = s + lane; i < e; i += 32) {
+            first[i] = s;
+            pages[i] = e - s > 1 ? shared : 0;
+        }
+        if (lane == 0) members[s] = e - s;
     }
-    // the sequences that have nodes, in order
-    const int place = plan_scan(n > 0, tmp, &total) - 1, m = total;
-    if (n > 0) {
-        active[place] = tid;
-        share[place] = place ? a.head->same[tid] : 0;
+};
+// Sequences s .. e - 1 (by place) of which all neighbours share the same number of pages: all are one group, or none are.
+__device__ __forceinline__ bool divide_even(const int* share, int s, int e, int ps, const Groups& groups) {
+    const int lane = threadIdx.x & 31;
+    int low = 0x7fffffff, high = 0;
+    for (int i = s + 1 + lane; i < e; i += 32) {
+        low = min(low, share[i]);
+        high = max(high, share[i]);
     }
-    __syncthreads();
-    if (tid < 32) {
-        // best[j]: of the first j. Lane l looks at groups that begin at i = l, l + 32, ..; least[k]: pages that i .. j - 1 share.
-        int least[kMaxSeqs / 32];
+    low = __reduce_min_sync(0xffffffffu, low);
+    high = __reduce_max_sync(0xffffffffu, high);
+    if (e - s > 1 && low != high) return false;
+    if (e - s > 1 && saving((float)(e - s), (float)low * (float)ps) > 0.f) {
+        groups.put(s, e, low);
+    } else {
+        for (int i = s + lane; i < e; i += 32) {
+            groups.first[i] = i;
+            groups.pages[i] = 0;
+        }
+    }
+    return true;
+}
+// The same where they differ, up to 32: a warp finds the best division, lane i holding best(i).
+__device__ __forceinline__ void divide_few(const int* share, int s, int e, int ps, const Groups& groups) {
+    const int lane = threadIdx.x & 31, many = e - s;
+    const int mine = lane < many ? share[s + lane] : 0;
+    const float tokens = (float)mine * (float)ps;
+    float best = 0.f, size = (float)-lane, least_f = INFINITY;      // size: of the group that begins here
+    int least = 0x7fffffff, from = 0, pages = 0;
+    for (int j = 1; j <= many; ++j) {
+        size += 1.f;
+        const int next = __shfl_sync(0xffffffffu, mine, j - 1);
+        const float next_f = __shfl_sync(0xffffffffu, tokens, j - 1);
+        if (lane < j - 1) {
+            least = min(least, next);
+            least_f = fminf(least_f, next_f);
+        }
+        const float v = best + (lane < j - 1 ? saving(size, least_f) : 0.f);
+        // (not negative: their bits are in order; of equal ones the shortest group)
+        const unsigned bits = lane < j ? __float_as_uint(v) + 1u : 0u, top = __reduce_max_sync(0xffffffffu, bits);
+        const int at = 31 - __clz(__ballot_sync(0xffffffffu, bits == top));
+        const int shared = __shfl_sync(0xffffffffu, least, at);
+        if (lane == j - 1) {
+            from = at;
+            pages = shared;
+        }
+        if (lane == j) best = __uint_as_float(top - 1u);
+    }
+    for (int j = many; j > 0;) {
+        const int at = __shfl_sync(0xffffffffu, from, j - 1), shared = __shfl_sync(0xffffffffu, pages, j - 1);
+        groups.put(s + at, s + j, shared);
+        j = at;
+    }
+}
+// The same for more, with best (e - s + 1 numbers), from and shared_by (e - s each, by place) in shared memory: lane l looks at
+// groups that begin at l, l + 32, ...
+__device__ __forceinline__ void divide_many(const int* share, int s, int e, int ps, const Groups& groups, float* best, int* from, int* shared_by) {
+    const int lane = threadIdx.x & 31, many = e - s;
+    int least[kMaxSeqs / 32];
 #pragma unroll
-        for (int k = 0; k < kMaxSeqs / 32; ++k) least[k] = 0x7fffffff;
-        if (lane == 0) best[0] = 0.f;
-        __syncwarp();
-        for (int j = 1; j <= m; ++j) {
-            float top = -1.f;
-            int at = 0, pages = 0;
-            const int next = share[j - 1];
+    for (int k = 0; k < kMaxSeqs / 32; ++k) least[k] = 0x7fffffff;
+    if (lane == 0) best[0] = 0.f;
+    __syncwarp();
+    for (int j = 1; j <= many; ++j) {
+        float top = -1.f;
+        int at = 0, pages = 0;
+        const int next = share[s + j - 1];
 #pragma unroll
-            for (int k = 0; k < kMaxSeqs / 32; ++k) {
-                const int i = lane + 32 * k;
-                if (32 * k >= j) break;
-                if (i < j - 1) least[k] = min(least[k], next);
-                if (i < j) {
-                    const float v = best[i] + (i < j - 1 ? saving(a, j - i, least[k]) : 0.f);
-                    if (v > top) {
-                        top = v;
-                        at = i;
-                        pages = least[k];
-                    }
+        for (int k = 0; k < kMaxSeqs / 32; ++k) {
+            const int i = lane + 32 * k;
+            if (32 * k >= j) break;
+            if (i < j - 1) least[k] = min(least[k], next);
+            if (i < j) {
+                const float v = best[i] + (i < j - 1 ? saving((float)(j - i), (float)least[k] * (float)ps) : 0.f);
+                if (v > top) {
+                    top = v;
+                    at = i;
+                    pages = least[k];
                 }
             }
-            // (not negative where there is one, so their bits are in order; of equal ones the shortest group)
-            const unsigned bits = top < 0.f ? 0u : __float_as_uint(top) + 1u, most = __reduce_max_sync(0xffffffffu, bits);
-            const int last = __reduce_max_sync(0xffffffffu, bits == most ? at : -1);
-            if (bits == most && at == last) {
-                best[j] = top;
-                from[j] = at;
-                shared_by[j] = pages;
+        }
+        const unsigned bits = top < 0.f ? 0u : __float_as_uint(top) + 1u, most = __reduce_max_sync(0xffffffffu, bits);
+        const int last = __reduce_max_sync(0xffffffffu, bits == most ? at : -1);
+        if (bits == most && at == last) {
+            best[j] = top;
+            from[j - 1] = at;
+            shared_by[j - 1] = pages;
+        }
+        __syncwarp();
+    }
+    for (int j = many; j > 0; j = from[j - 1]) groups.put(s + from[j - 1], s + j, shared_by[j - 1]);
+}
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+// A cluster with a warp for every sequence, which finds what it shares with the one before it; the first CTA goes on from there.
+// Segment 2 b is sequence b's own keys, 2 b + 1 the keys shared by the group that b leads.
+__global__ void __launch_bounds__(kPlanThreads) tree_shared_plan_kernel(const PlanArgs a) {
+    __shared__ int same[kMaxSeqs];
+    __shared__ int share[kMaxSeqs], begins[kMaxSeqs + 1], from[kMaxSeqs], shared_by[kMaxSeqs], active[kMaxSeqs];
+    __shared__ float best[2 * kMaxSeqs];
+    __shared__ int group_first[kMaxSeqs], group_members[kMaxSeqs], group_pages[kMaxSeqs];       // by place
+    __shared__ int pages_of[kMaxSeqs], node0[kMaxSeqs + 1], nodes_of[kMaxSeqs];                 // by sequence
+    __shared__ int n_of[kMaxSeqs], held_of[kMaxSeqs], ctx_of[kMaxSeqs], keys_of[kMaxSeqs];
+    __shared__ int seg_start[2 * kMaxSeqs], seg_unit[2 * kMaxSeqs], seg_tiles[2 * kMaxSeqs], seg_blocks[2 * kMaxSeqs], seg_weight[2 * kMaxSeqs];
+    __shared__ int2 tmp[kMaxSeqs / 32], totals;
+    cluster_arrive();       // (every CTA of the cluster has begun before one writes to another)
+    pdl_wait();
+    pdl_trigger();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t rank = cluster_rank();
+    const int b0 = (int)rank * (kPlanThreads / 32) + warp, found = b0 < a.batch ? pages_shared(a, b0) : 0;
+    cluster_wait();
+    if (lane == 0 && b0 < a.batch) {
+        uint32_t at;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(same + b0)));
+        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(found) : "memory");
+    }
+    cluster_arrive();
+    cluster_wait();
+    if (rank != 0) return;
+    if (tid < kMaxSeqs) {       // a thread for every sequence, up to the list of segments
+        int n = 0, held = 0, ctx = 0, keys = 0;
+        int2 total;
+        if (tid < a.batch) {
+            lengths_of(a, tid, n, held, ctx, keys);
+            n_of[tid] = n;
+            held_of[tid] = held;
+            ctx_of[tid] = ctx;
+            keys_of[tid] = keys;
+        }
+        // the sequences that have nodes, in order of their places, and those that share nothing with the one before
+        const bool begin = n > 0 && same[tid] == 0;
+        const int2 at = plan_scan(make_int2(n > 0, begin), tmp, &total);
+        const int place = at.x - 1, m = total.x, runs = total.y;
+        if (n > 0) {
+            active[place] = tid;
+            share[place] = same[tid];
+        }
+        if (begin) begins[at.y - 1] = place;
+        if (tid == 0) begins[runs] = m;
+        seq_barrier();
+        const Groups groups{group_first, group_members, group_pages};
+        for (int r = warp; r < runs; r += kMaxSeqs / 32) {
+            const int s = begins[r], e = begins[r + 1];
+            if (divide_even(share, s, e, a.pg.ps, groups)) continue;
+            if (e - s <= 32) divide_few(share, s, e, a.pg.ps, groups);
+            else divide_many(share, s, e, a.pg.ps, groups, best + s + r, from + s, shared_by + s);
+        }
+        seq_barrier();
+        const int first = n > 0 ? group_first[place] : 0, pages = n > 0 ? group_pages[place] : 0, lead = n > 0 ? active[first] : tid;
+        const bool grouped = pages > 0;
+        if (tid < a.batch) {
+            pages_of[tid] = pages;
+            if (a.groups) {
+                a.groups[2 * tid] = lead;
+                a.groups[2 * tid + 1] = pages;
             }
-            __syncwarp();
         }
-        if (lane == 0) {
-            for (int j = m; j > 0; j = from[j]) {
-                const int i = from[j];
-                members[i] = j - i;
-                if (j - i > 1) pages_of[i] = shared_by[j];
-            }
+        const int upto = plan_scan(make_int2(grouped ? n : 0, 0), tmp, &total).x;
+        if (tid < a.batch) node0[tid] = upto - (grouped ? n : 0);
+        if (tid == 0) node0[a.batch] = total.x;
+        seq_barrier();
+        // segments: own of sequence tid, and its group's where it leads one
+        int tiles[2] = {0, 0}, blocks[2] = {0, 0}, weight[2] = {a.weight1, a.weight1};
+        const int own_keys = keys - pages * a.pg.ps;
+        if (n > 0 && own_keys > 0) {
+            tiles[0] = (own_keys + (1 << a.kt) - 1) >> a.kt;
+            blocks[0] = (n * a.G + (1 << a.qt) - 1) >> a.qt;
+            if (n * a.G > 128) weight[0] = a.weight2;
         }
-    }
-    __syncthreads();
-    // (members and pages_of by place so far; from here on by sequence)
-    int lead = tid, pages = 0, many = 0;
-    if (n > 0) {
-        int i = place;
-        while (members[i] == 0) --i;        // (place 0 begins one)
-        lead = active[i];
-        pages = pages_of[i];
-        if (i == place && pages) many = members[i];
-    }
-    __syncthreads();
-    const bool grouped = n > 0 && pages > 0;
-    if (tid < a.batch) {
-        pages_of[tid] = grouped ? pages : 0;
-        a.head->groups[2 * tid] = lead;
-        a.head->groups[2 * tid + 1] = grouped ? pages : 0;
-        if (a.groups) {
-            a.groups[2 * tid] = lead;
-            a.groups[2 * tid + 1] = grouped ? pages : 0;
+        if (grouped && first == place) {        // its group's nodes lie before those of the next active one
+            const int after = place + group_members[place], nodes = (after < m ? node0[active[after]] : node0[a.batch]) - node0[tid];
+            nodes_of[tid] = nodes;
+            tiles[1] = (pages * a.pg.ps + (1 << a.kt) - 1) >> a.kt;
+            blocks[1] = (nodes * a.G + (1 << a.qt) - 1) >> a.qt;
+            if (nodes * a.G > 128) weight[1] = a.weight2;
         }
-    }
-    const int upto = plan_scan(grouped ? n : 0, tmp, &total);
-    if (tid < a.batch) node0[tid] = upto - (grouped ? n : 0);
-    if (tid == 0) node0[a.batch] = total;
-    __syncthreads();
-    // segments: own of sequence tid, and its group's where it leads one
-    int tiles[2] = {0, 0}, blocks[2] = {0, 0}, end = 0;
-    const int skip = grouped ? pages : 0, own_keys = keys - skip * a.pg.ps;
-    if (n > 0 && own_keys > 0) {
-        tiles[0] = (own_keys + a.KT - 1) / a.KT;
-        blocks[0] = (n * a.G + a.QT - 1) / a.QT;
-    }
-    if (many) {         // this thread's sequence leads: its group's nodes lie before those of the next active one
-        const int after = place + many;
-        end = after < m ? node0[active[after]] : node0[a.batch];
-        nodes_of[tid] = end - node0[tid];
-        tiles[1] = (int)(((long long)pages * a.pg.ps + a.KT - 1) / a.KT);
-        blocks[1] = ((end - node0[tid]) * a.G + a.QT - 1) / a.QT;
-    }
-    int cost[2], units[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        units[i] = blocks[i] * a.pg.hkv;
-        cost[i] = units[i] * (tiles[i] + a.extra);
-    }
-    int all, all_units;
-    const int cost_upto = plan_scan(cost[0] + cost[1], tmp, &all), unit_upto = plan_scan(units[0] + units[1], tmp, &all_units);
-    if (tid < a.batch) {
+        int cost[2], units[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            seg_start[2 * tid + i] = cost_upto - cost[1] - (i ? 0 : cost[0]);
-            seg_unit[2 * tid + i] = unit_upto - units[1] - (i ? 0 : units[0]);
+            units[i] = blocks[i] * a.pg.hkv;
+            cost[i] = units[i] * (tiles[i] * weight[i] + a.extra);
+        }
+        const int2 end = plan_scan(make_int2(cost[0] + cost[1], units[0] + units[1]), tmp, &total);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {       // (past the batch: empty, where the list ends)
+            seg_start[2 * tid + i] = end.x - cost[1] - (i ? 0 : cost[0]);
+            seg_unit[2 * tid + i] = end.y - units[1] - (i ? 0 : units[0]);
             seg_tiles[2 * tid + i] = tiles[i];
             seg_blocks[2 * tid + i] = blocks[i];
+            seg_weight[2 * tid + i] = weight[i];
+        }
+        if (tid == 0) totals = total;
+        seq_barrier();
+        if (tid < a.batch) {
+            const int e = 2 * lead + 1;
+            TreeSeq s;
+            s.n = n;
+            s.start = seg_start[2 * tid];
+            s.tiles = tiles[0];
+            s.blocks = blocks[0];
+            s.lead_start = seg_start[e];
+            s.lead_tiles = grouped ? seg_tiles[e] : 0;
+            s.lead_blocks = seg_blocks[e];
+            s.node0 = node0[tid] - node0[lead];
+            s.row = own_row(a, tid);
+            s.lead_row = lead_row(a, lead, node0[lead]);
+            s.weight = weight[0];
+            s.lead_weight = seg_weight[e];
+            a.seqs[tid] = s;
         }
     }
-    const int per = max((all + a.C - 1) / a.C, a.least);
+    __syncthreads();
+    const int all = totals.x, all_units = totals.y, per = max((all + a.C - 1) / a.C, a.least);
     if (tid == 0) {
         a.head->batch = a.batch;
         a.head->n_max = a.n_max;
         a.head->per = per;
         a.head->ok = 1;
     }
-    __syncthreads();
-    // rows of whole units: 2 C blocks of the CTAs, then the sequences' own, then the groups'
-    const int own0 = 2 * a.C * a.QT, lead0 = own0 + a.batch * a.pg.hkv * a.own_rows;
-    auto lead_row = [&](int b) { return lead0 + (node0[b] * a.G / 32 + b) * 32; };
-    if (tid < a.batch) {
-        const int e = 2 * lead + 1;
-        TreeSeq s{};
-        s.n = n;
-        s.start = seg_start[2 * tid];
-        s.tiles = tiles[0];
-        s.blocks = blocks[0];
-        s.lead_start = seg_start[e];
-        s.lead_tiles = grouped ? seg_tiles[e] : 0;
-        s.lead_blocks = seg_blocks[e];
-        s.node0 = node0[tid] - node0[lead];
-        s.row = own0 + tid * a.pg.hkv * a.own_rows;
-        s.lead_row = lead_row(lead);
-        a.seqs[tid] = s;
-    }
     for (int x = tid; x < a.batch * a.n_max; x += kPlanThreads) {
         const int b = x / a.n_max, i = x - b * a.n_max;
-        const int count = (b + 1 < a.batch ? node0[b + 1] : node0[a.batch]) - node0[b];
-        if (i < count) a.map[node0[b] + i] = x;
+        if (i < node0[b + 1] - node0[b]) a.map[node0[b] + i] = x;
     }
-    // The items of run c are numbers u + c for its units u: the list of units and the list of runs advance together. Four threads
-    // share a run's units.
-    constexpr int kShare = 4;
-    for (int x = tid; x < a.C * kShare; x += kPlanThreads) {
-        const int c = x / kShare, part = x % kShare;
-        const long long v0 = (long long)c * per, v1 = min(v0 + per, (long long)all);
-        if (v0 >= v1) {
-            if (part == 0) a.runs[c] = make_int2(0, 0);
-            continue;
-        }
-        int lo = 0, hi = 2 * a.batch;       // the last segment that begins at or before v0 and is not empty
+    // the last segment that begins at or before x and is not empty, of starts that do not fall
+    auto segment = [&](const int* begin, int x) {
+        int lo = 0, hi = 2 * a.batch;
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
-            if (seg_start[mid] <= v0) lo = mid; else hi = mid;
+            if (begin[mid] <= x) lo = mid; else hi = mid;
         }
-        while (lo > 0 && seg_blocks[lo] == 0) --lo;
-        int e = lo, unit = seg_tiles[e] + a.extra, idx = (int)((v0 - seg_start[e]) / unit);
-        long long start = seg_start[e] + (long long)idx * unit;
-        if (v0 - start >= seg_tiles[e]) {       // the run begins behind the unit's tiles
-            ++idx;
-            start += unit;
+        return lo;
+    };
+    // The items of run c are numbers u + c for its units u: the list of units and the list of runs advance together.
+    for (int c = tid; c < a.C; c += kPlanThreads) {
+        const long long v0 = (long long)c * per, v1 = min(v0 + per, (long long)all);
+        int2 run = make_int2(0, 0);
+        if (v0 < v1) {
+            auto unit_at = [&](int v, bool next) {      // the unit that has the tile at place v, or (next) the first tile from there on
+                const int e = segment(seg_start, v), w = seg_weight[e], t = seg_tiles[e], size = t * w + a.extra, idx = (v - seg_start[e]) / size;
+                return seg_unit[e] + idx + (next && v - seg_start[e] - idx * size > (t - 1) * w);
+            };
+            run.x = unit_at((int)v0, true) + c;
+            run.y = unit_at((int)v1 - 1, false) + c + 1;
         }
-        int u = seg_unit[e] + idx;
-        const int first = u;
-        for (; start < v1; ++u, ++idx, start += unit) {
-            while (e < 2 * a.batch && idx >= seg_blocks[e] * a.pg.hkv) {    // on to the next segment
-                idx = 0;
-                ++e;
-                if (e < 2 * a.batch) unit = seg_tiles[e] + a.extra;
-            }
-            if (e >= 2 * a.batch) break;
-            if ((u - first) % kShare != part) continue;
-            const int b = e >> 1, t = seg_tiles[e], bl = seg_blocks[e];
-            TreeItem it;
-            it.b = b;
-            it.h = idx / bl;
-            it.row0 = (idx - it.h * bl) * a.QT;
-            it.lo = (int)max(v0 - start, 0LL);
-            it.hi = (int)min(v1 - start, (long long)t);
-            const bool whole = it.lo == 0 && it.hi == t;
-            const int cut = (2 * c + (start < v0 ? 0 : 1)) * a.QT;
-            if (e & 1) {
-                it.page0 = 0;
-                it.held = pages_of[b];
-                it.ctx = it.keys = pages_of[b] * a.pg.ps;
-                it.first = ~node0[b];
-                it.nodes = nodes_of[b];
-                it.dst = whole ? lead_row(b) + it.h * a.lead_rows + it.row0 : cut;
-            } else {
-                int n2, held2, ctx2, keys2;
-                lengths_of(a, b, n2, held2, ctx2, keys2);
-                it.page0 = pages_of[b];
-                it.held = held2 - it.page0;
-                it.ctx = ctx2 - it.page0 * a.pg.ps;
-                it.keys = keys2 - it.page0 * a.pg.ps;
-                it.first = b * a.n_max;
-                it.nodes = n2;
-                it.dst = !whole ? cut : pages_of[b] ? own0 + (b * a.pg.hkv + it.h) * a.own_rows + it.row0 : -1;
-            }
+        a.runs[c] = run;
+    }
+    // Items by units, `share` threads for each, where there are few.
+    int share_log = 0;
+    while ((all_units << (share_log + 1)) <= kPlanThreads && share_log < 5) ++share_log;
+    for (int x = tid; x < all_units << share_log; x += kPlanThreads) {
+        const int u = x >> share_log, e = segment(seg_unit, u), idx = u - seg_unit[e], b = e >> 1;
+        const int t = seg_tiles[e], bl = seg_blocks[e], w = seg_weight[e], start = seg_start[e] + idx * (t * w + a.extra);
+        const int c0 = start / per, c1 = (start + (t - 1) * w) / per;
+        TreeItem it;
+        it.b = b;
+        it.h = bl == 1 ? idx : idx / bl;
+        it.row0 = (idx - it.h * bl) << a.qt;
+        int whole;          // where its rows go if the unit is one item
+        if (e & 1) {
+            it.page0 = 0;
+            it.held = pages_of[b];
+            it.ctx = it.keys = pages_of[b] * a.pg.ps;
+            it.first = ~node0[b];
+            it.nodes = nodes_of[b];
+            whole = lead_row(a, b, node0[b]) + it.h * a.lead_rows + it.row0;
+        } else {
+            it.page0 = pages_of[b];
+            it.held = held_of[b] - it.page0;
+            it.ctx = ctx_of[b] - it.page0 * a.pg.ps;
+            it.keys = keys_of[b] - it.page0 * a.pg.ps;
+            it.first = b * a.n_max;
+            it.nodes = n_of[b];
+            whole = pages_of[b] ? own_row(a, b) + it.h * a.own_rows + it.row0 : -1;
+        }
+        for (int c = c0 + (x & ((1 << share_log) - 1)); c <= c1; c += 1 << share_log) {
+            const long long v0 = (long long)c * per;
+            // (a tile is in the run that its place is in)
+            it.lo = c == c0 ? 0 : ((int)(v0 - start) + w - 1) / w;
+            it.hi = c == c1 ? t : ((int)(v0 + per - start) + w - 1) / w;
+            it.dst = c0 == c1 ? whole : (2 * c + (start < v0 ? 0 : 1)) << a.qt;
             a.items[u + c] = it;
         }
-        if (part == 0) a.runs[c] = make_int2(first + c, u + c);
     }
 }
 
@@ -405,10 +506,10 @@ __global__ void __launch_bounds__(kJoinThreads, join_blocks(HD, RW)) tree_shared
         const bool some = there && node < s.n;
         // own parts, then the group's: how many, the CTA of the first, the unit's place in the list, and the row
         const int r0 = node * a.G + g, r1 = (s.node0 + node) * a.G + g;
-        const int u0 = s.start + (h * s.blocks + r0 / QT) * (s.tiles + extra), c0 = u0 / per;
-        const int u1 = s.lead_start + (h * s.lead_blocks + r1 / QT) * (s.lead_tiles + extra), c1 = u1 / per;
-        const int n0 = some && s.tiles ? (u0 + s.tiles - 1) / per - c0 + 1 : 0;
-        const int n1 = some && s.lead_tiles ? (u1 + s.lead_tiles - 1) / per - c1 + 1 : 0;
+        const int u0 = s.start + (h * s.blocks + r0 / QT) * (s.tiles * s.weight + extra), c0 = u0 / per;
+        const int u1 = s.lead_start + (h * s.lead_blocks + r1 / QT) * (s.lead_tiles * s.lead_weight + extra), c1 = u1 / per;
+        const int n0 = some && s.tiles ? (u0 + (s.tiles - 1) * s.weight) / per - c0 + 1 : 0;
+        const int n1 = some && s.lead_tiles ? (u1 + (s.lead_tiles - 1) * s.lead_weight) / per - c1 + 1 : 0;
         const bool written = n0 == 1 && s.lead_tiles == 0;
         const int parts = written ? 0 : n0 + n1;
         if (!begun) pdl_wait();
@@ -503,6 +604,11 @@ cudaError_t launch_join(const dflare_cache* c, const TreeArgs& a, int QT, int ex
     return rows < 4096 ? go(tree_shared_join_kernel<T, HD, 1>, 1) : go(tree_shared_join_kernel<T, HD, 4>, 4);
 }
 
+int log2_of(int v) {
+    int l = 0;
+    while (1 << (l + 1) <= v) ++l;
+    return l;
+}
 dflare_status refuse(const char* call, const char* m) {
     noalloc_set_error(std::string(call) + ": " + m);
     return DFLARE_EINVAL;
@@ -552,12 +658,14 @@ dflare_status dflare_cache_share_plan(dflare_cache* c, const int32_t* n_nodes_de
     a.batch = batch;
     a.n_max = n_max;
     a.G = c->cfg.n_q_heads / c->cfg.n_kv_heads;
-    a.QT = y.QT, a.KT = y.KT, a.extra = y.extra, a.least = y.least, a.C = y.C;
+    a.qt = log2_of(y.QT), a.kt = log2_of(y.KT), a.C = y.C;      // (powers of two)
+    a.weight1 = y.weight1, a.weight2 = y.weight2, a.extra = y.extra, a.least = y.least;
     a.own_rows = y.own_rows, a.lead_rows = y.lead_rows;
     DeviceGuard guard(c->device);
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    cudaError_t e = launch_kernel(true, tree_same_kernel, dim3(batch), dim3(kSameThreads), 0, s, a);
-    if (e == cudaSuccess) e = launch_kernel(true, tree_shared_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
+    const int ctas = (batch + kPlanThreads / 32 - 1) / (kPlanThreads / 32);
+    static_assert(kMaxSeqs <= 8 * (kPlanThreads / 32), "a cluster of up to eight CTAs has a warp for every sequence");
+    const cudaError_t e = launch_cluster(true, ctas, tree_shared_plan_kernel, dim3(ctas), dim3(kPlanThreads), 0, s, a);
     if (e == cudaSuccess) return DFLARE_OK;
     noalloc_set_error(std::string(call) + ": " + cudaGetErrorString(e));
     return DFLARE_ECUDA;
