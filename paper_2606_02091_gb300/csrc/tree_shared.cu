@@ -175,10 +175,13 @@ __device__ __forceinline__ int pages_shared(const PlanArgs& a, int b) {
     }
 }
 
-// What a group of `many` saves that shares `tokens`, in keys: less what one more unit and the joining of its rows cost, in keys
-// that could be read meanwhile.
-constexpr float kGroupCost = 512.f, kMemberCost = 64.f;
-__device__ __forceinline__ float saving(float many, float tokens) { return fmaxf(fmaf(many - 1.f, tokens, -fmaf(kMemberCost, many, kGroupCost)), 0.f); }
+// What a group saves of which `many` share `tokens`, in keys, `costs` being the sum of its members' costs: a member's rows leave and
+// join one more partial result each, a group is one more unit. Measured with 32/8 heads of 128, a layer over groups of 4
+// that share 512 and 1024 tokens, together and apart: 16 groups, single tokens 32.2 and 37.1 us together, 43.2 and 59.3 apart; trees
+// of 16 nodes 52.9 and 59.0, 49.7 and 63.4; 4 groups, trees of 16 19.2 and 22.0, 17.4 and 20.8; 8 groups of 2 over 128 tokens, single
+// tokens 14.3 and 13.2, over 256 14.2 and 14.7.
+constexpr float kGroupCost = 128.f, kMemberCost = 16.f, kRowCost = 8.f;
+__device__ __forceinline__ float saving(float many, float tokens, float costs) { return fmaxf(fmaf(many - 1.f, tokens, -(costs + kGroupCost)), 0.f); }
 
 // The places s .. e - 1 are one group that shares `pages`, or one by itself (a warp).
 struct Groups {
@@ -193,17 +196,24 @@ struct Groups {
     }
 };
 // Sequences s .. e - 1 (by place) of which all neighbours share the same number of pages: all are one group, or none are.
-__device__ __forceinline__ bool divide_even(const int* share, int s, int e, int ps, const Groups& groups) {
+// (False: that is not so, as neighbours share differently or a member costs more than it saves.) costs: sums of what the places
+// before each cost.
+__device__ __forceinline__ bool divide_even(const int* share, const int* costs, int s, int e, int ps, const Groups& groups) {
     const int lane = threadIdx.x & 31;
-    int low = 0x7fffffff, high = 0;
-    for (int i = s + 1 + lane; i < e; i += 32) {
-        low = min(low, share[i]);
-        high = max(high, share[i]);
+    int low = 0x7fffffff, high = 0, dear = 0;
+    for (int i = s + lane; i < e; i += 32) {
+        if (i > s) {
+            low = min(low, share[i]);
+            high = max(high, share[i]);
+        }
+        dear = max(dear, costs[i + 1] - costs[i]);
     }
     low = __reduce_min_sync(0xffffffffu, low);
     high = __reduce_max_sync(0xffffffffu, high);
-    if (e - s > 1 && low != high) return false;
-    if (e - s > 1 && saving((float)(e - s), (float)low * (float)ps) > 0.f) {
+    dear = __reduce_max_sync(0xffffffffu, dear);
+    const float tokens = (float)low * (float)ps;
+    if (e - s > 1 && (low != high || (float)dear >= tokens)) return false;
+    if (e - s > 1 && saving((float)(e - s), tokens, (float)(costs[e] - costs[s])) > 0.f) {
         groups.put(s, e, low);
     } else {
         for (int i = s + lane; i < e; i += 32) {
@@ -214,8 +224,9 @@ __device__ __forceinline__ bool divide_even(const int* share, int s, int e, int 
     return true;
 }
 // The same where they differ, up to 32: a warp finds the best division, lane i holding best(i).
-__device__ __forceinline__ void divide_few(const int* share, int s, int e, int ps, const Groups& groups) {
+__device__ __forceinline__ void divide_few(const int* share, const int* costs, int s, int e, int ps, const Groups& groups) {
     const int lane = threadIdx.x & 31, many = e - s;
+    const int before = costs[min(s + lane, e)], upto = costs[min(s + lane + 1, e)];
     const int mine = lane < many ? share[s + lane] : 0;
     const float tokens = (float)mine * (float)ps;
     float best = 0.f, size = (float)-lane, least_f = INFINITY;      // size: of the group that begins here
@@ -228,7 +239,8 @@ __device__ __forceinline__ void divide_few(const int* share, int s, int e, int p
             least = min(least, next);
             least_f = fminf(least_f, next_f);
         }
-        const float v = best + (lane < j - 1 ? saving(size, least_f) : 0.f);
+        const float spent = (float)(__shfl_sync(0xffffffffu, upto, j - 1) - before);
+        const float v = best + (lane < j - 1 ? saving(size, least_f, spent) : 0.f);
         // (not negative: their bits are in order; of equal ones the shortest group)
         const unsigned bits = lane < j ? __float_as_uint(v) + 1u : 0u, top = __reduce_max_sync(0xffffffffu, bits);
         const int at = 31 - __clz(__ballot_sync(0xffffffffu, bits == top));
@@ -247,7 +259,7 @@ __device__ __forceinline__ void divide_few(const int* share, int s, int e, int p
 }
 // The same for more, with best (e - s + 1 numbers), from and shared_by (e - s each, by place) in shared memory: lane l looks at
 // groups that begin at l, l + 32, ...
-__device__ __forceinline__ void divide_many(const int* share, int s, int e, int ps, const Groups& groups, float* best, int* from, int* shared_by) {
+__device__ __forceinline__ void divide_many(const int* share, const int* costs, int s, int e, int ps, const Groups& groups, float* best, int* from, int* shared_by) {
     const int lane = threadIdx.x & 31, many = e - s;
     int least[kMaxSeqs / 32];
 #pragma unroll
@@ -264,7 +276,7 @@ __device__ __forceinline__ void divide_many(const int* share, int s, int e, int 
             if (32 * k >= j) break;
             if (i < j - 1) least[k] = min(least[k], next);
             if (i < j) {
-                const float v = best[i] + (i < j - 1 ? saving((float)(j - i), (float)least[k] * (float)ps) : 0.f);
+                const float v = best[i] + (i < j - 1 ? saving((float)(j - i), (float)least[k] * (float)ps, (float)(costs[s + j] - costs[s + i])) : 0.f);
                 if (v > top) {
                     top = v;
                     at = i;
@@ -296,7 +308,7 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 // Segment 2 b is sequence b's own keys, 2 b + 1 the keys shared by the group that b leads.
 __global__ void __launch_bounds__(kPlanThreads) tree_shared_plan_kernel(const PlanArgs a) {
     __shared__ int same[kMaxSeqs];
-    __shared__ int share[kMaxSeqs], begins[kMaxSeqs + 1], from[kMaxSeqs], shared_by[kMaxSeqs], active[kMaxSeqs];
+    __shared__ int share[kMaxSeqs], costs[kMaxSeqs + 1], begins[kMaxSeqs + 1], from[kMaxSeqs], shared_by[kMaxSeqs], active[kMaxSeqs];
     __shared__ float best[2 * kMaxSeqs];
     __shared__ int group_first[kMaxSeqs], group_members[kMaxSeqs], group_pages[kMaxSeqs];       // by place
     __shared__ int pages_of[kMaxSeqs], node0[kMaxSeqs + 1], nodes_of[kMaxSeqs];                 // by sequence
@@ -332,19 +344,22 @@ __global__ void __launch_bounds__(kPlanThreads) tree_shared_plan_kernel(const Pl
         const bool begin = n > 0 && same[tid] == 0;
         const int2 at = plan_scan(make_int2(n > 0, begin), tmp, &total);
         const int place = at.x - 1, m = total.x, runs = total.y;
+        const int cost_upto = plan_scan(make_int2(n > 0 ? (int)kMemberCost + (int)kRowCost * n * a.G : 0, 0), tmp, &total).x;
         if (n > 0) {
             active[place] = tid;
             share[place] = same[tid];
+            costs[place + 1] = cost_upto;
         }
+        if (tid == 0) costs[0] = 0;
         if (begin) begins[at.y - 1] = place;
         if (tid == 0) begins[runs] = m;
         seq_barrier();
         const Groups groups{group_first, group_members, group_pages};
         for (int r = warp; r < runs; r += kMaxSeqs / 32) {
             const int s = begins[r], e = begins[r + 1];
-            if (divide_even(share, s, e, a.pg.ps, groups)) continue;
-            if (e - s <= 32) divide_few(share, s, e, a.pg.ps, groups);
-            else divide_many(share, s, e, a.pg.ps, groups, best + s + r, from + s, shared_by + s);
+            if (divide_even(share, costs, s, e, a.pg.ps, groups)) continue;
+            if (e - s <= 32) divide_few(share, costs, s, e, a.pg.ps, groups);
+            else divide_many(share, costs, s, e, a.pg.ps, groups, best + s + r, from + s, shared_by + s);
         }
         seq_barrier();
         const int first = n > 0 ? group_first[place] : 0, pages = n > 0 ? group_pages[place] : 0, lead = n > 0 ? active[first] : tid;

@@ -203,6 +203,24 @@ def test_a_broadcast_input_and_gradient():
 
 
 @pytest.mark.gpu
+def test_rows_past_32_bit_offsets():
+    """4.6 GB of heads: the last rows against the same rows in a call of their own, and a wide stride between few rows."""
+    rows, hq, hd = 450000, 40, 128
+    x = torch.randn((rows, hq, hd), dtype=torch.bfloat16, device="cuda")
+    assert x[:-99].numel() > 2 ** 31
+    gain, phase, pos = torch.ones(hd, dtype=torch.bfloat16, device="cuda"), P.rope_phases(hd, 1e4)[0], torch.arange(rows, dtype=torch.int32, device="cuda")
+    out, few = torch.empty_like(x), torch.empty_like(x[:99])
+    P.qk_norm_rope(x, None, pos, phase, gain, None, out, None)
+    P.qk_norm_rope(x[-99:], None, pos[-99:].contiguous(), phase, gain, None, few, None)
+    assert torch.equal(out[-99:], few)
+    far = x[::150000][:, :2]        # rows 768 million elements apart
+    three, want = torch.zeros((3, 2, hd), dtype=x.dtype, device="cuda"), torch.zeros((3, 2, hd), dtype=x.dtype, device="cuda")
+    P.qk_norm_rope(far, None, pos[:3], phase, gain, None, three, None)
+    P.qk_norm_rope(far.contiguous(), None, pos[:3], phase, gain, None, want, None)
+    assert far.stride(0) == 150000 * hq * hd and torch.equal(three, want)
+
+
+@pytest.mark.gpu
 def test_on_another_stream_and_in_a_graph():
     rng = np.random.default_rng(10)
     q, k, qg, kg, dq, dk = inputs(rng, 700, 8, 2, 64, "bf16")

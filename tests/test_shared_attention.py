@@ -92,7 +92,7 @@ CASES = [
     (0, [(0, 30, 9, 4), (1, 1, 20, 4), (2, 1, 3, 4), (2, 1, 9, 4)], 4, 1, 64, 64, [1]),            # shared too little: by themselves
     (20, [(0, 12, 5, 4), (0, 12, 8, 4), (0, 12, 1, 3), (1, 20, 2, 4), (1, 20, 9, 1)], 14, 2, 64, 32, None),   # a system prompt under the prompts
     (0, [(0, 33, 4, 2), (0, 33, 9, 0), (0, 33, 12, 2), (2, 0, 0, 0), (0, 33, 50, 1)], 8, 1, 128, 32, [3]),    # some without nodes
-    (0, [(0, 50, 70, 70), (0, 50, 65, 65), (0, 50, 1, 3)], 4, 1, 64, 32, [3]),                     # mask rows of three words
+    (0, [(0, 200, 70, 70), (0, 200, 65, 65), (0, 200, 1, 3)], 4, 1, 64, 32, [3]),                  # mask rows of three words
     (0, [(0, 17, 5, 9), (0, 16, 40, 9), (0, 19, 2, 9)], 8, 8, 64, 128, [3]),                       # shared to different depths; one head each
     (0, [(0, 3, 0, 1)], 64, 1, 128, 16, [1]),                                                      # alone
 ]
@@ -114,7 +114,7 @@ def test_attend_shared_matches_the_definition(base, seqs, hq, hkv, hd, page, gro
         assert [x for x in sizes if x] == [x for x in groups if x > 1]
 
 
-def best_saving(lens, counts, table, page):
+def best_saving(lens, counts, table, page, heads):
     """The most that any division into groups of neighbours saves, in keys, and what a given one does."""
     act = [b for b, c in enumerate(counts) if c]
 
@@ -124,7 +124,8 @@ def best_saving(lens, counts, table, page):
         return int(np.argmin(same)) if not same.all() else most
 
     near = [0] + [shared(act[i - 1], act[i]) for i in range(1, len(act))]
-    value = lambda i, j: max((j - i - 1) * min(near[i + 1:j]) * page - 512 - 64 * (j - i), 0) if j - i > 1 else 0     # noqa: E731
+    cost = [16 + 8 * counts[b] * heads for b in act]
+    value = lambda i, j: max((j - i - 1) * min(near[i + 1:j]) * page - 128 - sum(cost[i:j]), 0) if j - i > 1 else 0     # noqa: E731
     best = [0]
     for j in range(1, len(act) + 1):
         best.append(max(best[i] + value(i, j) for i in range(j)))
@@ -152,14 +153,15 @@ def test_groups_save_the_most(seed):
     batch = [3, 17, 40, 64, 150, 256][seed]
     prompts = np.sort(rng.integers(0, max(2, batch // 5), batch)) if seed % 2 else rng.integers(0, 3, batch)
     depth = {x: int(rng.integers(0, 90)) for x in range(300)}
-    seqs = [(int(x), int(max(0, depth[int(x)] - rng.integers(0, 3))), int(rng.integers(0, 40)), int(rng.integers(0, 3))) for x in prompts]
-    p = Shared(rng, seqs, hq=2, hkv=1, hd=64, page=16, dtype="bf16", base=int(rng.integers(0, 8)), nodes=2)
-    work, groups = p.cache.shared_work(batch, 2), torch.full((batch, 2), 77, dtype=torch.int32, device="cuda")
-    p.cache.share_plan(i32(p.counts), 2, work, groups=groups)
-    most, of = best_saving(p.lens, p.counts, p.table, 16)
+    top = [2, 9, 3, 30, 2, 12][seed]
+    seqs = [(int(x), int(max(0, depth[int(x)] - rng.integers(0, 3))), int(rng.integers(0, 40)), int(rng.integers(0, top + 1))) for x in prompts]
+    p = Shared(rng, seqs, hq=2, hkv=1, hd=64, page=16, dtype="bf16", base=int(rng.integers(0, 8)), nodes=top)
+    work, groups = p.cache.shared_work(batch, top), torch.full((batch, 2), 77, dtype=torch.int32, device="cuda")
+    p.cache.share_plan(i32(p.counts), top, work, groups=groups)
+    most, of = best_saving(p.lens, p.counts, p.table, 16, 2)
     assert of(groups.cpu().numpy()) == most and p.cache.error() == 0
-    q = queries(rng, p, batch, 2)
-    mask, seen = tree_masks(rng, p.lens, p.counts, 2)
+    q = queries(rng, p, batch, top)
+    mask, seen = tree_masks(rng, p.lens, p.counts, top)
     check_shared(p, q, seen, mask)
 
 
@@ -191,13 +193,13 @@ def test_runs_that_cross_from_unit_to_unit(nodes, hq, hkv, hd, prompts, ways, pa
 def test_rows_that_see_none_of_their_own_keys(dtype, nodes):
     """Masks without a bit: a row has the shared keys alone, or, without a context, none at all."""
     rng = np.random.default_rng(nodes)
-    p = Shared(rng, [(0, 64, 0, nodes), (0, 64, 0, nodes), (1, 0, 0, nodes)], hq=8, hkv=2, hd=64, page=16, dtype=dtype)
+    p = Shared(rng, [(0, 200, 0, nodes), (0, 200, 0, nodes), (1, 0, 0, nodes)], hq=8, hkv=2, hd=64, page=16, dtype=dtype)
     a = np.zeros((3, nodes, nodes), bool)
     a[0, 1, 0] = True
     seen = [np.concatenate([np.ones((nodes, x), bool), a[b]], 1) for b, x in enumerate(p.lens)]
     q = queries(rng, p, 3, nodes)
     groups = check_shared(p, q, seen, i32(words(a)))
-    assert groups[:2].tolist() == [[0, 64], [0, 64]]
+    assert groups[:2].tolist() == [[0, 200], [0, 200]]
     out, lse, _ = run_shared(p, q, i32(words(a)))
     assert not host(out)[2].any() and np.isneginf(host(lse)[2]).all()
 
@@ -208,11 +210,11 @@ def test_rows_that_see_none_of_their_own_keys(dtype, nodes):
 def test_unseen_infinities_and_nans_stay_out(dtype, nodes, hd):
     """Node 1's key and value are NaN and infinite in each sequence of a group: rows that do not see it have the same bits."""
     rng = np.random.default_rng(nodes)
-    p = Shared(rng, [(0, 50, 17, nodes), (0, 50, 3, nodes - 2), (0, 50, 40, nodes)], hq=8, hkv=2, hd=hd, page=16, dtype=dtype)
+    p = Shared(rng, [(0, 250, 17, nodes), (0, 250, 3, nodes - 2), (0, 250, 40, nodes)], hq=8, hkv=2, hd=hd, page=16, dtype=dtype)
     q = queries(rng, p, 3, nodes)
     mask, seen = tree_masks(rng, p.lens, p.counts, nodes)
     clean, clean_lse, groups = run_shared(p, q, mask)
-    assert groups[:, 1].tolist() == [50] * 3
+    assert groups[:, 1].tolist() == [250] * 3
     for b, x in enumerate(p.lens):
         page, off = p.table[b, (x + 1) // 16], (x + 1) % 16
         p.v[0, page, :, off, 3], p.v[0, page, :, off, hd - 1] = math.inf, math.nan

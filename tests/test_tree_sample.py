@@ -284,6 +284,26 @@ def test_a_draft_with_more_rows_and_odd_addresses():
 
 
 @pytest.mark.gpu
+def test_rows_past_32_bit_offsets():
+    """Probabilities of 18 GB: the last sequences' rows lie behind 2^32 elements. Rows that no walk visits are left as they come."""
+    rng = np.random.default_rng(12)
+    batch, n, vocab = 41, 500, 220000
+    target, draft = (torch.empty((batch, n, vocab), device="cuda") for _ in range(2))
+    assert target[:-1].numel() > 2 ** 32
+    tokens, parents, p, q, u = make(rng, 1, 4, vocab, "drawn", 1)
+    wide = lambda x, fill: np.concatenate([np.tile(x, (batch, 1)), np.full((batch, n - 4), fill, x.dtype)], 1)     # noqa: E731
+    for b in (0, 39, 40):
+        target[b, :4], draft[b, :4] = torch.from_numpy(p[0]).cuda(), torch.from_numpy(q[0]).cuda()
+    counts = np.zeros(batch, np.int32)
+    counts[[0, 39, 40]] = 4
+    out = [torch.zeros(s, dtype=torch.int32, device="cuda") for s in ((batch,), (batch, n), (batch,))]
+    P.tree_sample(i32(wide(tokens, 0)), i32(wide(parents, -1)), i32(counts), target, draft, torch.from_numpy(wide(u, 0.5)).cuda(), *out)
+    want, token = walk(tokens[0], parents[0], 4, p[0], q[0], u[0], False)
+    for b in (0, 39, 40):
+        assert out[1][b, :int(out[0][b])].tolist() == want and int(out[2][b]) == token
+
+
+@pytest.mark.gpu
 def test_on_another_stream_and_in_a_graph():
     rng = np.random.default_rng(11)
     batch, n, vocab = 5, 12, 30000
