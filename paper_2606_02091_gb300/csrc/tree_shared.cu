@@ -500,20 +500,24 @@ __global__ void __launch_bounds__(kPlanThreads) tree_shared_plan_kernel(const Pl
 }
 
 // Rows whose keys several items read, each of them in the order own keys, shared keys; and rows that none did. As
-// tree_join_kernel, RW rows to a warp, with what the plan says of a row's sequence.
-constexpr int kJoinThreads = 128;
+// tree_join_kernel, RW rows to a warp or PW warps to a row, with what the plan says of a row's sequence.
+template <int PW> constexpr int kJoinThreads = PW > 4 ? 32 * PW : 128;
 constexpr int join_blocks(int HD, int RW) { return HD == 64 ? 6 : RW == 1 ? 5 : 4; }
 
-template <class T, int HD, int RW>
-__global__ void __launch_bounds__(kJoinThreads, join_blocks(HD, RW)) tree_shared_join_kernel(const TreeArgs a, int QT, int extra, bool blocks) {
-    constexpr int LPR = 32 / RW, E = HD / LPR, V = E < 4 ? E : 4, J = RW == 4 ? 4 : 8;
-    const int lane = threadIdx.x & 31, l = lane % LPR, warp = threadIdx.x >> 5;
+template <class T, int HD, int RW, int PW>
+__global__ void __launch_bounds__(kJoinThreads<PW>, PW > 4 ? 2 : join_blocks(HD, RW)) tree_shared_join_kernel(const TreeArgs a, int QT, int extra, bool blocks) {
+    static_assert(RW == 1 || PW == 1, "several rows per warp or several warps per row");
+    constexpr int LPR = 32 / RW, E = HD / LPR, V = E < 4 ? E : 4, J = RW == 4 ? 4 : 8, ROWS = kJoinThreads<PW> / 32 / PW * RW;
+    __shared__ float others[PW > 1 ? kJoinThreads<PW> / 32 : 1][HD + 2];     // of a row's warps: output, maximum, sum
+    const int lane = threadIdx.x & 31, l = lane % LPR, warp = threadIdx.x >> 5, pw = warp % PW;
     // the plan is older than the kernel before this one, which let this one start after its own wait
     const bool ok = a.head->batch == a.batch && a.head->n_max == a.n_max && a.head->ok;
     const int per = ok ? a.head->per : 1;
-    const unsigned rows = (unsigned)a.batch * a.n_max * a.hq, step = gridDim.x * (kJoinThreads / 32) * RW;
-    unsigned row = (blockIdx.x * (kJoinThreads / 32) + warp) * RW + lane / LPR;
-    for (bool begun = false; !begun || row - lane / LPR < rows; row += step) {
+    bool begun = false;
+    const unsigned rows = (unsigned)a.batch * a.n_max * a.hq, step = gridDim.x * ROWS;
+    unsigned row = blockIdx.x * ROWS + warp / PW * RW + lane / LPR;
+    // (the CTA's warps go round together: with several to a row they meet)
+    for (unsigned base = blockIdx.x * ROWS; base < rows; base += step, row += step) {
         const bool there = ok && row < rows;
         const int head = row % a.hq, node = row / a.hq % a.n_max, b = there ? row / a.hq / a.n_max : 0;
         const int h = head / a.G, g = head - h * a.G;
@@ -526,11 +530,12 @@ __global__ void __launch_bounds__(kJoinThreads, join_blocks(HD, RW)) tree_shared
         const int n0 = some && s.tiles ? (u0 + (s.tiles - 1) * s.weight) / per - c0 + 1 : 0;
         const int n1 = some && s.lead_tiles ? (u1 + (s.lead_tiles - 1) * s.lead_weight) / per - c1 + 1 : 0;
         const bool written = n0 == 1 && s.lead_tiles == 0;
-        const int parts = written ? 0 : n0 + n1;
+        const int whole = written ? 0 : n0 + n1, parts = (whole - pw + PW - 1) / PW;       // this warp's: pw, pw + PW, ...
         if (!begun) pdl_wait();
         begun = true;
         const int most = __reduce_max_sync(0xffffffffu, parts);
-        auto at = [&](int i) -> size_t {
+        auto at = [&](int k) -> size_t {
+            const int i = pw + k * PW;
             const bool own = i < n0;
             const int c = own ? c0 + i : c1 + i - n0, u = own ? u0 : u1, r = own ? r0 : r1;
             if ((own ? n0 : n1) == 1)
@@ -590,7 +595,36 @@ __global__ void __launch_bounds__(kJoinThreads, join_blocks(HD, RW)) tree_shared
         }
 #pragma unroll
         for (int o = LPR / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (!there || written) continue;
+        if constexpr (PW > 1) {
+            // the row's warps' results against their common maximum: each adds up its part of the elements
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < E; ++e) others[warp][l * E + e] = acc[e];
+            if (l == 0) {
+                others[warp][HD] = m;
+                others[warp][HD + 1] = sum;
+            }
+            __syncthreads();
+            if (pw == 0) {
+                float top = m;
+#pragma unroll
+                for (int q = 1; q < PW; ++q) top = fmaxf(top, others[warp + q][HD]);
+                const float ref = top == -INFINITY ? 0.f : top;
+                float f = exp2f(m - ref);
+                sum *= f;
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[e] *= f;
+#pragma unroll
+                for (int q = 1; q < PW; ++q) {
+                    f = exp2f(others[warp + q][HD] - ref);
+                    sum = fmaf(others[warp + q][HD + 1], f, sum);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) acc[e] = fmaf(others[warp + q][l * E + e], f, acc[e]);
+                }
+                m = top;
+            }
+        }
+        if (!there || written || pw) continue;
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         T* out = static_cast<T*>(a.out) + (size_t)row * HD;
 #pragma unroll
@@ -609,18 +643,27 @@ __global__ void __launch_bounds__(kJoinThreads, join_blocks(HD, RW)) tree_shared
     }
 }
 
+template <int R, int P>
+struct JoinForm {
+    static constexpr int RW = R, PW = P;
+};
 template <class T, int HD>
 cudaError_t launch_join(const dflare_cache* c, const TreeArgs& a, int QT, int extra, bool blocks, cudaStream_t s) {
     const long long rows = (long long)a.batch * a.n_max * a.hq;
-    auto go = [&](auto kernel, int RW) {
-        const long long per = kJoinThreads / 32 * RW, most = (long long)c->num_sms * join_blocks(HD, RW);
-        return launch_kernel(true, kernel, dim3((unsigned)std::min((rows + per - 1) / per, most)), dim3(kJoinThreads), 0, s, a, QT, extra, blocks);
+    auto go = [&](auto form) {
+        constexpr int RW = decltype(form)::RW, PW = decltype(form)::PW;
+        constexpr int per = kJoinThreads<PW> / 32 / PW * RW;
+        const long long most = (long long)c->num_sms * (PW > 4 ? 2 : join_blocks(HD, RW));
+        return launch_kernel(true, tree_shared_join_kernel<T, HD, RW, PW>, dim3((unsigned)std::min((rows + per - 1) / per, most)), dim3(kJoinThreads<PW>), 0, s,
+                             a, QT, extra, blocks);
     };
     // Measured, a layer: 512 rows 17.1 us with a warp for each (four parts at a time 18.4); 4096 rows 31.0 with one for two, 32.5 for
     // four, 35.8 for each; 8192 rows 157 for two, 154 for four.
-    if (rows < 4096) return go(tree_shared_join_kernel<T, HD, 1>, 1);
-    if (rows < 8192) return go(tree_shared_join_kernel<T, HD, 2>, 2);
-    return go(tree_shared_join_kernel<T, HD, 4>, 4);
+    if (rows < 256) return go(JoinForm<1, 8>());
+    if (rows < 1024) return go(JoinForm<1, 4>());
+    if (rows < 4096) return go(JoinForm<1, 1>());
+    if (rows < 8192) return go(JoinForm<2, 1>());
+    return go(JoinForm<4, 1>());
 }
 
 int log2_of(int v) {
