@@ -104,7 +104,11 @@ constexpr int kFKeys = 32, kFRows = 16, kFExtra = 0, kFLeast = 1;
 cudaError_t launch_tree_attention(dflare_cache* c, TreeArgs a, cudaStream_t s);
 // tcgen05 kernel for many query rows per kv head (bf16); sets a.QG, a.C and the rows of a query group
 cudaError_t launch_tree_attention_tc(dflare_cache* c, TreeArgs& a, int* QT, cudaStream_t s);
-// the same kernels over a plan's items, with QT (tcgen05: 128 or 256; fp32: kFRows) rows in a block
+// The warp-level bf16 kernel's.
+constexpr int kMmaKeys = 64, kMmaRows = 16, kMmaExtra = 3;
+constexpr int mma_least(int head_dim) { return 256 / head_dim; }
+// the same kernels over a plan's items, with QT (tcgen05: 128 or 256; warp level: kMmaRows; fp32: kFRows) rows in a block
+cudaError_t launch_shared_mma(dflare_cache* c, const TreeArgs& a, cudaStream_t s);
 cudaError_t launch_shared_tc(dflare_cache* c, const TreeArgs& a, int QT, cudaStream_t s);
 cudaError_t launch_shared_f32(dflare_cache* c, const TreeArgs& a, cudaStream_t s);
 int f32_ctas_per_sm(int head_dim);

@@ -45,15 +45,15 @@ __device__ __forceinline__ uint32_t tile_at(int r, int c) {
 // the four warps that compute (the fifth streams tiles)
 __device__ __forceinline__ void compute_barrier() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
-constexpr int kKeys = 64;           // keys per tile
-constexpr int kRows = 16;
+constexpr int kKeys = kMmaKeys;     // keys per tile
+constexpr int kRows = kMmaRows;
 constexpr int kStages = 2;
 constexpr int kMmaThreads = 160;
-constexpr int kExtra = 3;       // see tree_sched.cuh
+constexpr int kExtra = kMmaExtra;       // see tree_sched.cuh
 // 2 tiles of head_dim 128, 4 of 64: what the stages and a trip to memory hold anyway. Measured at 128 with 1, 2 and 4: 2048
 // keys 9.5, 8.6 and 9.6 us, 300 keys 7.5, 7.5 and 9.0; at 64 with 2 and 4: 4096 keys 8.4 and 8.1.
 template <int HD>
-constexpr int kLeast = 256 / HD;
+constexpr int kLeast = mma_least(HD);
 
 template <int HD>
 struct MmaLayout {
@@ -68,11 +68,12 @@ struct MmaLayout {
 // each; a fifth warp streams the tiles' pages by TMA into a ring of stages. Every warp keeps its own running
 // maximum and sum; when a pair's keys are done each warp sums up a quarter of the head dims of all four.
 // HBM-bound for long contexts (one token over 100000 keys, 8 kv heads of 128: 70 us, 5.9 TB/s); for short ones by
-// its chain of latencies, lengths, page table, keys (2048 keys: 8.6 us).
-template <int HD>
+// its chain of latencies, lengths, page table, keys (2048 keys: 8.6 us). SHARED: over the items of a plan (tree_shared.cu).
+template <int HD, bool SHARED>
 __global__ void __launch_bounds__(kMmaThreads, 2) tree_mma_kernel(const __grid_constant__ CUtensorMap mk,
                                                                   const __grid_constant__ CUtensorMap mv, const TreeArgs a) {
     using LY = MmaLayout<HD>;
+    using Pair = std::conditional_t<SHARED, TreeItem, TreePair>;
     constexpr uint32_t TB = LY::TB;
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ int32_t cum[kMaxSeqs + 1];
@@ -95,10 +96,11 @@ __global__ void __launch_bounds__(kMmaThreads, 2) tree_mma_kernel(const __grid_c
     if (tid < kMaxNodes / 32) odd[tid] = 0;
     pdl_wait();
     pdl_trigger();      // the joining launch reads the lengths at once: after this kernel's own wait
-    int qg, v, v1;
-    tree_runs<kRows, kKeys, kExtra, kLeast<HD>>(a, cum, qg, v, v1);
+    int qg = 0, v, v1;
+    if constexpr (SHARED) tree_items(a, v, v1);
+    else tree_runs<kRows, kKeys, kExtra, kLeast<HD>>(a, cum, qg, v, v1);
     const int v0 = v;
-    TreePair p, after;
+    Pair p, after;
     if (!tree_pair<kExtra>(a, cum, v, v1, p)) return;
 
     if (warp == 4) {
@@ -138,21 +140,25 @@ __global__ void __launch_bounds__(kMmaThreads, 2) tree_mma_kernel(const __grid_c
 
     const int r0 = lane >> 2;                    // this thread's rows r0 and r0 + 8
     const int cp = (lane & 3) * 2;
+    auto row0_of = [&](const Pair& p) {     // the first row of the block
+        if constexpr (SHARED) return p.row0;
+        else return 0;
+    };
     // Q of a pair into half `buf` of its memory, asynchronously: rows past R are never looked at
-    auto load_q = [&](const TreePair& p, int R, int buf) {
+    auto load_q = [&](const Pair& p, int R, int buf) {
         constexpr int PC = HD / 8;
 #pragma unroll
         for (int x = tid; x < kRows * PC; x += 128) {
-            const int r = x / PC, pc = x % PC, nd = group_of(a, r);
-            if (r < R)
+            const int r = x / PC, pc = x % PC, rr = row0_of(p) + r, nd = group_of(a, rr);
+            if (rr < R)
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(sb + LY::Q + buf * (kRows * HD * 2) + (pc >> 3) * (kRows * 128) + r * 128 + (((pc & 7) ^ (r & 7)) << 4)),
-                             "l"(static_cast<const bf16*>(a.q) + ((size_t)p.b * a.n_max + nd) * a.q_row + (size_t)(p.h * a.G + r - nd * a.G) * HD + pc * 8)
+                             "l"(static_cast<const bf16*>(a.q) + query_row(a, p, nd) * a.q_row + (size_t)(p.h * a.G + rr - nd * a.G) * HD + pc * 8)
                              : "memory");
         }
     };
-    TreeRaw raw = tree_raw(a, p.b);
+    TreeRaw raw = pair_raw(a, p);
     int n, ctx, keys;
-    tree_lengths(a, raw, n, ctx, keys);
+    pair_lengths<SHARED>(a, raw, n, ctx, keys);
     load_q(p, n * a.G, 0);
     asm volatile("bar.arrive 2, 160;" ::: "memory");
     // After a wait that gave up the warps go on without waiting: the results are invalid and the error is
@@ -165,11 +171,11 @@ __global__ void __launch_bounds__(kMmaThreads, 2) tree_mma_kernel(const __grid_c
         SeenRow row[2];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            node[half] = group_of(a, min(r0 + 8 * half, R - 1));
+            node[half] = mask_node(p, group_of(a, min(row0_of(p) + r0 + 8 * half, R - 1)));
             row[half] = seen_row(a, p.b, node[half]);
         }
         more = tree_pair<kExtra>(a, cum, v, v1, after);
-        if (more) raw = tree_raw(a, after.b);
+        if (more) raw = pair_raw(a, after);
         asm volatile("cp.async.wait_all;" ::: "memory");
         compute_barrier();
         uint32_t qa[HD / 16][4];
@@ -189,7 +195,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) tree_mma_kernel(const __grid_c
             const int st = i % kStages;
             if (ok) ok = __all_sync(0xffffffffu, bar_wait(full + 8 * st, (uint32_t)(i / kStages) & 1u, &abort_flag, a.pg.err));
             if (more && t == p.lo) {    // the next pair's queries, a pair ahead
-                tree_lengths(a, raw, n2, ctx2, keys2);
+                pair_lengths<SHARED>(a, raw, n2, ctx2, keys2);
                 load_q(after, n2 * a.G, (pair + 1) & 1);
             }
             const uint32_t sK = sb + st * 2 * TB, sV = sK + TB;
@@ -341,10 +347,19 @@ __global__ void __launch_bounds__(kMmaThreads, 2) tree_mma_kernel(const __grid_c
                 mine[y][2] += x.z;
                 mine[y][3] += x.w;
             }
+        bool partial;
+        size_t part0;       // the block's first row among the partial results
+        if constexpr (SHARED) {
+            partial = p.dst >= 0;
+            part0 = (size_t)max(p.dst, 0);
+        } else {
+            partial = p.partial();
+            part0 = ((size_t)blockIdx.x * 2 + (p.start < v0 ? 0 : 1)) * kRows;
+        }
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            const int r = r0 + 8 * half, col = warp * (HD / 4) + cp;
-            if (r >= R) continue;
+            const int r = r0 + 8 * half, rr = row0_of(p) + r, col = warp * (HD / 4) + cp;
+            if (rr >= R) continue;
             if (odds)
                 each_odd(a, odd, p, node[half], ctx, keys, [&](size_t at) {
                     for (int y = 0; y < QB; ++y)
@@ -353,14 +368,14 @@ __global__ void __launch_bounds__(kMmaThreads, 2) tree_mma_kernel(const __grid_c
                             if (!isfinite(f)) mine[y][2 * half + e] += f;
                         }
                 });
-            if (p.partial()) {
-                const size_t row = ((size_t)blockIdx.x * 2 + (p.start < v0 ? 0 : 1)) * kRows + r;
+            if (partial) {
+                const size_t row = part0 + r;
 #pragma unroll
                 for (int y = 0; y < QB; ++y)
                     *reinterpret_cast<float2*>(a.part_o + row * HD + col + y * 8) = make_float2(mine[y][2 * half], mine[y][2 * half + 1]);
                 if (warp == 0 && (lane & 3) == 0) a.part_ml[row] = make_float2(M[half], L[half]);
             } else {
-                const size_t row = ((size_t)p.b * a.n_max + node[half]) * a.hq + p.h * a.G + r - node[half] * a.G;
+                const size_t row = ((size_t)p.b * a.n_max + node[half]) * a.hq + p.h * a.G + rr - node[half] * a.G;
                 const float inv = L[half] == 0.f ? 0.f : 1.f / L[half];
 #pragma unroll
                 for (int y = 0; y < QB; ++y)
@@ -779,13 +794,12 @@ cudaError_t launch_join(const dflare_cache* c, const TreeArgs& a, int QT, int KT
 template <int HD>
 cudaError_t launch_mma(dflare_cache* c, TreeArgs a, cudaStream_t s) {
     static PerDeviceOnce once;
-    cudaError_t e = once([] {
-        return cudaFuncSetAttribute(tree_mma_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MmaLayout<HD>::BYTES);
-    });
+    auto kernel = tree_mma_kernel<HD, false>;
+    cudaError_t e = once([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MmaLayout<HD>::BYTES); });
     if (e != cudaSuccess) return e;
     a.QG = 1;
     a.C = 2 * c->num_sms;
-    e = launch_kernel(true, tree_mma_kernel<HD>, dim3(a.C), dim3(kMmaThreads), MmaLayout<HD>::BYTES, s, c->maps[0], c->maps[1], a);
+    e = launch_kernel(true, kernel, dim3(a.C), dim3(kMmaThreads), MmaLayout<HD>::BYTES, s, c->maps[0], c->maps[1], a);
     return e == cudaSuccess ? launch_join<bf16, HD>(c, a, kRows, kKeys, kExtra, kLeast<HD>, false, s) : e;
 }
 
@@ -800,6 +814,14 @@ cudaError_t launch_f32(dflare_cache* c, TreeArgs a, cudaStream_t s) {
     a.C = f32_ctas(HD) * c->num_sms;
     e = launch_kernel(true, kernel, dim3(std::max(a.QG, a.C)), dim3(kFThreads), bytes, s, a);
     return e == cudaSuccess ? launch_join<float, HD>(c, a, kFRows, kFKeys, kFExtra, kFLeast, false, s) : e;
+}
+
+template <int HD>
+cudaError_t launch_mma_items(dflare_cache* c, const TreeArgs& a, cudaStream_t s) {
+    static PerDeviceOnce once;
+    auto kernel = tree_mma_kernel<HD, true>;
+    cudaError_t e = once([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MmaLayout<HD>::BYTES); });
+    return e == cudaSuccess ? launch_kernel(true, kernel, dim3(a.C), dim3(kMmaThreads), MmaLayout<HD>::BYTES, s, c->maps[0], c->maps[1], a) : e;
 }
 
 template <int HD>
@@ -826,6 +848,9 @@ cudaError_t launch_hd(dflare_cache* c, TreeArgs a, cudaStream_t s) {
 
 }  // namespace
 
+cudaError_t launch_shared_mma(dflare_cache* c, const TreeArgs& a, cudaStream_t s) {
+    return c->cfg.head_dim == 128 ? launch_mma_items<128>(c, a, s) : launch_mma_items<64>(c, a, s);
+}
 cudaError_t launch_shared_f32(dflare_cache* c, const TreeArgs& a, cudaStream_t s) {
     return c->cfg.head_dim == 128 ? launch_f32_items<128>(a, s) : launch_f32_items<64>(a, s);
 }
