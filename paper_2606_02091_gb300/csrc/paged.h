@@ -65,7 +65,13 @@ struct __align__(16) TreeSeq {
 };
 // The head of an attend_shared workspace.
 struct SharedHead {
-    int batch, n_max, per, ok;      // per: length of a CTA's run
+    int batch, n_max, ok, per[2];       // per: length of a CTA's run in each list of work
+};
+// One kernel's list of work: log2 of its rows per block and keys per tile, its CTAs, what a tile of up to 128 rows and one of more costs, and
+// a unit beside its tiles, the shortest run, and the first of its CTAs' rows among the partial results.
+struct WorkList {
+    int qt, kt, C, weight1, weight2, extra, least, slot0;
+    bool blocks;         // its rows lie in blocks of 32 rows x 32 elements
 };
 
 // one launch of the paged attention
@@ -90,6 +96,7 @@ struct TreeArgs {
     const int32_t* map;        // query rows of the groups' nodes
     const TreeSeq* seqs;
     int own_rows, lead_rows;   // rows among the partial results between kv heads
+    bool follows;              // the kernel before this one is of the same call, and does not write what this one reads
 };
 
 // The tcgen05 kernel's keys per tile, and how its work is divided (see tree_sched.cuh). Measured with 1, 2, 3 and 4 extra
@@ -107,9 +114,9 @@ cudaError_t launch_tree_attention_tc(dflare_cache* c, TreeArgs& a, int* QT, cuda
 // The warp-level bf16 kernel's.
 constexpr int kMmaKeys = 64, kMmaRows = 16, kMmaExtra = 3;
 constexpr int mma_least(int head_dim) { return 256 / head_dim; }
-// the same kernels over a plan's items, with QT (tcgen05: 128 or 256; warp level: kMmaRows; fp32: kFRows) rows in a block
+// the same kernels over a plan's items, with 256 (tcgen05), kMmaRows (warp level) or kFRows (fp32) rows in a block
 cudaError_t launch_shared_mma(dflare_cache* c, const TreeArgs& a, cudaStream_t s);
-cudaError_t launch_shared_tc(dflare_cache* c, const TreeArgs& a, int QT, cudaStream_t s);
+cudaError_t launch_shared_tc(dflare_cache* c, const TreeArgs& a, cudaStream_t s);
 cudaError_t launch_shared_f32(dflare_cache* c, const TreeArgs& a, cudaStream_t s);
 int f32_ctas_per_sm(int head_dim);
 // rows of the partial buffers that any launch of a cache may use

@@ -148,7 +148,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_base;
-    pdl_wait();
+    // A launch that follows one of the same call does not wait for that to end: what the call reads was there before the first
+    // one let this one start, and the two write different rows. It waits at its own end, for the joining launch.
+    if (!SHARED || !a.follows) pdl_wait();
     // Dependents start only once this CTA holds its tensor memory: one of theirs that takes tensor memory
     // before its own dependency wait can never hold columns that this CTA waits for. After this kernel's own
     // wait: the joining launch reads the lengths at once.
@@ -159,7 +161,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     const int v0 = v;
     // Whether the streams take alternate tiles of the same 128 rows: always (NQ = 1), or, from a plan, where a unit has no more.
     auto alternate = [&](const Pair& p) {
-        if constexpr (SHARED && NQ == 2) return p.nodes * a.G - p.row0 <= 128;
+        if constexpr (SHARED) return p.nodes * a.G - p.row0 <= 128;
         else return NQ == 1;
     };
     Pair p, after;
@@ -350,7 +352,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                 // every S of the pair (of this stream, where each has rows of its own) has been computed: the next pair's Q
                 if (tile == n - 1 && more) {
                     pair_lengths<SHARED>(a, raw, nodes2, ctx2, keys2);
-                    if constexpr (SHARED && NQ == 2) {
+                    if constexpr (SHARED) {
                         if (alt == alternate(after)) {
                             load_q(after, nodes2 * a.G, alt ? 0 : w, r, 128);
                         } else if (alt) {       // (this stream had the last S that reads either half)
@@ -633,6 +635,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         // the partial results are in memory before this CTA ends (and with it what the joining launch waits for)
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
+    if (SHARED && a.follows) pdl_wait();
     tc_fence_before();
     __syncthreads();
     if (warp == 9) {
@@ -652,13 +655,13 @@ cudaError_t launch_tc(dflare_cache* c, TreeArgs& a, cudaStream_t s) {
     return launch_kernel(true, kernel, dim3(std::max(a.QG, a.C)), dim3(kThreads), TcLayout<HD, NQ>::BYTES, s, c->maps[0], c->maps[1], a);
 }
 
-template <int HD, int NQ>
+template <int HD>
 cudaError_t launch_items(dflare_cache* c, const TreeArgs& a, cudaStream_t s) {
     static PerDeviceOnce once;
-    auto kernel = tree_tc_kernel<HD, NQ, true>;
-    cudaError_t e = once([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TcLayout<HD, NQ>::BYTES); });
+    auto kernel = tree_tc_kernel<HD, 2, true>;
+    cudaError_t e = once([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TcLayout<HD, 2>::BYTES); });
     if (e != cudaSuccess) return e;
-    return launch_kernel(true, kernel, dim3(a.C), dim3(kThreads), TcLayout<HD, NQ>::BYTES, s, c->maps[0], c->maps[1], a);
+    return launch_kernel(true, kernel, dim3(a.C), dim3(kThreads), TcLayout<HD, 2>::BYTES, s, c->maps[0], c->maps[1], a);
 }
 
 }  // namespace
@@ -670,9 +673,8 @@ cudaError_t launch_tree_attention_tc(dflare_cache* c, TreeArgs& a, int* QT, cuda
     return one ? launch_tc<64, 1>(c, a, s) : launch_tc<64, 2>(c, a, s);
 }
 
-cudaError_t launch_shared_tc(dflare_cache* c, const TreeArgs& a, int QT, cudaStream_t s) {
-    if (c->cfg.head_dim == 128) return QT == 128 ? launch_items<128, 1>(c, a, s) : launch_items<128, 2>(c, a, s);
-    return QT == 128 ? launch_items<64, 1>(c, a, s) : launch_items<64, 2>(c, a, s);
+cudaError_t launch_shared_tc(dflare_cache* c, const TreeArgs& a, cudaStream_t s) {
+    return c->cfg.head_dim == 128 ? launch_items<128>(c, a, s) : launch_items<64>(c, a, s);
 }
 
 }  // namespace dfl

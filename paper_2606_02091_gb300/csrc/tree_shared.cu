@@ -37,46 +37,78 @@ constexpr int kFewRows = 128;
 // Costs of the tcgen05 kernel's work.
 constexpr int kTileCost = 4, kWideTileCost = 6, kUnitCost = 14;
 
+constexpr int log2_of(int v) { return v > 1 ? 1 + log2_of(v / 2) : 0; }
+
 // What a plan and the launches that follow it agree on, from the call's sizes alone.
+struct WorkLists {
+    // fp32: one list. bf16: the warp-level kernel's, where rows are few; a list of own keys for it and one of shared keys for the tcgen05
+    // kernel, where a sequence's rows fit one block of the first and there are own units for every SM; the tcgen05 kernel's of both. Measured,
+    // a layer with one list and with two: single tokens of 132 sequences, 64/8 heads of 64, own 300 keys behind 240 shared ones 65.2 and
+    // 34.7 us, of 88 behind 1250 34.6 and 23.1; 64 sequences of four nodes, own 1150 keys behind 32768 154 and 161; two nodes of 27
+    // sequences, 28/4 heads (108 own units) 16.3 and 21.9.
+    WorkList list[2];           // of own keys, of shared ones (the same, where there is one)
+    int many;
+};
 struct Layout {
     bool ok;                    // everything fits its numbers
-    int QT, KT, C;
-    int weight1, weight2, extra, least;     // cost of a tile of up to 128 rows and of more, of a unit beside its tiles; the shortest run
+    WorkLists work;
     int own_rows, lead_rows;    // rows of one kv head among the whole units' partial results
-    size_t runs, items, map, seqs, ml, o, bytes;    // offsets
+    int rows0;                  // the first of those
+    size_t runs[2], items[2], map, seqs, ml, o, bytes;      // offsets
 };
 Layout layout_of(const dflare_cache* c, int batch, int n_max) {
     const dflare_cache_config& g = c->cfg;
-    const int G = g.n_q_heads / g.n_kv_heads;
+    const int G = g.n_q_heads / g.n_kv_heads, sms = c->num_sms;
     Layout y{};
     const long long rows = (long long)batch * n_max * G;
+    const WorkList f32{log2_of(kFRows), log2_of(kFKeys), f32_ctas_per_sm(g.head_dim) * sms, 1, 1, kFExtra, kFLeast, 0, false};
+    const WorkList mma{log2_of(kMmaRows), log2_of(kMmaKeys), 2 * sms, 1, 1, kMmaExtra, mma_least(g.head_dim), 0, false};
+    const WorkList tc{8, log2_of(kTcKeys), sms, kTileCost, kWideTileCost, kUnitCost, kWideTileCost, 0, true};
+    y.work.many = 1;
     if (g.dtype == DFLARE_F32) {
-        y.QT = kFRows, y.KT = kFKeys, y.weight1 = y.weight2 = 1, y.extra = kFExtra, y.least = kFLeast, y.C = f32_ctas_per_sm(g.head_dim) * c->num_sms;
+        y.work.list[0] = y.work.list[1] = f32;
     } else if (rows <= kFewRows) {
-        y.QT = kMmaRows, y.KT = kMmaKeys, y.weight1 = y.weight2 = 1, y.extra = kMmaExtra, y.least = mma_least(g.head_dim), y.C = 2 * c->num_sms;
+        y.work.list[0] = y.work.list[1] = mma;
+    } else if (n_max * G <= kMmaRows && (long long)batch * g.n_kv_heads >= sms) {
+        y.work.list[0] = mma;
+        y.work.list[1] = tc;
+        y.work.many = 2;
     } else {
-        // (blocks of 128 rows where no group can have more)
-        y.QT = rows <= 128 ? 128 : 256, y.KT = kTcKeys, y.weight1 = kTileCost, y.weight2 = kWideTileCost, y.extra = kUnitCost, y.least = kWideTileCost, y.C = c->num_sms;
+        y.work.list[0] = y.work.list[1] = tc;
     }
-    const long long own = (long long)batch * (((long long)n_max * G + y.QT - 1) / y.QT), lead = (rows + y.QT - 1) / y.QT + batch / 2;
-    const long long units = (own + lead) * g.n_kv_heads, tiles = ((long long)g.max_pages * g.page_size + y.KT - 1) / y.KT * y.weight2 + y.extra;
-    const long long own_rows = ((long long)n_max * G + 31) / 32 * 32, lead_rows = (rows / 32 + batch + 1) * 32;
-    const long long part = 2LL * y.C * y.QT + (batch * own_rows + lead_rows) * g.n_kv_heads;
     const long long most = 0x7fffffffLL - 4096;
-    y.ok = units * tiles <= most && part <= most;
+    y.ok = true;
+    long long part = 0, units[2];
+    for (int l = 0; l < y.work.many; ++l) {
+        WorkList& w = y.work.list[l];
+        const long long QT = 1LL << w.qt, own = (long long)batch * (((long long)n_max * G + QT - 1) >> w.qt), lead = ((rows + QT - 1) >> w.qt) + batch / 2;
+        units[l] = ((y.work.many == 1 || l == 0 ? own : 0) + (l == y.work.many - 1 ? lead : 0)) * g.n_kv_heads;
+        const long long cost = (((long long)g.max_pages * g.page_size + (1LL << w.kt) - 1) >> w.kt) * w.weight2 + w.extra;
+        if (units[l] * cost > most) y.ok = false;
+        w.slot0 = (int)part;
+        part += 2LL * w.C * QT;
+    }
+    if (y.work.many == 1) y.work.list[1] = y.work.list[0];
+    const long long own_rows = ((long long)n_max * G + 31) / 32 * 32, lead_rows = (rows / 32 + batch + 1) * 32;
+    const long long rows0 = part;
+    part += (batch * own_rows + lead_rows) * g.n_kv_heads;
+    if (part > most) y.ok = false;
     if (!y.ok) return y;
     y.own_rows = (int)own_rows;
     y.lead_rows = (int)lead_rows;
+    y.rows0 = (int)rows0;
     auto place = [&](size_t bytes) {
         const size_t at = y.bytes;
         y.bytes += (bytes + 127) / 128 * 128;
         return at;
     };
     place(sizeof(SharedHead));
-    y.runs = place(sizeof(int2) * y.C);
     y.seqs = place(sizeof(TreeSeq) * batch);
     y.map = place(sizeof(int32_t) * (size_t)batch * n_max);
-    y.items = place(sizeof(TreeItem) * (size_t)(units + y.C));
+    for (int l = 0; l < y.work.many; ++l) {
+        y.runs[l] = place(sizeof(int2) * y.work.list[l].C);
+        y.items[l] = place(sizeof(TreeItem) * (size_t)(units[l] + y.work.list[l].C));
+    }
     y.ml = place(sizeof(float2) * (size_t)part);
     y.o = place(sizeof(float) * (size_t)part * g.head_dim);
     return y;
@@ -86,16 +118,17 @@ struct PlanArgs {
     PagesView pg;
     const int32_t* n_nodes;
     SharedHead* head;
-    int2* runs;
-    TreeItem* items;
+    int2* runs[2];
+    TreeItem* items[2];
     int32_t* map;
     TreeSeq* seqs;
     int32_t* groups;            // optional output
-    int batch, n_max, G, qt, kt, weight1, weight2, extra, least, C, own_rows, lead_rows;
+    WorkLists work;
+    int batch, n_max, G, own_rows, lead_rows, rows0;
 };
 
-// Rows among the partial results: 2 C blocks of the CTAs, then of whole units the sequences' own, then the groups'.
-__device__ __forceinline__ int own_row(const PlanArgs& a, int b) { return (2 * a.C << a.qt) + b * a.pg.hkv * a.own_rows; }
+// Rows among the partial results: blocks of the CTAs, then of whole units the sequences' own, then the groups'.
+__device__ __forceinline__ int own_row(const PlanArgs& a, int b) { return a.rows0 + b * a.pg.hkv * a.own_rows; }
 __device__ __forceinline__ int lead_row(const PlanArgs& a, int b, int node0) {
     return own_row(a, a.batch) + (int)((long long)node0 * a.G / 32 + b) * 32;
 }
@@ -311,8 +344,9 @@ __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 // A cluster with a warp for every sequence, which finds what it shares with the one before it; the first CTA goes on from there.
-// Segment 2 b is sequence b's own keys, 2 b + 1 the keys shared by the group that b leads.
-__global__ void __launch_bounds__(kPlanThreads) tree_shared_plan_kernel(const PlanArgs a) {
+// Segments: sequence b's own keys, and the keys shared by the group that b leads; one after the other in one list of work, or in a
+// list each (place_of).
+__global__ void __launch_bounds__(kPlanThreads) tree_shared_plan_kernel(const __grid_constant__ PlanArgs a) {
     __shared__ int same[kMaxSeqs];
     __shared__ int share[kMaxSeqs], costs[kMaxSeqs + 1], begins[kMaxSeqs + 1], from[kMaxSeqs], shared_by[kMaxSeqs], active[kMaxSeqs];
     __shared__ float best[2 * kMaxSeqs];
@@ -320,7 +354,9 @@ __global__ void __launch_bounds__(kPlanThreads) tree_shared_plan_kernel(const Pl
     __shared__ int pages_of[kMaxSeqs], node0[kMaxSeqs + 1], nodes_of[kMaxSeqs];                 // by sequence
     __shared__ int n_of[kMaxSeqs], held_of[kMaxSeqs], ctx_of[kMaxSeqs], keys_of[kMaxSeqs];
     __shared__ int seg_start[2 * kMaxSeqs], seg_unit[2 * kMaxSeqs], seg_tiles[2 * kMaxSeqs], seg_blocks[2 * kMaxSeqs], seg_weight[2 * kMaxSeqs];
-    __shared__ int2 tmp[kMaxSeqs / 32], totals;
+    __shared__ int2 tmp[kMaxSeqs / 32];
+    __shared__ int total_cost[2], total_units[2];       // of the lists
+    auto place_of = [&](int b, int which) { return a.work.many == 1 ? 2 * b + which : which * kMaxSeqs + b; };
     cluster_arrive();       // (every CTA of the cluster has begun before one writes to another)
     pdl_wait();
     pdl_trigger();
@@ -382,42 +418,49 @@ __global__ void __launch_bounds__(kPlanThreads) tree_shared_plan_kernel(const Pl
         if (tid == 0) node0[a.batch] = total.x;
         seq_barrier();
         // segments: own of sequence tid, and its group's where it leads one
-        int tiles[2] = {0, 0}, blocks[2] = {0, 0}, weight[2] = {a.weight1, a.weight1};
+        int tiles[2] = {0, 0}, blocks[2] = {0, 0}, weight[2] = {a.work.list[0].weight1, a.work.list[1].weight1}, cost[2], units[2];
         const int own_keys = keys - pages * a.pg.ps;
-        if (n > 0 && own_keys > 0) {
-            tiles[0] = (own_keys + (1 << a.kt) - 1) >> a.kt;
-            blocks[0] = (n * a.G + (1 << a.qt) - 1) >> a.qt;
-            if (n * a.G > 128) weight[0] = a.weight2;
-        }
+        auto segment_of = [&](int which, int count, int many) {
+            const WorkList& w = a.work.list[which];
+            tiles[which] = (count + (1 << w.kt) - 1) >> w.kt;
+            blocks[which] = (many * a.G + (1 << w.qt) - 1) >> w.qt;
+            if (many * a.G > 128) weight[which] = w.weight2;
+        };
+        if (n > 0 && own_keys > 0) segment_of(0, own_keys, n);
         if (grouped && first == place) {        // its group's nodes lie before those of the next active one
             const int after = place + group_members[place], nodes = (after < m ? node0[active[after]] : node0[a.batch]) - node0[tid];
             nodes_of[tid] = nodes;
-            tiles[1] = (pages * a.pg.ps + (1 << a.kt) - 1) >> a.kt;
-            blocks[1] = (nodes * a.G + (1 << a.qt) - 1) >> a.qt;
-            if (nodes * a.G > 128) weight[1] = a.weight2;
+            segment_of(1, pages * a.pg.ps, nodes);
         }
-        int cost[2], units[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             units[i] = blocks[i] * a.pg.hkv;
-            cost[i] = units[i] * (tiles[i] * weight[i] + a.extra);
+            cost[i] = units[i] * (tiles[i] * weight[i] + a.work.list[i].extra);
         }
-        const int2 end = plan_scan(make_int2(cost[0] + cost[1], units[0] + units[1]), tmp, &total);
+        int2 all_cost, all_units;
+        const int2 c = plan_scan(make_int2(cost[0], cost[1]), tmp, &all_cost), u = plan_scan(make_int2(units[0], units[1]), tmp, &all_units);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {       // (past the batch: empty, where the list ends)
-            seg_start[2 * tid + i] = end.x - cost[1] - (i ? 0 : cost[0]);
-            seg_unit[2 * tid + i] = end.y - units[1] - (i ? 0 : units[0]);
-            seg_tiles[2 * tid + i] = tiles[i];
-            seg_blocks[2 * tid + i] = blocks[i];
-            seg_weight[2 * tid + i] = weight[i];
+            const int e = place_of(tid, i);
+            const bool one = a.work.many == 1;
+            seg_start[e] = (one ? c.x + c.y - (i ? 0 : cost[0]) : i ? c.y : c.x - cost[0]) - (i || one ? cost[1] : 0);
+            seg_unit[e] = (one ? u.x + u.y - (i ? 0 : units[0]) : i ? u.y : u.x - units[0]) - (i || one ? units[1] : 0);
+            seg_tiles[e] = tiles[i];
+            seg_blocks[e] = blocks[i];
+            seg_weight[e] = weight[i];
         }
-        if (tid == 0) totals = total;
+        if (tid == 0) {
+            total_cost[0] = a.work.many == 1 ? all_cost.x + all_cost.y : all_cost.x;
+            total_units[0] = a.work.many == 1 ? all_units.x + all_units.y : all_units.x;
+            total_cost[1] = all_cost.y;
+            total_units[1] = all_units.y;
+        }
         seq_barrier();
         if (tid < a.batch) {
-            const int e = 2 * lead + 1;
+            const int e = place_of(lead, 1);
             TreeSeq s;
             s.n = n;
-            s.start = seg_start[2 * tid];
+            s.start = seg_start[place_of(tid, 0)];
             s.tiles = tiles[0];
             s.blocks = blocks[0];
             s.lead_start = seg_start[e];
@@ -432,75 +475,80 @@ __global__ void __launch_bounds__(kPlanThreads) tree_shared_plan_kernel(const Pl
         }
     }
     __syncthreads();
-    const int all = totals.x, all_units = totals.y, per = max((all + a.C - 1) / a.C, a.least);
     if (tid == 0) {
         a.head->batch = a.batch;
         a.head->n_max = a.n_max;
-        a.head->per = per;
         a.head->ok = 1;
     }
     for (int x = tid; x < a.batch * a.n_max; x += kPlanThreads) {
         const int b = x / a.n_max, i = x - b * a.n_max;
         if (i < node0[b + 1] - node0[b]) a.map[node0[b] + i] = x;
     }
-    // the last segment that begins at or before x and is not empty, of starts that do not fall
-    auto segment = [&](const int* begin, int x) {
-        int lo = 0, hi = 2 * a.batch;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (begin[mid] <= x) lo = mid; else hi = mid;
+    {       // the lists, each by its part of the threads
+        const int threads = kPlanThreads / a.work.many, list = tid / threads, me = tid - list * threads;
+        const WorkList& L = a.work.list[list];
+        const int all = total_cost[list], all_units = total_units[list], per = max((all + L.C - 1) / L.C, L.least);
+        if (me == 0) a.head->per[list] = per;
+        // the last of the list's segments that begins at or before x and is not empty, of starts that do not fall
+        auto segment = [&](const int* begin, int x) {
+            int lo = list * kMaxSeqs, hi = a.work.many == 1 ? 2 * a.batch : lo + a.batch;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (begin[mid] <= x) lo = mid; else hi = mid;
+            }
+            return lo;
+        };
+        // The items of run c are numbers u + c for its units u: the list of units and the list of runs advance together.
+        for (int c = me; c < L.C; c += threads) {
+            const long long v0 = (long long)c * per, v1 = min(v0 + per, (long long)all);
+            int2 run = make_int2(0, 0);
+            if (v0 < v1) {
+                auto unit_at = [&](int v, bool next) {      // the unit that has the tile at place v, or (next) the first tile from there on
+                    const int e = segment(seg_start, v), w = seg_weight[e], t = seg_tiles[e], size = t * w + L.extra, idx = (v - seg_start[e]) / size;
+                    return seg_unit[e] + idx + (next && v - seg_start[e] - idx * size > (t - 1) * w);
+                };
+                run.x = unit_at((int)v0, true) + c;
+                run.y = unit_at((int)v1 - 1, false) + c + 1;
+            }
+            a.runs[list][c] = run;
         }
-        return lo;
-    };
-    // The items of run c are numbers u + c for its units u: the list of units and the list of runs advance together.
-    for (int c = tid; c < a.C; c += kPlanThreads) {
-        const long long v0 = (long long)c * per, v1 = min(v0 + per, (long long)all);
-        int2 run = make_int2(0, 0);
-        if (v0 < v1) {
-            auto unit_at = [&](int v, bool next) {      // the unit that has the tile at place v, or (next) the first tile from there on
-                const int e = segment(seg_start, v), w = seg_weight[e], t = seg_tiles[e], size = t * w + a.extra, idx = (v - seg_start[e]) / size;
-                return seg_unit[e] + idx + (next && v - seg_start[e] - idx * size > (t - 1) * w);
-            };
-            run.x = unit_at((int)v0, true) + c;
-            run.y = unit_at((int)v1 - 1, false) + c + 1;
-        }
-        a.runs[c] = run;
-    }
-    // Items by units, `share` threads for each, where there are few.
-    int share_log = 0;
-    while ((all_units << (share_log + 1)) <= kPlanThreads && share_log < 5) ++share_log;
-    for (int x = tid; x < all_units << share_log; x += kPlanThreads) {
-        const int u = x >> share_log, e = segment(seg_unit, u), idx = u - seg_unit[e], b = e >> 1;
-        const int t = seg_tiles[e], bl = seg_blocks[e], w = seg_weight[e], start = seg_start[e] + idx * (t * w + a.extra);
-        const int c0 = start / per, c1 = (start + (t - 1) * w) / per;
-        TreeItem it;
-        it.b = b;
-        it.h = bl == 1 ? idx : idx / bl;
-        it.row0 = (idx - it.h * bl) << a.qt;
-        int whole;          // where its rows go if the unit is one item
-        if (e & 1) {
-            it.page0 = 0;
-            it.held = pages_of[b];
-            it.ctx = it.keys = pages_of[b] * a.pg.ps;
-            it.first = ~node0[b];
-            it.nodes = nodes_of[b];
-            whole = lead_row(a, b, node0[b]) + it.h * a.lead_rows + it.row0;
-        } else {
-            it.page0 = pages_of[b];
-            it.held = held_of[b] - it.page0;
-            it.ctx = ctx_of[b] - it.page0 * a.pg.ps;
-            it.keys = keys_of[b] - it.page0 * a.pg.ps;
-            it.first = b * a.n_max;
-            it.nodes = n_of[b];
-            whole = pages_of[b] ? own_row(a, b) + it.h * a.own_rows + it.row0 : -1;
-        }
-        for (int c = c0 + (x & ((1 << share_log) - 1)); c <= c1; c += 1 << share_log) {
-            const long long v0 = (long long)c * per;
-            // (a tile is in the run that its place is in)
-            it.lo = c == c0 ? 0 : ((int)(v0 - start) + w - 1) / w;
-            it.hi = c == c1 ? t : ((int)(v0 + per - start) + w - 1) / w;
-            it.dst = c0 == c1 ? whole : (2 * c + (start < v0 ? 0 : 1)) << a.qt;
-            a.items[u + c] = it;
+        // Items by units, `share` threads for each, where there are few.
+        int share_log = 0;
+        while (((long long)all_units << (share_log + 1)) <= threads && share_log < 5) ++share_log;
+        for (int x = me; x < all_units << share_log; x += threads) {
+            const int u = x >> share_log, e = segment(seg_unit, u), idx = u - seg_unit[e];
+            const int b = a.work.many == 1 ? e >> 1 : e & (kMaxSeqs - 1), which = a.work.many == 1 ? e & 1 : list;
+            const int t = seg_tiles[e], bl = seg_blocks[e], w = seg_weight[e], start = seg_start[e] + idx * (t * w + L.extra);
+            const int c0 = start / per, c1 = (start + (t - 1) * w) / per;
+            TreeItem it;
+            it.b = b;
+            it.h = bl == 1 ? idx : idx / bl;
+            it.row0 = (idx - it.h * bl) << L.qt;
+            int whole;          // where its rows go if the unit is one item
+            if (which) {
+                it.page0 = 0;
+                it.held = pages_of[b];
+                it.ctx = it.keys = pages_of[b] * a.pg.ps;
+                it.first = ~node0[b];
+                it.nodes = nodes_of[b];
+                whole = lead_row(a, b, node0[b]) + it.h * a.lead_rows + it.row0;
+            } else {
+                it.page0 = pages_of[b];
+                it.held = held_of[b] - it.page0;
+                it.ctx = ctx_of[b] - it.page0 * a.pg.ps;
+                it.keys = keys_of[b] - it.page0 * a.pg.ps;
+                it.first = b * a.n_max;
+                it.nodes = n_of[b];
+                whole = pages_of[b] ? own_row(a, b) + it.h * a.own_rows + it.row0 : -1;
+            }
+            for (int c = c0 + (x & ((1 << share_log) - 1)); c <= c1; c += 1 << share_log) {
+                const long long v0 = (long long)c * per;
+                // (a tile is in the run that its place is in)
+                it.lo = c == c0 ? 0 : ((int)(v0 - start) + w - 1) / w;
+                it.hi = c == c1 ? t : ((int)(v0 + per - start) + w - 1) / w;
+                it.dst = c0 == c1 ? whole : L.slot0 + ((2 * c + (start < v0 ? 0 : 1)) << L.qt);
+                a.items[list][u + c] = it;
+            }
         }
     }
 }
@@ -511,14 +559,15 @@ template <int PW> constexpr int kJoinThreads = PW > 4 ? 32 * PW : 128;
 constexpr int join_blocks(int HD, int RW) { return HD == 64 ? 6 : RW == 1 ? 5 : 4; }
 
 template <class T, int HD, int RW, int PW>
-__global__ void __launch_bounds__(kJoinThreads<PW>, PW > 4 ? 2 : join_blocks(HD, RW)) tree_shared_join_kernel(const TreeArgs a, int QT, int extra, bool blocks) {
+__global__ void __launch_bounds__(kJoinThreads<PW>, PW > 4 ? 2 : join_blocks(HD, RW)) tree_shared_join_kernel(const __grid_constant__ TreeArgs a, const __grid_constant__ WorkLists work) {
     static_assert(RW == 1 || PW == 1, "several rows per warp or several warps per row");
     constexpr int LPR = 32 / RW, E = HD / LPR, V = E < 4 ? E : 4, J = RW == 4 ? 4 : 8, ROWS = kJoinThreads<PW> / 32 / PW * RW;
     __shared__ float others[PW > 1 ? kJoinThreads<PW> / 32 : 1][HD + 2];     // of a row's warps: output, maximum, sum
     const int lane = threadIdx.x & 31, l = lane % LPR, warp = threadIdx.x >> 5, pw = warp % PW;
     // the plan is older than the kernel before this one, which let this one start after its own wait
     const bool ok = a.head->batch == a.batch && a.head->n_max == a.n_max && a.head->ok;
-    const int per = ok ? a.head->per : 1;
+    const int per0 = ok ? a.head->per[0] : 1, per1 = ok ? a.head->per[work.many - 1] : 1;
+    const WorkList &L0 = work.list[0], &L1 = work.list[1];
     bool begun = false;
     const unsigned rows = (unsigned)a.batch * a.n_max * a.hq, step = gridDim.x * ROWS;
     unsigned row = blockIdx.x * ROWS + warp / PW * RW + lane / LPR;
@@ -531,10 +580,10 @@ __global__ void __launch_bounds__(kJoinThreads<PW>, PW > 4 ? 2 : join_blocks(HD,
         const bool some = there && node < s.n;
         // own parts, then the group's: how many, the CTA of the first, the unit's place in the list, and the row
         const int r0 = node * a.G + g, r1 = (s.node0 + node) * a.G + g;
-        const int u0 = s.start + (h * s.blocks + r0 / QT) * (s.tiles * s.weight + extra), c0 = u0 / per;
-        const int u1 = s.lead_start + (h * s.lead_blocks + r1 / QT) * (s.lead_tiles * s.lead_weight + extra), c1 = u1 / per;
-        const int n0 = some && s.tiles ? (u0 + (s.tiles - 1) * s.weight) / per - c0 + 1 : 0;
-        const int n1 = some && s.lead_tiles ? (u1 + (s.lead_tiles - 1) * s.lead_weight) / per - c1 + 1 : 0;
+        const int u0 = s.start + (h * s.blocks + (r0 >> L0.qt)) * (s.tiles * s.weight + L0.extra), c0 = u0 / per0;
+        const int u1 = s.lead_start + (h * s.lead_blocks + (r1 >> L1.qt)) * (s.lead_tiles * s.lead_weight + L1.extra), c1 = u1 / per1;
+        const int n0 = some && s.tiles ? (u0 + (s.tiles - 1) * s.weight) / per0 - c0 + 1 : 0;
+        const int n1 = some && s.lead_tiles ? (u1 + (s.lead_tiles - 1) * s.lead_weight) / per1 - c1 + 1 : 0;
         const bool written = n0 == 1 && s.lead_tiles == 0;
         const int whole = written ? 0 : n0 + n1, parts = (whole - pw + PW - 1) / PW;       // this warp's: pw, pw + PW, ...
         if (!begun) pdl_wait();
@@ -543,10 +592,10 @@ __global__ void __launch_bounds__(kJoinThreads<PW>, PW > 4 ? 2 : join_blocks(HD,
         auto at = [&](int k) -> size_t {
             const int i = pw + k * PW;
             const bool own = i < n0;
-            const int c = own ? c0 + i : c1 + i - n0, u = own ? u0 : u1, r = own ? r0 : r1;
+            const int c = own ? c0 + i : c1 + i - n0, u = own ? u0 : u1, r = own ? r0 : r1, per = own ? per0 : per1, qt = own ? L0.qt : L1.qt;
             if ((own ? n0 : n1) == 1)
                 return own ? (size_t)s.row + (size_t)h * a.own_rows + r : (size_t)s.lead_row + (size_t)h * a.lead_rows + r;
-            return ((size_t)c * 2 + (u < c * per ? 0 : 1)) * QT + r % QT;
+            return (size_t)(own ? L0.slot0 : L1.slot0) + (((size_t)c * 2 + (u < c * per ? 0 : 1)) << qt) + (r & ((1 << qt) - 1));
         };
         float acc[E], x[J][E], m = -INFINITY, sum = 0.f;
 #pragma unroll
@@ -554,7 +603,7 @@ __global__ void __launch_bounds__(kJoinThreads<PW>, PW > 4 ? 2 : join_blocks(HD,
         auto load = [&](int i) {
 #pragma unroll
             for (int j = 0; j < J; ++j) {
-                const bool in = i + j < parts;
+                const bool in = i + j < parts, blocks = pw + (i + j) * PW < n0 ? L0.blocks : L1.blocks;
                 const size_t row = in ? at(i + j) : 0;
 #pragma unroll
                 for (int g = 0; g < E / V; ++g) {
@@ -654,14 +703,13 @@ struct JoinForm {
     static constexpr int RW = R, PW = P;
 };
 template <class T, int HD>
-cudaError_t launch_join(const dflare_cache* c, const TreeArgs& a, int QT, int extra, bool blocks, cudaStream_t s) {
+cudaError_t launch_join(const dflare_cache* c, const TreeArgs& a, const WorkLists& work, cudaStream_t s) {
     const long long rows = (long long)a.batch * a.n_max * a.hq;
     auto go = [&](auto form) {
         constexpr int RW = decltype(form)::RW, PW = decltype(form)::PW;
         constexpr int per = kJoinThreads<PW> / 32 / PW * RW;
         const long long most = (long long)c->num_sms * (PW > 4 ? 2 : join_blocks(HD, RW));
-        return launch_kernel(true, tree_shared_join_kernel<T, HD, RW, PW>, dim3((unsigned)std::min((rows + per - 1) / per, most)), dim3(kJoinThreads<PW>), 0, s,
-                             a, QT, extra, blocks);
+        return launch_kernel(true, tree_shared_join_kernel<T, HD, RW, PW>, dim3((unsigned)std::min((rows + per - 1) / per, most)), dim3(kJoinThreads<PW>), 0, s, a, work);
     };
     // Measured, a layer: 512 rows 17.1 us with a warp for each (four parts at a time 18.4); 4096 rows 31.0 with one for two, 32.5 for
     // four, 35.8 for each; 8192 rows 157 for two, 154 for four.
@@ -672,11 +720,6 @@ cudaError_t launch_join(const dflare_cache* c, const TreeArgs& a, int QT, int ex
     return go(JoinForm<4, 1>());
 }
 
-int log2_of(int v) {
-    int l = 0;
-    while (1 << (l + 1) <= v) ++l;
-    return l;
-}
 dflare_status refuse(const char* call, const char* m) {
     noalloc_set_error(std::string(call) + ": " + m);
     return DFLARE_EINVAL;
@@ -718,16 +761,18 @@ dflare_status dflare_cache_share_plan(dflare_cache* c, const int32_t* n_nodes_de
     a.pg = c->view;
     a.n_nodes = n_nodes_dev;
     a.head = reinterpret_cast<SharedHead*>(work);
-    a.runs = reinterpret_cast<int2*>(work + y.runs);
-    a.items = reinterpret_cast<TreeItem*>(work + y.items);
+    for (int l = 0; l < y.work.many; ++l) {
+        a.runs[l] = reinterpret_cast<int2*>(work + y.runs[l]);
+        a.items[l] = reinterpret_cast<TreeItem*>(work + y.items[l]);
+    }
     a.map = reinterpret_cast<int32_t*>(work + y.map);
     a.seqs = reinterpret_cast<TreeSeq*>(work + y.seqs);
     a.groups = groups_dev;
     a.batch = batch;
     a.n_max = n_max;
     a.G = c->cfg.n_q_heads / c->cfg.n_kv_heads;
-    a.qt = log2_of(y.QT), a.kt = log2_of(y.KT), a.C = y.C;      // (powers of two)
-    a.weight1 = y.weight1, a.weight2 = y.weight2, a.extra = y.extra, a.least = y.least;
+    a.work = y.work;
+    a.rows0 = y.rows0;
     a.own_rows = y.own_rows, a.lead_rows = y.lead_rows;
     DeviceGuard guard(c->device);
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -771,22 +816,25 @@ dflare_status dflare_cache_attend_shared(dflare_cache* c, int layer, const void*
     a.G = g.n_q_heads / g.n_kv_heads;
     a.G_inv = a.G > 1 ? 0xffffffffu / (uint32_t)a.G + 1u : 0u;
     a.QG = 1;
-    a.C = y.C;
     a.scale_log2 = scale * 1.4426950408889634f;
     a.head = reinterpret_cast<const SharedHead*>(work);
-    a.runs = reinterpret_cast<const int2*>(work + y.runs);
-    a.items = reinterpret_cast<const TreeItem*>(work + y.items);
     a.map = reinterpret_cast<const int32_t*>(work + y.map);
     a.seqs = reinterpret_cast<const TreeSeq*>(work + y.seqs);
     a.own_rows = y.own_rows;
     a.lead_rows = y.lead_rows;
     DeviceGuard guard(c->device);
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const bool f32 = g.dtype == DFLARE_F32, wide = g.head_dim == 128, few = y.QT == kMmaRows && !f32;
-    cudaError_t e = f32 ? launch_shared_f32(c, a, s) : few ? launch_shared_mma(c, a, s) : launch_shared_tc(c, a, y.QT, s);
-    if (e == cudaSuccess)
-        e = f32 ? (wide ? launch_join<float, 128>(c, a, y.QT, y.extra, false, s) : launch_join<float, 64>(c, a, y.QT, y.extra, false, s))
-                : (wide ? launch_join<bf16, 128>(c, a, y.QT, y.extra, !few, s) : launch_join<bf16, 64>(c, a, y.QT, y.extra, !few, s));
+    const bool f32 = g.dtype == DFLARE_F32, wide = g.head_dim == 128;
+    cudaError_t e = cudaSuccess;
+    for (int l = 0; l < y.work.many && e == cudaSuccess; ++l) {
+        a.runs = reinterpret_cast<const int2*>(work + y.runs[l]);
+        a.items = reinterpret_cast<const TreeItem*>(work + y.items[l]);
+        a.C = y.work.list[l].C;
+        a.follows = l > 0;
+        e = f32 ? launch_shared_f32(c, a, s) : y.work.list[l].blocks ? launch_shared_tc(c, a, s) : launch_shared_mma(c, a, s);
+    }
+    if (e == cudaSuccess) e = f32 ? (wide ? launch_join<float, 128>(c, a, y.work, s) : launch_join<float, 64>(c, a, y.work, s))
+                                  : (wide ? launch_join<bf16, 128>(c, a, y.work, s) : launch_join<bf16, 64>(c, a, y.work, s));
     if (e == cudaSuccess) return DFLARE_OK;
     noalloc_set_error(std::string(call) + ": " + cudaGetErrorString(e));
     return DFLARE_ECUDA;

@@ -95,6 +95,10 @@ CASES = [
     (0, [(0, 200, 70, 70), (0, 200, 65, 65), (0, 200, 1, 3)], 4, 1, 64, 32, [3]),                  # mask rows of three words
     (0, [(0, 17, 5, 9), (0, 16, 40, 9), (0, 19, 2, 9)], 8, 8, 64, 128, [3]),                       # shared to different depths; one head each
     (0, [(0, 3, 0, 1)], 64, 1, 128, 16, [1]),                                                      # alone
+    (0, [(i // 12, 40 + i // 12, 7 * i, 1 + i % 2) for i in range(24)], 16, 2, 64, 16, [12, 12]),      # few rows of many sequences
+    (0, [(i // 9, 11, 300 - 11 * i, (1, 0, 3, 4)[i % 4]) for i in range(18)], 12, 4, 128, 64, None),
+    (0, [(i, 2, 40 * i, 2) for i in range(20)], 32, 4, 128, 16, []),                                # as many, with nothing shared
+    (0, [(0, 100, 0, 1) for i in range(140)], 8, 4, 64, 16, [140]),                                 # a group of more than 128 sequences
 ]
 
 
@@ -189,15 +193,15 @@ def test_runs_that_cross_from_unit_to_unit(nodes, hq, hkv, hd, prompts, ways, pa
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("nodes", [3, 40])
-def test_rows_that_see_none_of_their_own_keys(dtype, nodes):
+@pytest.mark.parametrize("nodes,more", [(3, 0), (3, 12), (40, 0)])     # (few rows; few of each sequence; many)
+def test_rows_that_see_none_of_their_own_keys(dtype, nodes, more):
     """Masks without a bit: a row has the shared keys alone, or, without a context, none at all."""
     rng = np.random.default_rng(nodes)
-    p = Shared(rng, [(0, 200, 0, nodes), (0, 200, 0, nodes), (1, 0, 0, nodes)], hq=8, hkv=2, hd=64, page=16, dtype=dtype)
-    a = np.zeros((3, nodes, nodes), bool)
+    p = Shared(rng, [(0, 200, 0, nodes), (0, 200, 0, nodes), (1, 0, 0, nodes)] + [(2, 9, 40, nodes)] * more, hq=8, hkv=2, hd=64, page=16, dtype=dtype)
+    a = np.zeros((3 + more, nodes, nodes), bool)
     a[0, 1, 0] = True
     seen = [np.concatenate([np.ones((nodes, x), bool), a[b]], 1) for b, x in enumerate(p.lens)]
-    q = queries(rng, p, 3, nodes)
+    q = queries(rng, p, 3 + more, nodes)
     groups = check_shared(p, q, seen, i32(words(a)))
     assert groups[:2].tolist() == [[0, 200], [0, 200]]
     out, lse, _ = run_shared(p, q, i32(words(a)))
@@ -206,15 +210,16 @@ def test_rows_that_see_none_of_their_own_keys(dtype, nodes):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("nodes,hd", [(4, 64), (16, 128), (70, 64)])
-def test_unseen_infinities_and_nans_stay_out(dtype, nodes, hd):
+@pytest.mark.parametrize("nodes,hd,more", [(4, 64, 0), (4, 64, 9), (4, 128, 20), (16, 128, 0), (70, 64, 0)])
+def test_unseen_infinities_and_nans_stay_out(dtype, nodes, hd, more):
     """Node 1's key and value are NaN and infinite in each sequence of a group: rows that do not see it have the same bits."""
     rng = np.random.default_rng(nodes)
-    p = Shared(rng, [(0, 250, 17, nodes), (0, 250, 3, nodes - 2), (0, 250, 40, nodes)], hq=8, hkv=2, hd=hd, page=16, dtype=dtype)
-    q = queries(rng, p, 3, nodes)
+    many = 3 + more
+    p = Shared(rng, [(0, 250, 17 + 9 * i, nodes - 2 * (i == 1)) for i in range(many)], hq=8, hkv=2, hd=hd, page=16, dtype=dtype)
+    q = queries(rng, p, many, nodes)
     mask, seen = tree_masks(rng, p.lens, p.counts, nodes)
     clean, clean_lse, groups = run_shared(p, q, mask)
-    assert groups[:, 1].tolist() == [250] * 3
+    assert groups[:, 1].tolist() == [250] * many
     for b, x in enumerate(p.lens):
         page, off = p.table[b, (x + 1) // 16], (x + 1) % 16
         p.v[0, page, :, off, 3], p.v[0, page, :, off, hd - 1] = math.inf, math.nan
