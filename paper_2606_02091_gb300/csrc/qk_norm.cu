@@ -6,9 +6,8 @@
 // Backward, from dy:  dz = R^T dy,  a = g dz,  dx = r (a - x r^2 mean(a x)),  dg = sum over rows and heads of dz x r.
 // All of it in fp32, y and dx rounded once.
 //
-// Work: as in rope.cu a thread has 16 elements of a head, the head's threads (a power of two of them, neighbours in a
-// warp) add up their squares by shuffles, and a thread walks over several heads of one row, which share its cosines. A
-// thread has heads of queries or of keys, so that it needs one gain.
+// Work: as in rope.cu a thread has 16 elements of a head, and the head's threads (a power of two of them, neighbours in a
+// warp) add up their squares by shuffles. A CTA has heads of queries or of keys (or, in an append, values), so that a thread needs one gain.
 #include <math.h>
 
 #include <algorithm>
@@ -23,9 +22,7 @@ namespace dfl {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kBatch = 4;               // heads whose loads are in flight together
-constexpr int kForwardCtas = 2, kBackwardCtas = 2;
-template <class T> constexpr int kStreamCtas = 2;      // CTAs on an SM, as their registers and rings allow
+constexpr int kStreamCtas = 2;          // CTAs on an SM, as their registers and rings allow (three spill: 50 us instead of 43 for 10563 rows)
 constexpr int kWorkRows = DFLARE_QK_NORM_WORK_ROWS;     // CTAs that may leave a sum of gain gradients
 
 // queries, keys, values (values in an append only: copied)
@@ -39,8 +36,7 @@ struct Part {
     const void* gain;
     float* dgain;                       // backward, [hd]
     int heads;
-    int slots;                          // threads that share one row's 16 elements of these heads
-    int blocks;                         // backward: CTAs
+    int blocks;                         // CTAs
 };
 struct NormArgs {
     Part part[3];
@@ -48,8 +44,6 @@ struct NormArgs {
     const uint64_t* phase;
     float* work;                        // backward: [CTAs][hd]
     int rows, hd, rot;
-    int lanes;                          // threads of a head: the power of two from hd / 16 on
-    int per;                            // heads that a thread walks over, at most
     float magnitude, eps;
     PagesView pg;
     AppendRows rows_of;
@@ -95,10 +89,6 @@ __device__ __forceinline__ float sum2(uint64_t v) {
     unpack2(v, a, b);
     return a + b;
 }
-__device__ __forceinline__ float head_sum(float v, int lanes) {
-    for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
-}
 // 1 / sqrt(mean + eps), rounded once more than its argument
 __device__ __forceinline__ float inverse_rms(float sum_sq, float inv_hd, float eps) { return __frsqrt_rn(fmaf(sum_sq, inv_hd, eps)); }
 
@@ -135,88 +125,6 @@ __device__ __forceinline__ void make_turn(Turn& t, bool rotates, const float* c,
 template <bool INTER>
 __device__ __forceinline__ uint64_t partner(const uint64_t* v, int i) { return INTER ? swapped(v[i]) : v[i ^ 4]; }
 
-// Vector form: rot and hd multiples of 16, hd up to 512, everything 16-byte aligned.
-template <class T, bool INTER, bool APPEND>
-__global__ void __launch_bounds__(kThreads, kForwardCtas) qk_norm_kernel(const NormArgs a) {
-    pdl_wait();
-    pdl_trigger();
-    const int total = a.part[0].slots + a.part[1].slots + a.part[2].slots;
-    const long long t = (long long)blockIdx.x * kThreads + threadIdx.x;
-    const int u = (int)(t & (a.lanes - 1));
-    const long long g = t / a.lanes;
-    const long long row = g / total;
-    int s = (int)(g - row * total), part = 0;
-    if (s >= a.part[0].slots) {
-        s -= a.part[0].slots;
-        part = 1;
-        if (APPEND && s >= a.part[1].slots) {
-            s -= a.part[1].slots;
-            part = 2;
-        }
-    }
-    const Part& p = a.part[part];
-    // threads without work stay for the shuffles
-    long long pos = 0, slot = -1;
-    bool live = row < a.rows;
-    if (live) {
-        if (APPEND) live = append_row(a.pg, a.rows_of, (int)row, pos, slot);
-        else pos = a.positions ? a.positions[row] : 0;
-    }
-    live = live && u < a.hd / 16;
-    const bool rotates = u < a.rot / 16;
-    const int e0 = rotates && !INTER ? u * 8 : u * 16, e1 = rotates && !INTER ? a.rot / 2 + u * 8 : u * 16 + 8;
-    const float inv_hd = 1.f / (float)a.hd;
-    const T* from = static_cast<const T*>(p.x) + row * p.x_row;
-    Turn turn;
-    for (int i0 = 0; i0 < a.per; i0 += kBatch) {
-        Unit<T> x[kBatch];
-#pragma unroll
-        for (int k = 0; k < kBatch; ++k) {
-            const int h = s + (i0 + k) * p.slots;
-            x[k] = Unit<T>{};
-            if (live && h < p.heads) load_unit(x[k], from + h * p.x_head + e0, from + h * p.x_head + e1);
-        }
-        if (i0 == 0 && live && part < 2) {
-            Unit<T> g;
-            load_unit(g, static_cast<const T*>(p.gain) + e0, static_cast<const T*>(p.gain) + e1);
-            float c[8], sn[8];
-            if (rotates) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) pair_turn(pos, a.phase[u * 8 + j], 1.f, a.magnitude, c[j], sn[j]);
-            }
-            uint64_t gain[8];
-            values(g, gain);
-            make_turn<INTER>(turn, rotates, c, sn, gain);
-        }
-#pragma unroll
-        for (int k = 0; k < kBatch; ++k) {
-            const int h = s + (i0 + k) * p.slots;
-            uint64_t v[8], sq = 0ull;
-            values(x[k], v);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sq = fma2(v[i], v[i], sq);
-            const float sum = head_sum(sum2(sq), a.lanes);
-            if (!live || h >= p.heads) continue;
-            T* to = out_at<T, APPEND>(a, p, part, row, h, slot);
-            if (APPEND && !to) continue;
-            if (!APPEND || part < 2) {
-                const uint64_t r = both(inverse_rms(sum, inv_hd, a.eps));
-                uint64_t y[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = mul2(v[i], turn.a[i]);
-                if (rotates) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) y[i] = fma2(partner<INTER>(v, i), turn.b[i], y[i]);
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = mul2(y[i], r);
-                put(x[k], y);
-            }
-            store_unit(x[k], to + e0, to + e1);
-        }
-    }
-}
-
 // Sums of gain gradients: a thread's pairs to their places in its group's row; the groups' rows added up in order
 __device__ __forceinline__ void leave(float* row, const uint64_t* acc, int e0, int e1) {
 #pragma unroll
@@ -236,13 +144,14 @@ __device__ __forceinline__ void add_up(const float* sums, int groups, const Norm
     }
 }
 
-// ---------------- many rows
-// A warp has the heads of one part of a row after the other, 32 / LANES heads at a time, and copies its units ahead into shared memory, kStages
-// deep and across rows, so that as much as a load's latency asks for is always under way; a thread reads only what it
-// copied itself, so its own wait is enough. A row's cosines are worked out once per warp: a unit's eight pairs are shared out
-// among the threads that have the same unit of different heads.
-constexpr int kStages = 4;
-constexpr int kStreamLeast = 8;         // iterations of a warp per CTA of an SM
+// ---------------- rot and hd multiples of 16, hd up to 512, everything 16-byte aligned
+// The list of all (row, 32 / LANES heads) of a part is shared out evenly among its warps. A warp copies its units ahead into shared
+// memory, kStages deep and across rows, so that as much as a load's latency asks for is always under way; a thread reads only what it copied
+// itself, so its own wait is enough. A row's cosines are worked out once per warp: a unit's eight pairs are shared out among the threads
+// that have the same unit of different heads.
+// HBM-bound for many rows: 10563 rows of 40 heads of 128 37.6 us, 5.7 TB/s (52 with whole rows of several heads to a thread and loads
+// into registers), 8192 rows forward and backward 80 us, 5.3 TB/s; for few by latency, 64 rows 2.9 and 5.8 us.
+template <class T, int NA> constexpr int kStages = sizeof(T) * NA > 4 ? 2 : 4;
 
 __device__ __forceinline__ void copy16(uint32_t to, const void* from) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
@@ -254,7 +163,8 @@ template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("c
 template <class T, int NA>
 struct Ring {
     static constexpr int P = sizeof(T);             // pieces of a unit
-    static constexpr uint32_t BYTES = kStages * NA * P * 512;      // of a warp
+    static constexpr int STAGES = kStages<T, NA>;
+    static constexpr uint32_t BYTES = STAGES * NA * P * 512;       // of a warp
     uint32_t base;                                  // this thread's first piece
     __device__ __forceinline__ void copy(int stage, int array, const T* p0, const T* p1) const {
         const uint32_t to = base + (stage * NA + array) * (P * 512);
@@ -299,22 +209,23 @@ __device__ __forceinline__ float sum_of_head(float v) {
     return v;
 }
 
-// f(row, head of this thread, whether it is there, stage, issue) for the warp's part of the list of all (row, 32 / LANES heads),
-// which the part's warps share evenly; next(row) before the first of a row. NA arrays, whose units begin at elements e0 and e1.
-template <class T, int NA, int LANES, class Next, class F>
+// f(row, head of this thread, whether it is there, stage, issue) for the warp's part of the list of all (row, 32 / LANES heads); next(row)
+// before the first of a row; given(row): whether the row is to be read. NA arrays, whose units begin at elements e0 and e1.
+template <class T, int NA, int LANES, class Given, class Next, class F>
 __device__ __forceinline__ void each_unit(const NormArgs& a, const Part& p, int wid, int warps, const Ring<T, NA>& ring, int group, bool mine, int e0, int e1,
-                                          Next next, F f) {
-    constexpr int G = 32 / LANES;
+                                          Given given, Next next, F f) {
+    constexpr int G = 32 / LANES, S = kStages<T, NA>;
     const int iters = (p.heads + G - 1) / G;
     const long long all = (long long)a.rows * iters;
     const long long n0 = all * wid / warps;
     int left_i = (int)(all * (wid + 1) / warps - n0), left = left_i;
     int row = (int)(n0 / iters), h = (int)(n0 - (long long)row * iters) * G + group;
     int row_i = row, h_i = h, stage_i = 0, stage = 0;
+    bool given_i = left_i > 0 && given(row);
     auto issue = [&]() {
         if (left_i > 0) {
             --left_i;
-            if (mine && h_i < p.heads) {
+            if (mine && given_i && h_i < p.heads) {
                 const T* x = head_at<T>(p.x, row_i, p.x_row, h_i, p.x_head);
                 ring.copy(stage_i, 0, x + e0, x + e1);
                 if constexpr (NA == 2) {
@@ -326,19 +237,20 @@ __device__ __forceinline__ void each_unit(const NormArgs& a, const Part& p, int 
             if (h_i - group >= p.heads) {
                 h_i = group;
                 ++row_i;
+                given_i = left_i > 0 && given(row_i);
             }
         }
         copies_commit();
-        stage_i = stage_i + 1 == kStages ? 0 : stage_i + 1;
+        stage_i = stage_i + 1 == S ? 0 : stage_i + 1;
     };
 #pragma unroll
-    for (int i = 0; i < kStages - 1; ++i) issue();
+    for (int i = 0; i < S - 1; ++i) issue();
     for (; left > 0; ++row, h = group) {
         next(row);
         for (; h - group < p.heads && left > 0; h += G, --left) {
-            copies_wait<kStages - 2>();
+            copies_wait<S - 2>();
             f(row, h, mine && h < p.heads, stage, issue);
-            stage = stage + 1 == kStages ? 0 : stage + 1;
+            stage = stage + 1 == S ? 0 : stage + 1;
         }
     }
     copies_wait<0>();
@@ -352,9 +264,11 @@ struct StreamPlace {
 template <int LANES, bool INTER>
 __device__ __forceinline__ StreamPlace stream_place(const NormArgs& a) {
     StreamPlace y;
-    y.part = (int)blockIdx.x >= a.part[0].blocks;
     const int lane = threadIdx.x & 31;
-    y.wid = ((int)blockIdx.x - (y.part ? a.part[0].blocks : 0)) * (kThreads / 32) + (threadIdx.x >> 5);
+    int block = blockIdx.x;
+    y.part = 0;
+    while (y.part < 2 && block >= a.part[y.part].blocks) block -= a.part[y.part++].blocks;
+    y.wid = block * (kThreads / 32) + (threadIdx.x >> 5);
     y.warps = a.part[y.part].blocks * (kThreads / 32);
     y.u = lane % LANES;
     y.group = lane / LANES;
@@ -365,32 +279,37 @@ __device__ __forceinline__ StreamPlace stream_place(const NormArgs& a) {
     return y;
 }
 
-template <class T, bool INTER, int LANES>
-__global__ void __launch_bounds__(kThreads, kStreamCtas<T>) qk_norm_stream_kernel(const NormArgs a) {
+// APPEND: a step's new tokens on their way into the pages; values are copied. Rows past a sequence's new tokens are not read.
+template <class T, bool INTER, bool APPEND, int LANES>
+__global__ void __launch_bounds__(kThreads, kStreamCtas) qk_norm_stream_kernel(const NormArgs a) {
     extern __shared__ __align__(16) uint8_t smem[];
     pdl_wait();
     pdl_trigger();
     const StreamPlace y = stream_place<LANES, INTER>(a);
     const Part& p = a.part[y.part];
     const Ring<T, 1> ring{(uint32_t)__cvta_generic_to_shared(smem) + (threadIdx.x >> 5) * Ring<T, 1>::BYTES + (threadIdx.x & 31) * 16};
+    const bool norms = !APPEND || y.part < 2;
     Unit<T> gain{};
-    if (y.mine) load_unit(gain, static_cast<const T*>(p.gain) + y.e0, static_cast<const T*>(p.gain) + y.e1);
+    if (y.mine && norms) load_unit(gain, static_cast<const T*>(p.gain) + y.e0, static_cast<const T*>(p.gain) + y.e1);
     Pairs<LANES> pairs;
-    pairs.load(a.phase, y.u, y.group, y.rotates);
+    pairs.load(a.phase, y.u, y.group, y.rotates && norms);
     const float inv_hd = 1.f / (float)a.hd;
-    int pos = 0;
-    bool begun = false;
+    long long pos = 0, slot = -1;
+    bool begun = false, live = true;
     Turn turn;
     each_unit<T, 1, LANES>(a, p, y.wid, y.warps, ring, y.group, y.mine, y.e0, y.e1,
+        [&](int row) { return !APPEND || row % a.rows_of.n_max < a.rows_of.n_new[row / a.rows_of.n_max]; },
         [&](int row) {
             uint64_t g[8];
             float c[8], s[8];
-            if (a.positions) {
-                if (!begun) pos = a.positions[row];
+            if constexpr (APPEND) {
+                live = append_row(a.pg, a.rows_of, row, pos, slot);
+            } else if (a.positions && !begun) {
+                pos = a.positions[row];
                 begun = true;
             }
             pairs.at(pos, a.magnitude, y.u, c, s);
-            if (a.positions && row + 1 < a.rows) pos = a.positions[row + 1];     // (a row ahead)
+            if (!APPEND && a.positions && row + 1 < a.rows) pos = a.positions[row + 1];     // (a row ahead)
             values(gain, g);
             make_turn<INTER>(turn, y.rotates, c, s, g);
         },
@@ -403,18 +322,20 @@ __global__ void __launch_bounds__(kThreads, kStreamCtas<T>) qk_norm_stream_kerne
 #pragma unroll
             for (int i = 0; i < 8; ++i) sq = fma2(v[i], v[i], sq);
             const uint64_t r = both(inverse_rms(sum_of_head<LANES>(sum2(sq)), inv_hd, a.eps));
-            uint64_t out[8];
+            if (norms) {
+                uint64_t out[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) out[i] = mul2(v[i], turn.a[i]);
-            if (y.rotates) {
+                for (int i = 0; i < 8; ++i) out[i] = mul2(v[i], turn.a[i]);
+                if (y.rotates) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) out[i] = fma2(partner<INTER>(v, i), turn.b[i], out[i]);
+                    for (int i = 0; i < 8; ++i) out[i] = fma2(partner<INTER>(v, i), turn.b[i], out[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) out[i] = mul2(out[i], r);
+                put(x, out);
             }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) out[i] = mul2(out[i], r);
-            put(x, out);
-            T* to = static_cast<T*>(p.out) + row * p.out_row + h * p.out_head;
-            if (there) store_unit(x, to + y.e0, to + y.e1);
+            T* to = out_at<T, APPEND>(a, p, y.part, row, h, slot);
+            if (there && (!APPEND || (live && to))) store_unit(x, to + y.e0, to + y.e1);
         });
 }
 
@@ -436,7 +357,7 @@ __device__ __forceinline__ void turn_back(uint64_t* z, const float* c, const flo
 }
 
 template <class T, bool INTER, int LANES>
-__global__ void __launch_bounds__(kThreads, kBackwardCtas) qk_norm_backward_stream_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(kThreads, kStreamCtas) qk_norm_backward_stream_kernel(const NormArgs a) {
     extern __shared__ __align__(16) uint8_t smem[];
     pdl_wait();
     pdl_trigger();
@@ -457,7 +378,7 @@ __global__ void __launch_bounds__(kThreads, kBackwardCtas) qk_norm_backward_stre
     int pos = 0;
     bool begun = false;
     float c[8], s[8];
-    each_unit<T, 2, LANES>(a, p, y.wid, y.warps, ring, y.group, y.mine, y.e0, y.e1,
+    each_unit<T, 2, LANES>(a, p, y.wid, y.warps, ring, y.group, y.mine, y.e0, y.e1, [](int) { return true; },
         [&](int row) {
             if (a.positions) {
                 if (!begun) pos = a.positions[row];
@@ -546,107 +467,7 @@ __global__ void __launch_bounds__(kThreads) qk_norm_any_kernel(const NormArgs a)
     for (int e = a.rot + lane; e < a.hd; e += 32) to[e] = from_f<T>(to_f(x[e]) * r * to_f(gain[e]));
 }
 
-// Backward. A CTA has heads of one part and goes through rows a grid's width apart; every thread keeps the gain
-// gradients of its 16 elements, which the CTA adds up at the end in a fixed order and leaves in its row of `work`.
-template <class T, bool INTER>
-__global__ void __launch_bounds__(kThreads, kBackwardCtas) qk_norm_backward_kernel(const NormArgs a) {
-    constexpr int B = sizeof(T) == 2 ? 2 : 1;       // heads in flight
-    extern __shared__ float sums[];                 // [groups][hd]
-    pdl_wait();
-    pdl_trigger();
-    const int part = (int)blockIdx.x >= a.part[0].blocks;
-    const Part& p = a.part[part];
-    const int bid = blockIdx.x - (part ? a.part[0].blocks : 0), groups = kThreads / a.lanes;
-    const int u = threadIdx.x & (a.lanes - 1), group = threadIdx.x / a.lanes;
-    const bool mine = u < a.hd / 16, rotates = u < a.rot / 16;
-    const int e0 = rotates && !INTER ? u * 8 : u * 16, e1 = rotates && !INTER ? a.rot / 2 + u * 8 : u * 16 + 8;
-    uint64_t w[8], acc[8];
-    {
-        Unit<T> g{};
-        if (mine) load_unit(g, static_cast<const T*>(p.gain) + e0, static_cast<const T*>(p.gain) + e1);
-        values(g, w);
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) acc[i] = 0ull;
-    const float inv_hd = 1.f / (float)a.hd;
-    const long long items = (long long)a.rows * p.slots;
-    for (long long base = (long long)bid * groups; base < items; base += (long long)p.blocks * groups) {
-        const long long item = base + group;
-        const long long row = item / p.slots;
-        const int s = (int)(item - row * p.slots);
-        const bool live = item < items && mine;
-        const long long pos = live && a.positions ? a.positions[row] : 0;
-        // of the unit's pairs: cosines, and sines with the sign that each element's partner has in R^T
-        uint64_t c[INTER ? 8 : 4], sn[INTER ? 8 : 4];
-        for (int i0 = 0; i0 < a.per; i0 += B) {
-            Unit<T> x[B], d[B];
-#pragma unroll
-            for (int k = 0; k < B; ++k) {
-                const int h = s + (i0 + k) * p.slots;
-                x[k] = d[k] = Unit<T>{};
-                if (live && h < p.heads) {
-                    const T* from = head_at<T>(p.x, row, p.x_row, h, p.x_head);
-                    load_unit(x[k], from + e0, from + e1);
-                    from = head_at<T>(p.dy, row, p.dy_row, h, p.dy_head);
-                    load_unit(d[k], from + e0, from + e1);
-                }
-            }
-            if (i0 == 0 && rotates && live) {
-                float cf[8], sf[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) pair_turn(pos, a.phase[u * 8 + j], 1.f, a.magnitude, cf[j], sf[j]);
-#pragma unroll
-                for (int j = 0; j < (INTER ? 8 : 4); ++j) {
-                    c[j] = INTER ? both(cf[j]) : pack2(cf[2 * j], cf[2 * j + 1]);
-                    sn[j] = INTER ? pack2(sf[j], -sf[j]) : pack2(sf[2 * j], sf[2 * j + 1]);
-                }
-            }
-#pragma unroll
-            for (int k = 0; k < B; ++k) {
-                const int h = s + (i0 + k) * p.slots;
-                uint64_t v[8], z[8], sq = 0ull, ax = 0ull;
-                values(x[k], v);
-                values(d[k], z);
-                if (rotates && live) {
-                    if (INTER) {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) z[i] = fma2(swapped(z[i]), sn[i], mul2(z[i], c[i]));
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const uint64_t z0 = z[i], z1 = z[4 + i];
-                            z[i] = fma2(z1, sn[i], mul2(z0, c[i]));
-                            z[4 + i] = fma2(z1, c[i], mul2(z0, mul2(sn[i], both(-1.f))));
-                        }
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    sq = fma2(v[i], v[i], sq);
-                    ax = fma2(mul2(z[i], w[i]), v[i], ax);
-                }
-                const float all = head_sum(sum2(sq), a.lanes), dot = head_sum(sum2(ax), a.lanes);
-                if (!live || h >= p.heads) continue;
-                const float r = inverse_rms(all, inv_hd, a.eps);
-                const uint64_t rr = both(r), f = both(-(r * r * (dot * inv_hd)));
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint64_t n = mul2(v[i], rr);      // x r
-                    acc[i] = fma2(z[i], n, acc[i]);
-                    v[i] = fma2(n, f, mul2(mul2(z[i], w[i]), rr));
-                }
-                put(x[k], v);
-                T* to = static_cast<T*>(p.out) + row * p.out_row + h * p.out_head;
-                store_unit(x[k], to + e0, to + e1);
-            }
-        }
-    }
-    if (mine) leave(sums + group * a.hd, acc, e0, e1);
-    __syncthreads();
-    add_up(sums, groups, a);
-}
-
-// The same for any hd up to 1024, rot, strides and alignment: a warp per head, its gain gradients in shared memory (a
+// Backward for any hd up to 1024, rot, strides and alignment: a warp per head, its gain gradients in shared memory (a
 // lane's elements are its own).
 template <class T, bool INTER>
 __global__ void __launch_bounds__(kThreads) qk_norm_backward_any_kernel(const NormArgs a) {
@@ -741,72 +562,52 @@ dflare_status refuse(dflare_status st, const std::string& m) {
     return st;
 }
 
-// Threads of a head, and heads of a part that a thread walks over: one while all threads still fit the GPU at once, up
-// to eight where rows are many and a cosine should serve several heads.
-void plan_threads(NormArgs& a, int num_sms) {
-    a.lanes = 1;
-    while (a.lanes < a.hd / 16) a.lanes *= 2;
-    int heads = 0;
-    for (const Part& p : a.part) heads += p.heads;
-    const long long fit = std::max<long long>(1, (long long)a.rows * heads * a.lanes / ((long long)num_sms * 2048));
-    const int walk = (int)std::min<long long>(fit, 8);
-    a.per = 1;
-    for (Part& p : a.part) {
-        p.slots = (p.heads + walk - 1) / walk;
-        if (p.slots) a.per = std::max(a.per, (p.heads + p.slots - 1) / p.slots);
-    }
-}
-
-// Whether the kernels for many rows take a call: every warp that the GPU holds has some iterations of 32 / lanes heads.
-bool streams(const NormArgs& a, bool vec, int num_sms) {
-    if (!vec || a.hd <= 32 || a.hd > 256) return false;
-    const int lanes = a.hd <= 64 ? 4 : a.hd <= 128 ? 8 : 16, many = 32 / lanes;
-    const long long work = (long long)a.rows * ((a.part[0].heads + many - 1) / many + (a.part[1].heads + many - 1) / many);
-    return work >= (long long)kStreamLeast * num_sms * (kThreads / 32);
-}
 // CTAs of the parts, in proportion to their work, of `most`
 void share_blocks(NormArgs& a, const long long* need, long long most) {
-    const long long all = std::max<long long>(need[0] + need[1], 1);
-    for (int i = 0; i < 2; ++i)
-        a.part[i].blocks = (int)(all <= most ? need[i] : need[i] ? std::max<long long>(1, (most - 1) * need[i] / all) : 0);
+    const long long all = std::max<long long>(need[0] + need[1] + need[2], 1);
+    for (int i = 0; i < 3; ++i)
+        a.part[i].blocks = (int)(all <= most ? need[i] : need[i] ? std::max<long long>(1, (most - 2) * need[i] / all) : 0);
 }
-template <class T, bool INTER, int LANES>
+template <class T, bool INTER, bool APPEND, int LANES>
 cudaError_t launch_stream(NormArgs& a, bool backward, int num_sms, cudaStream_t s) {
-    static PerDeviceOnce once;
-    auto fwd = qk_norm_stream_kernel<T, INTER, LANES>;
-    auto bwd = qk_norm_backward_stream_kernel<T, INTER, LANES>;
-    constexpr int warps = kThreads / 32, bytes1 = warps * Ring<T, 1>::BYTES, ring2 = warps * Ring<T, 2>::BYTES;
-    constexpr int sums = kThreads / LANES * LANES * 16 * 4, bytes2 = ring2 > sums ? ring2 : sums;
-    cudaError_t e = once([&] {
-        cudaError_t e = cudaFuncSetAttribute(fwd, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes1);
-        return e == cudaSuccess ? cudaFuncSetAttribute(bwd, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes2) : e;
-    });
-    if (e != cudaSuccess) return e;
-    constexpr int many = 32 / LANES;
-    long long need[2];
+    constexpr int warps = kThreads / 32, many = 32 / LANES;
     // iterations, and one for a row's cosines; CTAs by their shares
-    for (int i = 0; i < 2; ++i) need[i] = a.part[i].heads ? (long long)a.rows * ((a.part[i].heads + many - 1) / many + 1) : 0;
-    const int most = std::min((backward ? kBackwardCtas : kStreamCtas<T>) * num_sms, kWorkRows);
-    share_blocks(a, need, most);
-    const dim3 grid(a.part[0].blocks + a.part[1].blocks);
-    return backward ? launch_kernel(true, bwd, grid, dim3(kThreads), bytes2, s, a) : launch_kernel(true, fwd, grid, dim3(kThreads), bytes1, s, a);
+    long long need[3], units = 0;
+    for (int i = 0; i < 3; ++i) {
+        need[i] = a.part[i].heads ? (long long)a.rows * ((a.part[i].heads + many - 1) / many + 1) : 0;
+        units += need[i];
+    }
+    if constexpr (!APPEND) {
+        if (backward) {
+            static PerDeviceOnce once;
+            auto kernel = qk_norm_backward_stream_kernel<T, INTER, LANES>;
+            constexpr int ring = warps * Ring<T, 2>::BYTES, sums = kThreads * 16 * 4, bytes = ring > sums ? ring : sums;
+            const cudaError_t e = once([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); });
+            if (e != cudaSuccess) return e;
+            // (two iterations for every warp at least: the CTAs' sums have to be added up. 64 rows 5.8 us, with a CTA for every SM 7.7)
+            share_blocks(a, need, std::max<long long>(3, std::min<long long>(std::min(kStreamCtas * num_sms, kWorkRows), units / (warps * 2))));
+            return launch_kernel(true, kernel, dim3(a.part[0].blocks + a.part[1].blocks), dim3(kThreads), bytes, s, a);
+        }
+    }
+    static PerDeviceOnce once;
+    auto kernel = qk_norm_stream_kernel<T, INTER, APPEND, LANES>;
+    constexpr int bytes = warps * Ring<T, 1>::BYTES;
+    const cudaError_t e = once([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); });
+    if (e != cudaSuccess) return e;
+    share_blocks(a, need, kStreamCtas * num_sms);
+    return launch_kernel(true, kernel, dim3(a.part[0].blocks + a.part[1].blocks + a.part[2].blocks), dim3(kThreads), bytes, s, a);
 }
-template <class T, bool INTER>
-cudaError_t stream_rows(NormArgs& a, bool backward, int num_sms, cudaStream_t s) {
-    if (a.hd <= 64) return launch_stream<T, INTER, 4>(a, backward, num_sms, s);
-    return a.hd <= 128 ? launch_stream<T, INTER, 8>(a, backward, num_sms, s) : launch_stream<T, INTER, 16>(a, backward, num_sms, s);
+template <class T, bool INTER, bool APPEND>
+cudaError_t launch_vec(NormArgs& a, bool backward, int num_sms, cudaStream_t s) {
+    if (a.hd <= 64) return launch_stream<T, INTER, APPEND, 4>(a, backward, num_sms, s);
+    if (a.hd <= 128) return launch_stream<T, INTER, APPEND, 8>(a, backward, num_sms, s);
+    if constexpr (APPEND) return cudaErrorInvalidValue;        // (a cache's heads have 64 or 128 elements)
+    else return a.hd <= 256 ? launch_stream<T, INTER, APPEND, 16>(a, backward, num_sms, s) : launch_stream<T, INTER, APPEND, 32>(a, backward, num_sms, s);
 }
 
 template <class T, bool INTER, bool APPEND>
 cudaError_t launch_forward(NormArgs& a, bool vec, int num_sms, cudaStream_t s) {
-    if constexpr (!APPEND)
-        if (streams(a, vec, num_sms)) return stream_rows<T, INTER>(a, false, num_sms, s);
-    plan_threads(a, num_sms);
-    if (vec) {
-        const long long threads = (long long)a.rows * (a.part[0].slots + a.part[1].slots + a.part[2].slots) * a.lanes;
-        return launch_kernel(true, qk_norm_kernel<T, INTER, APPEND>, dim3((unsigned)((threads + kThreads - 1) / kThreads)), dim3(kThreads), 0,
-                             s, a);
-    }
+    if (vec) return launch_vec<T, INTER, APPEND>(a, false, num_sms, s);
     const long long warps = (long long)a.rows * (a.part[0].heads + a.part[1].heads + a.part[2].heads);
     return launch_kernel(true, qk_norm_any_kernel<T, INTER, APPEND>, dim3((unsigned)((warps + kThreads / 32 - 1) / (kThreads / 32))),
                          dim3(kThreads), 0, s, a);
@@ -823,22 +624,18 @@ cudaError_t forward(NormArgs& a, int dtype, int layout, bool vec, int num_sms, c
 template <class T, bool INTER>
 cudaError_t launch_backward(NormArgs& a, bool vec, int num_sms, cudaStream_t s) {
     cudaError_t e;
-    const dim3 join((a.hd + 31) / 32, a.part[1].heads ? 2 : 1);
-    if (streams(a, vec, num_sms)) {
-        e = stream_rows<T, INTER>(a, true, num_sms, s);
-        return e == cudaSuccess ? launch_kernel(true, qk_norm_gain_kernel, join, dim3(kGainThreads), 0, s, a) : e;
+    if (vec) {
+        e = launch_vec<T, INTER, false>(a, true, num_sms, s);
+    } else {
+        constexpr int warps = kThreads / 32;
+        long long need[3];
+        for (int i = 0; i < 3; ++i) need[i] = ((long long)a.rows * a.part[i].heads + warps - 1) / warps;
+        share_blocks(a, need, std::min(kStreamCtas * num_sms, kWorkRows));     // CTAs that are resident at once
+        e = launch_kernel(true, qk_norm_backward_any_kernel<T, INTER>, dim3(a.part[0].blocks + a.part[1].blocks), dim3(kThreads),
+                          (size_t)warps * a.hd * sizeof(float), s, a);
     }
-    plan_threads(a, num_sms);
-    const int groups = vec ? kThreads / a.lanes : kThreads / 32;
-    long long need[2];
-    for (int i = 0; i < 2; ++i) need[i] = ((long long)a.rows * (vec ? a.part[i].slots : a.part[i].heads) + groups - 1) / groups;
-    share_blocks(a, need, std::min(kBackwardCtas * num_sms, kWorkRows));     // CTAs that are resident at once
-    const dim3 grid(a.part[0].blocks + a.part[1].blocks);
-    const size_t bytes = (size_t)groups * a.hd * sizeof(float);     // 16 KB at most; 32 KB for the other kernel
-    e = vec ? launch_kernel(true, qk_norm_backward_kernel<T, INTER>, grid, dim3(kThreads), bytes, s, a)
-                        : launch_kernel(true, qk_norm_backward_any_kernel<T, INTER>, grid, dim3(kThreads), bytes, s, a);
     if (e != cudaSuccess) return e;
-    return launch_kernel(true, qk_norm_gain_kernel, join, dim3(kGainThreads), 0, s, a);
+    return launch_kernel(true, qk_norm_gain_kernel, dim3((a.hd + 31) / 32, a.part[1].heads ? 2 : 1), dim3(kGainThreads), 0, s, a);
 }
 
 // What both directions ask of their arguments; nullptr: nothing is wrong.
@@ -870,7 +667,7 @@ const char* check_call(const dflare_qk_heads* q, const dflare_qk_heads* k, const
 
 Part part_of(const dflare_qk_heads* p) {
     if (!p) return Part{};
-    return Part{p->x, p->x_row, p->x_head, p->dy, p->dy_row, p->dy_head, p->out, p->out_row, p->out_head, p->gain, p->dgain, p->heads, 0, 0};
+    return Part{p->x, p->x_row, p->x_head, p->dy, p->dy_row, p->dy_head, p->out, p->out_row, p->out_head, p->gain, p->dgain, p->heads, 0};
 }
 bool part_vec(const Part& p, bool backward) {
     if (!p.heads) return true;
@@ -956,9 +753,9 @@ dflare_status dflare_cache_append_normed(dflare_cache* c, int layer, const void*
     const int hd = g.head_dim;
     if ((long long)batch * n_max * ((q_dev ? g.n_q_heads : 0) + 2 * g.n_kv_heads) * 32 / kThreads > 0x7ffffff0LL) return bad("too many heads");
     NormArgs a{};
-    if (q_dev) a.part[0] = Part{q_dev, q_row, hd, nullptr, 0, 0, q_out_dev, out_row, hd, q_gain_dev, nullptr, g.n_q_heads, 0, 0};
-    a.part[1] = Part{k_dev, k_row, hd, nullptr, 0, 0, nullptr, 0, 0, k_gain_dev, nullptr, g.n_kv_heads, 0, 0};
-    a.part[2] = Part{v_dev, v_row, hd, nullptr, 0, 0, nullptr, 0, 0, nullptr, nullptr, g.n_kv_heads, 0, 0};
+    if (q_dev) a.part[0] = Part{q_dev, q_row, hd, nullptr, 0, 0, q_out_dev, out_row, hd, q_gain_dev, nullptr, g.n_q_heads, 0};
+    a.part[1] = Part{k_dev, k_row, hd, nullptr, 0, 0, nullptr, 0, 0, k_gain_dev, nullptr, g.n_kv_heads, 0};
+    a.part[2] = Part{v_dev, v_row, hd, nullptr, 0, 0, nullptr, 0, 0, nullptr, nullptr, g.n_kv_heads, 0};
     a.phase = phase_dev;
     a.rows = batch * n_max;
     a.hd = hd;

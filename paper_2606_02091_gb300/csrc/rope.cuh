@@ -26,11 +26,12 @@ struct AppendRows {
 __device__ __forceinline__ bool append_row(const PagesView& pg, const AppendRows& a, int row, long long& pos, long long& slot) {
     slot = -1;
     const int b = row / a.n_max, i = row - b * a.n_max;
-    if (i >= a.n_new[b]) return false;
-    const int len = pg.lens[b];
-    pos = (long long)len + (a.depth ? a.depth[row] : i);
+    // (all of them under way before one is looked at)
+    const int n_new = a.n_new[b], len = pg.lens[b], held = pg.held[b], depth = a.depth ? a.depth[row] : i;
+    if (i >= n_new) return false;
+    pos = (long long)len + depth;
     const long long at = (long long)len + i;
-    const long long room = (long long)min(pg.held[b], pg.max_pages) * pg.ps;
+    const long long room = (long long)min(held, pg.max_pages) * pg.ps;
     uint32_t err = DFLARE_DEVERR_CAPACITY;
     if (len >= 0 && at < room) {
         const int page = pg.table[(size_t)b * pg.max_pages + at / pg.ps];
