@@ -10,8 +10,8 @@
 // busy while the other's scores are turned into weights. With 128 rows or fewer (NQ = 1) the streams take
 // alternate key tiles of the same rows and are joined per row at the end; with more (NQ = 2) each has 128 rows
 // of its own and both read every tile, so 256 rows cost one pass over the keys. Over a plan's items a kernel with NQ = 2 does
-// either, unit by unit (64 sequences of 4 nodes, their own 1150 keys and four shared contexts of 32768: 187 us with one stream
-// idle in units of few rows, 151 so).
+// either, unit by unit (two layers of 64 sequences of 4 nodes, their own 1150 keys and four shared contexts of 32768: 411 us with one
+// stream idle in units of few rows, 377 so).
 // m is raised (and O scaled) only when a tile's maximum exceeds it by 2^8: P <= 2^8 carries the same relative
 // precision, and O / l does not depend on m.
 // Bound by the chain of hand-offs between softmax and MMA (1.7 us per tile of 256 rows against 1.46 us of HBM time):

@@ -189,6 +189,31 @@ def test_rows_beside_the_call_stay_and_odd_values_stay_in_their_heads(dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("offset,row", [(1, 0), (0, 3), (4, 5)])
+def test_odd_addresses_and_strides(offset, row, dtype):
+    """Heads that begin off a 16-byte boundary, or rows an odd number of elements apart, of everything a call reads and writes."""
+    rng = np.random.default_rng(offset + row)
+    rows, heads, hd, t = 37, 3, 64, TYPES[dtype]
+    pos, phase, inv = rng.integers(0, 900, rows), P.rope_phases(32, 1e4)[0], frequencies(32, 1e4)[0]
+    gain = (1 + 0.2 * torch.from_numpy(rng.standard_normal(hd).astype(np.float32)).to(t)).cuda()
+
+    def odd():
+        wide = torch.from_numpy(rng.standard_normal(rows * (heads * hd + row) + offset).astype(np.float32)).to(t).cuda()
+        return wide[offset:].view(rows, heads * hd + row)[:, :heads * hd].view(rows, heads, hd)
+
+    x, dy, out, dx = odd(), odd(), odd(), odd()
+    P.qk_norm_rope(x, None, i32(pos), phase, gain, None, out, None)
+    want, bound = forward(host(x), host(gain), pos, inv, "half", 1.0, 1e-6)
+    within(out, want, bound, dtype)
+    dg = torch.zeros(hd, device="cuda")
+    P.qk_norm_rope_backward(x, None, dy, None, i32(pos), phase, gain, None, dx, None, dg, None, P.qk_norm_rope_work(hd))
+    want, want_gain, bound, gain_bound = backward(host(x), host(dy), host(gain), pos, inv, "half", 1.0, 1e-6)
+    within(dx, want, bound, dtype)
+    assert np.all(np.abs(host(dg) - want_gain) <= gain_bound)
+
+
+@pytest.mark.gpu
 def test_a_broadcast_input_and_gradient():
     """A row stride of zero: the same head for every row, its gradients one after another."""
     rng = np.random.default_rng(9)

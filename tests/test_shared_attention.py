@@ -273,21 +273,24 @@ def test_long_shared_contexts_past_32_bit_offsets(nodes):
 
 
 @pytest.mark.gpu
-def test_on_another_stream_in_graphs_and_with_two_workspaces():
+@pytest.mark.parametrize("n,more,dtype", [(6, 0, "bf16"), (3, 38, "bf16"), (9, 8, "bf16"), (3, 0, "f32")])       # (each of the kernels, and two together)
+def test_on_another_stream_in_graphs_and_with_two_workspaces(n, more, dtype):
     rng = np.random.default_rng(12)
-    p = Shared(rng, [(0, 80, 30, 6), (0, 80, 9, 6), (1, 20, 4, 6), (1, 20, 33, 6)], hq=16, hkv=4, hd=128, page=16, dtype="bf16", layers=2)
-    mask, _ = tree_masks(rng, p.lens, p.counts, 6)
-    q, q2 = queries(rng, p, 4, 6), queries(rng, p, 4, 6)
+    seqs = [(0, 80, 30, n), (0, 80, 9, n), (1, 20, 4, n), (1, 20, 33, n)] + [(2 + i // 8, 30, 7 * i, n) for i in range(more)]
+    batch = len(seqs)
+    p = Shared(rng, seqs, hq=16, hkv=4, hd=128, page=16, dtype=dtype, layers=2)
+    mask, _ = tree_masks(rng, p.lens, p.counts, n)
+    q, q2 = queries(rng, p, batch, n), queries(rng, p, batch, n)
     want, want2 = run_shared(p, q, mask)[0], run_shared(p, q2, mask, layer=1)[0]
     counts = i32(p.counts)
 
     def step(q, out, work, layer, stream=None):
-        p.cache.share_plan(counts, 6, work, stream=stream)
+        p.cache.share_plan(counts, n, work, stream=stream)
         p.cache.attend_shared(layer, q, out, work, mask=mask, stream=stream)
 
     torch.cuda.synchronize()
     side, out, out2 = torch.cuda.Stream(), torch.zeros_like(want), torch.zeros_like(want)
-    works = [p.cache.shared_work(4, 6) for _ in range(3)]
+    works = [p.cache.shared_work(batch, n) for _ in range(3)]
     torch.cuda.synchronize()
     step(q, out, works[0], 0, side)
     step(q2, out2, works[1], 1)         # at the same time
@@ -306,8 +309,8 @@ def test_on_another_stream_in_graphs_and_with_two_workspaces():
         graphs[1].replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want) and torch.equal(out2, want2)
-    # the lengths that the graph reads are those of the replay: shorter contexts, of which one shares a page less
-    p.cache.lens.add_(-16)
+    # the lengths that the graph reads are those of the replay: shorter contexts, of which some share a page less
+    p.cache.lens.add_(-4)
     p.cache.attend(0, q, counts, want, mask=mask)
     graphs[0].replay()
     torch.cuda.synchronize()
