@@ -145,34 +145,38 @@ def rope(x, positions, phase, out, *, layout="half", magnitude=1.0, backward=Fal
                                    _lib.DFLARE_BF16 if dtype is _BF16 else _lib.DFLARE_F32, _stream(stream, dev)))
 
 
-def _heads(name, t, shape, dtype, device):
+def _heads(name, what, t, shape, dtype, device):
     """Address and strides of [rows][heads][head_dim] heads."""
     if t.dtype is not dtype or t.get_device() != device:
-        _typed(name, t, dtype, device)
+        _typed(name + what, t, dtype, device)
     if t.shape != shape:
-        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+        raise ValueError(f"{name}{what} must be {list(shape)}, got {list(t.shape)}")
     row, head, one = t.stride()
     if one != 1 and shape[2] > 1:
-        raise ValueError(f"{name}: the elements of a head must be adjacent")
+        raise ValueError(f"{name}{what}: the elements of a head must be adjacent")
     return t.data_ptr(), row, head
 
 
 def _qk_part(name, x, dy, out, gain, dgain, rows, hd, dtype, device):
     """The struct of one call's queries or keys: [rows][heads][head_dim] tensors and their gain."""
     shape = x.shape
-    if x.dim() != 3 or shape[0] != rows or shape[2] != hd:
+    if len(shape) != 3 or shape[0] != rows or shape[2] != hd:
         raise ValueError(f"{name} must be [{rows}][heads][{hd}], got {list(shape)}")
-    return _lib.QkHeads(*_heads(name, x, shape, dtype, device), *((None, 0, 0) if dy is None else _heads(name + "'s gradient", dy, shape, dtype, device)),
-                        *_heads(name + "'s result", out, shape, dtype, device), _line(name + "'s gain", gain, dtype, hd, device),
-                        None if dgain is None else _line(name + "'s gain gradient", dgain, _F32, hd, device), shape[1])
+    xp, xr, xh = _heads(name, "", x, shape, dtype, device)
+    op, or_, oh = _heads(name, "'s result", out, shape, dtype, device)
+    gp = _line(name, "'s gain", gain, dtype, hd, device)
+    if dy is None:
+        return _lib.QkHeads(xp, xr, xh, None, 0, 0, op, or_, oh, gp, None, shape[1])
+    dp, dr, dh = _heads(name, "'s gradient", dy, shape, dtype, device)
+    return _lib.QkHeads(xp, xr, xh, dp, dr, dh, op, or_, oh, gp, _line(name, "'s gain gradient", dgain, _F32, hd, device), shape[1])
 
 
-def _line(name, t, dtype, numel, device):
+def _line(name, what, t, dtype, numel, device):
     """A tensor of `numel` elements without gaps; its address."""
     if t.dtype is not dtype or t.get_device() != device:
-        _typed(name, t, dtype, device)
+        _typed(name + what, t, dtype, device)
     if t.numel() != numel or not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous and hold {numel} elements, got {list(t.shape)}")
+        raise ValueError(f"{name}{what} must be contiguous and hold {numel} elements, got {list(t.shape)}")
     return t.data_ptr()
 
 
@@ -216,7 +220,7 @@ def qk_norm_rope_backward(q, k, dq_out, dk_out, positions, phase, q_gain, k_gain
     ks = None if k is None else _qk_part("k", k, dk_out, dk, k_gain, dk_gain, rows, hd, q.dtype, dev)
     _check(_lib.load().dflare_qk_norm_rope_backward(
         ctypes.byref(qs), None if ks is None else ctypes.byref(ks), pos, ph, rows, hd, rot, lay, magnitude, eps,
-        _line("work", work, _F32, _lib.QK_NORM_WORK_ROWS * hd, dev), _lib.DFLARE_BF16 if q.dtype is _BF16 else _lib.DFLARE_F32,
+        _line("work", "", work, _F32, _lib.QK_NORM_WORK_ROWS * hd, dev), _lib.DFLARE_BF16 if q.dtype is _BF16 else _lib.DFLARE_F32,
         _stream(stream, dev)))
 
 
@@ -383,8 +387,8 @@ class PagedCache:
                 raise ValueError("keys and, where there are queries, queries have a gain, or neither has")
             _check(self._L.dflare_cache_append_normed(
                 self._cache, layer, qp, qs, kp, ks, vp, vs, op, os_,
-                None if q_gain is None else _line("q_gain", q_gain, self.dtype, self.head_dim, dev),
-                _line("k_gain", k_gain, self.dtype, self.head_dim, dev), eps,
+                None if q_gain is None else _line("q_gain", "", q_gain, self.dtype, self.head_dim, dev),
+                _line("k_gain", "", k_gain, self.dtype, self.head_dim, dev), eps,
                 None if depth is None else _ints("depth", depth, batch * n, dev), _ints("n_new", n_new, batch, dev), batch, n,
                 None if phase is None else _phase(phase, dev), 0 if phase is None else 2 * phase.numel(), _layout(layout), magnitude,
                 _stream(stream, dev)))
