@@ -64,8 +64,9 @@ struct __align__(16) TreeSeq {
     int weight, lead_weight;    // cost of a tile
 };
 // The head of an attend_shared workspace.
-struct SharedHead {
-    int batch, n_max, ok, per[2];       // per: length of a CTA's run in each list of work
+struct __align__(16) SharedHead {
+    int ok, batch, n_max, max_pages, hkv, ps, G;        // what the plan was made for
+    int per[2];                                         // length of a CTA's run in each list of work
 };
 // One kernel's list of work: log2 of its rows per block and keys per tile, its CTAs, what a tile of up to 128 rows and one of more costs, and
 // a unit beside its tiles, the shortest run, and the first of its CTAs' rows among the partial results.

@@ -476,9 +476,13 @@ __global__ void __launch_bounds__(kPlanThreads) tree_shared_plan_kernel(const __
     }
     __syncthreads();
     if (tid == 0) {
+        a.head->ok = 1;
         a.head->batch = a.batch;
         a.head->n_max = a.n_max;
-        a.head->ok = 1;
+        a.head->max_pages = a.pg.max_pages;
+        a.head->hkv = a.pg.hkv;
+        a.head->ps = a.pg.ps;
+        a.head->G = a.G;
     }
     for (int x = tid; x < a.batch * a.n_max; x += kPlanThreads) {
         const int b = x / a.n_max, i = x - b * a.n_max;
@@ -565,7 +569,7 @@ __global__ void __launch_bounds__(kJoinThreads<PW>, PW > 4 ? 2 : join_blocks(HD,
     __shared__ float others[PW > 1 ? kJoinThreads<PW> / 32 : 1][HD + 2];     // of a row's warps: output, maximum, sum
     const int lane = threadIdx.x & 31, l = lane % LPR, warp = threadIdx.x >> 5, pw = warp % PW;
     // the plan is older than the kernel before this one, which let this one start after its own wait
-    const bool ok = a.head->batch == a.batch && a.head->n_max == a.n_max && a.head->ok;
+    const bool ok = plan_fits(a);
     const int per0 = ok ? a.head->per[0] : 1, per1 = ok ? a.head->per[work.many - 1] : 1;
     const WorkList &L0 = work.list[0], &L1 = work.list[1];
     bool begun = false;

@@ -327,6 +327,15 @@ def test_a_workspace_without_the_plan_is_reported_and_nothing_written():
         p.cache.attend_shared(0, q, out, work)
         assert p.cache.error() == _lib.DEVERR_PLAN and (out == 7).all()
         p.cache.share_plan(i32(p.counts), 4, work)
+    # plans of caches with longer tables, other pages, other heads
+    for kw in (dict(seqs=[(0, 90, 3, 2), (0, 90, 9, 2)]), dict(page=32), dict(hq=4), dict(hkv=4)):
+        other = Shared(rng, **{**dict(seqs=[(0, 40, 3, 2), (0, 40, 9, 2)], hq=8, hkv=2, hd=64, page=16, dtype="bf16", nodes=4), **kw})
+        more = other.cache.shared_work(2, 2)
+        other.cache.share_plan(i32(other.counts), 2, more)
+        room = torch.zeros(max(more.numel(), p.cache.shared_work(2, 2).numel()), dtype=torch.uint8, device="cuda")
+        room[:more.numel()] = more
+        p.cache.attend_shared(0, q, out, room)
+        assert p.cache.error() == _lib.DEVERR_PLAN and (out == 7).all()
     p.cache.share_plan(i32(p.counts), 2, work)
     p.cache.attend_shared(0, q, out, work)
     assert p.cache.error() == 0 and not (out == 7).any()
