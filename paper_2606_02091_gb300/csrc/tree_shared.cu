@@ -29,6 +29,7 @@ namespace dfl {
 namespace {
 
 constexpr int kPlanThreads = 1024;
+constexpr int kPlanRuns = 2048;         // CTAs of a call's kernels, at most
 
 // Query rows per kv head of a whole batch up to which the warp-level kernel has them, 16 at a time. Measured over 91 drawn calls, against
 // attention without sharing: 0.84 and 0.76 of its time with 16 rows and fewer (two sets, geometric means), 0.83 with up to 32, 0.79
@@ -92,7 +93,7 @@ Layout layout_of(const dflare_cache* c, int batch, int n_max) {
     const long long own_rows = ((long long)n_max * G + 31) / 32 * 32, lead_rows = (rows / 32 + batch + 1) * 32;
     const long long rows0 = part;
     part += (batch * own_rows + lead_rows) * g.n_kv_heads;
-    if (part > most) y.ok = false;
+    if (part > most || y.work.list[0].C + (y.work.many > 1 ? y.work.list[1].C : 0) > kPlanRuns) y.ok = false;
     if (!y.ok) return y;
     y.own_rows = (int)own_rows;
     y.lead_rows = (int)lead_rows;
@@ -357,26 +358,37 @@ __global__ void __launch_bounds__(kPlanThreads) tree_shared_plan_kernel(const __
     __shared__ int2 tmp[kMaxSeqs / 32];
     __shared__ int total_cost[2], total_units[2];       // of the lists
     auto place_of = [&](int b, int which) { return a.work.many == 1 ? 2 * b + which : which * kMaxSeqs + b; };
-    cluster_arrive();       // (every CTA of the cluster has begun before one writes to another)
+    __shared__ int first_of[kPlanRuns], last_of[kPlanRuns];        // of the runs of both lists: units
+    const bool alone = gridDim.x == 1;
+    if (!alone) cluster_arrive();       // (every CTA of the cluster has begun before one writes to another)
     pdl_wait();
     pdl_trigger();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t rank = cluster_rank();
-    const int b0 = (int)rank * (kPlanThreads / 32) + warp, found = b0 < a.batch ? pages_shared(a, b0) : 0;
-    cluster_wait();
-    if (lane == 0 && b0 < a.batch) {
-        uint32_t at;
-        asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(same + b0)));
-        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(found) : "memory");
+    int n = 0, held = 0, ctx = 0, keys = 0;
+    if (tid < a.batch && rank == 0) lengths_of(a, tid, n, held, ctx, keys);
+    for (int x = tid; x < kPlanRuns; x += kPlanThreads) {
+        first_of[x] = 0x7fffffff;
+        last_of[x] = -1;
     }
-    cluster_arrive();
-    cluster_wait();
-    if (rank != 0) return;
+    const int b0 = (int)rank * (kPlanThreads / 32) + warp, found = b0 < a.batch ? pages_shared(a, b0) : 0;
+    if (alone) {
+        if (lane == 0 && b0 < a.batch) same[b0] = found;
+        __syncthreads();
+    } else {
+        cluster_wait();
+        if (lane == 0 && b0 < a.batch) {
+            uint32_t at;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(same + b0)));
+            asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(found) : "memory");
+        }
+        cluster_arrive();
+        cluster_wait();
+        if (rank != 0) return;
+    }
     if (tid < kMaxSeqs) {       // a thread for every sequence, up to the list of segments
-        int n = 0, held = 0, ctx = 0, keys = 0;
         int2 total;
         if (tid < a.batch) {
-            lengths_of(a, tid, n, held, ctx, keys);
             n_of[tid] = n;
             held_of[tid] = held;
             ctx_of[tid] = ctx;
@@ -484,16 +496,14 @@ __global__ void __launch_bounds__(kPlanThreads) tree_shared_plan_kernel(const __
         a.head->ps = a.pg.ps;
         a.head->G = a.G;
     }
-    for (int x = tid; x < a.batch * a.n_max; x += kPlanThreads) {
-        const int b = x / a.n_max, i = x - b * a.n_max;
-        if (i < node0[b + 1] - node0[b]) a.map[node0[b] + i] = x;
-    }
+    for (int b = warp; b < a.batch; b += kPlanThreads / 32)
+        for (int i = lane; i < node0[b + 1] - node0[b]; i += 32) a.map[node0[b] + i] = b * a.n_max + i;
     {       // the lists, each by its part of the threads
         const int threads = kPlanThreads / a.work.many, list = tid / threads, me = tid - list * threads;
         const WorkList& L = a.work.list[list];
         const int all = total_cost[list], all_units = total_units[list], per = max((all + L.C - 1) / L.C, L.least);
         if (me == 0) a.head->per[list] = per;
-        // the last of the list's segments that begins at or before x and is not empty, of starts that do not fall
+        // the last of the list's segments that begins at or before x and is not empty
         auto segment = [&](const int* begin, int x) {
             int lo = list * kMaxSeqs, hi = a.work.many == 1 ? 2 * a.batch : lo + a.batch;
             while (hi - lo > 1) {
@@ -503,19 +513,8 @@ __global__ void __launch_bounds__(kPlanThreads) tree_shared_plan_kernel(const __
             return lo;
         };
         // The items of run c are numbers u + c for its units u: the list of units and the list of runs advance together.
-        for (int c = me; c < L.C; c += threads) {
-            const long long v0 = (long long)c * per, v1 = min(v0 + per, (long long)all);
-            int2 run = make_int2(0, 0);
-            if (v0 < v1) {
-                auto unit_at = [&](int v, bool next) {      // the unit that has the tile at place v, or (next) the first tile from there on
-                    const int e = segment(seg_start, v), w = seg_weight[e], t = seg_tiles[e], size = t * w + L.extra, idx = (v - seg_start[e]) / size;
-                    return seg_unit[e] + idx + (next && v - seg_start[e] - idx * size > (t - 1) * w);
-                };
-                run.x = unit_at((int)v0, true) + c;
-                run.y = unit_at((int)v1 - 1, false) + c + 1;
-            }
-            a.runs[list][c] = run;
-        }
+        int* const firsts = first_of + (list ? a.work.list[0].C : 0);
+        int* const lasts = last_of + (list ? a.work.list[0].C : 0);
         // Items by units, `share` threads for each, where there are few.
         int share_log = 0;
         while (((long long)all_units << (share_log + 1)) <= threads && share_log < 5) ++share_log;
@@ -552,8 +551,12 @@ __global__ void __launch_bounds__(kPlanThreads) tree_shared_plan_kernel(const __
                 it.hi = c == c1 ? t : ((int)(v0 + per - start) + w - 1) / w;
                 it.dst = c0 == c1 ? whole : L.slot0 + ((2 * c + (start < v0 ? 0 : 1)) << L.qt);
                 a.items[list][u + c] = it;
+                atomicMin(&firsts[c], u);
+                atomicMax(&lasts[c], u);
             }
         }
+        __syncthreads();
+        for (int c = me; c < L.C; c += threads) a.runs[list][c] = lasts[c] < 0 ? make_int2(0, 0) : make_int2(firsts[c] + c, lasts[c] + 1 + c);
     }
 }
 
