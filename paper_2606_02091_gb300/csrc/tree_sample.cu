@@ -24,6 +24,7 @@
 
 #include "common.cuh"
 #include "paged.h"
+#include "umma.cuh"
 
 namespace dfl {
 namespace {
@@ -89,9 +90,9 @@ __device__ __forceinline__ Sum times(const Sum& a, const Sum& b) {
     return settled(p, __fmaf_rn(a.h, b.l, __fmaf_rn(a.l, b.h, __fmaf_rn(a.h, b.h, -p))));
 }
 __device__ __forceinline__ Sum over(const Sum& a, const Sum& b) {
-    const float q = __fdiv_rn(a.h, b.h);
+    const float inv = __frcp_rn(b.h), q = __fmul_rn(a.h, inv);     // (the remainder makes up for what q lacks)
     const float rest = __fadd_rn(__fmaf_rn(-q, b.h, a.h), __fmaf_rn(-q, b.l, a.l));
-    return settled(q, __fdiv_rn(rest, b.h));
+    return settled(q, __fmul_rn(rest, inv));
 }
 __device__ __forceinline__ bool above(const Sum& a, const Sum& b) { return __fadd_rn(__fsub_rn(a.h, b.h), __fsub_rn(a.l, b.l)) > 0.f; }
 __device__ __forceinline__ Sum from_lane(const Sum& s, int lane) { return {__shfl_sync(0xffffffffu, s.h, lane), __shfl_sync(0xffffffffu, s.l, lane)}; }
@@ -202,17 +203,35 @@ __device__ __forceinline__ uint32_t cluster_size() {
 }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-// the Sum at address `p` of this CTA's shared memory, as CTA `rank` of the cluster has it
-__device__ __forceinline__ Sum sum_of(const Sum* p, uint32_t rank) {
-    uint32_t at;
-    Sum s;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
-    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(s.h), "=f"(s.l) : "r"(at) : "memory");
-    return s;
+// The CTAs' sums of one turn go from each to all, 8 bytes that count towards the receiver's barrier: one trip through the cluster, where a
+// barrier of the cluster and a read take three (1.0 and 0.4 us against 0.4).
+__device__ __forceinline__ void send(const Sum& s, Sum* to, uint64_t* bar, uint32_t rank) {
+    uint32_t at, there;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(to)), "r"(rank));
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(smem_u32(bar)), "r"(rank));
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(at), "f"(s.h), "f"(s.l), "r"(there) : "memory");
+}
+__device__ __forceinline__ bool received(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+// Waits for them, up to two seconds.
+__device__ __forceinline__ bool receive(uint32_t bar, uint32_t parity) {
+    for (int i = 0; i < 64; ++i)
+        if (received(bar, parity)) return true;
+    const uint64_t t0 = globaltimer_ns();
+    while (!received(bar, parity))
+        if (globaltimer_ns() - t0 > kTimeoutNs) return false;
+    return true;
 }
 
 enum { kSum, kLast, kNone };    // what warp 0 asks of the CTA: a residual's sum; the last one, with the token; nothing more
-enum { kGoOn, kSearch, kDone };     // what it found after the cluster's sum: the token is in this CTA's part; nothing more to do
+enum { kGoOn, kSearch, kDone, kGaveUp };        // what it found after the cluster's sum: the token is in this CTA's part; nothing more to do
 
 // The token at which the running sum passes goal, in warp w's part [s0, s1) behind base: the CTA's warps sum up sixteenths, and
 // warp 0 goes through one of them, 32 elements at a time.
@@ -260,15 +279,22 @@ __global__ void __launch_bounds__(kThreads, 2) tree_sample_kernel(const SampleAr
     __shared__ int32_t up[kMaxNodes], tok[kMaxNodes], first[kMaxNodes], list[kMaxNodes];
     __shared__ float u[kMaxNodes], px[kMaxNodes], qx[kMaxNodes];
     __shared__ Sum of_warp[2][kWarps];
-    __shared__ __align__(8) Sum of_cta[2];
+    __shared__ __align__(8) Sum of_cta[2][kMaxCluster];
+    __shared__ __align__(8) uint64_t bars[2];
     __shared__ Residual todo;
     __shared__ int what, steps, found, from_warp;
     __shared__ Sum from_base, goal;
-    pdl_wait();
-    pdl_trigger();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t rank = cluster_rank(), ctas = cluster_size();
     const int b = blockIdx.x / ctas;
+    if (tid == 0) {
+        mbar_init(smem_u32(bars), 1);
+        mbar_init(smem_u32(bars + 1), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    cluster_arrive();       // (before anything is sent, every CTA's barriers are there)
+    pdl_wait();
+    pdl_trigger();
     const float* target = a.target + (size_t)b * a.n_max * a.vocab;
     const float* draft = a.draft ? a.draft + (size_t)b * a.draft_rows * a.vocab : nullptr;
     // (rows past the tree's nodes are fetched with the others, and stay without effect: two trips to memory, not three)
@@ -309,16 +335,18 @@ __global__ void __launch_bounds__(kThreads, 2) tree_sample_kernel(const SampleAr
     }
     __syncthreads();
 
+    cluster_wait();
     // ---------------- warp 0 walks; the others sum what it asks for. Every CTA of the cluster finds the same.
     int at = 0, i = first[0], walked = 1, turn = 0;
     const Sum one = {1.f, 0.f}, zero = {0.f, 0.f};
     Sum F = zero, W = one, Q = one;
     bool again = false;         // the last residual was empty: p instead
+    bool lost = false;          // a wait gave up
     if (tid == 0 && rank == 0) a.path[(size_t)b * a.n_max] = 0;
     for (;; ++turn) {
         if (warp == 0) {
             int ask = again ? kLast : kNone;
-            while (ask == kNone) {
+            while (ask == kNone && !lost) {
                 if (i >= n) {
                     ask = kLast;
                     break;
@@ -389,11 +417,12 @@ __global__ void __launch_bounds__(kThreads, 2) tree_sample_kernel(const SampleAr
                 todo.fl = less ? F.l : 0.f;
                 todo.gone = list;
                 todo.n_gone = gone;
-                what = ask;
+                what = lost ? kNone : ask;
                 steps = walked;
             }
         }
         __syncthreads();
+        if (what == kNone) break;
         const Residual r = todo;
         const bool last = what == kLast;
         const bool vec = a.vocab % 4 == 0 && ((reinterpret_cast<uintptr_t>(r.p) | reinterpret_cast<uintptr_t>(r.q)) & 15u) == 0;
@@ -403,18 +432,17 @@ __global__ void __launch_bounds__(kThreads, 2) tree_sample_kernel(const SampleAr
         if (lane == 0) of_warp[turn & 1][warp] = mine;
         __syncthreads();
         if (warp == 0) {
-            const Sum s = warp_total(lane < kWarps ? of_warp[turn & 1][lane] : Sum{0.f, 0.f});
-            if (lane == 0) of_cta[turn & 1] = s;
-        }
-        cluster_arrive();
-        cluster_wait();
-        if (warp == 0) {
-            const Sum part = lane < (int)ctas ? sum_of(&of_cta[turn & 1], lane) : Sum{0.f, 0.f};
-            const Sum upto = warp_upto(part);
-            W = from_lane(upto, 31);
+            const Sum own = warp_total(lane < kWarps ? of_warp[turn & 1][lane] : Sum{0.f, 0.f});
+            const uint32_t bar = smem_u32(bars + (turn & 1));
+            if (lane == 0) mbar_expect_tx(bar, ctas * (uint32_t)sizeof(Sum));
+            if (lane < (int)ctas) send(own, &of_cta[turn & 1][rank], bars + (turn & 1), lane);
+            // (a slot is written again two turns on, by a CTA that has had this one's sum of the turn between)
+            const bool there = __all_sync(0xffffffffu, receive(bar, (uint32_t)(turn >> 1) & 1u));
+            const Sum part = lane < (int)ctas ? of_cta[turn & 1][lane] : Sum{0.f, 0.f};
+            W = warp_total(part);
             W = settled(W.h, W.l);
-            int next = kGoOn;
-            if (last) {
+            int next = there ? kGoOn : kGaveUp;
+            if (last && there) {
                 if (!(W.h > 0.f) && !again && (r.q || r.n_gone)) {
                     again = true;
                 } else if (!(W.h > 0.f)) {
@@ -437,8 +465,10 @@ __global__ void __launch_bounds__(kThreads, 2) tree_sample_kernel(const SampleAr
                     }
                 }
             }
+            lost = !there;
             if (lane == 0) found = next;
         }
+        if (!last) continue;        // (the others wait for what is asked next)
         __syncthreads();
         if (found == kSearch) {
             const long long f0 = ((long long)rank * kWarps + from_warp) * a.part;
@@ -446,13 +476,18 @@ __global__ void __launch_bounds__(kThreads, 2) tree_sample_kernel(const SampleAr
         }
         if (found != kGoOn) break;
     }
+    if (what == kNone || found == kGaveUp) {
+        // no CTA ends while another may still send it its sum
+        if (tid == 0 && a.err) atomicOr(a.err, DFLARE_DEVERR_TIMEOUT);
+        if (tid == 0 && rank == 0) a.next_token[b] = -1;
+        cluster_arrive();
+        cluster_wait();
+    }
     if (rank == 0) {
         if (tid == 0) a.accept_len[b] = steps;
         for (int x = steps + tid; x < a.n_max; x += kThreads) a.path[(size_t)b * a.n_max + x] = -1;
     }
-    // no CTA ends while another may still read its sums
-    cluster_arrive();
-    cluster_wait();
+    // (a CTA that has had every other's sum of the last turn is sent no more)
 }
 
 // CTAs per tree: those that take the least time by a model of it, waves of clusters x (what a tree costs beside its rows, in elements of a
