@@ -106,7 +106,7 @@ typedef enum { DFLARE_BF16 = 0, DFLARE_F32 = 1 } dflare_dtype;
 #define DFLARE_DEVERR_TOKEN     0x1u    /* a token id outside [0, vocab) was read (clamped to 0) */
 #define DFLARE_DEVERR_CAPACITY  0x2u    /* ctx_len + n_new > max_ctx, or n_new outside [0, n_max]:
                                            that sequence appended nothing */
-#define DFLARE_DEVERR_TIMEOUT   0x4u    /* a pipeline wait inside a GEMM gave up (results invalid) */
+#define DFLARE_DEVERR_TIMEOUT   0x4u    /* a wait inside a kernel, of a GEMM's pipeline or a cluster, gave up (results invalid) */
 /* the same word of a paged cache (dflare_cache_error) and of the tree calls: TIMEOUT as above, CAPACITY
    when pages or room ran out, and */
 #define DFLARE_DEVERR_PAGE      0x8u    /* a sequence or page number out of range, a fork into a sequence
@@ -451,7 +451,7 @@ typedef struct {
     const void* dy;             /* backward only: the gradient with respect to the results */
     long long dy_row, dy_head;
     void* out;                  /* the results; backward: the gradient with respect to x. x or dy itself with the same strides will do */
-    long long out_row, out_head;
+    long long out_row, out_head;  /* no two heads overlap: one stride is at least what the other spans */
     const void* gain;           /* [head_dim] T */
     float* dgain;               /* backward only: [head_dim] fp32, written: the sum over rows and heads */
     int heads;                  /* 1..4096 */
@@ -675,7 +675,8 @@ dflare_status dflare_tree_accept(const int32_t* tokens_dev, const int32_t* paren
  *   vocab       1..2^28.
  * Sums over the vocabulary are good to 2^-40 of themselves, in the same order on every run. Probabilities that are negative or
  * not finite weigh nothing in them. A token outside [0, vocab) is not kept and sets DFLARE_DEVERR_TOKEN; a row that weighs nothing
- * gives token 0 and sets it too.
+ * gives token 0 and sets it too. A tree's walk is shared by a cluster of CTAs; a wait among them that gives up sets
+ * DFLARE_DEVERR_TIMEOUT, and the tree's next token is -1.
  */
 dflare_status dflare_tree_sample(const int32_t* tokens_dev, const int32_t* parents_dev, const int32_t* n_nodes_dev,
                                  const float* target_dev, const float* draft_dev, int draft_rows, const float* u_dev,

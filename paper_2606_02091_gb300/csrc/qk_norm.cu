@@ -657,6 +657,10 @@ const char* check_call(const dflare_qk_heads* q, const dflare_qk_heads* k, const
         if (p->x_row < 0 || p->x_head < 0 || p->out_row < 0 || p->out_head < 0 || (backward && (p->dy_row < 0 || p->dy_head < 0)) ||
             (rows > 1 && p->out_row < head_dim) || (p->heads > 1 && p->out_head < head_dim))
             return "strides must not be negative, nor overlap in out";
+        // (one of the two strides clears all that the other spans; in floating point, where strides of any size fit)
+        const double over_heads = (double)p->out_head * (p->heads - 1) + head_dim, over_rows = (double)p->out_row * (rows - 1) + head_dim;
+        if (rows > 1 && p->heads > 1 && (double)p->out_row < over_heads && (double)p->out_head < over_rows)
+            return "strides must not be negative, nor overlap in out";
         if (p->x == p->out && (p->x_row != p->out_row || p->x_head != p->out_head)) return "in place needs equal strides";
         if (backward && p->dy == p->out && (p->dy_row != p->out_row || p->dy_head != p->out_head)) return "in place needs equal strides";
         heads += p->heads;

@@ -385,6 +385,17 @@ def test_bad_arguments_are_refused(raw):
     assert raw.dflare_cache_append_normed(None, 0, None, 0, FAKE, 64, FAKE, 64, None, 0, None, FAKE, 1e-6, None, FAKE, 1, 1, None, 0, 0, 1.0, None) == E
 
 
+@pytest.mark.parametrize("rows,n,row,head", [(4, 2, 64, 64), (4, 2, 64, 128), (4, 2, 127, 64), (4, 2, 64, 255), (2, 3, 191, 64), (1 << 24, 4096, 4096, 64)])
+def test_results_that_overlap_are_refused(raw, rows, n, row, head):
+    # (4 rows span 3 * 64 + 64 = 256 elements, 2 heads 128, 3 heads 192)
+    for i in (0, 1):
+        args = [ctypes.byref(heads()), ctypes.byref(heads()), FAKE, FAKE, rows, 64, 64, 0, 1.0, 1e-6, 0, None]
+        args[i] = ctypes.byref(heads(heads=n, out_row=row, out_head=head))
+        assert raw.dflare_qk_norm_rope(*args) == _lib.DFLARE_EINVAL
+        assert b"overlap" in raw.dflare_last_error(None)
+        assert raw.dflare_qk_norm_rope_backward(*args[:10], FAKE, *args[10:]) == _lib.DFLARE_EINVAL
+
+
 def test_the_binding_keeps_to_one_device_and_refuses_wrong_tensors(monkeypatch):
     from paper_2606_02091_gb300 import paged
     lib = Taken()
