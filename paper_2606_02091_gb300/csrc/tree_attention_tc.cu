@@ -329,6 +329,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
             __syncwarp();
             if (lane == 0) mbar_arrive(qsent);
             q_there();
+            // qfull counts arrivals and not whose they are: without this a stream that has no tile of the first pair would go on to arrive for
+            // the second, and the first S could be computed before the other stream's part of Q is there. (A pair ends with the streams
+            // meeting, so its successor's Q is complete before one of them can arrive for a third; streams that do not alternate have a tile each.)
+            if (alternate(p)) streams_meet();
         }
         while (more) {
             const int n = p.hi - p.lo;

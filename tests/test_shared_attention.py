@@ -449,6 +449,40 @@ def test_steps_of_a_sampling_server(hq, hkv, hd, page, n, dtype):
             assert torch.equal(x, y)
 
 
+def test_the_streams_meet_before_one_of_them_goes_on_to_a_second_unit():
+    """A stream without a tile of the first unit would arrive twice at the barrier of the queries, which counts arrivals only. No run can
+    show that for certain, so this reads the source: between the first arrival and the loop over the units the streams meet."""
+    import os
+    import re
+    src = open(os.path.join(os.path.dirname(P.__file__), "csrc", "tree_attention_tc.cu")).read()
+    src = re.sub(r"//[^\n]*", "", src)
+    first, loop = src.index("q_there();"), src.index("while (more) {")
+    assert first < loop and re.search(r"if \(alternate\(p\)\) streams_meet\(\);", src[first:loop])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hd,nodes", [(128, 24), (64, 24), (64, 40)])
+def test_units_of_one_tile_one_after_another(hd, nodes):
+    """Single tokens with up to 128 keys of their own beside one tree: every CTA goes through several units of one tile, of which one
+    softmax stream has none, from its first on. Queries of one call must not show in the next one's."""
+    rng = np.random.default_rng(nodes + hd)
+    seqs = [(i // 8, 20, int(rng.integers(0, 120)), 1) for i in range(119)] + [(90, 0, 30, nodes)]
+    p = Shared(rng, seqs, hq=32, hkv=8, hd=hd, page=16, dtype="bf16")
+    mask, seen = tree_masks(rng, p.lens, p.counts, nodes)
+    work = p.cache.shared_work(len(seqs), nodes)
+    p.cache.share_plan(i32(p.counts), nodes, work)
+    for _ in range(4):
+        q = queries(rng, p, len(seqs), nodes)
+        want, _, bound, _ = attend_reference(p, host(q), seen, hd ** -0.5)
+        shared, plain = torch.empty_like(q), torch.empty_like(q)
+        p.cache.attend_shared(0, q, shared, work, mask=mask)
+        p.cache.attend(0, q, i32(p.counts), plain, mask=mask)
+        for out in (shared, plain):
+            off = np.abs(host(out) - want) - bound
+            assert not (off > 1e-30).any() and not np.isnan(off).any(), off.max()
+    assert p.cache.error() == 0
+
+
 # ------------------------------------------------------------------------------------------ refusals (host)
 
 @pytest.fixture(scope="module")
