@@ -594,8 +594,8 @@ dflare_status dflare_cache_attend(dflare_cache* cache, int layer, const void* q_
  *   dflare_cache_attend_shared  as dflare_cache_attend, with the node counts and lengths of the plan.
  * A plan holds until the lengths, the pages or the node counts change; what a call with an older one computes is that of
  * the plan's lengths over the pages that the tables then name. A workspace without a plan for the call's batch and n_max,
- * and a cache of these sizes, sets DFLARE_DEVERR_PLAN, and nothing is written.
- *   work_dev  dflare_cache_shared_bytes bytes, 128-byte aligned, zero before its first plan; for one plan and the calls that
+ * and a cache of this type and these sizes, sets DFLARE_DEVERR_PLAN, and nothing is written.
+ *   work_dev  as many bytes as dflare_cache_shared_bytes gives for the call's own cache, batch and n_max, 128-byte aligned, zero before its first plan; for one plan and the calls that
  *             follow it at a time. Calls with a batch, n_max and cache so large that the list of work would not fit 31 bits are refused.
  */
 dflare_status dflare_cache_shared_bytes(dflare_cache* cache, int batch, int n_max, size_t* bytes);

@@ -63,9 +63,11 @@ struct __align__(16) TreeSeq {
     int row, lead_row;   // rows of whole units among the partial results: of kv head 0 (lead_row: of the group's row 0)
     int weight, lead_weight;    // cost of a tile
 };
+// The type and head_dim of a plan's cache, on which its lists of work and the places of everything in the workspace depend; never 0.
+inline int plan_kind(const dflare_cache_config& g) { return 1 | (int)g.dtype << 1 | g.head_dim << 2; }
 // The head of an attend_shared workspace.
 struct __align__(16) SharedHead {
-    int ok, batch, n_max, max_pages, hkv, ps, G;        // what the plan was made for
+    int kind, batch, n_max, max_pages, hkv, ps, G;      // what the plan was made for (kind: plan_kind)
     int per[2];                                         // length of a CTA's run in each list of work
 };
 // One kernel's list of work: log2 of its rows per block and keys per tile, its CTAs, what a tile of up to 128 rows and one of more costs, and
@@ -92,6 +94,7 @@ struct TreeArgs {
     float scale_log2;
     // attend_shared
     const SharedHead* head;
+    int kind;                  // of the plan that it must hold
     const int2* runs;          // [C]: the first and the last item of a CTA, plus one
     const TreeItem* items;
     const int32_t* map;        // query rows of the groups' nodes

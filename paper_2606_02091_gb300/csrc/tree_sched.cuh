@@ -198,11 +198,11 @@ __device__ __forceinline__ bool tree_pair(const TreeArgs& a, const int32_t*, int
     for (int i = 0; i < (int)(sizeof(TreeItem) / 16); ++i) to[i] = __ldg(from + i);
     return true;
 }
-// Whether a workspace holds a plan for this call's sizes, and a cache's: every number in it then fits.
+// Whether a workspace holds a plan for this call's sizes, and a cache's of this type and these sizes: every number in it then fits.
 __device__ __forceinline__ bool plan_fits(const TreeArgs& a) {
     const int4* head = reinterpret_cast<const int4*>(a.head);
     const int4 x = head[0], y = head[1];        // (all of it in one trip)
-    return ((x.x ^ 1) | (x.y ^ a.batch) | (x.z ^ a.n_max) | (x.w ^ a.pg.max_pages) | (y.x ^ a.pg.hkv) | (y.y ^ a.pg.ps) | (y.z ^ a.G)) == 0;
+    return ((x.x ^ a.kind) | (x.y ^ a.batch) | (x.z ^ a.n_max) | (x.w ^ a.pg.max_pages) | (y.x ^ a.pg.hkv) | (y.y ^ a.pg.ps) | (y.z ^ a.G)) == 0;
 }
 // This CTA's items; false (and reported) where there is no such plan.
 __device__ __forceinline__ bool tree_items(const TreeArgs& a, int& v, int& v1) {

@@ -119,6 +119,7 @@ struct PlanArgs {
     PagesView pg;
     const int32_t* n_nodes;
     SharedHead* head;
+    int kind;
     int2* runs[2];
     TreeItem* items[2];
     int32_t* map;
@@ -488,7 +489,7 @@ __global__ void __launch_bounds__(kPlanThreads) tree_shared_plan_kernel(const __
     }
     __syncthreads();
     if (tid == 0) {
-        a.head->ok = 1;
+        a.head->kind = a.kind;
         a.head->batch = a.batch;
         a.head->n_max = a.n_max;
         a.head->max_pages = a.pg.max_pages;
@@ -768,6 +769,7 @@ dflare_status dflare_cache_share_plan(dflare_cache* c, const int32_t* n_nodes_de
     a.pg = c->view;
     a.n_nodes = n_nodes_dev;
     a.head = reinterpret_cast<SharedHead*>(work);
+    a.kind = plan_kind(c->cfg);
     for (int l = 0; l < y.work.many; ++l) {
         a.runs[l] = reinterpret_cast<int2*>(work + y.runs[l]);
         a.items[l] = reinterpret_cast<TreeItem*>(work + y.items[l]);
@@ -825,6 +827,7 @@ dflare_status dflare_cache_attend_shared(dflare_cache* c, int layer, const void*
     a.QG = 1;
     a.scale_log2 = scale * 1.4426950408889634f;
     a.head = reinterpret_cast<const SharedHead*>(work);
+    a.kind = plan_kind(g);
     a.map = reinterpret_cast<const int32_t*>(work + y.map);
     a.seqs = reinterpret_cast<const TreeSeq*>(work + y.seqs);
     a.own_rows = y.own_rows;

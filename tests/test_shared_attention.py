@@ -344,6 +344,32 @@ def test_a_workspace_without_the_plan_is_reported_and_nothing_written():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("batch,n,hkv", [(2, 2, 2), (6, 8, 4), (80, 1, 2)])      # (bf16: few rows, many, a list each for own and shared keys)
+@pytest.mark.parametrize("dtype,hd", [("bf16", 64), ("bf16", 128), ("f32", 64), ("f32", 128)])
+def test_a_plan_of_another_type_or_head_size_is_reported(dtype, hd, batch, n, hkv):
+    """The lists of work, and where everything lies, go by them: a plan of another kind of cache is not used, either way round."""
+    rng = np.random.default_rng(15)
+    make = lambda t, d: Shared(rng, [(0, 40, 3, n)] * batch, hq=2 * hkv, hkv=hkv, hd=d, page=16, dtype=t, nodes=n)     # noqa: E731
+    p = make(dtype, hd)
+    q = queries(rng, p, batch, n)
+    out, need = torch.full_like(q, 7.0), p.cache.shared_work(batch, n).numel()
+    for t, d in (("bf16", 64), ("bf16", 128), ("f32", 64), ("f32", 128)):
+        if (t, d) == (dtype, hd):
+            continue
+        other = make(t, d)
+        more = other.cache.shared_work(batch, n)
+        other.cache.share_plan(i32(other.counts), n, more)
+        room = torch.zeros(max(more.numel(), need), dtype=torch.uint8, device="cuda")
+        room[:more.numel()] = more
+        p.cache.attend_shared(0, q, out, room)
+        assert p.cache.error() == _lib.DEVERR_PLAN and (out == 7).all(), (t, d)
+        p.cache.share_plan(i32(p.counts), n, room)
+        p.cache.attend_shared(0, q, out, room)
+        assert p.cache.error() == 0 and not (out == 7).any()
+        out.fill_(7.0)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_pages_that_do_not_exist_and_pages_that_are_missing(dtype):
     """A shared page number that does not exist ends the shared part; its keys read as zeros and it is reported, as without
