@@ -95,6 +95,8 @@ __device__ __forceinline__ Sum over(const Sum& a, const Sum& b) {
     return settled(q, __fmul_rn(rest, inv));
 }
 __device__ __forceinline__ bool above(const Sum& a, const Sum& b) { return __fadd_rn(__fsub_rn(a.h, b.h), __fsub_rn(a.l, b.l)) > 0.f; }
+// (what is left of p by less than half a step of it lies in `l` alone)
+__device__ __forceinline__ bool weighs(const Sum& s) { return __fadd_rn(s.h, s.l) > 0.f; }
 __device__ __forceinline__ Sum from_lane(const Sum& s, int lane) { return {__shfl_sync(0xffffffffu, s.h, lane), __shfl_sync(0xffffffffu, s.l, lane)}; }
 // Of parts that lie one after another behind `base`, one per lane of the first `many`: the first at which the running sum passes
 // goal (where rounding hides it, the last with any weight), and base is moved up to it.
@@ -103,7 +105,7 @@ __device__ __forceinline__ int part_of(const Sum& part, int many, const Sum& goa
     const Sum upto = warp_upto(part);
     Sum x = base;
     add(x, upto.h, upto.l);
-    const unsigned past = __ballot_sync(0xffffffffu, lane < many && above(x, goal)), some = __ballot_sync(0xffffffffu, lane < many && part.h > 0.f);
+    const unsigned past = __ballot_sync(0xffffffffu, lane < many && above(x, goal)), some = __ballot_sync(0xffffffffu, lane < many && weighs(part));
     const int at = past ? __ffs(past) - 1 : max(31 - __clz(some), 0);
     const Sum before = from_lane(x, max(at - 1, 0));
     if (at) base = before;
@@ -127,7 +129,7 @@ __device__ __forceinline__ Sum left_of(float p, float q, float fh, float fl) {
 // w = max(0, p - F q) added to s; not finite or negative: nothing
 __device__ __forceinline__ void add_weight(Sum& s, const Residual& r, float p, float q) {
     const Sum w = left_of(p, q, r.fh, r.fl);
-    if (__fadd_rn(w.h, w.l) > 0.f) add(s, w.h, w.l);
+    if (weighs(w)) add(s, w.h, w.l);
 }
 __device__ __forceinline__ void add_plain(Sum& s, float p) { add(s, p > 0.f && p < INFINITY ? p : 0.f, 0.f); }
 __device__ __forceinline__ bool is_gone(const Residual& r, int e) {
@@ -258,7 +260,7 @@ __device__ __forceinline__ void find_token(const Residual& r, int s0, int s1, Su
             const int e = e0 + i * 32 + lane;
             Sum w = {0.f, 0.f};
             if (e < end && !is_gone(r, e)) add_weight(w, r, p[i], q[i]);
-            const unsigned some = __ballot_sync(0xffffffffu, w.h > 0.f);
+            const unsigned some = __ballot_sync(0xffffffffu, weighs(w));
             if (!some) continue;
             const Sum upto = warp_upto(w);
             Sum x = base;

@@ -167,6 +167,28 @@ def test_random_numbers_at_the_ends_of_their_range(mode):
 
 
 @pytest.mark.gpu
+def test_many_rejected_siblings_leave_the_token_that_the_target_prefers():
+    """Token 20 has the only p above q, and up to 40 drafts of others are rejected: the residual is token 20's, smaller each time,
+    down to less than half a step of p and to nothing, where p counts and u_0 = 1/4 is token 20's again."""
+    rng = np.random.default_rng(16)
+    vocab, n = 64, 41
+    counts = np.tile(np.arange(2, n + 1), 25)
+    batch = len(counts)
+    p, q = np.zeros((batch, n, vocab), np.float32), np.zeros((batch, n, vocab), np.float32)
+    qx = rng.uniform(0.3, 0.95, batch)
+    px = qx * (1 + (1 / qx - 1) * rng.uniform(0.01, 0.99, batch))
+    p[:, 0, 20], q[:, 0, 20] = px, qx
+    p[:, 0, 41:49], q[:, 0, 41:49] = (1 - px[:, None]) / 8, (1 - qx[:, None]) / 8
+    tokens, parents = np.tile(41 + np.arange(n, dtype=np.int32) % 8, (batch, 1)), np.zeros((batch, n), np.int32)
+    parents[:, 0] = -1
+    u = np.full((batch, n), 1 - 2.0 ** -24, np.float32)
+    u[:, 0] = 0.25
+    accept, path, following, err = call(tokens, parents, counts, p, q, u, "drawn")
+    assert err == 0 and (accept == 1).all() and (path[:, 1:] == -1).all()
+    assert (following == 20).all(), sorted(set(zip(following[following != 20].tolist(), counts[following != 20].tolist())))[:8]
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("mode", MODES)
 def test_every_token_has_the_targets_distribution(mode):
     """65535 trees of one kind: how often each pair (first token, second token) follows the root, against the target's
