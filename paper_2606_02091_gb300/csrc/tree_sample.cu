@@ -98,14 +98,15 @@ __device__ __forceinline__ bool above(const Sum& a, const Sum& b) { return __fad
 // (what is left of p by less than half a step of it lies in `l` alone)
 __device__ __forceinline__ bool weighs(const Sum& s) { return __fadd_rn(s.h, s.l) > 0.f; }
 __device__ __forceinline__ Sum from_lane(const Sum& s, int lane) { return {__shfl_sync(0xffffffffu, s.h, lane), __shfl_sync(0xffffffffu, s.l, lane)}; }
-// Of parts that lie one after another behind `base`, one per lane of the first `many`: the first at which the running sum passes
-// goal (where rounding hides it, the last with any weight), and base is moved up to it.
+// Of parts that lie one after another behind `base`, one per lane of the first `many`: the first with any weight at which the running
+// sum passes goal (where rounding hides it, the last with any), and base is moved up to it. Neighbouring running sums add up
+// in different orders, so that the one behind a part without weight may be larger in its last bits.
 __device__ __forceinline__ int part_of(const Sum& part, int many, const Sum& goal, Sum& base) {
     const int lane = threadIdx.x & 31;
     const Sum upto = warp_upto(part);
     Sum x = base;
     add(x, upto.h, upto.l);
-    const unsigned past = __ballot_sync(0xffffffffu, lane < many && above(x, goal)), some = __ballot_sync(0xffffffffu, lane < many && weighs(part));
+    const unsigned some = __ballot_sync(0xffffffffu, lane < many && weighs(part)), past = __ballot_sync(0xffffffffu, above(x, goal)) & some;
     const int at = past ? __ffs(past) - 1 : max(31 - __clz(some), 0);
     const Sum before = from_lane(x, max(at - 1, 0));
     if (at) base = before;

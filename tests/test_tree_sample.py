@@ -167,6 +167,30 @@ def test_random_numbers_at_the_ends_of_their_range(mode):
 
 
 @pytest.mark.gpu
+def test_a_run_of_weightless_tokens_where_the_sum_is_reached():
+    """u_0 = 1/2, and the weight before a run of zeros is within 2^-46 of that behind it, on either side: the token before the run or
+    the one behind it, by the rounding of running sums (2^-40), but none of the run, nor token 0, which weighs nothing either."""
+    rng = np.random.default_rng(15)
+    batch, vocab = 6000, 64
+    p, ends = np.zeros((batch, 1, vocab), np.float32), []
+    for b in range(batch):
+        k = int(rng.integers(2, 14))        # the run: 4 k .. 4 k + 3
+        p[b, 0, 1:4 * k] = np.ldexp((2 ** 23 + rng.integers(0, 2 ** 23, 4 * k - 1)).astype(np.float64), -28 - rng.integers(0, 30, 4 * k - 1))
+        rest, at = math.fsum(p[b, 0].tolist()) * (1 + (int(rng.integers(0, 33)) - 16) * 2.0 ** -51), 4 * k + 4
+        while rest > 0 and at < min(4 * k + 8, vocab):
+            v = np.float32(rest)
+            p[b, 0, at] = v if v <= rest else np.nextafter(v, np.float32(0))
+            rest -= float(p[b, 0, at])
+            at += 1
+        ends.append((4 * k - 1, 4 * k + 4))
+    zero = np.zeros((batch, 1), np.int32)
+    accept, path, following, err = call(zero, zero - 1, [1] * batch, p, p, np.full((batch, 1), 0.5, np.float32), "picked")
+    assert err == 0 and (accept == 1).all() and (path == 0).all()
+    missed = [(b, int(x)) for b, (x, e) in enumerate(zip(following, ends)) if x not in e]
+    assert not missed, (len(missed), missed[:5])
+
+
+@pytest.mark.gpu
 def test_many_rejected_siblings_leave_the_token_that_the_target_prefers():
     """Token 20 has the only p above q, and up to 40 drafts of others are rejected: the residual is token 20's, smaller each time,
     down to less than half a step of p and to nothing, where p counts and u_0 = 1/4 is token 20's again."""
