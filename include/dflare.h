@@ -675,8 +675,8 @@ dflare_status dflare_tree_accept(const int32_t* tokens_dev, const int32_t* paren
  *   vocab       1..2^28.
  * Sums over the vocabulary are good to 2^-40 of themselves, in the same order on every run. Probabilities that are negative or
  * not finite weigh nothing in them. A token outside [0, vocab) is not kept and sets DFLARE_DEVERR_TOKEN; a row that weighs nothing
- * gives token 0 and sets it too. A tree's walk is shared by a cluster of CTAs; a wait among them that gives up sets
- * DFLARE_DEVERR_TIMEOUT, and the tree's next token is -1.
+ * gives token 0 and sets it too. A tree's walk is shared by a cluster of CTAs; where a wait among them gives up,
+ * DFLARE_DEVERR_TIMEOUT is set, and the tree has what one without nodes has: accepted length 0, path and next token -1.
  */
 dflare_status dflare_tree_sample(const int32_t* tokens_dev, const int32_t* parents_dev, const int32_t* n_nodes_dev,
                                  const float* target_dev, const float* draft_dev, int draft_rows, const float* u_dev,

@@ -479,16 +479,23 @@ __global__ void __launch_bounds__(kThreads, 2) tree_sample_kernel(const SampleAr
         }
         if (found != kGoOn) break;
     }
-    if (what == kNone || found == kGaveUp) {
-        // no CTA ends while another may still send it its sum
-        if (tid == 0 && a.err) atomicOr(a.err, DFLARE_DEVERR_TIMEOUT);
-        if (tid == 0 && rank == 0) a.next_token[b] = -1;
-        cluster_arrive();
-        cluster_wait();
-    }
-    if (rank == 0) {
+    const bool gave_up = what == kNone || found == kGaveUp;
+    if (rank == 0 && !gave_up) {
         if (tid == 0) a.accept_len[b] = steps;
         for (int x = steps + tid; x < a.n_max; x += kThreads) a.path[(size_t)b * a.n_max + x] = -1;
+    }
+    __syncwarp();
+    cluster_arrive();       // (what it has stored lies behind this)
+    if (gave_up) {
+        // No CTA that gave up ends while another may still send it its sum. Others may have had all of theirs and
+        // stored a walk and a token: the tree has none, whichever CTA it was.
+        cluster_wait();
+        if (tid == 0) {
+            if (a.err) atomicOr(a.err, DFLARE_DEVERR_TIMEOUT);
+            a.accept_len[b] = 0;
+            a.next_token[b] = -1;
+        }
+        for (int x = tid; x < a.n_max; x += kThreads) a.path[(size_t)b * a.n_max + x] = -1;
     }
     // (a CTA that has had every other's sum of the last turn is sent no more)
 }

@@ -376,6 +376,23 @@ def test_on_another_stream_and_in_a_graph():
         assert all(np.array_equal(a, b.cpu().numpy()) for a, b in zip(want[k], out))
 
 
+def test_whichever_cta_gives_up_the_tree_has_no_result():
+    """A wait among a tree's CTAs may give up in one of them and not in the others, which then store a walk and a token. No call makes a
+    wait give up, so this reads the source: every CTA stores its results, then arrives at the cluster's last barrier; those that
+    gave up wait there for all of them, and then store that there is no result, whatever their rank."""
+    import os
+    import re
+    src = open(os.path.join(os.path.dirname(P.__file__), "csrc", "tree_sample.cu")).read()
+    src = re.sub(r"//[^\n]*", "", src)
+    end = src[src.index("const bool gave_up"):src.index("constexpr int kTreeCost")]
+    results, last = end[:end.index("cluster_arrive();")], end[end.index("cluster_arrive();"):]
+    assert "if (rank == 0 && !gave_up)" in results and "a.accept_len[b] = steps;" in results and "cluster_wait" not in results
+    after = last[last.index("if (gave_up) {"):]
+    assert "steps" not in last and "rank" not in last and last.index("cluster_arrive();") < last.index("if (gave_up) {")
+    where = [after.index(x) for x in ("cluster_wait();", "DFLARE_DEVERR_TIMEOUT", "a.accept_len[b] = 0;", "a.next_token[b] = -1;", "a.path[")]
+    assert where == sorted(where)
+
+
 # ------------------------------------------------------------------------------------------ refusals (host)
 
 @pytest.fixture(scope="module")
