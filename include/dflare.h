@@ -673,8 +673,8 @@ dflare_status dflare_tree_accept(const int32_t* tokens_dev, const int32_t* paren
  *               token is drawn from p without the children's tokens.
  *   u_dev       [batch][n_max] fp32, uniform in [0, 1); other values count as the nearest number of that range, NaN as 0.
  *   vocab       1..2^28.
- * Sums over the vocabulary are good to 2^-40 of themselves, in the same order on every run. Probabilities that are negative or
- * not finite weigh nothing in them. A token outside [0, vocab) is not kept and sets DFLARE_DEVERR_TOKEN; a row that weighs nothing
+ * Sums over the vocabulary are good to 2^-40 of themselves, in the same order on every run. Probabilities, of either, that
+ * are negative or not finite count as 0. A token outside [0, vocab) is not kept and sets DFLARE_DEVERR_TOKEN; a row that weighs nothing
  * gives token 0 and sets it too. A tree's walk is shared by a cluster of CTAs; where a wait among them gives up,
  * DFLARE_DEVERR_TIMEOUT is set, and the tree has what one without nodes has: accepted length 0, path and next token -1.
  */

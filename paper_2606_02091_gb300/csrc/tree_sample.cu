@@ -121,18 +121,20 @@ struct Residual {
     const int32_t* gone;
     int n_gone;
 };
+// A probability that is negative or not finite counts as 0 (as whole numbers, those, with a sign or all of the exponent, are the larger).
+__device__ __forceinline__ float counted(float x) { return __float_as_uint(x) < 0x7f800000u ? x : 0.f; }
 // p - F q as two numbers where it is positive: there p >= F q in fp32 too, so that the difference's rounding is two subtractions
 __device__ __forceinline__ Sum left_of(float p, float q, float fh, float fl) {
     const float ph = __fmul_rn(fh, q), pl = __fmaf_rn(fl, q, __fmaf_rn(fh, q, -ph));
     const float d = __fsub_rn(p, ph);
     return {d, __fsub_rn(__fsub_rn(__fsub_rn(p, d), ph), pl)};
 }
-// w = max(0, p - F q) added to s; not finite or negative: nothing
+// w = max(0, p - F q) added to s (p not finite: w is NaN, and adds nothing)
 __device__ __forceinline__ void add_weight(Sum& s, const Residual& r, float p, float q) {
-    const Sum w = left_of(p, q, r.fh, r.fl);
+    const Sum w = left_of(p, counted(q), r.fh, r.fl);
     if (weighs(w)) add(s, w.h, w.l);
 }
-__device__ __forceinline__ void add_plain(Sum& s, float p) { add(s, p > 0.f && p < INFINITY ? p : 0.f, 0.f); }
+__device__ __forceinline__ void add_plain(Sum& s, float p) { add(s, counted(p), 0.f); }
 __device__ __forceinline__ bool is_gone(const Residual& r, int e) {
     for (int g = 0; g < r.n_gone; ++g)
         if (r.gone[g] == e) return true;
@@ -311,8 +313,8 @@ __global__ void __launch_bounds__(kThreads, 2) tree_sample_kernel(const SampleAr
         const float r = a.u[(size_t)b * a.n_max + i];
         const bool in = x >= 0 && x < a.vocab, wrong = i == 0 ? p != -1 : (p < -1 || p >= i);
         if (wrong) p = -1;
-        px[i] = p >= 0 && in ? target[(size_t)p * a.vocab + x] : 0.f;
-        qx[i] = p >= 0 && in && draft ? draft[(size_t)p * a.vocab + x] : 0.f;
+        px[i] = p >= 0 && in ? counted(target[(size_t)p * a.vocab + x]) : 0.f;
+        qx[i] = p >= 0 && in && draft ? counted(draft[(size_t)p * a.vocab + x]) : 0.f;
         up[i] = i < told ? p : -1;
         tok[i] = in ? x : -1;
         u[i] = r > 0.f ? fminf(r, 0x1.fffffep-1f) : 0.f;

@@ -286,6 +286,30 @@ def test_values_that_weigh_nothing(mode):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("vocab", [1000, 3001])
+def test_probabilities_that_are_none_count_as_zero(vocab, mode):
+    """Infinities, NaN and negative values in either's rows, of drafted tokens too: the walk of the rows with zeros there."""
+    rng = np.random.default_rng(vocab)
+    batch, n = 60, 7
+    tokens, parents, p, q, u = make(rng, batch, n, vocab, mode, 4)
+    u[:, 1:] = np.maximum(u[:, 1:], rng.random((batch, n - 1)).astype(np.float32))      # more rejections, and so more sums
+    odd = np.array([math.inf, -math.inf, math.nan, -1.0, -1e-3, -0.0], np.float32)
+    clean = [p.copy(), q.copy()]
+    for x, c in zip((p, q), clean):
+        spots = rng.random(x.shape) < 0.05
+        for b in range(batch):
+            for i in range(1, n):
+                spots[b, parents[b, i], tokens[b, i]] = rng.random() < 0.3
+        c[spots] = 0.0
+        x[spots] = rng.choice(odd, spots.sum())
+    want = call(tokens, parents, [n] * batch, *clean, u, mode)
+    got = call(tokens, parents, [n] * batch, p, q, u, mode)
+    assert want[3] == 0 and all(np.array_equal(a, b) for a, b in zip(want, got))
+    check(tokens, parents, [n] * batch, *clean, u, mode)
+
+
+@pytest.mark.gpu
 def test_what_cannot_be_is_reported():
     rng = np.random.default_rng(9)
     tokens, parents, p, q, u = make(rng, 5, 6, 50, "drawn", 2)
