@@ -464,7 +464,8 @@ typedef struct {
  * The root-mean-square norm of every head with the rotary embedding in the same pass: z = gain x / sqrt(mean(x^2) + eps)
  * over a head's elements, then the pairs of its first rot_dim elements turned and scaled as in dflare_rope (rot_dim = 0:
  * none; phase_dev and positions_dev may then be NULL). In fp32, rounded once.
- *   q, k      the query heads, and the key heads or NULL: one call for both, each with its own gain.
+ *   q, k      the query heads, and the key heads or NULL: one call for both, each with its own gain. What is written for one must not
+ *             overlap anything of the other (a gain that both share has two gradients, to be added up); equal addresses are refused.
  *   head_dim  2..1024; eps at least 0.
  * Fast where pointers are 16-byte aligned, strides multiples of 8, rot_dim and head_dim multiples of 16 and head_dim
  * at most 512.

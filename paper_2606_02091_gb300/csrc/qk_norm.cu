@@ -666,6 +666,12 @@ const char* check_call(const dflare_qk_heads* q, const dflare_qk_heads* k, const
         heads += p->heads;
     }
     if ((long long)rows * heads * 32 / kThreads > 0x7ffffff0LL) return "too many heads";
+    if (q && k) {       // (both are worked on at the same time)
+        if (q->out == k->out || q->out == k->x || k->out == q->x || (backward && (q->out == k->dy || k->out == q->dy)))
+            return "queries and keys must not overlap where one is written";
+        const uintptr_t a = reinterpret_cast<uintptr_t>(q->dgain), b = reinterpret_cast<uintptr_t>(k->dgain);
+        if (backward && (a > b ? a - b : b - a) < head_dim * sizeof(float)) return "the gradients of the gains must not overlap";
+    }
     return nullptr;
 }
 

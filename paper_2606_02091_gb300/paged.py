@@ -213,7 +213,8 @@ def qk_norm_rope_work(head_dim, device="cuda"):
 def qk_norm_rope_backward(q, k, dq_out, dk_out, positions, phase, q_gain, k_gain, dq, dk, dq_gain, dk_gain, work, *, eps=1e-6,
                           layout="half", magnitude=1.0, stream=None):
     """The gradients of qk_norm_rope from its arguments q and k and the gradients dq_out and dk_out of its results: dq
-    and dk (dq_out and dk_out themselves: in place), and dq_gain and dk_gain (fp32 [head_dim], overwritten)."""
+    and dk (dq_out and dk_out themselves: in place), and dq_gain and dk_gain (fp32 [head_dim], overwritten; two tensors, of
+    a gain that queries and keys share too)."""
     dev = _current()
     pos, ph, rows, hd, rot, lay = _qk_call(q, k, positions, phase, layout, dev)
     qs = _qk_part("q", q, dq_out, dq, q_gain, dq_gain, rows, hd, q.dtype, dev)

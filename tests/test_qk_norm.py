@@ -396,6 +396,28 @@ def test_results_that_overlap_are_refused(raw, rows, n, row, head):
         assert raw.dflare_qk_norm_rope_backward(*args[:10], FAKE, *args[10:]) == _lib.DFLARE_EINVAL
 
 
+def test_results_of_queries_and_keys_that_overlap_are_refused(raw):
+    """Both are worked on at the same time: a place that is written for one is nothing of the other's, and a gain that both share has
+    two gradients."""
+    key = dict(x=1 << 20, dy=2 << 20, out=3 << 20, dgain=4096)
+
+    def said(q, k, backward):
+        args = [ctypes.byref(heads(**q)), ctypes.byref(heads(**dict(key, **k))), FAKE, FAKE, 4, 64, 64, 0, 1.0, 1e-6, 0, None]
+        call = raw.dflare_qk_norm_rope_backward if backward else raw.dflare_qk_norm_rope
+        # (without a workspace the backward call is refused, but for what is asked before that)
+        assert call(*(args[:10] + [None] + args[10:] if backward else args)) == _lib.DFLARE_EINVAL
+        return raw.dflare_last_error(None)
+
+    for q, k in (({}, dict(out=8192)), ({}, dict(x=8192)), (dict(x=3 << 20), {})):
+        for backward in (False, True):
+            assert b"overlap" in said(q, k, backward), (q, k)
+    for q, k in (({}, dict(dy=8192)), (dict(dy=3 << 20), {}), ({}, dict(dgain=256)), ({}, dict(dgain=256 + 252)), (dict(dgain=4096 + 252), {})):
+        assert b"overlap" in said(q, k, True), (q, k)
+    # parts of one projection's rows, in place, and gradients side by side
+    for q, k in (({}, {}), (dict(x=1 << 16, out=1 << 16), dict(x=(1 << 16) + 128, out=(1 << 16) + 128)), ({}, dict(dgain=256 + 256))):
+        assert b"NULL" in said(q, k, True), (q, k)
+
+
 def test_the_binding_keeps_to_one_device_and_refuses_wrong_tensors(monkeypatch):
     from paper_2606_02091_gb300 import paged
     lib = Taken()
