@@ -318,6 +318,87 @@ def test_on_another_stream_in_graphs_and_with_two_workspaces(n, more, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n,more,dtype", [(6, 0, "bf16"), (3, 38, "bf16"), (9, 8, "bf16"), (3, 0, "f32")])       # (each of the kernels, and two together)
+def test_a_replayed_plan_goes_by_the_lengths_that_it_finds(n, more, dtype):
+    """The plan and the attention in one graph: after the lengths change a replay gives the bits of the plain calls at the new lengths,
+    which are those of the definition, and not the ones before."""
+    rng = np.random.default_rng(17)
+    seqs = [(0, 80, 30, n), (0, 80, 9, n), (1, 20, 4, n), (1, 20, 33, n)] + [(2 + i // 8, 30, 5 + 7 * i, n) for i in range(more)]
+    batch = len(seqs)
+    p = Shared(rng, seqs, hq=16, hkv=4, hd=128, page=16, dtype=dtype)
+    mask, seen = tree_masks(rng, p.lens, p.counts, n)
+    q, out, counts, work = queries(rng, p, batch, n), torch.zeros((batch, n, 16, 128), dtype=p.t, device="cuda"), i32(p.counts), p.cache.shared_work(batch, n)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        p.cache.share_plan(counts, n, work)
+        p.cache.attend_shared(0, q, out, work, mask=mask)
+    g.replay()
+    before = out.clone()
+    p.cache.lens.sub_(4)        # (of which some share a page less)
+    p.lens = [x - 4 for x in p.lens]
+    g.replay()
+    a = [s[:, 4:] for s in seen]        # four tokens of the context less: node j's key is where node j - 4's was
+    want, _, bound, _ = attend_reference(p, host(q), a, p.hd ** -0.5)
+    off = np.abs(host(out) - want) - bound
+    assert p.cache.error() == 0 and not (off > 1e-30).any() and not np.isnan(off).any(), off.max()
+    # (of the four keys that are gone the heaviest, for the row and head that give it most, has several times the bound: of 1300 keys a weight
+    # of e^3 / 1300 / e^0.5 = 0.009 and more for one of 48 rows and heads, and the bound is 2 2^-8 of the mean |v|, 0.006)
+    assert (np.abs(host(before) - want) > bound).any((1, 2, 3)).all()
+    fresh = torch.zeros_like(out)
+    p.cache.attend_shared(0, q, fresh, work, mask=mask)
+    assert torch.equal(fresh, out)
+    again, _, _ = run_shared(p, q, mask)
+    assert torch.equal(again, out)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv,hd,page,n", [(4, 2, 64, 16, 7), (32, 4, 128, 32, 12)])
+def test_a_forked_cache_against_the_definition(hq, hkv, hd, page, n, dtype):
+    """Steps of sampled trees over forked sequences, each layer's attention against the definition over the keys that the tables name, within the
+    bound of a result's own arithmetic."""
+    rng = np.random.default_rng(18 + n)
+    layers, batch = 2, 5
+    t = torch.float32 if dtype == "f32" else torch.bfloat16
+    make = lambda *s: torch.from_numpy(rng.standard_normal(s).astype(np.float32)).to(t).cuda()     # noqa: E731
+    c = P.PagedCache.allocate(n_layers=layers, n_pages=300, page_size=page, n_q_heads=hq, n_kv_heads=hkv, head_dim=hd, max_batch=batch, max_pages=60,
+                              max_nodes=n, dtype=dtype)
+    lens = i32([page * 22 + 3, 0, 0, page * 25, 0])
+    c.reserve(lens)
+    most = page * 25
+    for layer in range(layers):
+        c.append(layer, None, make(batch, most, hkv, hd), make(batch, most, hkv, hd), lens, None, None)
+    c.commit(lens, i32(np.tile(np.arange(most), (batch, 1))))
+    c.fork(i32([0, 0, 3]), i32([1, 2, 4]))
+    work, groups = c.shared_work(batch, n), torch.zeros((batch, 2), dtype=torch.int32, device="cuda")
+    for step in range(3):
+        counts = [int(x) for x in rng.integers(1, n + 1, batch)]
+        parents = np.stack([random_parents(rng, n, 3) for _ in range(batch)])
+        nodes = i32(counts)
+        mask, depth = torch.zeros((batch, n, up(n, 32)), dtype=torch.int32, device="cuda"), torch.zeros((batch, n), dtype=torch.int32, device="cuda")
+        P.tree_plan(i32(parents), nodes, mask, depth)
+        c.reserve(nodes)
+        c.share_plan(nodes, n, work, groups=groups)
+        most, of = best_saving(c.lens.tolist(), counts, c.table.cpu().numpy(), page, hq // hkv)
+        assert of(groups.cpu().numpy()) == most     # (where a member costs more than it saves it is by itself)
+        view = SimpleNamespace(lens=c.lens.tolist(), counts=counts, page=page, hq=hq, hkv=hkv, hd=hd, table=c.table.cpu().numpy(), k=c.k, v=c.v, t=t)
+        view.rows = lambda pool, b, layer=0: Paged.rows(view, pool, b, layer)     # noqa: B023
+        seen = [np.concatenate([np.ones((n, x), bool), ancestors(par)[:, :m]], 1) for x, par, m in zip(view.lens, parents, counts)]
+        for layer in range(layers):
+            q, k, v = make(batch, n, hq, hd), make(batch, n, hkv, hd), make(batch, n, hkv, hd)
+            out = torch.zeros_like(q)
+            c.append(layer, None, k, v, nodes, None, None)
+            c.attend_shared(layer, q, out, work, mask=mask)
+            want, _, bound, _ = attend_reference(view, host(q), seen, hd ** -0.5, layer)
+            for b, m in enumerate(counts):
+                off = np.abs(host(out)[b, :m] - want[b, :m]) - bound[b, :m]
+                assert not (off > 1e-30).any() and not np.isnan(off).any(), (step, layer, b, off.max())
+        accept = i32([int(rng.integers(1, m + 1)) for m in counts])
+        c.commit(accept, i32(np.tile(np.arange(n), (batch, 1))))
+        assert c.error() == 0
+
+
+@pytest.mark.gpu
 def test_a_workspace_without_the_plan_is_reported_and_nothing_written():
     rng = np.random.default_rng(13)
     p = Shared(rng, [(0, 40, 3, 2), (0, 40, 9, 2)], hq=8, hkv=2, hd=64, page=16, dtype="bf16", nodes=4)
