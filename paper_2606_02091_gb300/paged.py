@@ -455,7 +455,8 @@ class PagedCache:
                                                None if groups is None else _ints("groups", groups, 2 * batch, dev), _stream(stream, dev)))
 
     def attend_shared(self, layer, q, out, work, *, mask=None, scale=None, lse=None, stream=None):
-        """attend for the node counts and lengths of the plan in work, with shared pages read once for a whole group."""
+        """attend for the node counts and lengths of the plan in work, with shared pages read for blocks of a group's rows, not for each
+        sequence."""
         dev = self.device_index
         batch, n, qp, qs, op, lp = self._attend_args(q, out, lse, dev)
         _check(self._L.dflare_cache_attend_shared(
