@@ -584,8 +584,8 @@ dflare_status dflare_cache_attend(dflare_cache* cache, int layer, const void* q_
 
 /*
  * dflare_cache_attend for a batch whose sequences share their leading pages (dflare_cache_fork, or tables that name the same
- * pages): keys on shared pages are read for a block of a group's rows, not for each sequence (from HBM once, as the blocks that
- * read them run side by side). A block has 16 rows of a kv head where the batch has at most 128 and in fp32, 256 otherwise. The same
+ * pages): keys on shared pages are read for a block of a group's rows, not for each sequence (the blocks of a group run side
+ * by side, so that most of what one reads is in L2 for the others). A block has 16 rows of a kv head where the batch has at most 128 and in fp32, 256 otherwise. The same
  * result for a row, up to the rounding of sums.
  * Once per step, after dflare_cache_reserve:
  *   dflare_cache_share_plan     n_nodes_dev as in dflare_cache_attend. Finds the groups, sequences that are neighbours
@@ -598,9 +598,10 @@ dflare_status dflare_cache_attend(dflare_cache* cache, int layer, const void* q_
  * A plan holds until the lengths, the pages or the node counts change; what a call with an older one computes is that of
  * the plan's lengths over the pages that the tables then name. A workspace without a plan for the call's batch and n_max,
  * and a cache of this type and these sizes, sets DFLARE_DEVERR_PLAN, and nothing is written.
- *   work_dev  as many bytes as dflare_cache_shared_bytes gives for the call's own cache, batch and n_max, 128-byte aligned, zero before its first plan; for one plan and the calls that
- *             follow it at a time. They hold two partial results of every row, shared or not: for each sequence and kv head
- *             n_max n_q_heads / n_kv_heads rows, rounded up to 32, twice, of 4 head_dim + 8 bytes, and up to 50 MB beside them. Calls with a batch, n_max and cache so large that the list of work would not fit 31 bits are refused.
+ *   work_dev  as many bytes as dflare_cache_shared_bytes gives for the call's own cache, batch and n_max, 128-byte aligned, zero
+ *             before its first plan; for one plan and the calls that follow it at a time. They hold two partial results of
+ *             every row, shared or not: for each sequence and kv head n_max n_q_heads / n_kv_heads rows, rounded up to 32,
+ *             twice, of 4 head_dim + 8 bytes, and up to 50 MB beside them. Calls with a batch, n_max and cache so large that the list of work would not fit 31 bits are refused.
  */
 dflare_status dflare_cache_shared_bytes(dflare_cache* cache, int batch, int n_max, size_t* bytes);
 dflare_status dflare_cache_share_plan(dflare_cache* cache, const int32_t* n_nodes_dev, int batch, int n_max,

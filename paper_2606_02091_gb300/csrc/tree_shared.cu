@@ -1,6 +1,6 @@
 // Attention of a batch whose sequences share leading pages (samples and beams of one prompt): a shared page's keys are
 // read for a block of the group's rows (16 of a kv head by the warp-level and the fp32 kernel, 256 by the tcgen05 one), not for each
-// sequence. The blocks of a group run side by side, so that HBM gives each key once: 16 single tokens over 4096 shared keys, four
+// sequence. The blocks of a group run side by side, so that HBM gives a key that L2 can hold once: 16 single tokens over 4096 shared keys, four
 // blocks per kv head, read 28.7 MB of DRAM a layer, of which 27.9 are all keys and values, shared and own.
 //
 // The keys of a row are those that its group shares and the sequence's own, two disjoint sets; with o, m, l the weighted

@@ -263,7 +263,8 @@ def _grid(name, t, dtype, shape, device):
 def tree_sample(tokens, parents, n_nodes, target, draft, u, accept_len, path, next_token, *, distinct=False, error=None, stream=None):
     """Sampled acceptance in drafted trees: target [batch][n][vocab] and draft [batch][n - 1 or more][vocab] fp32
     probabilities after each node (a part of a tensor with more rows will do for draft; None: drafts were picked, not drawn), u fp32 [batch][n] uniform numbers in [0, 1).
-    distinct: siblings were drawn without replacement. The others as in tree_accept; error gets DEVERR_TREE, DEVERR_TOKEN."""
+    distinct: siblings were drawn without replacement. The others as in tree_accept; error gets DEVERR_TREE, DEVERR_TOKEN,
+    DEVERR_TIMEOUT (that tree has no result)."""
     if parents.dim() != 2 or target.dim() != 3:
         raise ValueError(f"parents must be [batch][n] and target [batch][n][vocab], got {list(parents.shape)} and {list(target.shape)}")
     batch, n = parents.shape
