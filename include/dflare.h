@@ -585,8 +585,8 @@ dflare_status dflare_cache_attend(dflare_cache* cache, int layer, const void* q_
 /*
  * dflare_cache_attend for a batch whose sequences share their leading pages (dflare_cache_fork, or tables that name the same
  * pages): keys on shared pages are read for a block of a group's rows, not for each sequence (the blocks of a group run side
- * by side, so that most of what one reads is in L2 for the others). A block has 16 rows of a kv head where the batch has at most 128 and in fp32, 256 otherwise. The same
- * result for a row, up to the rounding of sums.
+ * by side, so that most of what one reads is in L2 for the others). A block has 16 rows of a kv head where the batch has at most
+ * 128 and in fp32, 256 otherwise. The same result for a row, up to the rounding of sums.
  * Once per step, after dflare_cache_reserve:
  *   dflare_cache_share_plan     n_nodes_dev as in dflare_cache_attend. Finds the groups, sequences that are neighbours
  *                               (those without nodes left out) and hold the same pages in the same places, full of
@@ -601,7 +601,8 @@ dflare_status dflare_cache_attend(dflare_cache* cache, int layer, const void* q_
  *   work_dev  as many bytes as dflare_cache_shared_bytes gives for the call's own cache, batch and n_max, 128-byte aligned, zero
  *             before its first plan; for one plan and the calls that follow it at a time. They hold two partial results of
  *             every row, shared or not: for each sequence and kv head n_max n_q_heads / n_kv_heads rows, rounded up to 32,
- *             twice, of 4 head_dim + 8 bytes, and up to 50 MB beside them. Calls with a batch, n_max and cache so large that the list of work would not fit 31 bits are refused.
+ *             twice, of 4 head_dim + 8 bytes, and up to 50 MB beside them. Calls with a batch, n_max and cache so large that
+ *             the list of work would not fit 31 bits are refused.
  */
 dflare_status dflare_cache_shared_bytes(dflare_cache* cache, int batch, int n_max, size_t* bytes);
 dflare_status dflare_cache_share_plan(dflare_cache* cache, const int32_t* n_nodes_dev, int batch, int n_max,
@@ -678,10 +679,11 @@ dflare_status dflare_tree_accept(const int32_t* tokens_dev, const int32_t* paren
  *               token is drawn from p without the children's tokens.
  *   u_dev       [batch][n_max] fp32, uniform in [0, 1); other values count as the nearest number of that range, NaN as 0.
  *   vocab       1..2^28.
- * Sums over the vocabulary are good to 2^-40 of themselves, in the same order on every run. Probabilities, of either, that
- * are negative or not finite count as 0. A token outside [0, vocab) is not kept and sets DFLARE_DEVERR_TOKEN; a row that weighs nothing
- * gives token 0 and sets it too. A tree's walk is shared by a cluster of CTAs; where a wait among them gives up,
- * DFLARE_DEVERR_TIMEOUT is set, and the tree has what one without nodes has: accepted length 0, path and next token -1.
+ * Sums over the vocabulary are good to 2^-40 of themselves (of a residual: of the target's probabilities that it is left of), in the
+ * same order on every run. Probabilities, of either, that are negative or not finite count as 0. A token outside [0, vocab) is
+ * not kept and sets DFLARE_DEVERR_TOKEN; a row that weighs nothing gives token 0 and sets it too. A tree's walk is shared by a
+ * cluster of CTAs; where a wait among them gives up, DFLARE_DEVERR_TIMEOUT is set, and the tree has what one without nodes has:
+ * accepted length 0, path and next token -1.
  */
 dflare_status dflare_tree_sample(const int32_t* tokens_dev, const int32_t* parents_dev, const int32_t* n_nodes_dev,
                                  const float* target_dev, const float* draft_dev, int draft_rows, const float* u_dev,
